@@ -194,6 +194,76 @@ int decode_attention_static(step_pool* pool, int layer, const void* q,
                             const int32_t* block_table, const int32_t* seq_lens, int n,
                             void* out, void* stream);
 
+/* ---- drafted tokens and a bounded cache (the paper has no counterpart: these calls are for engines that draft several
+ * continuations of a trace and verify them in one pass, and for those that bound a trace's cache instead of, or before,
+ * giving the trace up).  All of them want the pool's device to be current (else STEP_ERR_INVALID_ARG), take their
+ * scratch from the caller (`workspace`: device, 256-byte aligned, in use from the call until its work on the stream is
+ * done; two calls that may overlap in time need two of them), and can be captured into a CUDA graph. */
+
+/* Attention of one layer for a tree of drafted tokens per trace:
+ *   out[i][u][h] = sum_j softmax_j(q[i][u][h] . k[j] / sqrt(d)) v[j],  j over the seq_lens[i] cached positions of row i (as
+ *   decode_attention) and over drafted token u of row i and its ancestors in the row's tree.
+ * q: [n, T, num_q_heads, head_dim]; k_draft, v_draft: [n, T, num_layers, num_kv_heads, head_dim], the layout append_kv
+ * takes (only this layer's rows are read; the drafts are not in the cache yet); pool dtype, 16-byte aligned.
+ * parents: [n, T] int32, the node that node u continues, which comes before u, or -1 if it continues the cached text
+ * itself.  A parent outside [-1, u) is read as -1 and sets the STEP_ERR_INVALID_ARG bit of the device status word.
+ * n_nodes: [n] int32 or NULL: row i has n_nodes[i] <= T drafted tokens (NULL: T); out rows behind them are zeros, and
+ * their q, k_draft, v_draft and parents are not read.  A count outside [0, T] is clamped and flagged likewise.
+ * out: [n, T, num_q_heads, head_dim] in POOL DTYPE (what the output projection behind it reads), rounded once; it must
+ * not overlap the inputs.  1 <= T <= 64, n <= 65535.
+ * decode_attention_tree_workspace_bytes (host-only) says how large the workspace has to be; NULL is fine for 0. */
+int decode_attention_tree_workspace_bytes(const step_pool* pool, int n, int T, size_t* bytes);
+int decode_attention_tree(step_pool* pool, int layer, const void* q, const void* k_draft, const void* v_draft,
+                          const int32_t* parents, const int32_t* n_nodes, int T, const int32_t* block_table,
+                          const int32_t* seq_lens, int n, void* out, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/* The accepted part of a draft goes into the cache: position S_t + s of trace trace_ids[i] gets row path[i][s] of
+ * k_draft[i], v_draft[i], for s < path_len[i] (S_t: the trace's length before the call).
+ * k_draft, v_draft: [n, T, num_layers, num_kv_heads, head_dim] pool dtype, 16-byte aligned; path: [n, max_path] int32, rows
+ * of the draft in the order they are to be stored (repeats are allowed); path_len: [n] int32, 0 .. max_path.  T has no
+ * upper bound here.  Allocation, and what is flagged, as append_kv: traces in the order listed, an entry that cannot be
+ * served is skipped whole; a path_len out of range or a path that names a row outside [0, T) skips its entry and sets the
+ * STEP_ERR_INVALID_ARG bit.  n <= min(max_traces, 2048).  Needs no workspace. */
+int append_kv_path(step_pool* pool, const int32_t* trace_ids, int n, int T, const void* k_draft, const void* v_draft,
+                   const int32_t* path, const int32_t* path_len, int max_path, void* stream);
+
+/* decode_attention that also accumulates how much each cached position is attended to:
+ *   weight_sum[i][kvh][j] += sum over the query heads h of KV head kvh of softmax_j(q[i][h] . K_i[j] / sqrt(d))
+ * for j < seq_lens[i]; entries from there on stay as they are.  Arguments as decode_attention; out [n, num_q_heads,
+ * head_dim] fp32, here accurate to fp32 (the probabilities are not rounded to bf16 on their way into the second product,
+ * so the results differ from decode_attention's in the last bits that call has).  weight_sum: [n, num_kv_heads,
+ * weight_stride] fp32; positions from weight_stride on are not counted and set the STEP_ERR_CAPACITY bit.
+ * q and out 16-byte aligned; n <= 65535; no two of q, out, weight_sum and workspace may overlap. */
+int decode_attention_weights_workspace_bytes(const step_pool* pool, int n, int weight_stride, size_t* bytes);
+int decode_attention_weights(step_pool* pool, int layer, const void* q, const int32_t* block_table,
+                             const int32_t* seq_lens, int n, void* out, float* weight_sum, int weight_stride,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* Every listed trace that holds more than `budget` positions is cut to `budget`: its last `recent` positions stay, and of
+ * those before them the budget - recent with the largest weights, chosen for every layer and KV head by itself.  Per
+ * (layer, entry, head), with S positions, first = S - recent and m = budget - recent:
+ *   chosen: the m positions of [0, first) with the largest weights[layer][entry][head][position]; of equal weights the
+ *   lower position; NaN comes last, and the two zeros are equal
+ *   slots m .. budget - 1 get positions first .. S - 1 in order; a chosen position below m stays where it is; the free slots
+ *   below m take the chosen positions from m on, both in ascending order.
+ * (The order of cached positions does not matter to attention; keeping the last ones in order makes `recent` mean the same
+ * at the next call.)  kept_out[layer][entry][head][slot] = the position the slot's rows came from.
+ * weights, weights_out: [num_layers, n, num_kv_heads, weight_stride] fp32, the same buffer or two that do not overlap:
+ * weights follow their positions, entries from budget on become 0.  weight_stride >= budget.
+ * kept_out: [num_layers, n, num_kv_heads, budget] int32.
+ * The pages behind the budget go back (references dropped in list order, pages ascending, as in an eviction).  A page that
+ * stays and is shared with another trace is replaced by a block of the trace's own, taken from the free list before
+ * anything is given back: a trace for which the free list is too short is left alone (STEP_ERR_NO_BLOCKS).
+ * A trace of at most `budget` positions is left alone; so is one with more positions than weight_stride
+ * (STEP_ERR_CAPACITY), and ids that are out of range, not live or repeated are passed over (STEP_ERR_BAD_TRACE; all
+ * in the status word).  For entries left alone kept_out is not written and weights_out gets the weights as they are.
+ * 0 <= recent <= budget, 1 <= budget <= max_pages_per_trace * page_size, n <= min(max_traces, 2048). */
+int kv_pool_evict_workspace_bytes(const step_pool* pool, int n, int budget, size_t* bytes);
+int kv_pool_evict_positions(step_pool* pool, const int32_t* trace_ids, int n, const float* weights, float* weights_out,
+                            int weight_stride, int budget, int recent, int32_t* kept_out, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
 /* Step scorer at step boundaries (Sec. 3.1) and running-mean update (Sec. 3.3):
  * for every row i with boundary_mask[i] != 0:
  *   y = sigmoid(w2 . ReLU(W1 hidden[i] + b1) + b2);  step_scores_out[i] = y;

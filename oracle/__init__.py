@@ -18,6 +18,8 @@ kv_pool.py    paged KV pool bookkeeping: InitTraces prefix fork, append,
               Algorithm 1 / Sec. 3.2, block reclaim; the weighted vote.
 steps.py      step-end test of a sampled token's text (Sec. 3.1 footnote).
 algorithm1.py the loop of Algorithm 1 over the pieces above.
+drafts.py     attention of drafted-token trees, storing the accepted path.
+bounded.py    accumulated attention weights, eviction of positions by them.
 training.py   weighted BCE-from-logits loss, its gradients and Adam for the
               scorer (Sec. 3.1 "Training Objective"; appendix parameters).
 

@@ -97,6 +97,14 @@ def lib():
     L.step_read_stream_probe.argtypes = [vp, C.c_size_t, i, i, vp, vp]
     L.decode_attention_layers.argtypes = [vp, i, i, vp, vp, vp, i, vp, vp]
     L.decode_attention_shared_prefix.argtypes = [vp, i, vp, vp, vp, i, vp, i, vp, vp]
+    szp, sz = C.POINTER(C.c_size_t), C.c_size_t
+    L.decode_attention_tree_workspace_bytes.argtypes = [vp, i, i, szp]
+    L.decode_attention_tree.argtypes = [vp, i, vp, vp, vp, vp, vp, i, vp, vp, i, vp, vp, sz, vp]
+    L.append_kv_path.argtypes = [vp, vp, i, i, vp, vp, vp, vp, i, vp]
+    L.decode_attention_weights_workspace_bytes.argtypes = [vp, i, i, szp]
+    L.decode_attention_weights.argtypes = [vp, i, vp, vp, vp, i, vp, vp, i, vp, sz, vp]
+    L.kv_pool_evict_workspace_bytes.argtypes = [vp, i, i, szp]
+    L.kv_pool_evict_positions.argtypes = [vp, vp, i, vp, vp, i, i, i, vp, vp, sz, vp]
     L.score_steps.argtypes = [vp, vp, vp, vp, i, C.POINTER(scorer_weights), vp, vp]
     L.score_steps_tokens.argtypes = [vp, vp, vp, vp, i, vp, i, C.POINTER(scorer_weights), vp, vp, vp]
     L.detect_step_ends.argtypes = [vp, vp, i, vp, i, vp, vp]
@@ -137,6 +145,13 @@ def _stream(stream=None):
 
 def _ptr(t):
     return C.c_void_p(0 if t is None else t.data_ptr())
+
+
+def _expect(fn, device, *wanted):
+    """Every (tensor, shape, dtype) of `wanted` is a contiguous tensor of that shape and type on `device`; None passes."""
+    for t, shape, dtype in wanted:
+        if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous()):
+            raise StepError(fn, 1)
 
 
 def kv_pool_required_bytes(**geometry):
@@ -264,6 +279,94 @@ class KVPool:
         _check("decode_attention_static", lib().decode_attention_static(self.handle, layer, _ptr(q), _ptr(block_table),
                                                                         _ptr(seq_lens), q.shape[0], _ptr(out), _stream(stream)))
         return out
+
+    # ---- drafted tokens and a bounded cache
+    def _run(self, fn, stream, workspace, size_args, call):
+        """call(workspace pointer, bytes, stream) with the pool's device current; without a `workspace` (uint8 tensor) one
+        is taken from torch's allocator on the call's stream."""
+        with torch.cuda.device(self.device), torch.cuda.stream(stream):
+            need = C.c_size_t()
+            if size_args is not None:
+                _check(fn + "_workspace_bytes", getattr(lib(), size_args[0])(self.handle, *size_args[1:], C.byref(need)))
+                if workspace is None:
+                    workspace = torch.empty(max(1, need.value), dtype=torch.uint8, device=self.device)
+                elif workspace.device != self.device or not workspace.is_contiguous():
+                    raise StepError(fn, 1)
+            _check(fn, call(_ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                            _stream()))
+
+    def _like_table(self, fn, n, block_table, seq_lens):
+        _expect(fn, self._device(), (block_table, (n, self.max_pages_per_trace), torch.int32), (seq_lens, (n,), torch.int32))
+
+    def _device(self):
+        return self.kv_storage.device
+
+    def decode_attention_tree(self, layer, q, k_draft, v_draft, parents, block_table, seq_lens, n_nodes=None, out=None,
+                              workspace=None, stream=None):
+        """q: [n, T, Hq, d] -> out [n, T, Hq, d] in the pool's type; k_draft, v_draft: [n, T, L, Hkv, d]; parents: [n, T]."""
+        fn, dev, dt = "decode_attention_tree", self._device(), self.torch_dtype
+        if q.dim() != 4:
+            raise StepError(fn, 1)
+        n, T = q.shape[:2]
+        draft, rows = (n, T, self.num_layers, self.num_kv_heads, self.head_dim), (n, T, self.num_q_heads, self.head_dim)
+        self._like_table(fn, n, block_table, seq_lens)
+        _expect(fn, dev, (q, rows, dt), (k_draft, draft, dt), (v_draft, draft, dt), (parents, (n, T), torch.int32),
+                (n_nodes, (n,), torch.int32), (out, rows, dt))
+        if out is None:
+            with torch.cuda.stream(stream):
+                out = torch.empty(rows, dtype=dt, device=dev)
+        self._run(fn, stream, workspace, (fn + "_workspace_bytes", n, T), lambda ws, nb, st: lib().decode_attention_tree(
+            self.handle, layer, _ptr(q), _ptr(k_draft), _ptr(v_draft), _ptr(parents), _ptr(n_nodes), T, _ptr(block_table),
+            _ptr(seq_lens), n, _ptr(out), ws, nb, st))
+        return out
+
+    def append_kv_path(self, trace_ids, k_draft, v_draft, path, path_len, stream=None):
+        """Stores rows path[i, :path_len[i]] of the drafts [n, T, L, Hkv, d] behind trace trace_ids[i]."""
+        fn, dev = "append_kv_path", self._device()
+        if k_draft.dim() != 5 or path.dim() != 2:
+            raise StepError(fn, 1)
+        n, T = k_draft.shape[:2]
+        draft = (n, T, self.num_layers, self.num_kv_heads, self.head_dim)
+        _expect(fn, dev, (trace_ids, (n,), torch.int32), (k_draft, draft, self.torch_dtype), (v_draft, draft, self.torch_dtype),
+                (path, (n, path.shape[1]), torch.int32), (path_len, (n,), torch.int32))
+        self._run(fn, stream, None, None, lambda ws, nb, st: lib().append_kv_path(
+            self.handle, _ptr(trace_ids), n, T, _ptr(k_draft), _ptr(v_draft), _ptr(path), _ptr(path_len), path.shape[1], st))
+
+    def decode_attention_weights(self, layer, q, block_table, seq_lens, weight_sum, out=None, workspace=None, stream=None):
+        """q: [n, Hq, d] -> out [n, Hq, d] fp32; adds to weight_sum [n, Hkv, stride] fp32."""
+        fn, dev = "decode_attention_weights", self._device()
+        if q.dim() != 3 or weight_sum.dim() != 3:
+            raise StepError(fn, 1)
+        n, stride = q.shape[0], weight_sum.shape[2]
+        rows = (n, self.num_q_heads, self.head_dim)
+        self._like_table(fn, n, block_table, seq_lens)
+        _expect(fn, dev, (q, rows, self.torch_dtype), (weight_sum, (n, self.num_kv_heads, stride), torch.float32),
+                (out, rows, torch.float32))
+        if out is None:
+            with torch.cuda.stream(stream):
+                out = torch.empty(rows, dtype=torch.float32, device=dev)
+        self._run(fn, stream, workspace, (fn + "_workspace_bytes", n, stride), lambda ws, nb, st: lib().decode_attention_weights(
+            self.handle, layer, _ptr(q), _ptr(block_table), _ptr(seq_lens), n, _ptr(out), _ptr(weight_sum), stride, ws, nb, st))
+        return out
+
+    def evict_positions(self, trace_ids, weights, budget, recent, weights_out=None, kept_out=None, workspace=None, stream=None):
+        """weights: [L, n, Hkv, stride] fp32, in place unless weights_out is given.  Returns kept_out [L, n, Hkv, budget]
+        (rows of entries that are left alone are not written: -1 in a tensor made here)."""
+        fn, dev = "kv_pool_evict_positions", self._device()
+        if weights.dim() != 4:
+            raise StepError(fn, 1)
+        n, stride = weights.shape[1], weights.shape[3]
+        shape = (self.num_layers, n, self.num_kv_heads)
+        _expect(fn, dev, (trace_ids, (n,), torch.int32), (weights, shape + (stride,), torch.float32),
+                (weights_out, shape + (stride,), torch.float32), (kept_out, shape + (budget,), torch.int32))
+        if weights_out is None:
+            weights_out = weights
+        if kept_out is None:
+            with torch.cuda.stream(stream):
+                kept_out = torch.full(shape + (max(budget, 0),), -1, dtype=torch.int32, device=dev)
+        self._run(fn, stream, workspace, ("kv_pool_evict_workspace_bytes", n, budget), lambda ws, nb, st: lib().kv_pool_evict_positions(
+            self.handle, _ptr(trace_ids), n, _ptr(weights), _ptr(weights_out), stride, budget, recent, _ptr(kept_out), ws, nb, st))
+        return kept_out
 
     def score_steps(self, hidden, boundary_mask, row_trace, weights, step_scores_out=None, stream=None):
         M = hidden.shape[0]

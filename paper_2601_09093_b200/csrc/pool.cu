@@ -444,6 +444,130 @@ append_fused_kernel(DevViews v, Geo g, uint4* __restrict__ kv, const uint4* __re
   }
 }
 
+// ---------------------------------------------------------------- append_kv_path
+// Every listed trace gets its own number of new positions, taken from rows of a draft in the order its path names them.
+// Two launches.  Phase 1 (one CTA): as append_alloc_kernel, with per-entry counts; an entry whose count or path is out of
+// range is flagged and skipped.  Leaves every entry's old length in v.append_base (-1: nothing to store) and the prefix
+// sum of the new positions in v.prune_off (scratch of max_traces + 1 ints), by which phase 2 finds its rows.
+__global__ void __launch_bounds__(256)
+path_alloc_kernel(DevViews v, Geo g, const int32_t* __restrict__ ids, int n, const int32_t* __restrict__ path,
+                  const int32_t* __restrict__ path_len, int max_path, int T) {
+  extern __shared__ int sm[];
+  dependents_may_launch();
+  int* s_need = sm;            // pages wanted, or -1 if the entry is skipped
+  int* s_off = sm + n;         // pops that precede this entry's
+  int* s_have = sm + 2 * n;
+  int* s_bad = sm + 3 * n;
+  __shared__ int s_fc;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nwarps = blockDim.x >> 5;
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    const int t = ids[i];
+    if (t >= 0 && t < g.max_traces) v.prune_rank[t] = 0x7fffffff;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    const int t = ids[i];
+    if (t >= 0 && t < g.max_traces) atomicMin(&v.prune_rank[t], i);
+  }
+  for (int i = warp; i < n; i += nwarps) {               // nodes outside the draft
+    const int k = path_len[i];
+    bool bad = k < 0 || k > max_path;
+    if (!bad)
+      for (int j = lane; j < k; j += 32) {
+        const int node = path[(size_t)i * max_path + j];
+        bad |= node < 0 || node >= T;
+      }
+    bad = __any_sync(0xffffffffu, bad);
+    if (lane == 0) s_bad[i] = bad;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    int need = -1, have = 0;
+    const int t = ids[i];
+    if (t < 0 || t >= g.max_traces || !v.live[t] || v.prune_rank[t] != i) {
+      flag_error(v.counters, STEP_ERR_BAD_TRACE);
+    } else if (s_bad[i]) {
+      flag_error(v.counters, STEP_ERR_INVALID_ARG);
+    } else {
+      const int S = v.seq_lens[t];
+      have = (S + g.P - 1) / g.P;
+      const long long want = ((long long)S + path_len[i] + g.P - 1) / g.P;
+      if (want > g.max_pages) flag_error(v.counters, STEP_ERR_CAPACITY);
+      else need = (int)want - have;
+    }
+    s_need[i] = need; s_have[i] = have;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const int fc = v.counters[C_FREE_COUNT];
+    int remaining = fc, rows = 0;
+    for (int i = 0; i < n; ++i) {
+      const int need = s_need[i];
+      v.prune_off[i] = rows;
+      if (need < 0) continue;
+      if (need > remaining) { s_need[i] = -1; flag_error(v.counters, STEP_ERR_NO_BLOCKS); continue; }
+      s_off[i] = fc - remaining;
+      remaining -= need;
+      rows += path_len[i];
+    }
+    v.prune_off[n] = rows;
+    s_fc = fc;
+    v.counters[C_FREE_COUNT] = remaining;
+  }
+  __syncthreads();
+  const int fc = s_fc;
+  for (int i = warp; i < n; i += nwarps) {
+    const int need = s_need[i];
+    if (need < 0) { if (lane == 0) v.append_base[i] = -1; continue; }
+    const int t = ids[i];
+    int32_t* row = v.block_table + (size_t)t * g.max_pages;
+    for (int p = lane; p < need; p += 32) {
+      const int b = v.free_list[fc - 1 - s_off[i] - p];
+      row[s_have[i] + p] = b;
+      v.refcount[b] = 1;
+    }
+    if (lane == 0) {
+      const int S = v.seq_lens[t];
+      v.append_base[i] = S;
+      v.seq_lens[t] = S + path_len[i];
+    }
+  }
+}
+
+// Phase 2: CTAs walk over the (entry, new position) pairs that phase 1 admitted and move their rows, a range of layers each.
+__global__ void __launch_bounds__(256)
+path_write_kernel(DevViews v, Geo g, uint4* __restrict__ kv, const uint4* __restrict__ kd, const uint4* __restrict__ vd,
+                  const int32_t* __restrict__ ids, int n, const int32_t* __restrict__ path, int max_path, int T, int cpr,
+                  int layers_per_cta) {
+  wait_for_primary();
+  const int total = v.prune_off[n];
+  const int l0 = blockIdx.y * layers_per_cta, l1 = min(g.L, l0 + layers_per_cta);
+  const int per_kv = g.Hkv * cpr;
+  const size_t page_chunks = (size_t)g.P * cpr;
+  const size_t layer_stride = (size_t)g.num_blocks * g.Hkv * 2 * page_chunks;
+  for (int e = blockIdx.x; e < total; e += gridDim.x) {
+    int lo = 0, hi = n - 1;                              // the last entry whose rows start at or before e
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (v.prune_off[mid] <= e) lo = mid; else hi = mid - 1;
+    }
+    const int j = e - v.prune_off[lo];
+    const int pos = v.append_base[lo] + j, page = pos / g.P, slot = pos % g.P;
+    const int b = v.block_table[(size_t)ids[lo] * g.max_pages + page];
+    const int node = path[(size_t)lo * max_path + j];
+    const size_t src_token = ((size_t)lo * T + node) * (size_t)g.L * per_kv;
+    for (int i = threadIdx.x; i < 2 * per_kv; i += blockDim.x) {
+      const int which = i >= per_kv;
+      const int r = which ? i - per_kv : i;
+      const int head = r / cpr, c = r - head * cpr;
+      const int cdst = g.swizzle ? ((c & ~7) | ((c ^ slot) & 7)) : c;
+      const uint4* src = (which ? vd : kd) + src_token + r;
+      const size_t dst0 = (((size_t)b * g.Hkv + head) * 2 + which) * page_chunks + (size_t)slot * cpr + cdst;
+      for (int l = l0; l < l1; ++l) kv[(size_t)l * layer_stride + dst0] = src[(size_t)l * per_kv];
+    }
+  }
+}
+
 // ---------------------------------------------------------------- read-back of logical rows
 __global__ void read_kv_kernel(Geo g, const uint4* __restrict__ kv, int layer, int head,
                                const int32_t* __restrict__ block_row, int seq_len, uint4* __restrict__ k_out,
@@ -594,6 +718,36 @@ int append_kv(step_pool* pool, const int32_t* trace_ids, int n, int n_tokens, co
               const void* v_new, void* stream) {
   if (!trace_ids && n > 0 && n_tokens > 0) return STEP_ERR_INVALID_ARG;
   return stepk::append_kv_impl(pool, trace_ids, n, n_tokens, k_new, v_new, nullptr, 0, (cudaStream_t)stream, nullptr, 0);
+}
+
+int append_kv_path(step_pool* pool, const int32_t* trace_ids, int n, int T, const void* k_draft, const void* v_draft,
+                   const int32_t* path, const int32_t* path_len, int max_path, void* stream) {
+  if (!pool || n < 0 || T < 1 || max_path < 0) return STEP_ERR_INVALID_ARG;
+  if (n == 0 || max_path == 0) return STEP_OK;
+  if (!trace_ids || !k_draft || !v_draft || !path || !path_len) return STEP_ERR_INVALID_ARG;
+  if (((uintptr_t)k_draft | (uintptr_t)v_draft) & 15) return STEP_ERR_INVALID_ARG;
+  // ids must be distinct; the list is served by one CTA from shared memory (16 bytes per entry)
+  if (n > pool->cfg.max_traces || n > kMaxTracesFast) return STEP_ERR_INVALID_ARG;
+  if ((long long)n * max_path > 0x7fffffffll) return STEP_ERR_INVALID_ARG;
+  const int st = on_pool_device(pool);
+  if (st != STEP_OK) return st;
+  Geo g = geo_of(pool);
+  cudaStream_t s = (cudaStream_t)stream;
+  const int cpe = 16 / pool->elem_bytes, cpr = g.d / cpe;
+  path_alloc_kernel<<<1, 256, (size_t)n * 4 * sizeof(int), s>>>(pool->v, g, trace_ids, n, path, path_len, max_path, T);
+  if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
+  // CTAs for every pair there may be, up to eight per SM; the layer range is split when there are few pairs
+  const long long pairs = (long long)n * max_path, most = 8ll * pool->num_sms;
+  const int grid = (int)(pairs < most ? pairs : most);
+  int splits = (int)((2ll * pool->num_sms + pairs - 1) / pairs);
+  if (splits > g.L) splits = g.L;
+  if (splits < 1) splits = 1;
+  const int layers_per_cta = (g.L + splits - 1) / splits;
+  splits = (g.L + layers_per_cta - 1) / layers_per_cta;
+  if (launch_dependent(path_write_kernel, dim3((unsigned)grid, (unsigned)splits), dim3(256), 0, s, pool->v, g,
+                       (uint4*)pool->cfg.kv_storage, (const uint4*)k_draft, (const uint4*)v_draft, trace_ids, n, path,
+                       max_path, T, cpr, layers_per_cta) != cudaSuccess) return STEP_ERR_CUDA;
+  return launch_ok();
 }
 
 }  // extern "C"

@@ -130,6 +130,13 @@ __device__ inline void flag_error(int32_t* counters, int code) {
     if (e__ != cudaSuccess) return STEP_ERR_CUDA;           \
   } while (0)
 
+// The entry points that launch more than one kernel on caller-provided workspace ask for the pool's device to be current.
+inline int on_pool_device(const step_pool* pool) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) return STEP_ERR_CUDA;
+  return dev == pool->device ? STEP_OK : STEP_ERR_INVALID_ARG;
+}
+
 inline int launch_ok() { return cudaGetLastError() == cudaSuccess ? STEP_OK : STEP_ERR_CUDA; }
 
 // Programmatic dependent launch.  A kernel launched with launch_dependent() may be scheduled while the kernel before
