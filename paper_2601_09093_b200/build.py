@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libstep.so")
 STAMP = os.path.join(HERE, "_build", "libstep.stamp")
 SOURCES = ["pool.cu", "attention.cu", "scorer.cu", "scorer_tc.cu", "prune.cu", "algorithm1.cu", "train.cu", "probe.cu",
-           "tree.cu", "weights.cu", "evict.cu"]
+           "tree.cu", "tree_tc.cu", "weights.cu", "evict.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
          "--use_fast_math", "-Xcompiler", "-fPIC", "-shared", "-Xptxas", "-v"]
 

@@ -189,4 +189,11 @@ bool score_tc_supported(const scorer_weights* w, const void* hidden);
 // C_SCORE_NB / C_SCORE_TC on the device and returns at once when C_SCORE_TC is 0.
 int score_tc_launch(step_pool* pool, const void* hidden, int Mc, const scorer_weights* w, cudaStream_t s);
 
+// ---- tensor-core tree attention (tree_tc.cu)
+bool tree_tc_supported(const step_pool* pool, int n);
+size_t tree_tc_workspace(const step_pool* pool, int T);
+int tree_tc_launch(step_pool* pool, int layer, const void* q, const void* k_draft, const void* v_draft, const int32_t* parents,
+                   const int32_t* n_nodes, int T, const int32_t* block_table, const int32_t* seq_lens, int n, void* out,
+                   void* workspace, cudaStream_t s);
+
 }  // namespace stepk

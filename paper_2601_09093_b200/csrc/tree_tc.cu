@@ -1,0 +1,677 @@
+// Tensor-core form of decode_attention_tree (bf16 pools, head_dim 128, page 16).
+//
+// The query rows of one trace and KV head are the G heads of its group for every drafted token (row = token * G + head,
+// up to 64 * 16 of them).  Against one read of the cache they do 4 * 128 operations per row and position, against 512
+// bytes: 64 rows are a small fraction of what the tensor cores do in the time of that read, 256 rows are about as much.
+// So every K and V byte is brought to an SM once per 256 rows, and the products run on tcgen05 with M = 128:
+//   * keys are taken 128 at a time: the cached positions, then the drafted tokens, as one sequence.  A tile of 128
+//     cached positions is eight pages, fetched by TMA: a page of one KV head is stored with its 16-byte chunks swizzled
+//     by the slot, so boxes of 16 rows x 128 bytes land in shared memory in the arrangement the tensor cores read (rows
+//     of 128 bytes, 128-byte swizzle), K as a K-major operand of the first product, V as an MN-major operand of the
+//     second.  Tiles that hold the end of the cache or drafted tokens are copied row by row (cp.async), with zeros behind
+//     the last key: what a page holds behind a trace's end never reaches a product;
+//   * scores S (128 x 128, fp32) are made in tensor memory; 128 threads, a row each, read them, keep the running maximum
+//     and sum in fp32, and write the probabilities back as bf16 (one rounding, half a step of 2^-8 at most) over the
+//     same columns, from where they are the A operand of the second product, which adds to O (128 x 128, fp32) in tensor
+//     memory.  O is rescaled only when a row's maximum has grown by more than 2^8 (the probabilities are relative to an
+//     older maximum until then), so the accumulators are almost never touched;
+//   * two such chains ("lanes") run side by side in a CTA, so that the tensor cores work on one while the other is at
+//     its softmax.  Up to 128 rows: the lanes take even and odd tiles of the same rows and are combined at the end.
+//     More: the lanes take 128 rows each of the same tile, and 256 rows are one row group;
+//   * the tiles of all (trace, KV head, row group) sequences form one stream that is cut into one equal contiguous
+//     share per CTA; what a share holds of a sequence leaves its (m, l, O) in the share's first or last slot, and
+//     tree_merge_kernel - a programmatic dependent - combines the pieces of every sequence in stream order.
+// Warps: 4 + 4 softmax (lane 0, lane 1), one that fetches, one whose first thread issues the products.
+// Every wait is bounded; one that runs out raises STEP_ERR_TIMEOUT and the CTA winds down.
+#include "attention_rows.cuh"
+#include "async_copy.cuh"
+#include "tensor_core.cuh"
+
+#include <string.h>
+
+using namespace stepk;
+
+namespace {
+
+constexpr int kP = 16, kD = 128;
+constexpr int kTile = 128;                        // keys per tile
+constexpr int kSlotBytes = kTile * kD * 2;        // K or V of one tile: two halves of 128 rows x 128 bytes
+constexpr int kHalfSlot = kSlotBytes / 2;
+constexpr int kSlots = 4;
+constexpr int kQBytes = kHalfRows * kD * 2;       // 128 query rows, same arrangement
+constexpr int kWarpFetch = 8, kWarpMma = 9;
+constexpr int kThreads = 320;
+constexpr int kTmemCols = 512;                    // S of both lanes (P over them), then O of both
+constexpr float kRescale = 8.f;                   // log2 of how far a row's maximum may run ahead of its reference
+constexpr unsigned long long kDrainNs = 100000000ull;
+
+struct TreeArgs {
+  const __nv_bfloat16* kv;
+  const __nv_bfloat16* q; const __nv_bfloat16* k_draft; const __nv_bfloat16* v_draft;
+  const int32_t* parents; const int32_t* n_nodes;
+  const int32_t* block_table; const int32_t* seq_lens;
+  __nv_bfloat16* out;
+  float* ws_ml;                     // [share][2][group rows][2]
+  float* ws_o;                      // [share][2][group rows][kD]
+  int32_t* counters;
+  int n, T, Hq, Hkv, G, L, layer, max_pages, num_blocks;
+  int rows, groups;                 // query rows of a (trace, KV head): T * G; row groups they make
+  int group_rows;                   // 128 or 256
+  int shares;                       // CTAs of the attention launch
+  float scale_log2;
+};
+
+// ---- the stream of tiles
+__device__ inline int cached(const TreeArgs& a, int t, bool flag) {
+  int S = a.seq_lens[t];
+  if (S < 0) S = 0;
+  if ((long long)S > (long long)a.max_pages * kP) { S = a.max_pages * kP; if (flag) flag_error(a.counters, STEP_ERR_CAPACITY); }
+  return S;
+}
+__device__ inline int nodes_of(const TreeArgs& a, int t, bool flag) {
+  if (!a.n_nodes) return a.T;
+  const int k = a.n_nodes[t];
+  if (flag && (k < 0 || k > a.T)) flag_error(a.counters, STEP_ERR_INVALID_ARG);
+  return min(max(k, 0), a.T);
+}
+// One warp: cum[n + 1], the tiles of every trace (of one KV head and row group) as a prefix sum.  A trace without any
+// key has one tile all the same, which writes its zeros.
+__device__ inline void build_stream(const TreeArgs& a, int lane, bool flag, int* cum) {
+  int run = 0;
+  for (int base = 0; base < a.n; base += 32) {
+    const int t = base + lane;
+    int tiles = 0;
+    if (t < a.n) {
+      const long long keys = (long long)cached(a, t, flag) + nodes_of(a, t, flag);
+      tiles = keys > 0 ? (int)((keys + kTile - 1) / kTile) : 1;
+    }
+    int incl = tiles;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += x;
+    }
+    if (t < a.n) cum[t] = run + incl - tiles;
+    run += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  if (lane == 0) cum[a.n] = run;
+}
+// A piece: tiles [tile0, tile0 + cnt) of the sequence of (trace t, row group and head hr), at stream position pos.
+struct Piece { int t, hr, tile0, cnt, tiles; };
+__device__ inline Piece piece_at(const int* cum, int n, int HR, long long pos, long long end) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if ((long long)HR * cum[mid] <= pos) lo = mid; else hi = mid - 1;
+  }
+  Piece p;
+  p.t = lo;
+  p.tiles = cum[lo + 1] - cum[lo];
+  const long long r = pos - (long long)HR * cum[lo];
+  p.hr = (int)(r / p.tiles);
+  p.tile0 = (int)(r % p.tiles);
+  p.cnt = (int)min((long long)(p.tiles - p.tile0), end - pos);
+  return p;
+}
+
+// ---- instructions
+__device__ inline void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
+// 16 bytes, or 16 zero bytes (src is then not read)
+__device__ inline void cp_async16_or_zero(uint32_t dst, const void* src, bool real) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+// 32 columns of this thread's TMEM lane, without waiting for them
+__device__ inline void tc_ld32_async(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr) : "memory");
+}
+__device__ inline void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// The values of an asynchronous load may be used only behind the wait: ties them to this place.
+template <int N> __device__ inline void pin(uint32_t* r) {
+#pragma unroll
+  for (int i = 0; i < N; i += 8)
+    asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
+}
+__device__ inline void tc_st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+      :: "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+         "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+         "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+         "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]),
+         "r"(taddr) : "memory");
+}
+__device__ inline void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// D[tmem] (+)= A[tmem] * B[smem]
+__device__ inline void tc_mma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Descriptor of V as an MN-major operand: 64 of the N index are 128 contiguous (swizzled) bytes, the next 64 lie a half slot
+// further (leading byte offset), 8 of the K index (tokens) are 1024 bytes (stride byte offset).
+__device__ inline uint64_t umma_desc_v(uint32_t smem_addr) {
+  const uint32_t lo = ((smem_addr >> 4) & 0x3FFFu) | ((uint32_t)(kHalfSlot >> 4) << 16);
+  const uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+  return ((uint64_t)hi << 32) | lo;
+}
+__device__ inline uint32_t pack2(float lo, float hi) {
+  __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<uint32_t*>(&v);
+}
+
+template <bool kTwoRows>   // the lanes take 128 rows each of a 256-row group; else even and odd tiles of the same 128 rows
+__global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_constant__ CUtensorMap map, TreeArgs a) {
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  unsigned char* sm = smem_raw + (base - raw);
+  const uint32_t sm_q = base, sm_ring = base + 2 * kQBytes;
+  unsigned char* tail = sm + 2 * kQBytes + kSlots * kSlotBytes;
+  uint64_t* s_bar = reinterpret_cast<uint64_t*>(tail);
+  float* s_ml = reinterpret_cast<float*>(s_bar + 32);                  // [2][128][2]
+  int* s_up = reinterpret_cast<int*>(s_ml + 512);                      // [2][64]
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_up + 128);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
+  int* s_cum = reinterpret_cast<int*>(s_tmem + 4);                     // [n + 1]
+  const uint32_t bars = smem_u32(s_bar);
+  const uint32_t bar_full = bars, bar_empty = bars + 8 * kSlots;
+  const uint32_t bar_q = bars + 16 * kSlots, bar_s = bar_q + 8, bar_p = bar_s + 16, bar_o = bar_p + 16,
+                 bar_both = bar_o + 16, bar_lane = bar_both + 8, bar_drain = bar_lane + 16;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(bar_full + 8 * s, 33);              // the fetching warp's threads, and its announcement of bytes
+      mbar_init(bar_empty + 8 * s, 1);              // tcgen05.commit
+    }
+    mbar_init(bar_q, 256);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(bar_s + 8 * s, 1);                  // tcgen05.commit: scores made (and the products before them done)
+      mbar_init(bar_p + 8 * s, 128);
+      mbar_init(bar_o + 8 * s, 1);                  // tcgen05.commit: a piece's last product
+      mbar_init(bar_lane + 8 * s, 128);
+    }
+    mbar_init(bar_both, 256);
+    mbar_init(bar_drain, 1);
+    *s_abort = 0;
+    mbar_init_fence();
+  }
+  if (warp == kWarpMma) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (warp == 0) build_stream(a, lane, blockIdx.x == 0, s_cum);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  dependents_may_launch();
+  const uint32_t tmem = *s_tmem;
+  const int HR = a.Hkv * a.groups;
+  const long long total = (long long)HR * s_cum[a.n];
+  const long long W = (total + a.shares - 1) / a.shares;
+  const long long pos0 = min(total, (long long)blockIdx.x * W), end = min(total, pos0 + W);
+
+  auto wait = [&](uint32_t bar, uint32_t parity) {
+    if (*s_abort) return false;
+    if (mbar_wait_bounded(bar, parity)) return true;
+    flag_error(a.counters, STEP_ERR_TIMEOUT);
+    *s_abort = 1;
+    return false;
+  };
+
+  // the same, with one answer for the whole warp: what follows has to be executed by all of it
+  auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
+
+  if (warp < 8) {
+    // ------------------------------------------------ softmax: lane `ln` of the CTA, row `row` of its 128
+    const int ln = warp >> 2, row = (warp & 3) * 32 + lane, tid = threadIdx.x;
+    const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t t_s = t_row + ln * 128, t_o = t_row + 256 + ln * 128;
+    uint32_t ph_s = 0, ph_piece = 0, ph_both = 0, ph_lane = 0;
+    bool ok = true;
+    for (long long pos = pos0; pos < end && ok;) {
+      const Piece pc = piece_at(s_cum, a.n, HR, pos, end);
+      const int h = pc.hr / a.groups, r0 = (pc.hr - h * a.groups) * a.group_rows;
+      const int S = cached(a, pc.t, false), nodes = nodes_of(a, pc.t, false);
+      // ---- query rows into shared memory (zeros behind the last), the node's ancestors
+      {
+        const int qrow = kTwoRows ? row : tid >> 1;                    // row of the tile this thread copies
+        const int c0 = kTwoRows ? 0 : (tid & 1) * 8, c1 = kTwoRows ? 16 : c0 + 8;
+        const int r = r0 + (kTwoRows ? ln * 128 : 0) + qrow;
+        const bool real = r < nodes * a.G;
+        const uint4* src = reinterpret_cast<const uint4*>(a.q + (((size_t)pc.t * a.T + (real ? r / a.G : 0)) * a.Hq + (size_t)h * a.G + (real ? r % a.G : 0)) * kD);
+        unsigned char* dst = sm + (kTwoRows ? ln * kQBytes : 0) + qrow * 128;
+#pragma unroll
+        for (int c = c0; c < c1; ++c)
+          *reinterpret_cast<uint4*>(dst + (c >> 3) * (kQBytes / 2) + (((c ^ qrow) & 7) << 4)) = real ? src[c] : make_uint4(0, 0, 0, 0);
+      }
+      if (row < nodes) {
+        int p = a.parents[(size_t)pc.t * a.T + row];
+        if (p >= row || p < -1) { flag_error(a.counters, STEP_ERR_INVALID_ARG); p = -1; }
+        s_up[ln * 64 + row] = p;
+      }
+      fence_async_smem();
+      tc_fence_before();
+      mbar_arrive(bar_q);
+      mbar_arrive(bar_lane + 8 * ln);
+      if (!wait_warp(bar_lane + 8 * ln, ph_lane)) { ok = false; break; }
+      ph_lane ^= 1;
+      const int r = r0 + (kTwoRows ? ln * 128 : 0) + row, u = r / a.G;
+      const bool mine = r < nodes * a.G;
+      unsigned long long sees = 0;
+      if (mine)
+        for (int w = u; w >= 0; w = s_up[ln * 64 + w]) sees |= 1ull << w;
+
+      float m_ref = -INFINITY, l = 0.f;
+      bool started = false;
+      for (int i = kTwoRows ? 0 : ln; i < pc.cnt; i += kTwoRows ? 1 : 2) {
+        if (!wait_warp(bar_s + 8 * ln, ph_s)) { ok = false; break; }
+        ph_s ^= 1;
+        tc_fence_after();
+        uint32_t s[128];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tc_ld32_async(t_s + 32 * c, s + 32 * c);
+        tc_wait_ld();
+        pin<128>(s);
+        const int j0 = (pc.tile0 + i) * kTile;
+        if (j0 + kTile > S) {                                          // the end of the cache, drafted tokens
+#pragma unroll
+          for (int c = 0; c < kTile; ++c) {
+            const int j = j0 + c - S;                                  // < 0: cached; else drafted token j
+            const bool see = j < 0 || (j < 64 && ((sees >> (j & 63)) & 1));
+            if (!see) s[c] = 0xff800000u;
+          }
+        }
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < kTile; c += 4) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) mx[x] = fmaxf(mx[x], __uint_as_float(s[c + x]));
+        }
+        const float m_new = fmaxf(m_ref, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2);
+        if (!started) {
+          m_ref = m_new;
+          started = true;
+        } else {
+          const bool grow = m_new > m_ref + kRescale;
+          if (__any_sync(0xffffffffu, grow)) {
+            const float corr = grow ? exp2f(m_ref - m_new) : 1.f;
+            if (grow) m_ref = m_new;
+            l *= corr;
+#pragma unroll 1
+            for (int c = 0; c < kD; c += 32) {
+              uint32_t o[32];
+              tc_ld32_async(t_o + c, o);
+              tc_wait_ld();
+              pin<32>(o);
+#pragma unroll
+              for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * corr);
+              tc_st32(t_o + c, o);
+            }
+          }
+        }
+        const float off = m_ref == -INFINITY ? 0.f : m_ref;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < kTile; c += 2) {
+          const float p0 = exp2f(fmaf(__uint_as_float(s[c]), a.scale_log2, -off));
+          const float p1 = exp2f(fmaf(__uint_as_float(s[c + 1]), a.scale_log2, -off));
+          sum[c & 2] += p0;
+          sum[(c & 2) + 1] += p1;
+          s[c / 2] = pack2(p0, p1);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tc_st32(t_s, s);
+        tc_st32(t_s + 32, s + 32);
+        tc_wait_st();
+        tc_fence_before();
+        mbar_arrive(bar_p + 8 * ln);
+      }
+      if (!ok || !wait_warp(bar_o + 8 * ln, ph_piece)) { ok = false; break; }
+      tc_fence_after();
+      ph_piece ^= 1;
+
+      // ---- the piece is done
+      const bool whole = pc.cnt == pc.tiles;
+      const long long seq_start = pos - pc.tile0;
+      const size_t slot = (size_t)blockIdx.x * 2 + (seq_start <= pos0 ? 0 : 1);
+      auto put = [&](int c, const float* o, float inv) {               // columns c .. c + 31 of this thread's row
+        if (whole) {
+          if (r < a.rows) {
+            uint4* dst = reinterpret_cast<uint4*>(a.out + (((size_t)pc.t * a.T + u) * a.Hq + (size_t)h * a.G + r % a.G) * kD + c);
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              dst[x] = mine ? make_uint4(pack2(o[8 * x] * inv, o[8 * x + 1] * inv), pack2(o[8 * x + 2] * inv, o[8 * x + 3] * inv),
+                                         pack2(o[8 * x + 4] * inv, o[8 * x + 5] * inv), pack2(o[8 * x + 6] * inv, o[8 * x + 7] * inv))
+                            : make_uint4(0, 0, 0, 0);
+          }
+        } else if (mine) {
+          float4* dst = reinterpret_cast<float4*>(a.ws_o + (slot * a.group_rows + (r - r0)) * kD + c);
+#pragma unroll
+          for (int x = 0; x < 8; ++x) dst[x] = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+        }
+      };
+      if constexpr (kTwoRows) {
+        if (!whole && mine) *reinterpret_cast<float2*>(a.ws_ml + (slot * a.group_rows + (r - r0)) * 2) = make_float2(m_ref, l);
+        const float inv = 1.f / l;
+#pragma unroll 1
+        for (int c = 0; c < kD; c += 32) {
+          uint32_t o[32];
+          tc_ld32_async(t_o + c, o);
+          tc_wait_ld();
+          pin<32>(o);
+          put(c, reinterpret_cast<float*>(o), inv);
+        }
+      } else {
+        // the two lanes hold the even and the odd tiles of the same rows: each takes 64 columns of the sum, the other
+        // lane's part of them through shared memory (the query rows are not needed any more)
+        s_ml[(ln * 128 + row) * 2] = m_ref;
+        s_ml[(ln * 128 + row) * 2 + 1] = l;
+        float* s_x = reinterpret_cast<float*>(sm);                     // [2][64][128]: columns lane 0 gives, lane 1 gives
+        const bool some = ln < pc.cnt;                                 // a piece of one tile leaves lane 1 without any
+#pragma unroll 1
+        for (int c = 0; c < 64; c += 32) {
+          uint32_t o[32];
+          tc_ld32_async(t_o + (ln == 0 ? 64 : 0) + c, o);
+          tc_wait_ld();
+          pin<32>(o);
+#pragma unroll
+          for (int x = 0; x < 32; ++x) s_x[(ln * 64 + c + x) * 128 + row] = some ? __uint_as_float(o[x]) : 0.f;
+        }
+        mbar_arrive(bar_both);
+        if (!wait_warp(bar_both, ph_both)) { ok = false; break; }
+        ph_both ^= 1;
+        const float m0 = s_ml[row * 2], m1 = s_ml[(128 + row) * 2], l0 = s_ml[row * 2 + 1], l1 = s_ml[(128 + row) * 2 + 1];
+        const float M = fmaxf(m0, m1), off = M == -INFINITY ? 0.f : M;
+        const float w0 = exp2f(m0 - off), w1 = exp2f(m1 - off);
+        const float lsum = l0 * w0 + l1 * w1, inv = 1.f / lsum;
+        const float w_own = ln == 0 ? w0 : w1, w_other = ln == 0 ? w1 : w0;
+        if (!whole && mine && ln == 0) *reinterpret_cast<float2*>(a.ws_ml + (slot * a.group_rows + (r - r0)) * 2) = make_float2(M, lsum);
+#pragma unroll 1
+        for (int c = 0; c < 64; c += 32) {
+          uint32_t o[32];
+          float x32[32];
+          tc_ld32_async(t_o + (ln == 0 ? 0 : 64) + c, o);
+          tc_wait_ld();
+          pin<32>(o);
+#pragma unroll
+          for (int x = 0; x < 32; ++x)
+            x32[x] = (some ? __uint_as_float(o[x]) * w_own : 0.f) + s_x[((1 - ln) * 64 + c + x) * 128 + row] * w_other;
+          put((ln == 0 ? 0 : 64) + c, x32, inv);
+        }
+        mbar_arrive(bar_both);                                         // the exchange area becomes the next query rows
+        if (!wait_warp(bar_both, ph_both)) { ok = false; break; }
+        ph_both ^= 1;
+      }
+      pos += pc.cnt;
+    }
+  } else if (warp == kWarpFetch) {
+    // ------------------------------------------------ K and V tiles into the ring
+    int slot = 0;
+    uint32_t ph = 1;
+    bool ok = true;
+    Piece pc = {};
+    int h = 0, S = 0, nodes = 0;
+    // tile i of the piece, K (kv = 0) or V, into the next slot
+    auto fetch = [&](int i, int kv) {
+      if (!ok) return;
+      if (!wait_warp(bar_empty + 8 * slot, ph)) { ok = false; return; }
+      const uint32_t bar = bar_full + 8 * slot, dst = sm_ring + slot * kSlotBytes;
+      const int j0 = (pc.tile0 + i) * kTile;
+      // the block of every page of the tile (lanes 0 .. 7)
+      int b = 0;
+      const int page = j0 / kP + lane;
+      if (lane < kTile / kP && page * kP < S) {
+        b = a.block_table[(size_t)pc.t * a.max_pages + page];
+        if (b < 0 || b >= a.num_blocks) { flag_error(a.counters, STEP_ERR_BAD_BLOCK); b = 0; }
+      }
+      if (j0 + kTile <= S) {
+        if (lane == 0) mbar_expect_tx(bar, kSlotBytes); else mbar_arrive(bar);
+        __syncwarp();
+        const int pg = lane >> 1, half = lane & 1;
+        const int bb = __shfl_sync(0xffffffffu, b, pg);
+        if (lane < 2 * (kTile / kP))
+          tma_load_3d(dst + half * kHalfSlot + pg * (kP * 128), &map, 0, half,
+                      ((((a.layer * a.num_blocks) + bb) * a.Hkv + h) * 2 + kv) * kP, bar);
+        if (lane == 0) mbar_arrive(bar);
+      } else {
+        // two rows of 16 chunks at a time; a cached row is copied as it is stored, which is the arrangement wanted here
+        const int c = lane & 15;
+        const __nv_bfloat16* draft = (kv ? a.v_draft : a.k_draft) + (((size_t)pc.t * a.T * a.L + a.layer) * a.Hkv + h) * kD + c * 8;
+        const size_t draft_row = (size_t)a.L * a.Hkv * kD;
+#pragma unroll 4
+        for (int x = 0; x < kTile / 2; ++x) {
+          const int rr = 2 * x + (lane >> 4), j = j0 + rr;
+          const int bb = __shfl_sync(0xffffffffu, b, rr / kP);
+          const __nv_bfloat16* src = a.kv;
+          int at = c;
+          const bool real = j < S + nodes;
+          if (j < S)
+            src = a.kv + ((((size_t)a.layer * a.num_blocks + bb) * a.Hkv + h) * 2 + kv) * (kP * kD) + (rr % kP) * kD + c * 8;
+          else {
+            if (real) src = draft + (size_t)(j - S) * draft_row;
+            at = (c & 8) | ((c ^ rr) & 7);
+          }
+          cp_async16_or_zero(dst + (at >> 3) * kHalfSlot + rr * 128 + (at & 7) * 16, src, real);
+        }
+        cp_async_arrive_when_done(bar);
+        if (lane == 0) mbar_arrive(bar);
+      }
+      __syncwarp();
+      if (++slot == kSlots) { slot = 0; ph ^= 1; }
+    };
+    for (long long pos = pos0; pos < end && ok; pos += pc.cnt) {
+      pc = piece_at(s_cum, a.n, HR, pos, end);
+      h = pc.hr / a.groups;
+      S = cached(a, pc.t, false);
+      nodes = nodes_of(a, pc.t, false);
+      if constexpr (kTwoRows) {
+        for (int i = 0; i < pc.cnt; ++i) { fetch(i, 0); fetch(i, 1); }
+      } else {
+        fetch(0, 0);
+        if (pc.cnt > 1) fetch(1, 0);
+        for (int i = 0; i < pc.cnt; ++i) { fetch(i, 1); if (i + 2 < pc.cnt) fetch(i + 2, 0); }
+      }
+    }
+    cp_async_wait_all();
+    if (*s_abort)                                                      // copies in flight still target this CTA's shared memory
+      for (int s = 0; s < kSlots; ++s) {
+        mbar_wait_bounded(bar_full + 8 * s, 0, kDrainNs);
+        mbar_wait_bounded(bar_full + 8 * s, 1, kDrainNs);
+      }
+  } else if (lane == 0) {
+    // ------------------------------------------------ products
+    const uint32_t id_qk = umma_idesc_bf16(kTile), id_pv = umma_idesc_bf16(kD) | (1u << 16);   // B of the second is MN-major
+    int slot = 0;
+    uint32_t ph = 0, ph_q = 0, ph_p[2] = {0, 0};
+    bool ok = true;
+    // waits for the next slot of the ring; its index
+    auto next = [&]() -> int {
+      if (!ok || !wait(bar_full + 8 * slot, ph)) { ok = false; return 0; }
+      fence_async_smem();                                              // rows copied by cp.async came through the generic proxy
+      const int s = slot;
+      if (++slot == kSlots) { slot = 0; ph ^= 1; }
+      return s;
+    };
+    auto scores = [&](int ln, int s) {
+      if (!ok) return;
+      tc_fence_after();
+      const uint32_t qa = sm_q + (kTwoRows ? ln * kQBytes : 0), kb = sm_ring + s * kSlotBytes;
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+        tc_mma_bf16(tmem + ln * 128, umma_desc_sw128(qa + (x >> 2) * (kQBytes / 2) + (x & 3) * 32),
+                    umma_desc_sw128(kb + (x >> 2) * kHalfSlot + (x & 3) * 32), id_qk, x != 0);
+      tc_commit(bar_s + 8 * ln);
+    };
+    auto values = [&](int ln, int s, bool first) {
+      if (!ok || !wait(bar_p + 8 * ln, ph_p[ln])) { ok = false; return; }
+      ph_p[ln] ^= 1;
+      tc_fence_after();
+      const uint32_t vb = sm_ring + s * kSlotBytes;
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+        tc_mma_bf16_ta(tmem + 256 + ln * 128, tmem + ln * 128 + x * 8, umma_desc_v(vb + x * 2048), id_pv, !(first && x == 0));
+    };
+    auto release = [&](int s) { if (ok) tc_commit(bar_empty + 8 * s); };
+    for (long long pos = pos0; pos < end && ok;) {
+      const Piece pc = piece_at(s_cum, a.n, HR, pos, end);
+      if (!wait(bar_q, ph_q)) { ok = false; break; }
+      ph_q ^= 1;
+      if constexpr (kTwoRows) {
+        int k = next();
+        scores(0, k);
+        scores(1, k);
+        release(k);
+        for (int i = 0; i < pc.cnt && ok; ++i) {
+          const int v = next();
+          const bool more = i + 1 < pc.cnt;
+          values(0, v, i == 0);
+          if (more) { k = next(); scores(0, k); }
+          values(1, v, i == 0);
+          release(v);
+          if (more) { scores(1, k); release(k); }
+        }
+      } else {
+        int k = next();
+        scores(0, k);
+        release(k);
+        if (pc.cnt > 1) { k = next(); scores(1, k); release(k); }
+        for (int i = 0; i < pc.cnt && ok; ++i) {
+          const int v = next();
+          values(i & 1, v, i < 2);
+          release(v);
+          if (i + 2 < pc.cnt) { k = next(); scores(i & 1, k); release(k); }
+        }
+      }
+      if (ok) { tc_commit(bar_o); tc_commit(bar_o + 8); }
+      pos += pc.cnt;
+    }
+    tc_commit(bar_drain);                                              // no product is in flight when the tensor memory goes back
+    mbar_wait_bounded(bar_drain, 0);
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kWarpMma) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+
+// Combines the pieces of every sequence that more than one share holds: a warp per query row, lanes over the 128 dims, the
+// pieces in stream order with a running (max, sum, weighted values).  The same bits whatever ran when.
+constexpr int kMergeWarps = 4;
+
+__global__ void __launch_bounds__(kMergeWarps * 32) tree_merge_kernel(TreeArgs a) {
+  extern __shared__ int s_cum[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (warp == 0) build_stream(a, lane, false, s_cum);
+  __syncthreads();
+  wait_for_primary();
+  const int HR = a.Hkv * a.groups;
+  const long long total = (long long)HR * s_cum[a.n];
+  const long long W = (total + a.shares - 1) / a.shares;
+  const long long items = (long long)a.n * a.Hkv * a.rows;
+  for (long long item = (long long)blockIdx.x * kMergeWarps + warp; item < items; item += (long long)gridDim.x * kMergeWarps) {
+    const int r = (int)(item % a.rows);
+    const long long th = item / a.rows;
+    const int t = (int)(th / a.Hkv), h = (int)(th - (long long)t * a.Hkv);
+    const int tiles = s_cum[t + 1] - s_cum[t];
+    const int group = r / a.group_rows, rr = r - group * a.group_rows;
+    const long long start = (long long)HR * s_cum[t] + ((long long)h * a.groups + group) * tiles;
+    const int w0 = (int)(start / W), w1 = (int)((start + tiles - 1) / W);
+    if (w0 == w1) continue;                                            // one piece: written by the attention kernel
+    uint2* out = reinterpret_cast<uint2*>(a.out + (((size_t)t * a.T + r / a.G) * a.Hq + (size_t)h * a.G + r % a.G) * kD) + lane;
+    if (r >= nodes_of(a, t, false) * a.G) { *out = make_uint2(0, 0); continue; }
+    float M = -INFINITY, den = 0.f;
+    float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int w = w0; w <= w1; ++w) {
+      const size_t slot = (size_t)w * 2 + (start <= (long long)w * W ? 0 : 1);
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(a.ws_ml + (slot * a.group_rows + rr) * 2));
+      const float4 o = __ldcg(reinterpret_cast<const float4*>(a.ws_o + (slot * a.group_rows + rr) * kD) + lane);
+      const float Mb = fmaxf(M, ml.x), off = Mb == -INFINITY ? 0.f : Mb;   // a row may see nothing of a piece
+      const float keep = exp2f(M - off), wgt = exp2f(ml.x - off);
+      den = den * keep + wgt * ml.y;
+      num.x = num.x * keep + wgt * o.x; num.y = num.y * keep + wgt * o.y;
+      num.z = num.z * keep + wgt * o.z; num.w = num.w * keep + wgt * o.w;
+      M = Mb;
+    }
+    const float inv = 1.f / den;
+    *out = make_uint2(pack2(num.x * inv, num.y * inv), pack2(num.z * inv, num.w * inv));
+  }
+}
+
+size_t smem_bytes(int n) { return 1024 + 2 * kQBytes + kSlots * kSlotBytes + 32 * 8 + 512 * 4 + 128 * 4 + 16 + (size_t)(n + 1) * 4; }
+
+}  // namespace
+
+namespace stepk {
+
+bool tree_tc_supported(const step_pool* pool, int n) {
+  const kv_pool_config& c = pool->cfg;
+  return c.dtype == STEP_BF16 && c.head_dim == kD && c.page_size == kP && pool->swizzle && n <= kMaxTracesFast && pool->fast_path > 0 &&
+         (long long)c.num_layers * c.num_blocks * c.num_kv_heads * 2 * kP < (1ll << 31) && encode_tiled_fn() != nullptr;
+}
+
+size_t tree_tc_workspace(const step_pool* pool, int T) {
+  const size_t rows = T * pool->G > kHalfRows ? 2 * kHalfRows : kHalfRows;
+  return (size_t)pool->num_sms * 2 * rows * (kD + 2) * sizeof(float);
+}
+
+int tree_tc_launch(step_pool* pool, int layer, const void* q, const void* k_draft, const void* v_draft, const int32_t* parents,
+                   const int32_t* n_nodes, int T, const int32_t* block_table, const int32_t* seq_lens, int n, void* out,
+                   void* workspace, cudaStream_t s) {
+  const Geo g = geo_of(pool);
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (!enc) return STEP_ERR_CUDA;
+  // the pool as rows of 128 dims, a row as two halves of 128 bytes; a box is one half of a page's 16 K or V rows
+  CUtensorMap map;
+  const cuuint64_t dims[3] = {64, 2, (cuuint64_t)g.L * g.num_blocks * g.Hkv * 2 * kP};
+  const cuuint64_t strides[2] = {128, 256};
+  const cuuint32_t box[3] = {64, 1, kP};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  if (enc(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, pool->cfg.kv_storage, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+          CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return STEP_ERR_CUDA;
+  TreeArgs a;
+  a.kv = (const __nv_bfloat16*)pool->cfg.kv_storage;
+  a.q = (const __nv_bfloat16*)q; a.k_draft = (const __nv_bfloat16*)k_draft; a.v_draft = (const __nv_bfloat16*)v_draft;
+  a.parents = parents; a.n_nodes = n_nodes; a.block_table = block_table; a.seq_lens = seq_lens;
+  a.out = (__nv_bfloat16*)out;
+  a.counters = pool->v.counters;
+  a.n = n; a.T = T; a.Hq = g.Hq; a.Hkv = g.Hkv; a.G = g.G; a.L = g.L; a.layer = layer; a.max_pages = g.max_pages; a.num_blocks = g.num_blocks;
+  a.rows = T * g.G;
+  a.group_rows = a.rows > kHalfRows ? 2 * kHalfRows : kHalfRows;
+  a.groups = (a.rows + a.group_rows - 1) / a.group_rows;
+  a.shares = pool->num_sms;
+  a.scale_log2 = 1.4426950408889634f / sqrtf((float)kD);
+  a.ws_o = (float*)workspace;
+  a.ws_ml = a.ws_o + (size_t)a.shares * 2 * a.group_rows * kD;
+  const size_t smem = smem_bytes(n);
+  auto kern = a.group_rows > kHalfRows ? tree_tc_kernel<true> : tree_tc_kernel<false>;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return STEP_ERR_CUDA;
+  kern<<<a.shares, kThreads, smem, s>>>(map, a);
+  if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
+  long long mgrid = ((long long)n * g.Hkv * a.rows + kMergeWarps - 1) / kMergeWarps;
+  if (mgrid > 2ll * pool->num_sms) mgrid = 2ll * pool->num_sms;
+  if (launch_dependent(tree_merge_kernel, dim3((unsigned)mgrid), dim3(kMergeWarps * 32), (size_t)(n + 1) * 4, s, a) != cudaSuccess) return STEP_ERR_CUDA;
+  return launch_ok();
+}
+
+}  // namespace stepk
