@@ -284,22 +284,33 @@ class KVPool:
     def _run(self, fn, stream, workspace, size_args, call):
         """call(workspace pointer, bytes, stream) with the pool's device current; without a `workspace` (uint8 tensor) one
         is taken from torch's allocator on the call's stream."""
-        with torch.cuda.device(self.device), torch.cuda.stream(stream):
-            need = C.c_size_t()
-            if size_args is not None:
-                _check(fn + "_workspace_bytes", getattr(lib(), size_args[0])(self.handle, *size_args[1:], C.byref(need)))
-                if workspace is None:
-                    workspace = torch.empty(max(1, need.value), dtype=torch.uint8, device=self.device)
-                elif workspace.device != self.device or not workspace.is_contiguous():
-                    raise StepError(fn, 1)
-            _check(fn, call(_ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                            _stream()))
+        if stream is not None or torch.cuda.current_device() != self._device().index:
+            with torch.cuda.device(self._device()), torch.cuda.stream(stream):
+                return self._run(fn, None, workspace, size_args, call)
+        nbytes = 0
+        if size_args is not None:
+            if workspace is None:
+                need = C.c_size_t()
+                _check(size_args[0], getattr(lib(), size_args[0])(self.handle, *size_args[1:], C.byref(need)))
+                workspace, nbytes = torch.empty(max(1, need.value), dtype=torch.uint8, device=self._device()), need.value
+            elif workspace.device != self._device() or not workspace.is_contiguous():
+                raise StepError(fn, 1)
+            else:
+                nbytes = workspace.numel() * workspace.element_size()
+        _check(fn, call(_ptr(workspace), nbytes, _stream()))
 
     def _like_table(self, fn, n, block_table, seq_lens):
         _expect(fn, self._device(), (block_table, (n, self.max_pages_per_trace), torch.int32), (seq_lens, (n,), torch.int32))
 
     def _device(self):
         return self.kv_storage.device
+
+    def _empty(self, shape, dtype, stream):
+        """A tensor of torch's allocator for use on `stream`."""
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=self._device())
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=self._device())
 
     def decode_attention_tree(self, layer, q, k_draft, v_draft, parents, block_table, seq_lens, n_nodes=None, out=None,
                               workspace=None, stream=None):
@@ -313,8 +324,7 @@ class KVPool:
         _expect(fn, dev, (q, rows, dt), (k_draft, draft, dt), (v_draft, draft, dt), (parents, (n, T), torch.int32),
                 (n_nodes, (n,), torch.int32), (out, rows, dt))
         if out is None:
-            with torch.cuda.stream(stream):
-                out = torch.empty(rows, dtype=dt, device=dev)
+            out = self._empty(rows, dt, stream)
         self._run(fn, stream, workspace, (fn + "_workspace_bytes", n, T), lambda ws, nb, st: lib().decode_attention_tree(
             self.handle, layer, _ptr(q), _ptr(k_draft), _ptr(v_draft), _ptr(parents), _ptr(n_nodes), T, _ptr(block_table),
             _ptr(seq_lens), n, _ptr(out), ws, nb, st))
@@ -343,8 +353,7 @@ class KVPool:
         _expect(fn, dev, (q, rows, self.torch_dtype), (weight_sum, (n, self.num_kv_heads, stride), torch.float32),
                 (out, rows, torch.float32))
         if out is None:
-            with torch.cuda.stream(stream):
-                out = torch.empty(rows, dtype=torch.float32, device=dev)
+            out = self._empty(rows, torch.float32, stream)
         self._run(fn, stream, workspace, (fn + "_workspace_bytes", n, stride), lambda ws, nb, st: lib().decode_attention_weights(
             self.handle, layer, _ptr(q), _ptr(block_table), _ptr(seq_lens), n, _ptr(out), _ptr(weight_sum), stride, ws, nb, st))
         return out

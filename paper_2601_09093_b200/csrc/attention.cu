@@ -139,6 +139,10 @@ struct AttnArgs {
   int n_static;                    // equal shares of the static stream: warps of the attention launch
   int merge_ctas;                  // CTAs of the launch that combines the pieces, at most (one per SM)
   unsigned long long wait_ns;      // limit of the wait for one page copy
+  // decode_attention_weights only (kCount)
+  float* scores;                   // [n][Hq][score_stride] log2-scaled scores
+  long long score_stride;          // a multiple of the page size; positions behind it are not recorded
+  float* row_ml;                   // [n][Hq][2] (max, sum) of every row
 };
 
 // kMode of attn_mma_kernel: the plain kernel; the pass over the shared pages, whose 16 query rows are the G heads of
@@ -162,6 +166,15 @@ __device__ inline void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_
 __device__ inline uint32_t pack_bf16(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
+}
+
+// What the bf16 pair `high` leaves of (x, y), as two more bf16 pairs: each difference is exact in fp32.
+__device__ inline void split_rest(float x, float y, uint32_t high, uint32_t& mid, uint32_t& low) {
+  const float2 h = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&high));
+  const float rx = x - h.x, ry = y - h.y;
+  mid = pack_bf16(rx, ry);
+  const float2 m = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&mid));
+  low = pack_bf16(rx - m.x, ry - m.y);
 }
 
 // Largest t with Hkv * cum[t] <= pos (cum is an exclusive prefix sum over the launch's sequences).
@@ -276,6 +289,12 @@ __device__ inline void build_partition(const AttnArgs& a, int n, int lane, bool 
   if (lane == 0) { cum[n] = run_a; cumc[n] = run_c; *chunk = C; }
 }
 
+// kCount (decode_attention_weights): every score is also stored, every row's final (max, sum) too, and the probabilities
+// enter the second product as three bf16 terms (high, middle and low bits: 24 bits in all) instead of one, so that out
+// is accurate to fp32.  Up to eight query heads a KV head occupy the tile's upper eight rows only; the middle terms then
+// ride in its lower eight, and the low terms cost one more product per page: 48 instead of 32 instructions, which the
+// stream of pages still hides (64 traces of 4.6k to 16.9k tokens, 32 / 8 heads: see weights.cu).
+
 // How a launch's pages are spread over the SMs.
 //
 // Every (trace, KV head) sequence is cut in two: its first pages - all but dyn16 sixteenths - belong to the "static"
@@ -290,8 +309,9 @@ __device__ inline void build_partition(const AttnArgs& a, int n, int lane, bool 
 // the piece's slot; a second launch (attn_merge_kernel, a programmatic dependent of this one) combines the pieces
 // of every sequence.  (An earlier form combined them in this kernel, by tickets: the fence and the atomic round trip
 // at the end of every chunk cost more, in a saturated memory system, than the hand-out gained.)
-template <int kWarps, int kStages, bool kRows16, int kMode>
+template <int kWarps, int kStages, bool kRows16, int kMode, bool kCount>
 __global__ void __launch_bounds__(kWarps * 32, 1) attn_mma_kernel(AttnArgs a) {
+  static_assert(!kCount || kMode == kPlain, "scores are kept by the plain kernel only");
   static_assert(kMode != kPrefixPass || kRows16, "the prefix pass uses all 16 rows of the tile");
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char* s_pages = smem;                                              // [kWarps][kStages][8 KiB]
@@ -533,6 +553,20 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_mma_kernel(AttnArgs a) {
         s1[2] = v10 ? s1[2] * a.scale_log2 : -INFINITY; s1[3] = v11 ? s1[3] * a.scale_log2 : -INFINITY;
       }
     }
+    if constexpr (kCount) {
+      if ((long long)cc.page * kP < a.score_stride) {          // (a page lies before the stride or behind it)
+        before_first_write();
+        float* sc = a.scores + ((size_t)cc.t * a.Hq + (size_t)cc.h * G) * a.score_stride + (size_t)cc.page * kP + 2 * tq;
+        if (g_row < G) {
+          *reinterpret_cast<float2*>(sc + (size_t)g_row * a.score_stride) = make_float2(s0[0], s0[1]);
+          *reinterpret_cast<float2*>(sc + (size_t)g_row * a.score_stride + 8) = make_float2(s1[0], s1[1]);
+        }
+        if (kRows16 && g_row + 8 < G) {
+          *reinterpret_cast<float2*>(sc + (size_t)(g_row + 8) * a.score_stride) = make_float2(s0[2], s0[3]);
+          *reinterpret_cast<float2*>(sc + (size_t)(g_row + 8) * a.score_stride + 8) = make_float2(s1[2], s1[3]);
+        }
+      }
+    }
     float mx0 = fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s1[0], s1[1]));
     mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 1));
     mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 2));
@@ -542,6 +576,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_mma_kernel(AttnArgs a) {
     const float p00 = exp2f(s0[0] - mn0), p01 = exp2f(s0[1] - mn0), p10 = exp2f(s1[0] - mn0), p11 = exp2f(s1[1] - mn0);
     l_run[0] = l_run[0] * corr0 + (p00 + p01) + (p10 + p11);
     uint32_t pa0 = pack_bf16(p00, p01), pa2 = pack_bf16(p10, p11), pa1 = 0u, pa3 = 0u;
+    // kCount: what the first term leaves, in two more terms (mid .., low ..); rows + 8: their own or, below, the middle
+    uint32_t mid0 = 0u, mid2 = 0u, low0 = 0u, low2 = 0u, mid1 = 0u, mid3 = 0u, low1 = 0u, low3 = 0u;
+    if constexpr (kCount) { split_rest(p00, p01, pa0, mid0, low0); split_rest(p10, p11, pa2, mid2, low2); }
     float corr1 = 1.f;
     if (kRows16) {
       float mx1 = fmaxf(fmaxf(s0[2], s0[3]), fmaxf(s1[2], s1[3]));
@@ -553,10 +590,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_mma_kernel(AttnArgs a) {
       const float q00 = exp2f(s0[2] - mn1), q01 = exp2f(s0[3] - mn1), q10 = exp2f(s1[2] - mn1), q11 = exp2f(s1[3] - mn1);
       l_run[1] = l_run[1] * corr1 + (q00 + q01) + (q10 + q11);
       pa1 = pack_bf16(q00, q01); pa3 = pack_bf16(q10, q11);
+      if constexpr (kCount) { split_rest(q00, q01, pa1, mid1, low1); split_rest(q10, q11, pa3, mid3, low3); }
+    } else if constexpr (kCount) {
+      pa1 = mid0; pa3 = mid2;
     }
     // rescale O only when some row's maximum moved (warp-uniform branch)
     const bool moved = (corr0 != 1.f) || (kRows16 && corr1 != 1.f);
-    if (__any_sync(0xffffffffu, moved)) {
+    if (!kCount && __any_sync(0xffffffffu, moved)) {
 #pragma unroll
       for (int dt = 0; dt < 16; ++dt) {
         o_acc[dt][0] *= corr0; o_acc[dt][1] *= corr0;
@@ -570,8 +610,32 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_mma_kernel(AttnArgs a) {
       const uint32_t addr = vpage + v_row * 256 + ((((chunk & 8) | ((chunk ^ v_row) & 7))) << 4);
       uint32_t b0, b1, b2, b3;
       ldsm_x4_t(addr, b0, b1, b2, b3);
-      mma_bf16(o_acc[2 * dp], pa0, pa1, pa2, pa3, b0, b1);
-      mma_bf16(o_acc[2 * dp + 1], pa0, pa1, pa2, pa3, b2, b3);
+      if constexpr (kCount) {
+        // a page's products start from zero and are added to the running sums in fp32: the tensor cores' own
+        // accumulation cuts low bits off, always downwards, and over a thousand pages that adds up (out 5.6e-6 off where
+        // it is 1e-6 this way)
+        float t0[4] = {0.f, 0.f, 0.f, 0.f}, t1[4] = {0.f, 0.f, 0.f, 0.f};
+        mma_bf16(t0, low0, low1, low2, low3, b0, b1);
+        mma_bf16(t1, low0, low1, low2, low3, b2, b3);
+        if constexpr (kRows16) {
+          mma_bf16(t0, mid0, mid1, mid2, mid3, b0, b1);
+          mma_bf16(t1, mid0, mid1, mid2, mid3, b2, b3);
+        }
+        mma_bf16(t0, pa0, pa1, pa2, pa3, b0, b1);
+        mma_bf16(t1, pa0, pa1, pa2, pa3, b2, b3);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          o_acc[2 * dp][x] = fmaf(o_acc[2 * dp][x], corr0, kRows16 ? t0[x] : t0[x] + t0[x + 2]);       // (+ the middle terms)
+          o_acc[2 * dp + 1][x] = fmaf(o_acc[2 * dp + 1][x], corr0, kRows16 ? t1[x] : t1[x] + t1[x + 2]);
+          if constexpr (kRows16) {
+            o_acc[2 * dp][x + 2] = fmaf(o_acc[2 * dp][x + 2], corr1, t0[x + 2]);
+            o_acc[2 * dp + 1][x + 2] = fmaf(o_acc[2 * dp + 1][x + 2], corr1, t1[x + 2]);
+          }
+        }
+      } else {
+        mma_bf16(o_acc[2 * dp], pa0, pa1, pa2, pa3, b0, b1);
+        mma_bf16(o_acc[2 * dp + 1], pa0, pa1, pa2, pa3, b2, b3);
+      }
     }
     __syncwarp();
     --in_flight;
@@ -612,6 +676,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_mma_kernel(AttnArgs a) {
         }
       } else if (complete) {
         float* ob = a.out + ((size_t)cc.t * a.Hq + (size_t)cc.h * G) * kD;
+        if constexpr (kCount) {
+          float2* rm = reinterpret_cast<float2*>(a.row_ml) + (size_t)cc.t * a.Hq + (size_t)cc.h * G;
+          if (tq == 0 && g_row < G) rm[g_row] = make_float2(m_run[0], l0);
+          if (kRows16 && tq == 0 && g_row + 8 < G) rm[g_row + 8] = make_float2(m_run[1], l1);
+        }
         if (g_row < G) {
           float ws = 1.f, wp = 0.f, lp = 0.f;
           const float* po = nullptr;
@@ -723,7 +792,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_mma_kernel(AttnArgs a) {
 // had to queue for an SM would hold back the next layer's launch until this layer is over.)
 constexpr int kMergeBatch = 8, kMergeWarps = 4;
 
-template <int kMode>
+template <int kMode, bool kCount>
 __global__ void __launch_bounds__(kMergeWarps * 32, 5) attn_merge_kernel(AttnArgs a) {
   extern __shared__ int s_part[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -820,6 +889,8 @@ __global__ void __launch_bounds__(kMergeWarps * 32, 5) attn_merge_kernel(AttnArg
     } else {
       float* og = a.out + ((size_t)t * a.Hq + (size_t)h * G + g) * kD;
       const float inv = 1.f / den;
+      if constexpr (kCount)
+        if (lane == 0) reinterpret_cast<float2*>(a.row_ml)[(size_t)t * a.Hq + (size_t)h * G + g] = make_float2(M, den);
       reinterpret_cast<float4*>(og)[lane] = make_float4(num.x * inv, num.y * inv, num.z * inv, num.w * inv);
     }
   }
@@ -830,12 +901,12 @@ constexpr int kWarpsDefault = 8, kStagesDefault = 3;
 // The attention kernel, then the kernel that combines its pieces as its programmatic dependent.
 // dependent: the attention launch itself may be scheduled before the kernel ahead of it in the stream has completed
 // (see the kernel's note on its first write).
-template <int kWarps, int kStages, bool kRows16, int kMode>
+template <int kWarps, int kStages, bool kRows16, int kMode, bool kCount = false>
 int launch_one(AttnArgs a, int grid, cudaStream_t s, bool dependent = false) {
   const int n_seq = kMode == kPrefixPass ? a.n_bundles : a.n;
   const size_t smem = (size_t)kWarps * kStages * kPageBytes + (size_t)kWarps * kStages * 8 + (size_t)(3 * n_seq + 3) * 4;
   a.n_static = grid * kWarps;
-  auto kern = attn_mma_kernel<kWarps, kStages, kRows16, kMode>;
+  auto kern = attn_mma_kernel<kWarps, kStages, kRows16, kMode, kCount>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return STEP_ERR_CUDA;
   if (dependent) {
     if (launch_dependent(kern, dim3(grid), dim3(kWarps * 32), smem, s, a) != cudaSuccess) return STEP_ERR_CUDA;
@@ -846,17 +917,17 @@ int launch_one(AttnArgs a, int grid, cudaStream_t s, bool dependent = false) {
   const int rows = kMode == kPrefixPass ? a.tpb * a.G : a.G;
   long long mgrid = ((long long)n_seq * a.Hkv * rows + kMergeWarps - 1) / kMergeWarps;
   if (mgrid > a.merge_ctas) mgrid = a.merge_ctas;
-  if (launch_dependent(attn_merge_kernel<kMode>, dim3((int)mgrid), dim3(kMergeWarps * 32), (size_t)(3 * n_seq + 3) * 4, s, a) != cudaSuccess) return STEP_ERR_CUDA;
+  if (launch_dependent(attn_merge_kernel<kMode, kCount>, dim3((int)mgrid), dim3(kMergeWarps * 32), (size_t)(3 * n_seq + 3) * 4, s, a) != cudaSuccess) return STEP_ERR_CUDA;
   return launch_ok();
 }
 
-template <int kWarps, int kStages, int kMode>
+template <int kWarps, int kStages, int kMode, bool kCount = false>
 int launch_mma(const step_pool* pool, const AttnArgs& a, cudaStream_t s, bool dependent = false) {
   int grid = pool->attn_grid;
   if (grid * kWarps > kMaxPartitions) grid = kMaxPartitions / kWarps;
   if (grid < 1) grid = 1;
-  return a.G > 8 ? launch_one<kWarps, kStages, true, kMode>(a, grid, s, dependent)
-                 : launch_one<kWarps, kStages, false, kMode>(a, grid, s, dependent);
+  return a.G > 8 ? launch_one<kWarps, kStages, true, kMode, kCount>(a, grid, s, dependent)
+                 : launch_one<kWarps, kStages, false, kMode, kCount>(a, grid, s, dependent);
 }
 
 void fill_args(AttnArgs& a, const step_pool* pool, const Geo& g, int layer, const void* q, const int32_t* block_table,
@@ -874,6 +945,7 @@ void fill_args(AttnArgs& a, const step_pool* pool, const Geo& g, int layer, cons
   a.n_static = 0;                                      // set by the launcher
   a.merge_ctas = pool->num_sms;
   a.wait_ns = pool->wait_limit_ns;
+  a.scores = nullptr; a.score_stride = 0; a.row_ml = nullptr;
 }
 
 bool mma_shape(const step_pool* pool, const Geo& g, int n) {
@@ -881,6 +953,16 @@ bool mma_shape(const step_pool* pool, const Geo& g, int n) {
 }
 
 }  // namespace
+
+bool stepk::attn_mma_covers(const step_pool* pool, int n) { return pool->fast_path > 0 && mma_shape(pool, geo_of(pool), n); }
+
+int stepk::attn_mma_scores(step_pool* pool, int layer, const void* q, const int32_t* block_table, const int32_t* seq_lens, int n,
+                           void* out, float* scores, long long score_stride, float* row_ml, cudaStream_t s) {
+  AttnArgs a;
+  fill_args(a, pool, geo_of(pool), layer, q, block_table, seq_lens, n, out);
+  a.scores = scores; a.score_stride = score_stride; a.row_ml = row_ml;
+  return launch_mma<kWarpsDefault, kStagesDefault, kPlain, true>(pool, a, s);
+}
 
 // How a launch relates to the kernel before it in the stream: an ordinary launch; a programmatic dependent of
 // another launch of this kernel on the same pool (waits in front of its first write); a programmatic dependent of

@@ -10,7 +10,8 @@
 // order, which is what makes "the most recent ones" mean the same at the next call.
 //
 // Three launches, each a programmatic dependent of the one before:
-//   1. evict_plan_kernel    one CTA: which traces are cut; a block of its own for every kept page that is shared
+//   1. evict_plan_kernel    a cluster of CTAs: which traces are cut; a block of its own for every kept page that is shared;
+//                           the list of the pages that drop a reference
 //   2. evict_move_kernel    one CTA per (KV head, trace, layer): selection, then the rows and weights move
 //   3. evict_finish_kernel  a cluster of CTAs: references dropped, free list, block table, lengths
 #include "release.cuh"
@@ -29,52 +30,61 @@ struct EvictArgs {
   int stride, budget, recent;
   int32_t* kept;                              // [L, n, Hkv, budget]
   int32_t* old_len;                           // workspace [n]: cached positions of the entry before the call; -1: left alone
-  int32_t* off;                               // workspace [n + 1]
+  int32_t* need;                              // workspace [n]: blocks of its own that it takes; -1: left alone
+  int32_t* base;                              // workspace [n + 1]: blocks taken by the entries before it (then of all)
+  int32_t* off;                               // workspace [n + 1]: pages dropped by the entries before it (then by all)
   int32_t* new_row;                           // workspace [n, pages of a budget]
+  int2* drop;                                 // workspace [n * max_pages]: (entry, page) of every reference dropped, in order
   int cpr;
+  int cache_keys;                             // positions whose keys evict_move_kernel keeps in shared memory
 };
 
-constexpr int kPlanThreads = 1024;
-
-__global__ void __launch_bounds__(kPlanThreads) evict_plan_kernel(EvictArgs a) {
-  extern __shared__ int sm[];
-  dependents_may_launch();
-  int* s_need = sm;                   // blocks wanted for shared kept pages; -1: the entry is left alone
-  int* s_off = sm + a.n;
+// Pages are examined by a warp per entry, spread over the cluster: a kept page's reference count is a scattered 4-byte
+// read, and one SM alone takes 10 us for the 16,000 of them that 64 traces of 4,096 positions have.
+__global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kPruneThreads, 1) evict_plan_kernel(EvictArgs a) {
+  namespace cg = cooperative_groups;
+  cg::cluster_group cluster = cg::this_cluster();
+  __shared__ int s_warp[33];
   __shared__ int s_fc;
+  dependents_may_launch();
   const DevViews& v = a.v;
   const Geo& g = a.g;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nwarps = blockDim.x >> 5;
+  const int rank = (int)cluster.block_rank(), lane = threadIdx.x & 31;
+  const int warp = (threadIdx.x >> 5) * kClusterCtas + rank, nwarps = kPruneThreads / 32 * kClusterCtas;
   const int nbp = (a.budget + g.P - 1) / g.P;
-  for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
-    const int t = a.ids[i];
-    if (t >= 0 && t < g.max_traces) v.prune_rank[t] = 0x7fffffff;
+  // first place of every listed trace (a repeat is flagged and left alone)
+  if (rank == 0) {
+    for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
+      const int t = a.ids[i];
+      if (t >= 0 && t < g.max_traces) v.prune_rank[t] = 0x7fffffff;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
+      const int t = a.ids[i];
+      if (t >= 0 && t < g.max_traces) atomicMin(&v.prune_rank[t], i);
+    }
+    __threadfence();
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
-    const int t = a.ids[i];
-    if (t >= 0 && t < g.max_traces) atomicMin(&v.prune_rank[t], i);
-  }
-  __syncthreads();
+  cluster.sync();
   for (int i = warp; i < a.n; i += nwarps) {
     const int t = a.ids[i];
-    int need = -1;
-    if (t < 0 || t >= g.max_traces || !v.live[t] || v.prune_rank[t] != i) {
+    int need = -1, S = -1;
+    if (t < 0 || t >= g.max_traces || !v.live[t] || __ldcg(&v.prune_rank[t]) != i) {
       if (lane == 0) flag_error(v.counters, STEP_ERR_BAD_TRACE);
     } else {
-      const int S = v.seq_lens[t];
+      S = v.seq_lens[t];
       if (S > a.stride && S > a.budget) {
         if (lane == 0) flag_error(v.counters, STEP_ERR_CAPACITY);          // positions without a weight
       } else if (S > a.budget) {
-        // the pages that stay, by block; a block out of range leaves the whole entry alone
         const int32_t* row = v.block_table + (size_t)t * g.max_pages;
         const int pages = (S + g.P - 1) / g.P;
         int shared = 0;
         bool bad = false;
+#pragma unroll 4
         for (int p = lane; p < pages; p += 32) {
           const int b = row[p];
-          if (b < 0 || b >= g.num_blocks) bad = true;
-          else if (p < nbp && v.refcount[b] > 1) ++shared;
+          if (b < 0 || b >= g.num_blocks) bad = true;                      // (leaves the whole entry alone)
+          else if (p < nbp) shared += v.refcount[b] > 1;
         }
         bad = __any_sync(0xffffffffu, bad);
 #pragma unroll
@@ -83,47 +93,83 @@ __global__ void __launch_bounds__(kPlanThreads) evict_plan_kernel(EvictArgs a) {
         else need = shared;
       }
     }
-    if (lane == 0) s_need[i] = need;
+    if (lane == 0) { a.need[i] = need; a.old_len[i] = S; }
   }
-  __syncthreads();
-  if (threadIdx.x == 0) {
+  __threadfence();
+  cluster.sync();
+  if (rank == 0) {
+    // the free list serves everybody, or a serial walk decides who is left alone
     const int fc = v.counters[C_FREE_COUNT];
-    int remaining = fc, pages = 0;
-    for (int i = 0; i < a.n; ++i) {
-      a.off[i] = pages;
-      const int need = s_need[i];
-      if (need < 0) continue;
-      if (need > remaining) { s_need[i] = -1; flag_error(v.counters, STEP_ERR_NO_BLOCKS); continue; }
-      s_off[i] = fc - remaining;
-      remaining -= need;
-      pages += (v.seq_lens[a.ids[i]] + g.P - 1) / g.P;
+    int taken = 0;
+    for (int i0 = 0; i0 < a.n; i0 += blockDim.x) {
+      const int i = i0 + threadIdx.x;
+      int total;
+      block_excl_scan(i < a.n ? max(__ldcg(&a.need[i]), 0) : 0, s_warp, &total);
+      taken += total;
     }
-    a.off[a.n] = pages;
-    s_fc = fc;
-    v.counters[C_FREE_COUNT] = remaining;
+    if (taken > fc && threadIdx.x == 0) {
+      int remaining = fc;
+      for (int i = 0; i < a.n; ++i) {
+        const int need = __ldcg(&a.need[i]);
+        if (need > remaining) { a.need[i] = -1; flag_error(v.counters, STEP_ERR_NO_BLOCKS); }
+        else if (need > 0) remaining -= need;
+      }
+    }
+    __syncthreads();
+    int run_b = 0, run_p = 0;
+    for (int i0 = 0; i0 < a.n; i0 += blockDim.x) {
+      const int i = i0 + threadIdx.x;
+      int need = 0, pages = 0;
+      if (i < a.n) {
+        need = __ldcg(&a.need[i]);
+        if (need >= 0) pages = need + (__ldcg(&a.old_len[i]) + g.P - 1) / g.P - nbp;
+        else { need = 0; a.old_len[i] = -1; }
+      }
+      int total_b, total_p;
+      const int at_b = run_b + block_excl_scan(need, s_warp, &total_b);
+      const int at_p = run_p + block_excl_scan(pages, s_warp, &total_p);
+      if (i < a.n) { a.base[i] = at_b; a.off[i] = at_p; }
+      run_b += total_b; run_p += total_p;
+    }
+    if (threadIdx.x == 0) { a.base[a.n] = run_b; a.off[a.n] = run_p; v.counters[C_FREE_COUNT] = fc - run_b; }
+    __threadfence();
   }
+  cluster.sync();
+  if (threadIdx.x == 0) s_fc = __ldcg(&v.counters[C_FREE_COUNT]) + __ldcg(&a.base[a.n]);     // before this call
   __syncthreads();
   for (int i = warp; i < a.n; i += nwarps) {
-    if (s_need[i] < 0) { if (lane == 0) a.old_len[i] = -1; continue; }
-    const int t = a.ids[i];
-    const int32_t* row = v.block_table + (size_t)t * g.max_pages;
+    if (__ldcg(&a.old_len[i]) < 0) continue;
+    const int pages = (__ldcg(&a.old_len[i]) + g.P - 1) / g.P;
+    const int32_t* row = v.block_table + (size_t)a.ids[i] * g.max_pages;
     int32_t* to = a.new_row + (size_t)i * nbp;
-    int taken = s_fc - 1 - s_off[i];
-    for (int p0 = 0; p0 < nbp; p0 += 32) {
-      const int p = p0 + lane;
-      const int b = p < nbp ? row[p] : -1;
-      const bool shared = b >= 0 && v.refcount[b] > 1;
-      const unsigned who = __ballot_sync(0xffffffffu, shared);
-      if (p < nbp) to[p] = shared ? v.free_list[taken - __popc(who & ((1u << lane) - 1))] : b;
-      taken -= __popc(who);
+    const bool any = __ldcg(&a.need[i]) > 0;
+    int taken = s_fc - 1 - __ldcg(&a.base[i]);
+    int2* out = a.drop + __ldcg(&a.off[i]);
+    if (any) {
+      for (int p0 = 0; p0 < nbp; p0 += 32) {
+        const int p = p0 + lane;
+        const int b = p < nbp ? row[p] : -1;
+        const bool shared = b >= 0 && v.refcount[b] > 1;
+        const unsigned who = __ballot_sync(0xffffffffu, shared);
+        const int before = __popc(who & ((1u << lane) - 1));
+        if (p < nbp) to[p] = shared ? v.free_list[taken - before] : b;
+        if (shared) out[before] = make_int2(i, p);
+        taken -= __popc(who);
+        out += __popc(who);
+      }
+    } else {
+#pragma unroll 4
+      for (int p = lane; p < nbp; p += 32) to[p] = row[p];
     }
-    if (lane == 0) a.old_len[i] = v.seq_lens[t];
+    for (int p = nbp + lane; p < pages; p += 32) out[p - nbp] = make_int2(i, p);
   }
 }
 
 // ---------------------------------------------------------------- selection and moves
 constexpr int kMoveThreads = 256, kMoveWarps = kMoveThreads / 32;
 constexpr int kBins = 2048;                   // selection by digits of 11, 11 and 10 bits
+constexpr int kMostCachedKeys = 12288;        // 48 KiB of keys: three CTAs per SM still fit
+constexpr int kBatch = 8;                     // rows a warp has in flight
 
 // Larger weight -> larger key; NaN below everything; the two zeros are equal.
 __device__ inline uint32_t weight_key(float w) {
@@ -132,32 +178,14 @@ __device__ inline uint32_t weight_key(float w) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// Exclusive prefix sum over the CTA of kMoveThreads; *total gets the sum.
-__device__ inline int move_scan(int x, int* s_warp, int* total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int incl = x;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int u = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += u;
-  }
-  __syncthreads();
-  if (lane == 31) s_warp[warp] = incl;
-  __syncthreads();
-  int before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kMoveWarps; ++w) {
-    const int c = s_warp[w];
-    if (w < warp) before += c;
-    all += c;
-  }
-  *total = all;
-  return before + incl - x;
-}
-
+// What bounds it: for a cut of a few positions the passes over the weights (each a read of shared memory, or of L2 for
+// long caches) and the copies' latency; the positions are split into one contiguous run per warp, so that ranks need one
+// exchange of counts between the warps and none per step.
 __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(EvictArgs a) {
-  __shared__ int s_hist[kBins];
-  __shared__ int s_warp[kMoveWarps];
+  extern __shared__ uint32_t s_key[];                   // [cache_keys]
+  __shared__ int s_hist[kBins];                         // the histogram, then the list of positions that move
+  __shared__ int s_cnt[kMoveWarps][4];                  // per warp: above and equal in [0, m), above and equal in [m, first)
+  __shared__ int s_scan[kMoveWarps];
   __shared__ int s_digit, s_left;
   const Geo& g = a.g;
   const int h = blockIdx.x, i = blockIdx.y, l = blockIdx.z;
@@ -176,153 +204,210 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(EvictArgs a) {
   }
   const int first = S - a.recent, m = a.budget - a.recent;
 
-  // ---- the m-th largest key of [0, first), and how many of the positions that have it are chosen
-  uint32_t prefix = 0;
-  int want = m;                                         // still to be found among the keys that share the prefix
-  if (m > 0) {
-#pragma unroll 1
-    for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bits = pass == 2 ? 10 : 11;
-      for (int b = tid; b < kBins; b += kMoveThreads) s_hist[b] = 0;
-      __syncthreads();
-      for (int j = tid; j < first; j += kMoveThreads) {
-        const uint32_t k = weight_key(w[j]);
-        if (pass == 0 || (k >> (shift + bits)) == prefix) atomicAdd(&s_hist[(k >> shift) & ((1u << bits) - 1)], 1);
-      }
-      __syncthreads();
-      // bins from the top: thread x owns bins [hi - 8 x - 7, hi - 8 x]
-      constexpr int per = kBins / kMoveThreads;
-      int c[per], sum = 0;
-#pragma unroll
-      for (int x = 0; x < per; ++x) { c[x] = s_hist[kBins - 1 - (tid * per + x)]; sum += c[x]; }
-      int total;
-      int at = move_scan(sum, s_warp, &total);
-#pragma unroll
-      for (int x = 0; x < per; ++x) {
-        if (at < want && at + c[x] >= want) { s_digit = kBins - 1 - (tid * per + x); s_left = want - at; }
-        at += c[x];
-      }
-      __syncthreads();
-      prefix = (prefix << bits) | (uint32_t)s_digit;
-      want = s_left;
-      __syncthreads();
-    }
+  // ---- the m-th largest key of [0, first), and how many of the positions that have it are chosen (`want`): position j is
+  // chosen if its key is above the threshold, or equal to it and among the first `want` such positions
+  const bool in_smem = first <= a.cache_keys;
+  if (in_smem) {
+#pragma unroll 4
+    for (int j = tid; j < first; j += kMoveThreads) s_key[j] = weight_key(w[j]);
   }
-  // position j is chosen if its key is above the threshold, or equal to it and among the first `want` such positions
-
-  // ---- the chosen positions from m on, ascending, into the last places of [0, m) of the list.  (Its free slots are
-  // filled below in ascending order: the place a moving position waits in lies at or behind the slot that takes it.)
-  int equal = 0;                                        // positions so far whose key equals the threshold
-  int moving = 0;
-  if (m > 0) {
-    // how many come from [m, first): the chosen ones of [0, m) are counted on the way
-    int stay = 0;
-    for (int j0 = 0; j0 < m; j0 += kMoveThreads) {
-      const int j = j0 + tid;
-      const uint32_t k = j < m ? weight_key(w[j]) : 0u;
-      const bool eq = j < m && k == prefix;
-      int n_eq;
-      const int before = move_scan(eq, s_warp, &n_eq);
-      const bool c = j < m && (k > prefix || (eq && equal + before < want));
-      stay += __syncthreads_count(c);
-      equal += n_eq;
-    }
-    moving = m - stay;
-    int put = m - moving;
-    for (int j0 = m; j0 < first && put < m; j0 += kMoveThreads) {
-      const int j = j0 + tid;
-      const uint32_t k = j < first ? weight_key(w[j]) : 0u;
-      const bool eq = j < first && k == prefix;
-      int n_eq, n_c;
-      const int before = move_scan(eq, s_warp, &n_eq);
-      const bool c = j < first && (k > prefix || (eq && equal + before < want));
-      const int at = move_scan(c, s_warp, &n_c);
-      if (c) kept[put + at] = j;
-      put += n_c;
-      equal += n_eq;
+  auto key = [&](int j) { return in_smem ? s_key[j] : weight_key(w[j]); };
+  uint32_t limit = 0;
+  int want = m;                                         // still to be found among the keys that share the prefix
+#pragma unroll 1
+  for (int pass = 0; pass < 3 && m > 0; ++pass) {
+    const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bits = pass == 2 ? 10 : 11;
+    for (int b = tid; b < kBins; b += kMoveThreads) s_hist[b] = 0;
+    __syncthreads();
+    for (int j = tid; j < first; j += kMoveThreads) {
+      const uint32_t k = key(j);
+      if (pass == 0 || (k >> (shift + bits)) == limit) atomicAdd(&s_hist[(k >> shift) & ((1u << bits) - 1)], 1);
     }
     __syncthreads();
-    equal = 0;
-    int filled = 0;
-    for (int j0 = 0; j0 < m; j0 += kMoveThreads) {
-      const int j = j0 + tid;
-      const uint32_t k = j < m ? weight_key(w[j]) : 0u;
-      const bool eq = j < m && k == prefix;
-      int n_eq, n_free;
-      const int before = move_scan(eq, s_warp, &n_eq);
-      const bool is_free = j < m && !(k > prefix || (eq && equal + before < want));
-      const int at = move_scan(is_free, s_warp, &n_free);
-      int from = j;
-      if (is_free) from = kept[m - moving + filled + at];
-      __syncthreads();
-      if (j < m) kept[j] = from;
-      equal += n_eq;
-      filled += n_free;
+    // bins from the top, eight to a thread
+    constexpr int per = kBins / kMoveThreads;
+    int c[per], sum = 0;
+#pragma unroll
+    for (int x = 0; x < per; ++x) { c[x] = s_hist[kBins - 1 - (tid * per + x)]; sum += c[x]; }
+    int incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += u;
     }
+    if (lane == 31) s_scan[warp] = incl;
+    __syncthreads();
+    int at = incl - sum;
+    for (int x = 0; x < warp; ++x) at += s_scan[x];
+#pragma unroll
+    for (int x = 0; x < per; ++x) {
+      if (at < want && at + c[x] >= want) { s_digit = kBins - 1 - (tid * per + x); s_left = want - at; }
+      at += c[x];
+    }
+    __syncthreads();
+    limit = (limit << bits) | (uint32_t)s_digit;
+    want = s_left;
+    __syncthreads();
   }
-  for (int r = tid; r < a.recent; r += kMoveThreads) kept[m + r] = first + r;
-  __syncthreads();
 
-  // ---- rows.  A row of K (or V) is cpr chunks of 16 bytes; both rows of a position are one warp's work.
+  // ---- a contiguous run of [0, m) and one of [m, first) per warp; how many of each are above and equal
+  const int run0 = ((m + kMoveWarps - 1) / kMoveWarps + 31) & ~31, run1 = ((first - m + kMoveWarps - 1) / kMoveWarps + 31) & ~31;
+  const int a0 = min(m, warp * run0), b0 = min(m, a0 + run0);
+  const int a1 = min(first, m + warp * run1), b1 = min(first, a1 + run1);
+  auto count = [&](int lo, int hi, int& above, int& equal) {
+    above = equal = 0;
+    for (int j = lo + lane; j < hi; j += 32) {
+      const uint32_t k = key(j);
+      above += k > limit;
+      equal += k == limit;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) { above += __shfl_xor_sync(0xffffffffu, above, o); equal += __shfl_xor_sync(0xffffffffu, equal, o); }
+  };
+  {
+    int x, y, z, u;
+    count(a0, b0, x, y);
+    count(a1, b1, z, u);
+    if (lane == 0) { s_cnt[warp][0] = x; s_cnt[warp][1] = y; s_cnt[warp][2] = z; s_cnt[warp][3] = u; }
+  }
+  __syncthreads();
+  // of this warp's runs: equal keys before them, free slots before the first, moving positions before the second
+  int eq0 = 0, eq1 = 0, free0 = 0, move0 = 0, moving = 0;
+  {
+    int eq = 0, fr = 0, mv = 0;
+    for (int x = 0; x < kMoveWarps; ++x) {
+      if (x == warp) { eq0 = eq; free0 = fr; }
+      const int len = min(m, (x + 1) * run0) - min(m, x * run0);
+      fr += len - s_cnt[x][0] - min(max(want - eq, 0), s_cnt[x][1]);
+      eq += s_cnt[x][1];
+    }
+    for (int x = 0; x < kMoveWarps; ++x) {
+      if (x == warp) { eq1 = eq; move0 = mv; }
+      mv += s_cnt[x][2] + min(max(want - eq, 0), s_cnt[x][3]);
+      eq += s_cnt[x][3];
+    }
+    moving = mv;
+    if (m == 0) moving = 0;
+  }
+
+  // ---- rows: a row of K (or V) is cpr chunks of 16 bytes; both rows of a position are one warp's work
   const int nbp = (a.budget + g.P - 1) / g.P;
   const int32_t* old_row = a.v.block_table + (size_t)a.ids[i] * g.max_pages;
   const int32_t* new_row = a.new_row + (size_t)i * nbp;
+  const bool fresh_pages = a.need[i] > 0;               // some kept pages are shared: all that they hold is copied
   const size_t page_chunks = (size_t)g.P * a.cpr;
   uint4* base = a.kv + (size_t)l * g.num_blocks * g.Hkv * 2 * page_chunks + (size_t)h * 2 * page_chunks;
   const size_t block_chunks = (size_t)g.Hkv * 2 * page_chunks;
   const int row_chunks = 2 * a.cpr;
-  auto row_at = [&](const int32_t* table, int j) { return base + (size_t)table[j / g.P] * block_chunks + (size_t)(j % g.P) * a.cpr; };
   // chunk c of the row pair (K, then V) of slot j, as stored
-  auto place = [&](int j, int c) {
-    const int kv = c >= a.cpr;
+  auto place = [&](const int32_t* table, int j, int c) {
+    const int kv = c >= a.cpr, slot = j % g.P;
     const int cc = c - kv * a.cpr;
-    return (size_t)kv * page_chunks + (g.swizzle ? ((cc & ~7) | ((cc ^ (j % g.P)) & 7)) : cc);
+    return base + (size_t)table[j / g.P] * block_chunks + (size_t)slot * a.cpr + (size_t)kv * page_chunks +
+           (g.swizzle ? ((cc & ~7) | ((cc ^ slot) & 7)) : cc);
   };
-  // slots [0, m): the sources are slots from m on, or the same slot of a page that was shared; nothing written here is read
-  // here
-  for (int j = warp; j < m; j += kMoveWarps) {
-    const int from = kept[j];
-    if (from == j && new_row[j / g.P] == old_row[j / g.P]) continue;
-    const uint4* src = row_at(old_row, from);
-    uint4* dst = row_at(new_row, j);
-    for (int c = lane; c < row_chunks; c += 32) dst[place(j, c)] = src[place(from, c)];
-    if (lane == 0) w_out[j] = w[from];
+  // Slots [0, m), kBins moving positions a round: they are listed in shared memory, then the free slots take them.  The
+  // sources are positions from m on, or the same slot of a page that was shared: nothing written here is read here.
+  for (int round = 0; round == 0 || round * kBins < moving; ++round) {
+    const int lo = round * kBins, hi = lo + kBins;
+    __syncthreads();
+    if (moving > 0) {
+      int eq = eq1, at = move0;
+      for (int j0 = a1; j0 < b1; j0 += 32) {
+        const int j = j0 + lane;
+        const uint32_t k = j < b1 ? key(j) : 0u;
+        const bool is_eq = j < b1 && k == limit;
+        const unsigned eqs = __ballot_sync(0xffffffffu, is_eq), below = (1u << lane) - 1;
+        const bool c = j < b1 && (k > limit || (is_eq && eq + __popc(eqs & below) < want));
+        const unsigned cs = __ballot_sync(0xffffffffu, c);
+        const int r = at + __popc(cs & below);
+        if (c && r >= lo && r < hi) s_hist[r - lo] = j;
+        eq += __popc(eqs);
+        at += __popc(cs);
+      }
+    }
+    __syncthreads();
+    int eq = eq0, at = free0;
+    for (int j0 = a0; j0 < b0; j0 += 32) {
+      const int j = j0 + lane;
+      const uint32_t k = j < b0 ? key(j) : 0u;
+      const bool is_eq = j < b0 && k == limit;
+      const unsigned eqs = __ballot_sync(0xffffffffu, is_eq), below = (1u << lane) - 1;
+      const bool is_free = j < b0 && !(k > limit || (is_eq && eq + __popc(eqs & below) < want));
+      const unsigned fr = __ballot_sync(0xffffffffu, is_free);
+      const int r = at + __popc(fr & below);
+      eq += __popc(eqs);
+      at += __popc(fr);
+      // a free slot belongs to the round that lists its position, everything else to the first
+      const bool mine = j < b0 && (is_free ? r >= lo && r < hi : round == 0);
+      int from = j;
+      if (mine) {
+        if (is_free) from = s_hist[r - lo];
+        kept[j] = from;
+        if (w_out != w) w_out[j] = w[from];
+      }
+      unsigned todo = __ballot_sync(0xffffffffu, mine && (is_free || (fresh_pages && new_row[j / g.P] != old_row[j / g.P])));
+      while (todo) {
+        int slot[kBatch], src[kBatch], cnt = 0;
+#pragma unroll
+        for (int x = 0; x < kBatch; ++x) {
+          const int b = todo ? __ffs(todo) - 1 : 0;
+          slot[x] = j0 + b;
+          src[x] = __shfl_sync(0xffffffffu, from, b);
+          if (todo) { ++cnt; todo &= todo - 1; }
+        }
+        for (int c = lane; c < row_chunks; c += 32) {
+          uint4 v[kBatch];
+#pragma unroll
+          for (int x = 0; x < kBatch; ++x)
+            if (x < cnt) v[x] = *place(old_row, src[x], c);
+#pragma unroll
+          for (int x = 0; x < kBatch; ++x)
+            if (x < cnt) *place(new_row, slot[x], c) = v[x];
+        }
+      }
+    }
   }
-  if (w_out != w)
-    for (int j = tid; j < m; j += kMoveThreads)
-      if (kept[j] == j) w_out[j] = w[j];
+  // in place, the weights follow only now: until here they say which slots are free
+  if (w_out == w)
+    for (int j = a0 + lane; j < b0; j += 32) {
+      const int from = kept[j];
+      if (from != j) w_out[j] = w[from];
+    }
   __syncthreads();
   // the most recent positions, in order: a batch is read whole before it is written (a slot may be the source of an
   // earlier one, never of a later one)
-  constexpr int kBatch = 4;
+  for (int r = tid; r < a.recent; r += kMoveThreads) kept[m + r] = first + r;
+  for (int r0 = 0; r0 < a.recent; r0 += kMoveThreads) {
+    const int r = r0 + tid;
+    const float x = r < a.recent ? w[first + r] : 0.f;
+    __syncthreads();
+    if (r < a.recent) w_out[m + r] = x;
+    __syncthreads();
+  }
   for (int r0 = 0; r0 < a.recent; r0 += kMoveWarps * kBatch) {
     for (int c0 = 0; c0 < row_chunks; c0 += 32) {
       const int c = c0 + lane;
       uint4 x[kBatch];
-      float ww[kBatch];
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
         const int r = r0 + b * kMoveWarps + warp;
-        if (r < a.recent && c < row_chunks) x[b] = row_at(old_row, first + r)[place(first + r, c)];
-        if (r < a.recent && c == 0) ww[b] = w[first + r];
+        if (r < a.recent && c < row_chunks) x[b] = *place(old_row, first + r, c);
       }
       __syncthreads();
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
         const int r = r0 + b * kMoveWarps + warp;
-        if (r < a.recent && c < row_chunks) row_at(new_row, m + r)[place(m + r, c)] = x[b];
-        if (r < a.recent && c == 0) w_out[m + r] = ww[b];
+        if (r < a.recent && c < row_chunks) *place(new_row, m + r, c) = x[b];
       }
-      __syncthreads();
     }
   }
   for (int j = a.budget + tid; j < a.stride; j += kMoveThreads) w_out[j] = 0.f;
 }
 
 // ---------------------------------------------------------------- bookkeeping
-// The (entry, page) pairs of all traces that were cut, in list order and page order, form one sequence; a pair whose page
-// is behind the budget, or was replaced by a block of its own, drops one reference.  A block whose count reaches zero is
-// pushed on the free list at the place of the last pair that names it, as a serial walk would (see release.cuh).
+// The listed (entry, page) pairs drop one reference each.  A block whose count reaches zero is pushed on the free list at
+// the place of the last pair that names it, as a serial walk would (see release.cuh).
 __global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kPruneThreads, 1) evict_finish_kernel(EvictArgs a) {
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
@@ -336,19 +421,9 @@ __global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kPruneThr
   const int R = ((E + C - 1) / C + blockDim.x - 1) / blockDim.x * blockDim.x;
   const int lo = min(E, rank * R), hi = min(E, lo + R);
   const int fc = v.counters[C_FREE_COUNT];
-  int32_t* slot = nullptr;
-  int i = 0, p = 0;
-  // pair e: its place in the block table, its block if it drops a reference, else -1
-  auto dropped = [&](int e) {
-    i = find_list_index(a.off, a.n, e);
-    p = e - a.off[i];
-    slot = v.block_table + (size_t)a.ids[i] * g.max_pages + p;
-    const int b = *slot;
-    return p >= nbp || a.new_row[(size_t)i * nbp + p] != b ? b : -1;
-  };
+  auto place = [&](int2 e) { return v.block_table + (size_t)a.ids[e.x] * g.max_pages + e.y; };
   for (int e = lo + threadIdx.x; e < hi; e += blockDim.x) {
-    const int b = dropped(e);
-    if (b < 0) continue;
+    const int b = *place(a.drop[e]);
     atomicSub(&v.refcount[b], 1);
     atomicMax(&v.claim[b], e);
   }
@@ -356,8 +431,8 @@ __global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kPruneThr
   cluster.sync();
   int pushes = 0;
   for (int e = lo + threadIdx.x; e < hi; e += blockDim.x) {
-    const int b = dropped(e);
-    pushes += b >= 0 && __ldcg(&v.claim[b]) == e && __ldcg(&v.refcount[b]) == 0;
+    const int b = *place(a.drop[e]);
+    pushes += __ldcg(&v.claim[b]) == e && __ldcg(&v.refcount[b]) == 0;
   }
   int total;
   block_excl_scan(pushes, s_warp, &total);
@@ -380,14 +455,14 @@ __global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kPruneThr
     int b = -1;
     bool own = false, push = false;
     if (e < hi) {
-      b = dropped(e);
-      if (b >= 0) {
-        own = __ldcg(&v.claim[b]) == e;                  // (only its owner clears a claim)
-        push = own && __ldcg(&v.refcount[b]) == 0;
-        const int fresh = p < nbp ? a.new_row[(size_t)i * nbp + p] : -1;
-        *slot = fresh;
-        if (fresh >= 0) v.refcount[fresh] = 1;
-      }
+      const int2 d = a.drop[e];
+      int32_t* at = place(d);
+      b = *at;
+      own = __ldcg(&v.claim[b]) == e;                    // (only its owner clears a claim)
+      push = own && __ldcg(&v.refcount[b]) == 0;
+      const int fresh = d.y < nbp ? a.new_row[(size_t)d.x * nbp + d.y] : -1;
+      *at = fresh;
+      if (fresh >= 0) v.refcount[fresh] = 1;
     }
     int row_total;
     const int at = at_base + block_excl_scan(push ? 1 : 0, s_warp, &row_total);
@@ -413,7 +488,7 @@ extern "C" {
 int kv_pool_evict_workspace_bytes(const step_pool* pool, int n, int budget, size_t* bytes) {
   if (!pool || !bytes || !evict_sizes_ok(pool, n, budget)) return STEP_ERR_INVALID_ARG;
   const size_t nbp = (budget + pool->cfg.page_size - 1) / pool->cfg.page_size;
-  *bytes = ((size_t)2 * n + 1 + n * nbp) * sizeof(int32_t);
+  *bytes = ((size_t)4 * n + 2 + n * nbp) * sizeof(int32_t) + (size_t)n * pool->cfg.max_pages_per_trace * sizeof(int2);
   return STEP_OK;
 }
 
@@ -437,11 +512,16 @@ int kv_pool_evict_positions(step_pool* pool, const int32_t* trace_ids, int n, co
   a.ids = trace_ids; a.n = n;
   a.weights = weights; a.weights_out = weights_out; a.stride = weight_stride; a.budget = budget; a.recent = recent;
   a.kept = kept_out;
-  a.old_len = (int32_t*)workspace; a.off = a.old_len + n; a.new_row = a.off + n + 1;
+  a.drop = (int2*)workspace;
+  a.old_len = (int32_t*)(a.drop + (size_t)n * a.g.max_pages);
+  a.need = a.old_len + n; a.base = a.need + n; a.off = a.base + n + 1; a.new_row = a.off + n + 1;
   a.cpr = a.g.d * pool->elem_bytes / 16;
-  evict_plan_kernel<<<1, kPlanThreads, (size_t)n * 2 * sizeof(int), s>>>(a);
+  a.cache_keys = weight_stride <= kMostCachedKeys ? weight_stride : 0;
+  evict_plan_kernel<<<kClusterCtas, kPruneThreads, 0, s>>>(a);
   if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
-  if (launch_dependent(evict_move_kernel, dim3(a.g.Hkv, n, a.g.L), dim3(kMoveThreads), 0, s, a) != cudaSuccess) return STEP_ERR_CUDA;
+  const size_t smem = (size_t)a.cache_keys * sizeof(uint32_t);
+  if (cudaFuncSetAttribute(evict_move_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostCachedKeys * 4) != cudaSuccess) return STEP_ERR_CUDA;
+  if (launch_dependent(evict_move_kernel, dim3(a.g.Hkv, n, a.g.L), dim3(kMoveThreads), smem, s, a) != cudaSuccess) return STEP_ERR_CUDA;
   if (launch_dependent(evict_finish_kernel, dim3(kClusterCtas), dim3(kPruneThreads), 0, s, a) != cudaSuccess) return STEP_ERR_CUDA;
   return launch_ok();
 }

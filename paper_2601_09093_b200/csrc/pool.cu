@@ -456,8 +456,9 @@ path_alloc_kernel(DevViews v, Geo g, const int32_t* __restrict__ ids, int n, con
   dependents_may_launch();
   int* s_need = sm;            // pages wanted, or -1 if the entry is skipped
   int* s_off = sm + n;         // pops that precede this entry's
-  int* s_have = sm + 2 * n;
-  int* s_bad = sm + 3 * n;
+  int* s_S = sm + 2 * n;       // length before the call
+  int* s_len = sm + 3 * n;     // new positions; -1: the count or the path is out of range
+  int* s_rows = sm + 4 * n;    // new positions of the entries before it
   __shared__ int s_fc;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nwarps = blockDim.x >> 5;
   for (int i = threadIdx.x; i < n; i += blockDim.x) {
@@ -478,37 +479,36 @@ path_alloc_kernel(DevViews v, Geo g, const int32_t* __restrict__ ids, int n, con
         bad |= node < 0 || node >= T;
       }
     bad = __any_sync(0xffffffffu, bad);
-    if (lane == 0) s_bad[i] = bad;
+    if (lane == 0) s_len[i] = bad ? -1 : k;
   }
   __syncthreads();
   for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    int need = -1, have = 0;
-    const int t = ids[i];
+    int need = -1, S = 0;
+    const int t = ids[i], k = s_len[i];
     if (t < 0 || t >= g.max_traces || !v.live[t] || v.prune_rank[t] != i) {
       flag_error(v.counters, STEP_ERR_BAD_TRACE);
-    } else if (s_bad[i]) {
+    } else if (k < 0) {
       flag_error(v.counters, STEP_ERR_INVALID_ARG);
     } else {
-      const int S = v.seq_lens[t];
-      have = (S + g.P - 1) / g.P;
-      const long long want = ((long long)S + path_len[i] + g.P - 1) / g.P;
+      S = v.seq_lens[t];
+      const long long want = ((long long)S + k + g.P - 1) / g.P;
       if (want > g.max_pages) flag_error(v.counters, STEP_ERR_CAPACITY);
-      else need = (int)want - have;
+      else need = (int)want - (S + g.P - 1) / g.P;
     }
-    s_need[i] = need; s_have[i] = have;
+    s_need[i] = need; s_S[i] = S;
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 0) {                                // (shared memory only: a step of this walk is a few cycles)
     const int fc = v.counters[C_FREE_COUNT];
     int remaining = fc, rows = 0;
     for (int i = 0; i < n; ++i) {
       const int need = s_need[i];
-      v.prune_off[i] = rows;
+      s_rows[i] = rows;
       if (need < 0) continue;
       if (need > remaining) { s_need[i] = -1; flag_error(v.counters, STEP_ERR_NO_BLOCKS); continue; }
       s_off[i] = fc - remaining;
       remaining -= need;
-      rows += path_len[i];
+      rows += s_len[i];
     }
     v.prune_off[n] = rows;
     s_fc = fc;
@@ -517,20 +517,20 @@ path_alloc_kernel(DevViews v, Geo g, const int32_t* __restrict__ ids, int n, con
   __syncthreads();
   const int fc = s_fc;
   for (int i = warp; i < n; i += nwarps) {
-    const int need = s_need[i];
-    if (need < 0) { if (lane == 0) v.append_base[i] = -1; continue; }
+    const int need = s_need[i], S = s_S[i];
+    if (lane == 0) {
+      v.prune_off[i] = s_rows[i];
+      v.append_base[i] = need < 0 ? -1 : S;
+    }
+    if (need < 0) continue;
     const int t = ids[i];
-    int32_t* row = v.block_table + (size_t)t * g.max_pages;
+    int32_t* row = v.block_table + (size_t)t * g.max_pages + (S + g.P - 1) / g.P;
     for (int p = lane; p < need; p += 32) {
       const int b = v.free_list[fc - 1 - s_off[i] - p];
-      row[s_have[i] + p] = b;
+      row[p] = b;
       v.refcount[b] = 1;
     }
-    if (lane == 0) {
-      const int S = v.seq_lens[t];
-      v.append_base[i] = S;
-      v.seq_lens[t] = S + path_len[i];
-    }
+    if (lane == 0) v.seq_lens[t] = S + s_len[i];
   }
 }
 
@@ -726,7 +726,7 @@ int append_kv_path(step_pool* pool, const int32_t* trace_ids, int n, int T, cons
   if (n == 0 || max_path == 0) return STEP_OK;
   if (!trace_ids || !k_draft || !v_draft || !path || !path_len) return STEP_ERR_INVALID_ARG;
   if (((uintptr_t)k_draft | (uintptr_t)v_draft) & 15) return STEP_ERR_INVALID_ARG;
-  // ids must be distinct; the list is served by one CTA from shared memory (16 bytes per entry)
+  // ids must be distinct; the list is served by one CTA from shared memory (20 bytes per entry)
   if (n > pool->cfg.max_traces || n > kMaxTracesFast) return STEP_ERR_INVALID_ARG;
   if ((long long)n * max_path > 0x7fffffffll) return STEP_ERR_INVALID_ARG;
   const int st = on_pool_device(pool);
@@ -734,7 +734,7 @@ int append_kv_path(step_pool* pool, const int32_t* trace_ids, int n, int T, cons
   Geo g = geo_of(pool);
   cudaStream_t s = (cudaStream_t)stream;
   const int cpe = 16 / pool->elem_bytes, cpr = g.d / cpe;
-  path_alloc_kernel<<<1, 256, (size_t)n * 4 * sizeof(int), s>>>(pool->v, g, trace_ids, n, path, path_len, max_path, T);
+  path_alloc_kernel<<<1, 256, (size_t)n * 5 * sizeof(int), s>>>(pool->v, g, trace_ids, n, path, path_len, max_path, T);
   if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
   // CTAs for every pair there may be, up to eight per SM; the layer range is split when there are few pairs
   const long long pairs = (long long)n * max_path, most = 8ll * pool->num_sms;

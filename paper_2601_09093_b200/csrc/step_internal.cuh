@@ -189,6 +189,12 @@ bool score_tc_supported(const scorer_weights* w, const void* hidden);
 // C_SCORE_NB / C_SCORE_TC on the device and returns at once when C_SCORE_TC is 0.
 int score_tc_launch(step_pool* pool, const void* hidden, int Mc, const scorer_weights* w, cudaStream_t s);
 
+// ---- decode attention that keeps its scores (attention.cu): every log2-scaled score in scores [n][Hq][score_stride]
+// (score_stride a multiple of the page size) and every row's (max, sum) in row_ml [n][Hq][2]
+bool attn_mma_covers(const step_pool* pool, int n);
+int attn_mma_scores(step_pool* pool, int layer, const void* q, const int32_t* block_table, const int32_t* seq_lens, int n,
+                    void* out, float* scores, long long score_stride, float* row_ml, cudaStream_t s);
+
 // ---- tensor-core tree attention (tree_tc.cu)
 bool tree_tc_supported(const step_pool* pool, int n);
 size_t tree_tc_workspace(const step_pool* pool, int T);

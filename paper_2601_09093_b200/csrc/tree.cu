@@ -12,7 +12,7 @@ extern "C" {
 
 int decode_attention_tree_workspace_bytes(const step_pool* pool, int n, int T, size_t* bytes) {
   if (!pool || !bytes || n < 0 || T < 1 || T > kMaxTreeNodes) return STEP_ERR_INVALID_ARG;
-  *bytes = tree_tc_supported(pool, n) ? tree_tc_workspace(pool, T) : 0;
+  *bytes = tree_tc_supported(pool, n) ? tree_tc_workspace(pool, T) : attn_rows_workspace(pool, n, T);
   return STEP_OK;
 }
 
@@ -31,14 +31,16 @@ int decode_attention_tree(step_pool* pool, int layer, const void* q, const void*
     if (!workspace || (uintptr_t)workspace & 255 || workspace_bytes < tree_tc_workspace(pool, T)) return STEP_ERR_INVALID_ARG;
     return tree_tc_launch(pool, layer, q, k_draft, v_draft, parents, n_nodes, T, block_table, seq_lens, n, out, workspace, s);
   }
+  const size_t need = attn_rows_workspace(pool, n, T);
+  if (need > 0 && (!workspace || (uintptr_t)workspace & 255 || workspace_bytes < need)) return STEP_ERR_INVALID_ARG;
   RowsArgs a = {};
   a.g = geo_of(pool);
   a.kv = pool->cfg.kv_storage; a.layer = layer;
   a.q = q; a.k_draft = k_draft; a.v_draft = v_draft; a.parents = parents; a.n_nodes = n_nodes; a.T = T;
   a.block_table = block_table; a.seq_lens = seq_lens; a.out = out;
   a.counters = pool->v.counters;
-  if (pool->cfg.dtype == STEP_BF16) return launch_attn_rows<__nv_bfloat16, __nv_bfloat16, true, false>(a, n, s);
-  return launch_attn_rows<float, float, true, false>(a, n, s);
+  if (pool->cfg.dtype == STEP_BF16) return launch_attn_rows<__nv_bfloat16, __nv_bfloat16, true, false>(pool, a, n, (float*)workspace, s);
+  return launch_attn_rows<float, float, true, false>(pool, a, n, (float*)workspace, s);
 }
 
 }  // extern "C"

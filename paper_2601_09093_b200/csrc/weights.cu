@@ -12,10 +12,10 @@ using namespace stepk;
 
 namespace {
 
-constexpr int kAccThreads = 256;
+constexpr int kAccThreads = 256, kAccKeys = 4 * kAccThreads;
 
-// weight_sum[t][h][j] += sum_g exp2(scores[t][h G + g][j] - m_g) / l_g.  grid (position chunks, Hkv, n); the heads are added
-// in ascending order by one thread, so the sums do not depend on the launch.
+// weight_sum[t][h][j] += sum_g exp2(scores[t][h G + g][j] - m_g) / l_g.  grid (chunks of kAccKeys positions, Hkv, n), a thread
+// takes four positions; the heads are added in ascending order, so the sums do not depend on the launch.
 __global__ void __launch_bounds__(kAccThreads)
 weights_add_kernel(Geo g, const float* __restrict__ scores, long long score_stride, const float* __restrict__ ml,
                    const int32_t* __restrict__ seq_lens, float* __restrict__ weight_sum, int weight_stride, int32_t* counters) {
@@ -24,14 +24,32 @@ weights_add_kernel(Geo g, const float* __restrict__ scores, long long score_stri
   long long S = seq_lens[t];
   const long long cap = (long long)g.max_pages * g.P;
   if (S > cap) S = cap;
-  if (S > weight_stride) { S = weight_stride; if (threadIdx.x == 0) flag_error(counters, STEP_ERR_CAPACITY); }
-  const float* sc = scores + ((size_t)t * g.Hq + (size_t)h * g.G) * score_stride;
-  const float* mlh = ml + ((size_t)t * g.Hq + (size_t)h * g.G) * 2;
-  float* w = weight_sum + ((size_t)t * g.Hkv + h) * weight_stride;
-  for (long long j = (long long)blockIdx.x * kAccThreads + threadIdx.x; j < S; j += (long long)gridDim.x * kAccThreads) {
-    float sum = 0.f;
-    for (int k = 0; k < g.G; ++k) sum += exp2f(sc[(size_t)k * score_stride + j] - mlh[2 * k]) / mlh[2 * k + 1];
-    w[j] += sum;
+  if (S > weight_stride) { S = weight_stride; if (threadIdx.x == 0 && blockIdx.x == 0) flag_error(counters, STEP_ERR_CAPACITY); }
+  const long long j = (long long)blockIdx.x * kAccKeys + threadIdx.x * 4;
+  if (j >= S) return;
+  const float4* sc = reinterpret_cast<const float4*>(scores + ((size_t)t * g.Hq + (size_t)h * g.G) * score_stride + j);
+  const float2* mlh = reinterpret_cast<const float2*>(ml) + (size_t)t * g.Hq + (size_t)h * g.G;
+  float* w = weight_sum + ((size_t)t * g.Hkv + h) * weight_stride + j;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int k = 0; k < g.G; ++k) {
+    const float4 s = __ldcs(sc + (size_t)k * (score_stride / 4));
+    const float2 r = mlh[k];
+    const float inv = 1.f / r.y;
+    sum.x += exp2f(s.x - r.x) * inv;
+    sum.y += exp2f(s.y - r.x) * inv;
+    sum.z += exp2f(s.z - r.x) * inv;
+    sum.w += exp2f(s.w - r.x) * inv;
+  }
+  if (j + 4 <= S && ((uintptr_t)w & 15) == 0) {
+    float4 old = *reinterpret_cast<float4*>(w);
+    old.x += sum.x; old.y += sum.y; old.z += sum.z; old.w += sum.w;
+    *reinterpret_cast<float4*>(w) = old;
+  } else {
+    w[0] += sum.x;
+    if (j + 1 < S) w[1] += sum.y;
+    if (j + 2 < S) w[2] += sum.z;
+    if (j + 3 < S) w[3] += sum.w;
   }
 }
 
@@ -45,6 +63,7 @@ int decode_attention_weights_workspace_bytes(const step_pool* pool, int n, int w
   if (!pool || !bytes || n < 0 || weight_stride < 1) return STEP_ERR_INVALID_ARG;
   const size_t rows = (size_t)n * pool->cfg.num_q_heads;
   *bytes = rows * stride_of_scores(weight_stride) * sizeof(float) + rows * 2 * sizeof(float);
+  if (!attn_mma_covers(pool, n)) *bytes += 12 + attn_rows_workspace(pool, n, 1);
   return STEP_OK;
 }
 
@@ -62,21 +81,28 @@ int decode_attention_weights(step_pool* pool, int layer, const void* q, const in
   st = on_pool_device(pool);
   if (st != STEP_OK) return st;
   cudaStream_t s = (cudaStream_t)stream;
-  RowsArgs a = {};
-  a.g = geo_of(pool);
-  a.kv = pool->cfg.kv_storage; a.layer = layer;
-  a.q = q; a.T = 1;
-  a.block_table = block_table; a.seq_lens = seq_lens; a.out = out;
-  a.scores = (float*)workspace; a.score_stride = stride_of_scores(weight_stride);
-  a.ml = a.scores + (size_t)n * a.g.Hq * a.score_stride;
-  a.counters = pool->v.counters;
-  st = pool->cfg.dtype == STEP_BF16 ? launch_attn_rows<__nv_bfloat16, float, false, true>(a, n, s)
-                                    : launch_attn_rows<float, float, false, true>(a, n, s);
+  const Geo g = geo_of(pool);
+  float* scores = (float*)workspace;
+  const long long score_stride = stride_of_scores(weight_stride);
+  float* ml = scores + (size_t)n * g.Hq * score_stride;
+  if (attn_mma_covers(pool, n)) {
+    st = attn_mma_scores(pool, layer, q, block_table, seq_lens, n, out, scores, score_stride, ml, s);
+  } else {
+    RowsArgs a = {};
+    a.g = g;
+    a.kv = pool->cfg.kv_storage; a.layer = layer;
+    a.q = q; a.T = 1;
+    a.block_table = block_table; a.seq_lens = seq_lens; a.out = out;
+    a.scores = scores; a.score_stride = score_stride; a.ml = ml;
+    a.counters = pool->v.counters;
+    float* part = ml + ((size_t)n * g.Hq * 2 + 3) / 4 * 4;          // 16-byte aligned
+    st = pool->cfg.dtype == STEP_BF16 ? launch_attn_rows<__nv_bfloat16, float, false, true>(pool, a, n, part, s)
+                                      : launch_attn_rows<float, float, false, true>(pool, a, n, part, s);
+  }
   if (st != STEP_OK) return st;
-  int chunks = (weight_stride + 4 * kAccThreads - 1) / (4 * kAccThreads);
-  if (chunks > 64) chunks = 64;
-  if (launch_dependent(weights_add_kernel, dim3(chunks, a.g.Hkv, n), dim3(kAccThreads), 0, s, a.g, a.scores, a.score_stride,
-                       a.ml, seq_lens, weight_sum, weight_stride, a.counters) != cudaSuccess) return STEP_ERR_CUDA;
+  const int chunks = (int)(((long long)weight_stride + kAccKeys - 1) / kAccKeys);
+  if (launch_dependent(weights_add_kernel, dim3(chunks, g.Hkv, n), dim3(kAccThreads), 0, s, g, scores, score_stride, ml,
+                       seq_lens, weight_sum, weight_stride, pool->v.counters) != cudaSuccess) return STEP_ERR_CUDA;
   return launch_ok();
 }
 

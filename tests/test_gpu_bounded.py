@@ -189,11 +189,12 @@ def test_evict_leaves_alone_what_cannot_be_served():
     assert run_evict(tw, [-1, 5], w[:, :2].copy(), 96, 10) == 1 << 3
 
 
-def test_evict_from_a_long_cache():
+@pytest.mark.parametrize("in_place", [False, True])
+def test_evict_from_a_long_cache(in_place):
     cfg = config((2, 1, 128), "bf16", layers=1, n=2)
     tw = twin(cfg, [40000, 9000])
     w = some_weights(np.random.default_rng(5), (1, 2, 1, 40000))
-    run_evict(tw, [0, 1], w, 8000, 700)
+    run_evict(tw, [0, 1], w, 8000, 700, in_place)
 
 
 def test_evict_under_a_graph_on_another_stream():
