@@ -19,10 +19,13 @@
 //     its softmax.  Up to 128 rows: the lanes take even and odd tiles of the same rows and are combined at the end.
 //     More: the lanes take 128 rows each of the same tile, and 256 rows are one row group;
 //   * the tiles of all (trace, KV head, row group) sequences form one stream that is cut into one equal contiguous
-//     share per CTA; what a share holds of a sequence leaves its (m, l, O) in the share's first or last slot, and
-//     tree_merge_kernel - a programmatic dependent - combines the pieces of every sequence in stream order.
-// Warps: 4 + 4 softmax (lane 0, lane 1), one that fetches, one whose first thread issues the products.
-// Every wait is bounded; one that runs out raises STEP_ERR_TIMEOUT and the CTA winds down.
+//     share per CTA; what a share holds of a sequence is a piece.  A piece that is not a whole sequence leaves its
+//     (m, l, O) in the share's first or last slot, and tree_merge_kernel - a programmatic dependent - combines the pieces of
+//     every sequence in stream order.  Row groups without a drafted token of theirs (a short tree) are not in the stream;
+//   * two warps bring the next piece's query rows in (cp.async) as soon as the last scores of the current one are made,
+//     so that the next piece's first scores overlap this one's last softmax and its output.
+// Warps: 4 + 4 softmax (lane 0, lane 1), one that fetches K and V, one whose first thread issues the products, two for
+// the query rows.  Every wait is bounded; one that runs out raises STEP_ERR_TIMEOUT and the CTA winds down.
 #include "attention_rows.cuh"
 #include "async_copy.cuh"
 #include "tensor_core.cuh"
@@ -37,10 +40,13 @@ constexpr int kP = 16, kD = 128;
 constexpr int kTile = 128;                        // keys per tile
 constexpr int kSlotBytes = kTile * kD * 2;        // K or V of one tile: two halves of 128 rows x 128 bytes
 constexpr int kHalfSlot = kSlotBytes / 2;
-constexpr int kSlots = 4;
 constexpr int kQBytes = kHalfRows * kD * 2;       // 128 query rows, same arrangement
-constexpr int kWarpFetch = 8, kWarpMma = 9;
-constexpr int kThreads = 320;
+constexpr int kSlots = 5;                         // ring of K and V tiles: 160 KiB
+constexpr int kXCols = 16;                        // columns per round in which the lanes exchange their sums (below 128 rows)
+constexpr int kXBytes = 2 * kXCols * kHalfRows * 4;
+constexpr int kWarpFetch = 8, kWarpMma = 9, kWarpQ = 10;
+constexpr int kThreads = 384;                      // three warpgroups
+constexpr int kRegsSoftmax = 208, kRegsOther = 88; // 2 x 128 x 208 + 128 x 88 = 384 x 168, what the launch has
 constexpr int kTmemCols = 512;                    // S of both lanes (P over them), then O of both
 constexpr float kRescale = 8.f;                   // log2 of how far a row's maximum may run ahead of its reference
 constexpr unsigned long long kDrainNs = 100000000ull;
@@ -55,7 +61,7 @@ struct TreeArgs {
   float* ws_o;                      // [share][2][group rows][kD]
   int32_t* counters;
   int n, T, Hq, Hkv, G, L, layer, max_pages, num_blocks;
-  int rows, groups;                 // query rows of a (trace, KV head): T * G; row groups they make
+  int rows;                         // query rows of a (trace, KV head): T * G
   int group_rows;                   // 128 or 256
   int shares;                       // CTAs of the attention launch
   float scale_log2;
@@ -74,45 +80,68 @@ __device__ inline int nodes_of(const TreeArgs& a, int t, bool flag) {
   if (flag && (k < 0 || k > a.T)) flag_error(a.counters, STEP_ERR_INVALID_ARG);
   return min(max(k, 0), a.T);
 }
-// One warp: cum[n + 1], the tiles of every trace (of one KV head and row group) as a prefix sum.  A trace without any
-// key has one tile all the same, which writes its zeros.
-__device__ inline void build_stream(const TreeArgs& a, int lane, bool flag, int* cum) {
-  int run = 0;
+// Trace t in the stream: tiles of a sequence, row groups that hold one of its drafted tokens (one at least: a trace without
+// any key has one tile, of which nothing is written).
+struct Shape { int S, nodes, tiles, groups; };
+__device__ inline Shape shape_of(const TreeArgs& a, int t, bool flag) {
+  Shape x;
+  x.S = cached(a, t, flag);
+  x.nodes = nodes_of(a, t, flag);
+  const long long keys = (long long)x.S + x.nodes;
+  x.tiles = keys > 0 ? (int)((keys + kTile - 1) / kTile) : 1;
+  x.groups = max(1, (x.nodes * a.G + a.group_rows - 1) / a.group_rows);
+  return x;
+}
+// The stream: for every trace, for every KV head, for every row group, the sequence's tiles.  A warp's place in it:
+struct Place { int t, hr, tile; Shape x; };
+// One warp: how many tiles there are in all.
+__device__ inline long long stream_total(const TreeArgs& a, int lane, bool flag) {
+  long long sum = 0;
+  for (int t = lane; t < a.n; t += 32) {
+    const Shape x = shape_of(a, t, flag);
+    sum += (long long)x.tiles * x.groups;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  return sum * a.Hkv;
+}
+// One warp: the place of position pos (inside the stream).
+__device__ inline Place seek(const TreeArgs& a, int lane, long long pos) {
+  long long run = 0;
+  Place p = {};
   for (int base = 0; base < a.n; base += 32) {
     const int t = base + lane;
-    int tiles = 0;
-    if (t < a.n) {
-      const long long keys = (long long)cached(a, t, flag) + nodes_of(a, t, flag);
-      tiles = keys > 0 ? (int)((keys + kTile - 1) / kTile) : 1;
-    }
-    int incl = tiles;
+    long long mine = 0;
+    if (t < a.n) { const Shape x = shape_of(a, t, false); mine = (long long)x.tiles * x.groups * a.Hkv; }
+    long long incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += x;
+      const long long u = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += u;
     }
-    if (t < a.n) cum[t] = run + incl - tiles;
+    const unsigned past = __ballot_sync(0xffffffffu, run + incl > pos);      // (lanes behind the last trace count nothing)
+    if (past) {
+      const int who = __ffs(past) - 1;
+      const long long start = run + __shfl_sync(0xffffffffu, incl - mine, who);
+      p.t = base + who;
+      p.x = shape_of(a, p.t, false);
+      p.hr = (int)((pos - start) / p.x.tiles);
+      p.tile = (int)((pos - start) % p.x.tiles);
+      return p;
+    }
     run += __shfl_sync(0xffffffffu, incl, 31);
   }
-  if (lane == 0) cum[a.n] = run;
-}
-// A piece: tiles [tile0, tile0 + cnt) of the sequence of (trace t, row group and head hr), at stream position pos.
-struct Piece { int t, hr, tile0, cnt, tiles; };
-__device__ inline Piece piece_at(const int* cum, int n, int HR, long long pos, long long end) {
-  int lo = 0, hi = n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if ((long long)HR * cum[mid] <= pos) lo = mid; else hi = mid - 1;
-  }
-  Piece p;
-  p.t = lo;
-  p.tiles = cum[lo + 1] - cum[lo];
-  const long long r = pos - (long long)HR * cum[lo];
-  p.hr = (int)(r / p.tiles);
-  p.tile0 = (int)(r % p.tiles);
-  p.cnt = (int)min((long long)(p.tiles - p.tile0), end - pos);
   return p;
 }
+// The place behind a whole rest of a sequence.
+__device__ inline void next_sequence(const TreeArgs& a, Place& p) {
+  p.tile = 0;
+  if (++p.hr < a.Hkv * p.x.groups) return;
+  p.hr = 0;
+  if (++p.t < a.n) p.x = shape_of(a, p.t, false);
+}
+// A piece, as the query warps announce it: tiles [tile0, tile0 + cnt) of the sequence's `tiles`.
+struct Piece { int t, h, r0, tile0, cnt, tiles, S, nodes; };
 
 // ---- instructions
 __device__ inline void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
@@ -170,6 +199,11 @@ __device__ inline uint64_t umma_desc_v(uint32_t smem_addr) {
   const uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);
   return ((uint64_t)hi << 32) | lo;
 }
+// 32 bytes (a whole sector) per thread
+__device__ inline void st_global32(void* dst, const uint32_t* r) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(dst), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
 __device__ inline uint32_t pack2(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
@@ -181,18 +215,21 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
   unsigned char* sm = smem_raw + (base - raw);
-  const uint32_t sm_q = base, sm_ring = base + 2 * kQBytes;
-  unsigned char* tail = sm + 2 * kQBytes + kSlots * kSlotBytes;
+  constexpr int kQAll = (kTwoRows ? 2 : 1) * kQBytes, kX = kTwoRows ? 0 : kXBytes;
+  const uint32_t sm_q = base, sm_ring = base + kQAll + kX;
+  float* s_x = reinterpret_cast<float*>(sm + kQAll);                   // [2][kXCols][128]: columns lane 0 gives, lane 1 gives
+  unsigned char* tail = sm + kQAll + kX + kSlots * kSlotBytes;
   uint64_t* s_bar = reinterpret_cast<uint64_t*>(tail);
-  float* s_ml = reinterpret_cast<float*>(s_bar + 32);                  // [2][128][2]
-  int* s_up = reinterpret_cast<int*>(s_ml + 512);                      // [2][64]
-  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_up + 128);
+  unsigned long long* s_mask = reinterpret_cast<unsigned long long*>(s_bar + 32);   // [2][64] by piece parity
+  Piece* s_piece = reinterpret_cast<Piece*>(s_mask + 128);             // [2]
+  int* s_up = reinterpret_cast<int*>(s_piece + 2);                     // [64]
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_up + 64);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
-  int* s_cum = reinterpret_cast<int*>(s_tmem + 4);                     // [n + 1]
+  float* s_ml = reinterpret_cast<float*>(s_tmem + 4);                  // [2][128][2] (below 128 rows)
   const uint32_t bars = smem_u32(s_bar);
   const uint32_t bar_full = bars, bar_empty = bars + 8 * kSlots;
   const uint32_t bar_q = bars + 16 * kSlots, bar_s = bar_q + 8, bar_p = bar_s + 16, bar_o = bar_p + 16,
-                 bar_both = bar_o + 16, bar_lane = bar_both + 8, bar_drain = bar_lane + 16;
+                 bar_both = bar_o + 16, bar_qfree = bar_both + 8, bar_drain = bar_qfree + 8;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -200,12 +237,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       mbar_init(bar_full + 8 * s, 33);              // the fetching warp's threads, and its announcement of bytes
       mbar_init(bar_empty + 8 * s, 1);              // tcgen05.commit
     }
-    mbar_init(bar_q, 256);
+    mbar_init(bar_q, 128);                          // the query warps' threads, and their copies
+    mbar_init(bar_qfree, 257);                      // tcgen05.commit: a piece's last scores; all softmax threads have begun it
     for (int s = 0; s < 2; ++s) {
       mbar_init(bar_s + 8 * s, 1);                  // tcgen05.commit: scores made (and the products before them done)
       mbar_init(bar_p + 8 * s, 128);
       mbar_init(bar_o + 8 * s, 1);                  // tcgen05.commit: a piece's last product
-      mbar_init(bar_lane + 8 * s, 128);
     }
     mbar_init(bar_both, 256);
     mbar_init(bar_drain, 1);
@@ -216,16 +253,17 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "r"(kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  if (warp == 0) build_stream(a, lane, blockIdx.x == 0, s_cum);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   dependents_may_launch();
   const uint32_t tmem = *s_tmem;
-  const int HR = a.Hkv * a.groups;
-  const long long total = (long long)HR * s_cum[a.n];
-  const long long W = (total + a.shares - 1) / a.shares;
-  const long long pos0 = min(total, (long long)blockIdx.x * W), end = min(total, pos0 + W);
+  // this CTA's share of the stream: every warp that walks it asks
+  auto my_share = [&](bool flag, long long& pos0, long long& end) {
+    const long long total = stream_total(a, lane, flag), W = (total + a.shares - 1) / a.shares;
+    pos0 = min(total, (long long)blockIdx.x * W);
+    end = min(total, pos0 + W);
+  };
 
   auto wait = [&](uint32_t bar, uint32_t parity) {
     if (*s_abort) return false;
@@ -239,44 +277,21 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
 
   if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
     // ------------------------------------------------ softmax: lane `ln` of the CTA, row `row` of its 128
-    const int ln = warp >> 2, row = (warp & 3) * 32 + lane, tid = threadIdx.x;
+    const int ln = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t t_s = t_row + ln * 128, t_o = t_row + 256 + ln * 128;
-    uint32_t ph_s = 0, ph_piece = 0, ph_both = 0, ph_lane = 0;
-    bool ok = true;
-    for (long long pos = pos0; pos < end && ok;) {
-      const Piece pc = piece_at(s_cum, a.n, HR, pos, end);
-      const int h = pc.hr / a.groups, r0 = (pc.hr - h * a.groups) * a.group_rows;
-      const int S = cached(a, pc.t, false), nodes = nodes_of(a, pc.t, false);
-      // ---- query rows into shared memory (zeros behind the last), the node's ancestors
-      {
-        const int qrow = kTwoRows ? row : tid >> 1;                    // row of the tile this thread copies
-        const int c0 = kTwoRows ? 0 : (tid & 1) * 8, c1 = kTwoRows ? 16 : c0 + 8;
-        const int r = r0 + (kTwoRows ? ln * 128 : 0) + qrow;
-        const bool real = r < nodes * a.G;
-        const uint4* src = reinterpret_cast<const uint4*>(a.q + (((size_t)pc.t * a.T + (real ? r / a.G : 0)) * a.Hq + (size_t)h * a.G + (real ? r % a.G : 0)) * kD);
-        unsigned char* dst = sm + (kTwoRows ? ln * kQBytes : 0) + qrow * 128;
-#pragma unroll
-        for (int c = c0; c < c1; ++c)
-          *reinterpret_cast<uint4*>(dst + (c >> 3) * (kQBytes / 2) + (((c ^ qrow) & 7) << 4)) = real ? src[c] : make_uint4(0, 0, 0, 0);
-      }
-      if (row < nodes) {
-        int p = a.parents[(size_t)pc.t * a.T + row];
-        if (p >= row || p < -1) { flag_error(a.counters, STEP_ERR_INVALID_ARG); p = -1; }
-        s_up[ln * 64 + row] = p;
-      }
-      fence_async_smem();
-      tc_fence_before();
-      mbar_arrive(bar_q);
-      mbar_arrive(bar_lane + 8 * ln);
-      if (!wait_warp(bar_lane + 8 * ln, ph_lane)) { ok = false; break; }
-      ph_lane ^= 1;
-      const int r = r0 + (kTwoRows ? ln * 128 : 0) + row, u = r / a.G;
-      const bool mine = r < nodes * a.G;
-      unsigned long long sees = 0;
-      if (mine)
-        for (int w = u; w >= 0; w = s_up[ln * 64 + w]) sees |= 1ull << w;
+    uint32_t ph_s = 0, ph_piece = 0, ph_both = 0;
+    bool ok = true, first = true;
+    for (;;) {
+      if (!wait_warp(bar_q, ph_piece)) { ok = false; break; }
+      const Piece pc = s_piece[ph_piece];
+      if (pc.cnt == 0) break;                                          // the share is done
+      const int S = pc.S, r = pc.r0 + (kTwoRows ? ln * 128 : 0) + row, u = r / a.G;
+      const bool mine = r < pc.nodes * a.G;
+      const unsigned long long sees = mine ? s_mask[ph_piece * 64 + u] : 0ull;
+      mbar_arrive(bar_qfree);
 
       float m_ref = -INFINITY, l = 0.f;
       bool started = false;
@@ -349,96 +364,106 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
 
       // ---- the piece is done
       const bool whole = pc.cnt == pc.tiles;
-      const long long seq_start = pos - pc.tile0;
-      const size_t slot = (size_t)blockIdx.x * 2 + (seq_start <= pos0 ? 0 : 1);
-      auto put = [&](int c, const float* o, float inv) {               // columns c .. c + 31 of this thread's row
+      const size_t slot = (size_t)blockIdx.x * 2 + (pc.tile0 > 0 || first ? 0 : 1);
+      first = false;
+      float2* ml_out = reinterpret_cast<float2*>(a.ws_ml) + slot * a.group_rows + (r - pc.r0);
+      float* o_out = a.ws_o + (slot * a.group_rows + (r - pc.r0)) * kD;
+      __nv_bfloat16* out = a.out + (((size_t)pc.t * a.T + (mine ? u : 0)) * a.Hq + (size_t)pc.h * a.G + (mine ? r - u * a.G : 0)) * kD;
+      // N columns, from c on, of this thread's row
+      auto put = [&](int c, uint32_t* o, int N, float inv) {
+        if (!mine) return;
         if (whole) {
-          if (r < a.rows) {
-            uint4* dst = reinterpret_cast<uint4*>(a.out + (((size_t)pc.t * a.T + u) * a.Hq + (size_t)h * a.G + r % a.G) * kD + c);
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-              dst[x] = mine ? make_uint4(pack2(o[8 * x] * inv, o[8 * x + 1] * inv), pack2(o[8 * x + 2] * inv, o[8 * x + 3] * inv),
-                                         pack2(o[8 * x + 4] * inv, o[8 * x + 5] * inv), pack2(o[8 * x + 6] * inv, o[8 * x + 7] * inv))
-                            : make_uint4(0, 0, 0, 0);
-          }
-        } else if (mine) {
-          float4* dst = reinterpret_cast<float4*>(a.ws_o + (slot * a.group_rows + (r - r0)) * kD + c);
+          for (int x = 0; x < N / 2; ++x) o[x] = pack2(__uint_as_float(o[2 * x]) * inv, __uint_as_float(o[2 * x + 1]) * inv);
 #pragma unroll
-          for (int x = 0; x < 8; ++x) dst[x] = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+          for (int x = 0; x < N / 2; x += 8) st_global32(out + c + 2 * x, o + x);
+        } else {
+#pragma unroll
+          for (int x = 0; x < N; x += 8) st_global32(o_out + c + x, o + x);
         }
       };
       if constexpr (kTwoRows) {
-        if (!whole && mine) *reinterpret_cast<float2*>(a.ws_ml + (slot * a.group_rows + (r - r0)) * 2) = make_float2(m_ref, l);
+        if (!whole && mine) *ml_out = make_float2(m_ref, l);
         const float inv = 1.f / l;
-#pragma unroll 1
-        for (int c = 0; c < kD; c += 32) {
-          uint32_t o[32];
+#pragma unroll
+        for (int c = 0; c < kD; c += 64) {
+          uint32_t o[64];
           tc_ld32_async(t_o + c, o);
+          tc_ld32_async(t_o + c + 32, o + 32);
           tc_wait_ld();
-          pin<32>(o);
-          put(c, reinterpret_cast<float*>(o), inv);
+          pin<64>(o);
+          put(c, o, 32, inv);
+          put(c + 32, o + 32, 32, inv);
         }
       } else {
         // the two lanes hold the even and the odd tiles of the same rows: each takes 64 columns of the sum, the other
-        // lane's part of them through shared memory (the query rows are not needed any more)
+        // lane's part of them through shared memory
         s_ml[(ln * 128 + row) * 2] = m_ref;
         s_ml[(ln * 128 + row) * 2 + 1] = l;
-        float* s_x = reinterpret_cast<float*>(sm);                     // [2][64][128]: columns lane 0 gives, lane 1 gives
         const bool some = ln < pc.cnt;                                 // a piece of one tile leaves lane 1 without any
-#pragma unroll 1
-        for (int c = 0; c < 64; c += 32) {
-          uint32_t o[32];
-          tc_ld32_async(t_o + (ln == 0 ? 64 : 0) + c, o);
-          tc_wait_ld();
-          pin<32>(o);
+        uint32_t o[128];
 #pragma unroll
-          for (int x = 0; x < 32; ++x) s_x[(ln * 64 + c + x) * 128 + row] = some ? __uint_as_float(o[x]) : 0.f;
-        }
-        mbar_arrive(bar_both);
-        if (!wait_warp(bar_both, ph_both)) { ok = false; break; }
-        ph_both ^= 1;
-        const float m0 = s_ml[row * 2], m1 = s_ml[(128 + row) * 2], l0 = s_ml[row * 2 + 1], l1 = s_ml[(128 + row) * 2 + 1];
-        const float M = fmaxf(m0, m1), off = M == -INFINITY ? 0.f : M;
-        const float w0 = exp2f(m0 - off), w1 = exp2f(m1 - off);
-        const float lsum = l0 * w0 + l1 * w1, inv = 1.f / lsum;
-        const float w_own = ln == 0 ? w0 : w1, w_other = ln == 0 ? w1 : w0;
-        if (!whole && mine && ln == 0) *reinterpret_cast<float2*>(a.ws_ml + (slot * a.group_rows + (r - r0)) * 2) = make_float2(M, lsum);
-#pragma unroll 1
-        for (int c = 0; c < 64; c += 32) {
-          uint32_t o[32];
-          float x32[32];
-          tc_ld32_async(t_o + (ln == 0 ? 0 : 64) + c, o);
-          tc_wait_ld();
-          pin<32>(o);
+        for (int c = 0; c < 4; ++c) tc_ld32_async(t_o + 32 * c, o + 32 * c);
+        tc_wait_ld();
+        pin<128>(o);
+        if (!some) {
 #pragma unroll
-          for (int x = 0; x < 32; ++x)
-            x32[x] = (some ? __uint_as_float(o[x]) * w_own : 0.f) + s_x[((1 - ln) * 64 + c + x) * 128 + row] * w_other;
-          put((ln == 0 ? 0 : 64) + c, x32, inv);
+          for (int c = 0; c < 128; ++c) o[c] = 0u;
         }
-        mbar_arrive(bar_both);                                         // the exchange area becomes the next query rows
-        if (!wait_warp(bar_both, ph_both)) { ok = false; break; }
-        ph_both ^= 1;
+        if (ln) {                                                      // so that o[0 .. 63] are kept, o[64 .. 127] given
+#pragma unroll
+          for (int c = 0; c < 64; ++c) { const uint32_t x = o[c]; o[c] = o[64 + c]; o[64 + c] = x; }
+        }
+        float w_own = 0.f, w_other = 0.f, inv = 0.f;
+#pragma unroll
+        for (int c = 0; c < 64; c += kXCols) {
+#pragma unroll
+          for (int x = 0; x < kXCols; ++x) s_x[(ln * kXCols + x) * 128 + row] = __uint_as_float(o[64 + c + x]);
+          mbar_arrive(bar_both);
+          if (!wait_warp(bar_both, ph_both)) { ok = false; break; }
+          ph_both ^= 1;
+          if (c == 0) {
+            const float m0 = s_ml[row * 2], m1 = s_ml[(128 + row) * 2], l0 = s_ml[row * 2 + 1], l1 = s_ml[(128 + row) * 2 + 1];
+            const float M = fmaxf(m0, m1), off = M == -INFINITY ? 0.f : M;
+            const float w0 = exp2f(m0 - off), w1 = exp2f(m1 - off);
+            const float lsum = l0 * w0 + l1 * w1;
+            inv = 1.f / lsum;
+            w_own = ln == 0 ? w0 : w1;
+            w_other = ln == 0 ? w1 : w0;
+            if (!whole && mine && ln == 0) *ml_out = make_float2(M, lsum);
+          }
+#pragma unroll
+          for (int x = 0; x < kXCols; ++x)
+            o[c + x] = __float_as_uint(__uint_as_float(o[c + x]) * w_own + s_x[((1 - ln) * kXCols + x) * 128 + row] * w_other);
+          put((ln == 0 ? 0 : 64) + c, o + c, kXCols, inv);
+          mbar_arrive(bar_both);                                       // the exchange area may be written again
+          if (!wait_warp(bar_both, ph_both)) { ok = false; break; }
+          ph_both ^= 1;
+        }
+        if (!ok) break;
       }
-      pos += pc.cnt;
     }
-  } else if (warp == kWarpFetch) {
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
+   if (warp == kWarpFetch) {
     // ------------------------------------------------ K and V tiles into the ring
     int slot = 0;
     uint32_t ph = 1;
     bool ok = true;
-    Piece pc = {};
-    int h = 0, S = 0, nodes = 0;
+    Place pl = {};
+    int h = 0;
     // tile i of the piece, K (kv = 0) or V, into the next slot
     auto fetch = [&](int i, int kv) {
       if (!ok) return;
       if (!wait_warp(bar_empty + 8 * slot, ph)) { ok = false; return; }
       const uint32_t bar = bar_full + 8 * slot, dst = sm_ring + slot * kSlotBytes;
-      const int j0 = (pc.tile0 + i) * kTile;
+      const int j0 = (pl.tile + i) * kTile;
+      const int S = pl.x.S, nodes = pl.x.nodes;
       // the block of every page of the tile (lanes 0 .. 7)
       int b = 0;
       const int page = j0 / kP + lane;
       if (lane < kTile / kP && page * kP < S) {
-        b = a.block_table[(size_t)pc.t * a.max_pages + page];
+        b = a.block_table[(size_t)pl.t * a.max_pages + page];
         if (b < 0 || b >= a.num_blocks) { flag_error(a.counters, STEP_ERR_BAD_BLOCK); b = 0; }
       }
       if (j0 + kTile <= S) {
@@ -453,7 +478,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       } else {
         // two rows of 16 chunks at a time; a cached row is copied as it is stored, which is the arrangement wanted here
         const int c = lane & 15;
-        const __nv_bfloat16* draft = (kv ? a.v_draft : a.k_draft) + (((size_t)pc.t * a.T * a.L + a.layer) * a.Hkv + h) * kD + c * 8;
+        const __nv_bfloat16* draft = (kv ? a.v_draft : a.k_draft) + (((size_t)pl.t * a.T * a.L + a.layer) * a.Hkv + h) * kD + c * 8;
         const size_t draft_row = (size_t)a.L * a.Hkv * kD;
 #pragma unroll 4
         for (int x = 0; x < kTile / 2; ++x) {
@@ -476,18 +501,21 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       __syncwarp();
       if (++slot == kSlots) { slot = 0; ph ^= 1; }
     };
-    for (long long pos = pos0; pos < end && ok; pos += pc.cnt) {
-      pc = piece_at(s_cum, a.n, HR, pos, end);
-      h = pc.hr / a.groups;
-      S = cached(a, pc.t, false);
-      nodes = nodes_of(a, pc.t, false);
+    long long pos, end;
+    my_share(blockIdx.x == 0, pos, end);
+    if (pos < end) pl = seek(a, lane, pos);
+    while (pos < end && ok) {
+      const int cnt = (int)min((long long)(pl.x.tiles - pl.tile), end - pos);
+      h = pl.hr / pl.x.groups;
       if constexpr (kTwoRows) {
-        for (int i = 0; i < pc.cnt; ++i) { fetch(i, 0); fetch(i, 1); }
+        for (int i = 0; i < cnt; ++i) { fetch(i, 0); fetch(i, 1); }
       } else {
         fetch(0, 0);
-        if (pc.cnt > 1) fetch(1, 0);
-        for (int i = 0; i < pc.cnt; ++i) { fetch(i, 1); if (i + 2 < pc.cnt) fetch(i + 2, 0); }
+        if (cnt > 1) fetch(1, 0);
+        for (int i = 0; i < cnt; ++i) { fetch(i, 1); if (i + 2 < cnt) fetch(i + 2, 0); }
       }
+      pos += cnt;
+      next_sequence(a, pl);
     }
     cp_async_wait_all();
     if (*s_abort)                                                      // copies in flight still target this CTA's shared memory
@@ -495,7 +523,55 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         mbar_wait_bounded(bar_full + 8 * s, 0, kDrainNs);
         mbar_wait_bounded(bar_full + 8 * s, 1, kDrainNs);
       }
-  } else if (lane == 0) {
+  } else if (warp >= kWarpQ) {
+    // ------------------------------------------------ query rows and ancestor masks of one piece after another
+    const int qt = threadIdx.x - kWarpQ * 32;                          // 0 .. 63
+    uint32_t par = 0;
+    long long pos, end;
+    my_share(false, pos, end);
+    Place pl = {};
+    if (pos < end) pl = seek(a, lane, pos);
+    for (;; par ^= 1) {
+      // the scores of the piece before are made, and its announcement has been read (the very first wait passes at once)
+      if (!wait_warp(bar_qfree, par ^ 1)) break;
+      Piece pc = {};
+      if (pos < end) {
+        pc.t = pl.t; pc.h = pl.hr / pl.x.groups; pc.r0 = (pl.hr - pc.h * pl.x.groups) * a.group_rows;
+        pc.tile0 = pl.tile; pc.tiles = pl.x.tiles; pc.S = pl.x.S; pc.nodes = pl.x.nodes;
+        pc.cnt = (int)min((long long)(pl.x.tiles - pl.tile), end - pos);
+        // four rows of 16 chunks at a time; rows behind the last drafted token are zeros
+        const int c = qt & 15;
+#pragma unroll 4
+        for (int x = 0; x < kQAll / 256 / 4; ++x) {
+          const int rr = x * 4 + (qt >> 4), r = pc.r0 + rr, u = r / a.G;
+          const bool real = r < pc.nodes * a.G;
+          const __nv_bfloat16* src = a.q + (((size_t)pc.t * a.T + (real ? u : 0)) * a.Hq + (size_t)pc.h * a.G + (real ? r - u * a.G : 0)) * kD + c * 8;
+          cp_async16_or_zero(sm_q + (rr >> 7) * kQBytes + (c >> 3) * (kQBytes / 2) + (rr & 127) * 128 + (((c ^ rr) & 7) << 4), src, real);
+        }
+        if (warp == kWarpQ) {
+          for (int u = lane; u < pc.nodes; u += 32) {
+            int p = a.parents[(size_t)pc.t * a.T + u];
+            if (p >= u || p < -1) { flag_error(a.counters, STEP_ERR_INVALID_ARG); p = -1; }
+            s_up[u] = p;
+          }
+          __syncwarp();
+          for (int u = lane; u < pc.nodes; u += 32) {
+            unsigned long long m = 0;
+            for (int w = u; w >= 0; w = s_up[w]) m |= 1ull << w;
+            s_mask[par * 64 + u] = m;
+          }
+          __syncwarp();
+        }
+        pos += pc.cnt;
+        next_sequence(a, pl);
+      }
+      if (qt == 0) s_piece[par] = pc;
+      cp_async_arrive_when_done(bar_q);
+      mbar_arrive(bar_q);
+      if (pc.cnt == 0) break;
+    }
+    cp_async_wait_all();
+  } else if (warp == kWarpMma && lane == 0) {
     // ------------------------------------------------ products
     const uint32_t id_qk = umma_idesc_bf16(kTile), id_pv = umma_idesc_bf16(kD) | (1u << 16);   // B of the second is MN-major
     int slot = 0;
@@ -529,41 +605,48 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         tc_mma_bf16_ta(tmem + 256 + ln * 128, tmem + ln * 128 + x * 8, umma_desc_v(vb + x * 2048), id_pv, !(first && x == 0));
     };
     auto release = [&](int s) { if (ok) tc_commit(bar_empty + 8 * s); };
-    for (long long pos = pos0; pos < end && ok;) {
-      const Piece pc = piece_at(s_cum, a.n, HR, pos, end);
+    for (;;) {
       if (!wait(bar_q, ph_q)) { ok = false; break; }
+      const int cnt = s_piece[ph_q].cnt;
       ph_q ^= 1;
+      if (cnt == 0) break;
+      fence_async_smem();                                              // (the query rows too)
+      auto last_scores = [&]() { if (ok) tc_commit(bar_qfree); };
       if constexpr (kTwoRows) {
         int k = next();
         scores(0, k);
         scores(1, k);
         release(k);
-        for (int i = 0; i < pc.cnt && ok; ++i) {
+        if (cnt == 1) last_scores();
+        for (int i = 0; i < cnt && ok; ++i) {
           const int v = next();
-          const bool more = i + 1 < pc.cnt;
+          const bool more = i + 1 < cnt;
           values(0, v, i == 0);
           if (more) { k = next(); scores(0, k); }
           values(1, v, i == 0);
           release(v);
           if (more) { scores(1, k); release(k); }
+          if (i + 2 == cnt) last_scores();
         }
       } else {
         int k = next();
         scores(0, k);
         release(k);
-        if (pc.cnt > 1) { k = next(); scores(1, k); release(k); }
-        for (int i = 0; i < pc.cnt && ok; ++i) {
+        if (cnt > 1) { k = next(); scores(1, k); release(k); }
+        if (cnt <= 2) last_scores();
+        for (int i = 0; i < cnt && ok; ++i) {
           const int v = next();
           values(i & 1, v, i < 2);
           release(v);
-          if (i + 2 < pc.cnt) { k = next(); scores(i & 1, k); release(k); }
+          if (i + 2 < cnt) { k = next(); scores(i & 1, k); release(k); }
+          if (i + 3 == cnt) last_scores();
         }
       }
       if (ok) { tc_commit(bar_o); tc_commit(bar_o + 8); }
-      pos += pc.cnt;
     }
     tc_commit(bar_drain);                                              // no product is in flight when the tensor memory goes back
     mbar_wait_bounded(bar_drain, 0);
+  }
   }
   __syncwarp();
   tc_fence_before();
@@ -579,26 +662,41 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
 constexpr int kMergeWarps = 4;
 
 __global__ void __launch_bounds__(kMergeWarps * 32) tree_merge_kernel(TreeArgs a) {
-  extern __shared__ int s_cum[];
+  extern __shared__ long long s_start[];                               // [n] tiles before trace t, per KV head
+  __shared__ long long s_total;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (warp == 0) build_stream(a, lane, false, s_cum);
+  if (warp == 0) {
+    long long run = 0;
+    for (int base = 0; base < a.n; base += 32) {
+      const int t = base + lane;
+      long long mine = 0;
+      if (t < a.n) { const Shape x = shape_of(a, t, false); mine = (long long)x.tiles * x.groups; }
+      long long incl = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long u = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += u;
+      }
+      if (t < a.n) s_start[t] = run + incl - mine;
+      run += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (lane == 0) s_total = run * a.Hkv;
+  }
   __syncthreads();
+  const long long W = (s_total + a.shares - 1) / a.shares;
   wait_for_primary();
-  const int HR = a.Hkv * a.groups;
-  const long long total = (long long)HR * s_cum[a.n];
-  const long long W = (total + a.shares - 1) / a.shares;
   const long long items = (long long)a.n * a.Hkv * a.rows;
   for (long long item = (long long)blockIdx.x * kMergeWarps + warp; item < items; item += (long long)gridDim.x * kMergeWarps) {
     const int r = (int)(item % a.rows);
     const long long th = item / a.rows;
     const int t = (int)(th / a.Hkv), h = (int)(th - (long long)t * a.Hkv);
-    const int tiles = s_cum[t + 1] - s_cum[t];
-    const int group = r / a.group_rows, rr = r - group * a.group_rows;
-    const long long start = (long long)HR * s_cum[t] + ((long long)h * a.groups + group) * tiles;
-    const int w0 = (int)(start / W), w1 = (int)((start + tiles - 1) / W);
-    if (w0 == w1) continue;                                            // one piece: written by the attention kernel
+    const Shape x = shape_of(a, t, false);
     uint2* out = reinterpret_cast<uint2*>(a.out + (((size_t)t * a.T + r / a.G) * a.Hq + (size_t)h * a.G + r % a.G) * kD) + lane;
-    if (r >= nodes_of(a, t, false) * a.G) { *out = make_uint2(0, 0); continue; }
+    if (r >= x.nodes * a.G) { *out = make_uint2(0, 0); continue; }     // behind the row's last drafted token
+    const int group = r / a.group_rows, rr = r - group * a.group_rows;
+    const long long start = (long long)a.Hkv * s_start[t] + ((long long)h * x.groups + group) * x.tiles;
+    const int w0 = (int)(start / W), w1 = (int)((start + x.tiles - 1) / W);
+    if (w0 == w1) continue;                                            // one piece: written by the attention kernel
     float M = -INFINITY, den = 0.f;
     float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int w = w0; w <= w1; ++w) {
@@ -617,7 +715,10 @@ __global__ void __launch_bounds__(kMergeWarps * 32) tree_merge_kernel(TreeArgs a
   }
 }
 
-size_t smem_bytes(int n) { return 1024 + 2 * kQBytes + kSlots * kSlotBytes + 32 * 8 + 512 * 4 + 128 * 4 + 16 + (size_t)(n + 1) * 4; }
+size_t smem_bytes(bool two_rows) {
+  return 1024 + (two_rows ? 2 * kQBytes : kQBytes + kXBytes + 512 * 4) + kSlots * kSlotBytes + 32 * 8 + 128 * 8 + 2 * sizeof(Piece) + 64 * 4 + 16;
+}
+static_assert(1024 + 2 * kQBytes + kSlots * kSlotBytes + 32 * 8 + 128 * 8 + 2 * sizeof(Piece) + 64 * 4 + 16 <= 232448, "shared memory of one CTA");
 
 }  // namespace
 
@@ -658,19 +759,18 @@ int tree_tc_launch(step_pool* pool, int layer, const void* q, const void* k_draf
   a.n = n; a.T = T; a.Hq = g.Hq; a.Hkv = g.Hkv; a.G = g.G; a.L = g.L; a.layer = layer; a.max_pages = g.max_pages; a.num_blocks = g.num_blocks;
   a.rows = T * g.G;
   a.group_rows = a.rows > kHalfRows ? 2 * kHalfRows : kHalfRows;
-  a.groups = (a.rows + a.group_rows - 1) / a.group_rows;
   a.shares = pool->num_sms;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)kD);
   a.ws_o = (float*)workspace;
   a.ws_ml = a.ws_o + (size_t)a.shares * 2 * a.group_rows * kD;
-  const size_t smem = smem_bytes(n);
+  const size_t smem = smem_bytes(a.group_rows > kHalfRows);
   auto kern = a.group_rows > kHalfRows ? tree_tc_kernel<true> : tree_tc_kernel<false>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return STEP_ERR_CUDA;
   kern<<<a.shares, kThreads, smem, s>>>(map, a);
   if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
   long long mgrid = ((long long)n * g.Hkv * a.rows + kMergeWarps - 1) / kMergeWarps;
   if (mgrid > 2ll * pool->num_sms) mgrid = 2ll * pool->num_sms;
-  if (launch_dependent(tree_merge_kernel, dim3((unsigned)mgrid), dim3(kMergeWarps * 32), (size_t)(n + 1) * 4, s, a) != cudaSuccess) return STEP_ERR_CUDA;
+  if (launch_dependent(tree_merge_kernel, dim3((unsigned)mgrid), dim3(kMergeWarps * 32), (size_t)n * sizeof(long long), s, a) != cudaSuccess) return STEP_ERR_CUDA;
   return launch_ok();
 }
 
