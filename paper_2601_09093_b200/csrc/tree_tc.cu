@@ -38,8 +38,7 @@ namespace {
 
 constexpr int kP = 16, kD = 128;
 constexpr int kTile = 128;                        // keys per tile
-constexpr int kSlotBytes = kTile * kD * 2;        // K or V of one tile: two halves of 128 rows x 128 bytes
-constexpr int kHalfSlot = kSlotBytes / 2;
+constexpr int kSlotBytes = kTile * kD * 2;        // K or V of one tile
 constexpr int kQBytes = kHalfRows * kD * 2;       // 128 query rows, same arrangement
 constexpr int kSlots = 5;                         // ring of K and V tiles: 160 KiB
 constexpr int kXCols = 16;                        // columns per round in which the lanes exchange their sums (below 128 rows)
@@ -144,10 +143,13 @@ __device__ inline void next_sequence(const TreeArgs& a, Place& p) {
 struct Piece { int t, h, r0, tile0, cnt, tiles, S, nodes; };
 
 // ---- instructions
-__device__ inline void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+__device__ inline void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
   asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ inline void mbar_arrive_n(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
 // 16 bytes, or 16 zero bytes (src is then not read)
 __device__ inline void cp_async16_or_zero(uint32_t dst, const void* src, bool real) {
@@ -192,11 +194,20 @@ __device__ inline void tc_mma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
-// Descriptor of V as an MN-major operand: 64 of the N index are 128 contiguous (swizzled) bytes, the next 64 lie a half slot
-// further (leading byte offset), 8 of the K index (tokens) are 1024 bytes (stride byte offset).
+// A K or V tile in a ring slot: groups of 8 rows (tokens), a group as two halves of 8 rows x 128 bytes with the 128-byte
+// swizzle.  Byte offset of 16-byte chunk `at` (0 .. 15, as stored) of row rr:
+__device__ inline uint32_t tile_chunk(int rr, int at) { return (rr >> 3) * 2048 + (at >> 3) * 1024 + (rr & 7) * 128 + (at & 7) * 16; }
+// K as a K-major operand: the next 8 keys (N) are 2048 bytes further; dims from 64 on start 1024 bytes further.
+__device__ inline uint64_t umma_desc_k(uint32_t smem_addr) {
+  const uint32_t lo = ((smem_addr >> 4) & 0x3FFFu) | (1u << 16);
+  const uint32_t hi = (2048u >> 4) | (1u << 14) | (2u << 29);
+  return ((uint64_t)hi << 32) | lo;
+}
+// V as an MN-major operand: 64 of the N index (dims) are 128 contiguous bytes, the next 64 lie 1024 bytes further (leading
+// byte offset), the next 8 of the K index (tokens) 2048 bytes (stride byte offset).
 __device__ inline uint64_t umma_desc_v(uint32_t smem_addr) {
-  const uint32_t lo = ((smem_addr >> 4) & 0x3FFFu) | ((uint32_t)(kHalfSlot >> 4) << 16);
-  const uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+  const uint32_t lo = ((smem_addr >> 4) & 0x3FFFu) | ((1024u >> 4) << 16);
+  const uint32_t hi = (2048u >> 4) | (1u << 14) | (2u << 29);
   return ((uint64_t)hi << 32) | lo;
 }
 // 32 bytes (a whole sector) per thread
@@ -238,13 +249,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       mbar_init(bar_empty + 8 * s, 1);              // tcgen05.commit
     }
     mbar_init(bar_q, 128);                          // the query warps' threads, and their copies
-    mbar_init(bar_qfree, 257);                      // tcgen05.commit: a piece's last scores; all softmax threads have begun it
+    mbar_init(bar_qfree, 9);                        // tcgen05.commit: a piece's last scores; all softmax warps have begun it
     for (int s = 0; s < 2; ++s) {
       mbar_init(bar_s + 8 * s, 1);                  // tcgen05.commit: scores made (and the products before them done)
-      mbar_init(bar_p + 8 * s, 128);
+      mbar_init(bar_p + 8 * s, 4);                  // (one arrival per warp: arrivals at one barrier queue up)
       mbar_init(bar_o + 8 * s, 1);                  // tcgen05.commit: a piece's last product
     }
-    mbar_init(bar_both, 256);
+    mbar_init(bar_both, 8);
     mbar_init(bar_drain, 1);
     *s_abort = 0;
     mbar_init_fence();
@@ -276,6 +287,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   // the same, with one answer for the whole warp: what follows has to be executed by all of it
   auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
 
+  // one arrival for all of the warp's threads
+  auto arrive_warp = [&](uint32_t bar) { __syncwarp(); if (lane == 0) mbar_arrive(bar); };
+
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
     // ------------------------------------------------ softmax: lane `ln` of the CTA, row `row` of its 128
@@ -291,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       const int S = pc.S, r = pc.r0 + (kTwoRows ? ln * 128 : 0) + row, u = r / a.G;
       const bool mine = r < pc.nodes * a.G;
       const unsigned long long sees = mine ? s_mask[ph_piece * 64 + u] : 0ull;
-      mbar_arrive(bar_qfree);
+      arrive_warp(bar_qfree);
 
       float m_ref = -INFINITY, l = 0.f;
       bool started = false;
@@ -356,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         tc_st32(t_s + 32, s + 32);
         tc_wait_st();
         tc_fence_before();
-        mbar_arrive(bar_p + 8 * ln);
+        arrive_warp(bar_p + 8 * ln);
       }
       if (!ok || !wait_warp(bar_o + 8 * ln, ph_piece)) { ok = false; break; }
       tc_fence_after();
@@ -419,7 +433,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         for (int c = 0; c < 64; c += kXCols) {
 #pragma unroll
           for (int x = 0; x < kXCols; ++x) s_x[(ln * kXCols + x) * 128 + row] = __uint_as_float(o[64 + c + x]);
-          mbar_arrive(bar_both);
+          arrive_warp(bar_both);
           if (!wait_warp(bar_both, ph_both)) { ok = false; break; }
           ph_both ^= 1;
           if (c == 0) {
@@ -436,7 +450,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
           for (int x = 0; x < kXCols; ++x)
             o[c + x] = __float_as_uint(__uint_as_float(o[c + x]) * w_own + s_x[((1 - ln) * kXCols + x) * 128 + row] * w_other);
           put((ln == 0 ? 0 : 64) + c, o + c, kXCols, inv);
-          mbar_arrive(bar_both);                                       // the exchange area may be written again
+          arrive_warp(bar_both);                                       // the exchange area may be written again
           if (!wait_warp(bar_both, ph_both)) { ok = false; break; }
           ph_both ^= 1;
         }
@@ -452,6 +466,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     bool ok = true;
     Place pl = {};
     int h = 0;
+    // Block ids of 64 pages (eight tiles): lane i holds those of pages win + i and win + 32 + i.  The second half is asked
+    // for when V enters the first, four tiles before K needs it: with a read of the table in front of every tile, the read's
+    // latency set the pace of the whole kernel (1,800 cycles a tile and operand).
+    int win = 0, ids0 = 0, ids1 = 0;
+    auto load_ids = [&](const Place& of, int first) {
+      const int page = first + lane;
+      return of.t < a.n && (long long)page * kP < of.x.S ? a.block_table[(size_t)of.t * a.max_pages + page] : 0;
+    };
     // tile i of the piece, K (kv = 0) or V, into the next slot
     auto fetch = [&](int i, int kv) {
       if (!ok) return;
@@ -459,44 +481,40 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       const uint32_t bar = bar_full + 8 * slot, dst = sm_ring + slot * kSlotBytes;
       const int j0 = (pl.tile + i) * kTile;
       const int S = pl.x.S, nodes = pl.x.nodes;
-      // the block of every page of the tile (lanes 0 .. 7)
-      int b = 0;
-      const int page = j0 / kP + lane;
-      if (lane < kTile / kP && page * kP < S) {
-        b = a.block_table[(size_t)pl.t * a.max_pages + page];
-        if (b < 0 || b >= a.num_blocks) { flag_error(a.counters, STEP_ERR_BAD_BLOCK); b = 0; }
-      }
-      if (j0 + kTile <= S) {
-        if (lane == 0) mbar_expect_tx(bar, kSlotBytes); else mbar_arrive(bar);
-        __syncwarp();
-        const int pg = lane >> 1, half = lane & 1;
-        const int bb = __shfl_sync(0xffffffffu, b, pg);
-        if (lane < 2 * (kTile / kP))
-          tma_load_3d(dst + half * kHalfSlot + pg * (kP * 128), &map, 0, half,
-                      ((((a.layer * a.num_blocks) + bb) * a.Hkv + h) * 2 + kv) * kP, bar);
-        if (lane == 0) mbar_arrive(bar);
+      if (kv && j0 / kP >= win + 32) { win += 32; ids0 = ids1; ids1 = load_ids(pl, win + 32); }
+      const int in_win = j0 / kP - win;
+      // block of page pg (0 .. 7) of this tile; one out of range is flagged and read as block 0
+      auto block_of = [&](int pg) {
+        int bb = __shfl_sync(0xffffffffu, in_win < 32 ? ids0 : ids1, (in_win + pg) & 31);
+        if (bb < 0 || bb >= a.num_blocks) { flag_error(a.counters, STEP_ERR_BAD_BLOCK); bb = 0; }
+        return bb;
+      };
+      // whole pages by TMA; behind the last of them (the end of the cache, drafted tokens) row by row, zeros up to a
+      // multiple of 16 keys, which is as far as the second product goes
+      const int pages = min(kTile / kP, max(0, (S - j0) / kP));
+      if (lane == 0 && pages > 0) mbar_expect_tx(bar, pages * (kP * kD * 2));
+      __syncwarp();
+      const int own = block_of(lane & 7);
+      if (lane < pages)                                                // a box is the K or the V of a page
+        tma_load_4d(dst + lane * (kP * kD * 2), &map, 0, 0, 0, ((((a.layer * a.num_blocks) + own) * a.Hkv + h) * 2 + kv) * (kP / 8), bar);
+      if (pages == kTile / kP) {
+        if (lane == 0) mbar_arrive_n(bar, 32);
       } else {
         // two rows of 16 chunks at a time; a cached row is copied as it is stored, which is the arrangement wanted here
-        const int c = lane & 15;
+        const int c = lane & 15, rows = min(kTile, (S + nodes - j0 + 15) & ~15);
+        const int bb = block_of(pages);                                // the page that the cache ends in
+        const __nv_bfloat16* tail = a.kv + ((((size_t)a.layer * a.num_blocks + bb) * a.Hkv + h) * 2 + kv) * (kP * kD) + c * 8;
         const __nv_bfloat16* draft = (kv ? a.v_draft : a.k_draft) + (((size_t)pl.t * a.T * a.L + a.layer) * a.Hkv + h) * kD + c * 8;
         const size_t draft_row = (size_t)a.L * a.Hkv * kD;
 #pragma unroll 4
-        for (int x = 0; x < kTile / 2; ++x) {
-          const int rr = 2 * x + (lane >> 4), j = j0 + rr;
-          const int bb = __shfl_sync(0xffffffffu, b, rr / kP);
-          const __nv_bfloat16* src = a.kv;
-          int at = c;
+        for (int rr = pages * kP + (lane >> 4); rr < rows; rr += 2) {
+          const int j = j0 + rr;
           const bool real = j < S + nodes;
-          if (j < S)
-            src = a.kv + ((((size_t)a.layer * a.num_blocks + bb) * a.Hkv + h) * 2 + kv) * (kP * kD) + (rr % kP) * kD + c * 8;
-          else {
-            if (real) src = draft + (size_t)(j - S) * draft_row;
-            at = (c & 8) | ((c ^ rr) & 7);
-          }
-          cp_async16_or_zero(dst + (at >> 3) * kHalfSlot + rr * 128 + (at & 7) * 16, src, real);
+          const __nv_bfloat16* src = j < S ? tail + (rr % kP) * kD : (real ? draft + (size_t)(j - S) * draft_row : a.kv);
+          cp_async16_or_zero(dst + tile_chunk(rr, j < S ? c : (c & 8) | ((c ^ rr) & 7)), src, real);
         }
         cp_async_arrive_when_done(bar);
-        if (lane == 0) mbar_arrive(bar);
+        if (lane == 0 && pages == 0) mbar_arrive(bar);                 // (the announcement of bytes is the other form of this arrival)
       }
       __syncwarp();
       if (++slot == kSlots) { slot = 0; ph ^= 1; }
@@ -504,9 +522,17 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     long long pos, end;
     my_share(blockIdx.x == 0, pos, end);
     if (pos < end) pl = seek(a, lane, pos);
+    int next0 = load_ids(pl, (pl.tile * (kTile / kP)) & ~31), next1 = load_ids(pl, ((pl.tile * (kTile / kP)) & ~31) + 32);
     while (pos < end && ok) {
       const int cnt = (int)min((long long)(pl.x.tiles - pl.tile), end - pos);
       h = pl.hr / pl.x.groups;
+      win = (pl.tile * (kTile / kP)) & ~31;
+      ids0 = next0;
+      ids1 = next1;
+      Place nx = pl;                                                   // the sequence behind this one, its block ids too
+      next_sequence(a, nx);
+      next0 = load_ids(nx, 0);
+      next1 = load_ids(nx, 32);
       if constexpr (kTwoRows) {
         for (int i = 0; i < cnt; ++i) { fetch(i, 0); fetch(i, 1); }
       } else {
@@ -515,7 +541,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         for (int i = 0; i < cnt; ++i) { fetch(i, 1); if (i + 2 < cnt) fetch(i + 2, 0); }
       }
       pos += cnt;
-      next_sequence(a, pl);
+      pl = nx;
     }
     cp_async_wait_all();
     if (*s_abort)                                                      // copies in flight still target this CTA's shared memory
@@ -532,23 +558,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     Place pl = {};
     if (pos < end) pl = seek(a, lane, pos);
     for (;; par ^= 1) {
-      // the scores of the piece before are made, and its announcement has been read (the very first wait passes at once)
-      if (!wait_warp(bar_qfree, par ^ 1)) break;
       Piece pc = {};
       if (pos < end) {
         pc.t = pl.t; pc.h = pl.hr / pl.x.groups; pc.r0 = (pl.hr - pc.h * pl.x.groups) * a.group_rows;
         pc.tile0 = pl.tile; pc.tiles = pl.x.tiles; pc.S = pl.x.S; pc.nodes = pl.x.nodes;
         pc.cnt = (int)min((long long)(pl.x.tiles - pl.tile), end - pos);
-        // four rows of 16 chunks at a time; rows behind the last drafted token are zeros
-        const int c = qt & 15;
-#pragma unroll 4
-        for (int x = 0; x < kQAll / 256 / 4; ++x) {
-          const int rr = x * 4 + (qt >> 4), r = pc.r0 + rr, u = r / a.G;
-          const bool real = r < pc.nodes * a.G;
-          const __nv_bfloat16* src = a.q + (((size_t)pc.t * a.T + (real ? u : 0)) * a.Hq + (size_t)pc.h * a.G + (real ? r - u * a.G : 0)) * kD + c * 8;
-          cp_async16_or_zero(sm_q + (rr >> 7) * kQBytes + (c >> 3) * (kQBytes / 2) + (rr & 127) * 128 + (((c ^ rr) & 7) << 4), src, real);
-        }
-        if (warp == kWarpQ) {
+        if (warp == kWarpQ) {                                          // (the other piece's masks are the ones in use)
           for (int u = lane; u < pc.nodes; u += 32) {
             int p = a.parents[(size_t)pc.t * a.T + u];
             if (p >= u || p < -1) { flag_error(a.counters, STEP_ERR_INVALID_ARG); p = -1; }
@@ -565,12 +580,34 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         pos += pc.cnt;
         next_sequence(a, pl);
       }
+      // the scores of the piece before are made, and its announcement has been read (the very first wait passes at once)
+      if (!wait_warp(bar_qfree, par ^ 1)) break;
+      if (pc.cnt > 0) {
+        // four rows of 16 chunks at a time; rows behind the last drafted token are zeros
+        const int c = qt & 15, last = pc.nodes * a.G;
+        int rr = qt >> 4, u = (pc.r0 + rr) / a.G, g = pc.r0 + rr - u * a.G;
+        const __nv_bfloat16* heads = a.q + ((size_t)pc.t * a.T * a.Hq + (size_t)pc.h * a.G) * kD + c * 8;
+        const uint32_t dst = sm_q + (c >> 3) * (kQBytes / 2);
+#pragma unroll 4
+        for (; rr < kQAll / 256; rr += 4) {
+          cp_async16_or_zero(dst + (rr >> 7) * kQBytes + (rr & 127) * 128 + (((c ^ rr) & 7) << 4),
+                             heads + ((size_t)u * a.Hq + g) * kD, pc.r0 + rr < last);
+          for (g += 4; g >= a.G; g -= a.G) ++u;
+        }
+      }
       if (qt == 0) s_piece[par] = pc;
       cp_async_arrive_when_done(bar_q);
       mbar_arrive(bar_q);
       if (pc.cnt == 0) break;
     }
     cp_async_wait_all();
+    // out rows behind a trace's last drafted token
+    for (int t = blockIdx.x; t < a.n; t += gridDim.x) {
+      const int nodes = nodes_of(a, t, false);
+      uint4* dst = reinterpret_cast<uint4*>(a.out + ((size_t)t * a.T + nodes) * a.Hq * kD);
+      const int chunks = (a.T - nodes) * a.Hq * (kD / 8);
+      for (int x = qt; x < chunks; x += 64) dst[x] = make_uint4(0, 0, 0, 0);
+    }
   } else if (warp == kWarpMma && lane == 0) {
     // ------------------------------------------------ products
     const uint32_t id_qk = umma_idesc_bf16(kTile), id_pv = umma_idesc_bf16(kD) | (1u << 16);   // B of the second is MN-major
@@ -592,22 +629,24 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
 #pragma unroll
       for (int x = 0; x < 8; ++x)
         tc_mma_bf16(tmem + ln * 128, umma_desc_sw128(qa + (x >> 2) * (kQBytes / 2) + (x & 3) * 32),
-                    umma_desc_sw128(kb + (x >> 2) * kHalfSlot + (x & 3) * 32), id_qk, x != 0);
+                    umma_desc_k(kb + (x >> 2) * 1024 + (x & 3) * 32), id_qk, x != 0);
       tc_commit(bar_s + 8 * ln);
     };
-    auto values = [&](int ln, int s, bool first) {
+    // steps of 16 keys; those of a tile behind the last key are left out, so nothing that lies there matters
+    auto values = [&](int ln, int s, bool first, int steps) {
       if (!ok || !wait(bar_p + 8 * ln, ph_p[ln])) { ok = false; return; }
       ph_p[ln] ^= 1;
       tc_fence_after();
       const uint32_t vb = sm_ring + s * kSlotBytes;
 #pragma unroll
       for (int x = 0; x < 8; ++x)
-        tc_mma_bf16_ta(tmem + 256 + ln * 128, tmem + ln * 128 + x * 8, umma_desc_v(vb + x * 2048), id_pv, !(first && x == 0));
+        if (x < steps) tc_mma_bf16_ta(tmem + 256 + ln * 128, tmem + ln * 128 + x * 8, umma_desc_v(vb + x * 4096), id_pv, !(first && x == 0));
     };
     auto release = [&](int s) { if (ok) tc_commit(bar_empty + 8 * s); };
     for (;;) {
       if (!wait(bar_q, ph_q)) { ok = false; break; }
-      const int cnt = s_piece[ph_q].cnt;
+      const int cnt = s_piece[ph_q].cnt, keys = s_piece[ph_q].S + s_piece[ph_q].nodes - s_piece[ph_q].tile0 * kTile;
+      auto steps = [&](int i) { return min(8, (keys - i * kTile + 15) / 16); };
       ph_q ^= 1;
       if (cnt == 0) break;
       fence_async_smem();                                              // (the query rows too)
@@ -621,9 +660,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         for (int i = 0; i < cnt && ok; ++i) {
           const int v = next();
           const bool more = i + 1 < cnt;
-          values(0, v, i == 0);
+          values(0, v, i == 0, steps(i));
+          if (ok && !more) tc_commit(bar_o);
           if (more) { k = next(); scores(0, k); }
-          values(1, v, i == 0);
+          values(1, v, i == 0, steps(i));
+          if (ok && !more) tc_commit(bar_o + 8);
           release(v);
           if (more) { scores(1, k); release(k); }
           if (i + 2 == cnt) last_scores();
@@ -636,13 +677,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         if (cnt <= 2) last_scores();
         for (int i = 0; i < cnt && ok; ++i) {
           const int v = next();
-          values(i & 1, v, i < 2);
+          values(i & 1, v, i < 2, steps(i));
           release(v);
           if (i + 2 < cnt) { k = next(); scores(i & 1, k); release(k); }
           if (i + 3 == cnt) last_scores();
         }
+        if (ok) { tc_commit(bar_o); tc_commit(bar_o + 8); }
       }
-      if (ok) { tc_commit(bar_o); tc_commit(bar_o + 8); }
     }
     tc_commit(bar_drain);                                              // no product is in flight when the tensor memory goes back
     mbar_wait_bounded(bar_drain, 0);
@@ -657,48 +698,36 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   }
 }
 
-// Combines the pieces of every sequence that more than one share holds: a warp per query row, lanes over the 128 dims, the
-// pieces in stream order with a running (max, sum, weighted values).  The same bits whatever ran when.
-constexpr int kMergeWarps = 4;
+// Combines the pieces of every sequence that more than one share holds.  A CTA takes one border between two shares (and 32
+// of the rows): if the sequence it cuts has no border before it, the CTA combines all of that sequence's pieces, a warp per
+// query row, lanes over the 128 dims, in stream order with a running (max, sum, weighted values).  The same bits whatever
+// ran when.  The search runs while the attention kernel is still at work.
+constexpr int kMergeWarps = 8, kMergeRows = 32;
 
 __global__ void __launch_bounds__(kMergeWarps * 32) tree_merge_kernel(TreeArgs a) {
-  extern __shared__ long long s_start[];                               // [n] tiles before trace t, per KV head
-  __shared__ long long s_total;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  __shared__ Place s_place;
+  __shared__ long long s_W;
+  const int w0 = blockIdx.x;                                           // the share in front of the border
   if (warp == 0) {
-    long long run = 0;
-    for (int base = 0; base < a.n; base += 32) {
-      const int t = base + lane;
-      long long mine = 0;
-      if (t < a.n) { const Shape x = shape_of(a, t, false); mine = (long long)x.tiles * x.groups; }
-      long long incl = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long u = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += u;
-      }
-      if (t < a.n) s_start[t] = run + incl - mine;
-      run += __shfl_sync(0xffffffffu, incl, 31);
-    }
-    if (lane == 0) s_total = run * a.Hkv;
+    const long long total = stream_total(a, lane, false), W = (total + a.shares - 1) / a.shares, border = (w0 + 1) * W;
+    Place p = {};
+    p.t = -1;
+    if (border < total) p = seek(a, lane, border);
+    if (lane == 0) { s_place = p; s_W = W; }
   }
   __syncthreads();
-  const long long W = (s_total + a.shares - 1) / a.shares;
   wait_for_primary();
-  const long long items = (long long)a.n * a.Hkv * a.rows;
-  for (long long item = (long long)blockIdx.x * kMergeWarps + warp; item < items; item += (long long)gridDim.x * kMergeWarps) {
-    const int r = (int)(item % a.rows);
-    const long long th = item / a.rows;
-    const int t = (int)(th / a.Hkv), h = (int)(th - (long long)t * a.Hkv);
-    const Shape x = shape_of(a, t, false);
-    uint2* out = reinterpret_cast<uint2*>(a.out + (((size_t)t * a.T + r / a.G) * a.Hq + (size_t)h * a.G + r % a.G) * kD) + lane;
-    if (r >= x.nodes * a.G) { *out = make_uint2(0, 0); continue; }     // behind the row's last drafted token
-    const int group = r / a.group_rows, rr = r - group * a.group_rows;
-    const long long start = (long long)a.Hkv * s_start[t] + ((long long)h * x.groups + group) * x.tiles;
-    const int w0 = (int)(start / W), w1 = (int)((start + x.tiles - 1) / W);
-    if (w0 == w1) continue;                                            // one piece: written by the attention kernel
+  const Place p = s_place;
+  const long long W = s_W, start = (w0 + 1) * W - p.tile;              // where the sequence begins
+  if (p.t < 0 || p.tile == 0 || start < w0 * W) return;                // no border, no cut, or not the first cut of the sequence
+  const int h = p.hr / p.x.groups, r0 = (p.hr - h * p.x.groups) * a.group_rows;
+  const int w1 = (int)((start + p.x.tiles - 1) / W);
+  const int rows = min(a.group_rows, p.x.nodes * a.G - r0);
+  for (int rr = blockIdx.y * kMergeRows + warp; rr < min(rows, (int)(blockIdx.y + 1) * kMergeRows); rr += kMergeWarps) {
     float M = -INFINITY, den = 0.f;
     float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
     for (int w = w0; w <= w1; ++w) {
       const size_t slot = (size_t)w * 2 + (start <= (long long)w * W ? 0 : 1);
       const float2 ml = __ldcg(reinterpret_cast<const float2*>(a.ws_ml + (slot * a.group_rows + rr) * 2));
@@ -711,7 +740,9 @@ __global__ void __launch_bounds__(kMergeWarps * 32) tree_merge_kernel(TreeArgs a
       M = Mb;
     }
     const float inv = 1.f / den;
-    *out = make_uint2(pack2(num.x * inv, num.y * inv), pack2(num.z * inv, num.w * inv));
+    const int r = r0 + rr;
+    reinterpret_cast<uint2*>(a.out + (((size_t)p.t * a.T + r / a.G) * a.Hq + (size_t)h * a.G + r % a.G) * kD)[lane] =
+        make_uint2(pack2(num.x * inv, num.y * inv), pack2(num.z * inv, num.w * inv));
   }
 }
 
@@ -741,13 +772,14 @@ int tree_tc_launch(step_pool* pool, int layer, const void* q, const void* k_draf
   const Geo g = geo_of(pool);
   EncodeTiledFn enc = encode_tiled_fn();
   if (!enc) return STEP_ERR_CUDA;
-  // the pool as rows of 128 dims, a row as two halves of 128 bytes; a box is one half of a page's 16 K or V rows
+  // the pool as groups of 8 rows of 128 dims, seen as [group][half of the dims][row][64 dims]; a box is the two groups of a
+  // page's K or V
   CUtensorMap map;
-  const cuuint64_t dims[3] = {64, 2, (cuuint64_t)g.L * g.num_blocks * g.Hkv * 2 * kP};
-  const cuuint64_t strides[2] = {128, 256};
-  const cuuint32_t box[3] = {64, 1, kP};
-  const cuuint32_t estr[3] = {1, 1, 1};
-  if (enc(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, pool->cfg.kv_storage, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  const cuuint64_t dims[4] = {64, 8, 2, (cuuint64_t)g.L * g.num_blocks * g.Hkv * 2 * (kP / 8)};
+  const cuuint64_t strides[3] = {256, 128, 2048};
+  const cuuint32_t box[4] = {64, 8, 2, kP / 8};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  if (enc(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, pool->cfg.kv_storage, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
           CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return STEP_ERR_CUDA;
   TreeArgs a;
@@ -768,9 +800,8 @@ int tree_tc_launch(step_pool* pool, int layer, const void* q, const void* k_draf
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return STEP_ERR_CUDA;
   kern<<<a.shares, kThreads, smem, s>>>(map, a);
   if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
-  long long mgrid = ((long long)n * g.Hkv * a.rows + kMergeWarps - 1) / kMergeWarps;
-  if (mgrid > 2ll * pool->num_sms) mgrid = 2ll * pool->num_sms;
-  if (launch_dependent(tree_merge_kernel, dim3((unsigned)mgrid), dim3(kMergeWarps * 32), (size_t)n * sizeof(long long), s, a) != cudaSuccess) return STEP_ERR_CUDA;
+  if (a.shares > 1 &&
+      launch_dependent(tree_merge_kernel, dim3(a.shares - 1, a.group_rows / kMergeRows), dim3(kMergeWarps * 32), 0, s, a) != cudaSuccess) return STEP_ERR_CUDA;
   return launch_ok();
 }
 
