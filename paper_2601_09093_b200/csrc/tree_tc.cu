@@ -22,10 +22,10 @@
 //     share per CTA; what a share holds of a sequence is a piece.  A piece that is not a whole sequence leaves its
 //     (m, l, O) in the share's first or last slot, and tree_merge_kernel - a programmatic dependent - combines the pieces of
 //     every sequence in stream order.  Row groups without a drafted token of theirs (a short tree) are not in the stream;
-//   * two warps bring the next piece's query rows in (cp.async) as soon as the last scores of the current one are made,
-//     so that the next piece's first scores overlap this one's last softmax and its output.
-// Warps: 4 + 4 softmax (lane 0, lane 1), one that fetches K and V, one whose first thread issues the products, two for
-// the query rows.  Every wait is bounded; one that runs out raises STEP_ERR_TIMEOUT and the CTA winds down.
+//   * query rows come by TMA too (a box: the group's heads of as many tokens as fit 128 rows), the next piece's as soon as 
+//     the last scores of the current one are made, so that the next piece's first scores overlap this one's last softmax and its output.
+// Warps: 4 + 4 softmax (lane 0, lane 1), one that fetches K, one for V (a TMA instruction takes its thread some 70 cycles:
+// with both in one warp that warp set the pace), one whose first thread issues the products, one for the query rows.  Every wait is bounded; one that runs out raises STEP_ERR_TIMEOUT and the CTA winds down.
 #include "attention_rows.cuh"
 #include "async_copy.cuh"
 #include "tensor_core.cuh"
@@ -40,10 +40,10 @@ constexpr int kP = 16, kD = 128;
 constexpr int kTile = 128;                        // keys per tile
 constexpr int kSlotBytes = kTile * kD * 2;        // K or V of one tile
 constexpr int kQBytes = kHalfRows * kD * 2;       // 128 query rows, same arrangement
-constexpr int kSlots = 5;                         // ring of K and V tiles: 160 KiB
+constexpr int kKSlots = 2, kVSlots = 3, kSlots = kKSlots + kVSlots;   // rings of K and of V tiles, 160 KiB: a V tile waits for its softmax
 constexpr int kXCols = 16;                        // columns per round in which the lanes exchange their sums (below 128 rows)
 constexpr int kXBytes = 2 * kXCols * kHalfRows * 4;
-constexpr int kWarpFetch = 8, kWarpMma = 9, kWarpQ = 10;
+constexpr int kWarpK = 8, kWarpMma = 9, kWarpQ = 10, kWarpV = 11;
 constexpr int kThreads = 384;                      // three warpgroups
 constexpr int kRegsSoftmax = 208, kRegsOther = 88; // 2 x 128 x 208 + 128 x 88 = 384 x 168, what the launch has
 constexpr int kTmemCols = 512;                    // S of both lanes (P over them), then O of both
@@ -60,7 +60,8 @@ struct TreeArgs {
   float* ws_o;                      // [share][2][group rows][kD]
   int32_t* counters;
   int n, T, Hq, Hkv, G, L, layer, max_pages, num_blocks;
-  int rows;                         // query rows of a (trace, KV head): T * G
+  int tokens;                       // drafted tokens whose heads fill a tile of query rows: 128 / G
+  int lanes;                        // tiles of query rows in a group: 1 or 2
   int group_rows;                   // 128 or 256
   int shares;                       // CTAs of the attention launch
   float scale_log2;
@@ -88,7 +89,7 @@ __device__ inline Shape shape_of(const TreeArgs& a, int t, bool flag) {
   x.nodes = nodes_of(a, t, flag);
   const long long keys = (long long)x.S + x.nodes;
   x.tiles = keys > 0 ? (int)((keys + kTile - 1) / kTile) : 1;
-  x.groups = max(1, (x.nodes * a.G + a.group_rows - 1) / a.group_rows);
+  x.groups = max(1, (x.nodes + a.tokens * a.lanes - 1) / (a.tokens * a.lanes));
   return x;
 }
 // The stream: for every trace, for every KV head, for every row group, the sequence's tiles.  A warp's place in it:
@@ -140,9 +141,14 @@ __device__ inline void next_sequence(const TreeArgs& a, Place& p) {
   if (++p.t < a.n) p.x = shape_of(a, p.t, false);
 }
 // A piece, as the query warps announce it: tiles [tile0, tile0 + cnt) of the sequence's `tiles`.
-struct Piece { int t, h, r0, tile0, cnt, tiles, S, nodes; };
+struct Piece { int t, h, u0, tile0, cnt, tiles, S, nodes; };
 
 // ---- instructions
+__device__ inline void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
 __device__ inline void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
@@ -221,7 +227,7 @@ __device__ inline uint32_t pack2(float lo, float hi) {
 }
 
 template <bool kTwoRows>   // the lanes take 128 rows each of a 256-row group; else even and odd tiles of the same 128 rows
-__global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_constant__ CUtensorMap map, TreeArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap map_q, TreeArgs a) {
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -245,10 +251,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kSlots; ++s) {
-      mbar_init(bar_full + 8 * s, 33);              // the fetching warp's threads, and its announcement of bytes
+      mbar_init(bar_full + 8 * s, 33);              // a fetching warp's threads, and its announcement of bytes
       mbar_init(bar_empty + 8 * s, 1);              // tcgen05.commit
     }
-    mbar_init(bar_q, 128);                          // the query warps' threads, and their copies
+    mbar_init(bar_q, 1);                            // the query warp's announcement
     mbar_init(bar_qfree, 9);                        // tcgen05.commit: a piece's last scores; all softmax warps have begun it
     for (int s = 0; s < 2; ++s) {
       mbar_init(bar_s + 8 * s, 1);                  // tcgen05.commit: scores made (and the products before them done)
@@ -302,8 +308,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       if (!wait_warp(bar_q, ph_piece)) { ok = false; break; }
       const Piece pc = s_piece[ph_piece];
       if (pc.cnt == 0) break;                                          // the share is done
-      const int S = pc.S, r = pc.r0 + (kTwoRows ? ln * 128 : 0) + row, u = r / a.G;
-      const bool mine = r < pc.nodes * a.G;
+      const int S = pc.S, u = pc.u0 + (kTwoRows ? ln * a.tokens : 0) + row / a.G;
+      const bool mine = row < a.tokens * a.G && u < pc.nodes;
       const unsigned long long sees = mine ? s_mask[ph_piece * 64 + u] : 0ull;
       arrive_warp(bar_qfree);
 
@@ -380,9 +386,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       const bool whole = pc.cnt == pc.tiles;
       const size_t slot = (size_t)blockIdx.x * 2 + (pc.tile0 > 0 || first ? 0 : 1);
       first = false;
-      float2* ml_out = reinterpret_cast<float2*>(a.ws_ml) + slot * a.group_rows + (r - pc.r0);
-      float* o_out = a.ws_o + (slot * a.group_rows + (r - pc.r0)) * kD;
-      __nv_bfloat16* out = a.out + (((size_t)pc.t * a.T + (mine ? u : 0)) * a.Hq + (size_t)pc.h * a.G + (mine ? r - u * a.G : 0)) * kD;
+      float2* ml_out = reinterpret_cast<float2*>(a.ws_ml) + slot * a.group_rows + (kTwoRows ? ln * 128 : 0) + row;
+      float* o_out = a.ws_o + (slot * a.group_rows + (kTwoRows ? ln * 128 : 0) + row) * kD;
+      __nv_bfloat16* out = a.out + (((size_t)pc.t * a.T + (mine ? u : 0)) * a.Hq + (size_t)pc.h * a.G + (mine ? row % a.G : 0)) * kD;
       // N columns, from c on, of this thread's row
       auto put = [&](int c, uint32_t* o, int N, float inv) {
         if (!mine) return;
@@ -459,29 +465,30 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
-   if (warp == kWarpFetch) {
-    // ------------------------------------------------ K and V tiles into the ring
+   if (warp == kWarpK || warp == kWarpV) {
+    // ------------------------------------------------ K or V tiles into their ring
+    const int kv = warp == kWarpV, ring0 = kv ? kKSlots : 0, ring_n = kv ? kVSlots : kKSlots;
     int slot = 0;
     uint32_t ph = 1;
     bool ok = true;
     Place pl = {};
     int h = 0;
     // Block ids of 64 pages (eight tiles): lane i holds those of pages win + i and win + 32 + i.  The second half is asked
-    // for when V enters the first, four tiles before K needs it: with a read of the table in front of every tile, the read's
+    // for when the first is entered, four tiles before it is needed: with a read of the table in front of every tile, the read's
     // latency set the pace of the whole kernel (1,800 cycles a tile and operand).
     int win = 0, ids0 = 0, ids1 = 0;
     auto load_ids = [&](const Place& of, int first) {
       const int page = first + lane;
       return of.t < a.n && (long long)page * kP < of.x.S ? a.block_table[(size_t)of.t * a.max_pages + page] : 0;
     };
-    // tile i of the piece, K (kv = 0) or V, into the next slot
-    auto fetch = [&](int i, int kv) {
+    // tile i of the piece into the next slot
+    auto fetch = [&](int i) {
       if (!ok) return;
-      if (!wait_warp(bar_empty + 8 * slot, ph)) { ok = false; return; }
-      const uint32_t bar = bar_full + 8 * slot, dst = sm_ring + slot * kSlotBytes;
+      if (!wait_warp(bar_empty + 8 * (ring0 + slot), ph)) { ok = false; return; }
+      const uint32_t bar = bar_full + 8 * (ring0 + slot), dst = sm_ring + (ring0 + slot) * kSlotBytes;
       const int j0 = (pl.tile + i) * kTile;
       const int S = pl.x.S, nodes = pl.x.nodes;
-      if (kv && j0 / kP >= win + 32) { win += 32; ids0 = ids1; ids1 = load_ids(pl, win + 32); }
+      if (j0 / kP >= win + 32) { win += 32; ids0 = ids1; ids1 = load_ids(pl, win + 32); }
       const int in_win = j0 / kP - win;
       // block of page pg (0 .. 7) of this tile; one out of range is flagged and read as block 0
       auto block_of = [&](int pg) {
@@ -517,10 +524,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         if (lane == 0 && pages == 0) mbar_arrive(bar);                 // (the announcement of bytes is the other form of this arrival)
       }
       __syncwarp();
-      if (++slot == kSlots) { slot = 0; ph ^= 1; }
+      if (++slot == ring_n) { slot = 0; ph ^= 1; }
     };
     long long pos, end;
-    my_share(blockIdx.x == 0, pos, end);
+    my_share(kv == 0 && blockIdx.x == 0, pos, end);
     if (pos < end) pl = seek(a, lane, pos);
     int next0 = load_ids(pl, (pl.tile * (kTile / kP)) & ~31), next1 = load_ids(pl, ((pl.tile * (kTile / kP)) & ~31) + 32);
     while (pos < end && ok) {
@@ -533,25 +540,18 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       next_sequence(a, nx);
       next0 = load_ids(nx, 0);
       next1 = load_ids(nx, 32);
-      if constexpr (kTwoRows) {
-        for (int i = 0; i < cnt; ++i) { fetch(i, 0); fetch(i, 1); }
-      } else {
-        fetch(0, 0);
-        if (cnt > 1) fetch(1, 0);
-        for (int i = 0; i < cnt; ++i) { fetch(i, 1); if (i + 2 < cnt) fetch(i + 2, 0); }
-      }
+      for (int i = 0; i < cnt; ++i) fetch(i);
       pos += cnt;
       pl = nx;
     }
     cp_async_wait_all();
     if (*s_abort)                                                      // copies in flight still target this CTA's shared memory
-      for (int s = 0; s < kSlots; ++s) {
+      for (int s = ring0; s < ring0 + ring_n; ++s) {
         mbar_wait_bounded(bar_full + 8 * s, 0, kDrainNs);
         mbar_wait_bounded(bar_full + 8 * s, 1, kDrainNs);
       }
-  } else if (warp >= kWarpQ) {
+  } else if (warp == kWarpQ) {
     // ------------------------------------------------ query rows and ancestor masks of one piece after another
-    const int qt = threadIdx.x - kWarpQ * 32;                          // 0 .. 63
     uint32_t par = 0;
     long long pos, end;
     my_share(false, pos, end);
@@ -560,66 +560,61 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     for (;; par ^= 1) {
       Piece pc = {};
       if (pos < end) {
-        pc.t = pl.t; pc.h = pl.hr / pl.x.groups; pc.r0 = (pl.hr - pc.h * pl.x.groups) * a.group_rows;
+        pc.t = pl.t; pc.h = pl.hr / pl.x.groups; pc.u0 = (pl.hr - pc.h * pl.x.groups) * a.tokens * a.lanes;
         pc.tile0 = pl.tile; pc.tiles = pl.x.tiles; pc.S = pl.x.S; pc.nodes = pl.x.nodes;
         pc.cnt = (int)min((long long)(pl.x.tiles - pl.tile), end - pos);
-        if (warp == kWarpQ) {                                          // (the other piece's masks are the ones in use)
-          for (int u = lane; u < pc.nodes; u += 32) {
-            int p = a.parents[(size_t)pc.t * a.T + u];
-            if (p >= u || p < -1) { flag_error(a.counters, STEP_ERR_INVALID_ARG); p = -1; }
-            s_up[u] = p;
-          }
-          __syncwarp();
-          for (int u = lane; u < pc.nodes; u += 32) {
-            unsigned long long m = 0;
-            for (int w = u; w >= 0; w = s_up[w]) m |= 1ull << w;
-            s_mask[par * 64 + u] = m;
-          }
-          __syncwarp();
+        for (int u = lane; u < pc.nodes; u += 32) {                    // (the other piece's masks are the ones in use)
+          int p = a.parents[(size_t)pc.t * a.T + u];
+          if (p >= u || p < -1) { flag_error(a.counters, STEP_ERR_INVALID_ARG); p = -1; }
+          s_up[u] = p;
         }
+        __syncwarp();
+        for (int u = lane; u < pc.nodes; u += 32) {
+          unsigned long long m = 0;
+          for (int w = u; w >= 0; w = s_up[w]) m |= 1ull << w;
+          s_mask[par * 64 + u] = m;
+        }
+        __syncwarp();
         pos += pc.cnt;
         next_sequence(a, pl);
       }
       // the scores of the piece before are made, and its announcement has been read (the very first wait passes at once)
       if (!wait_warp(bar_qfree, par ^ 1)) break;
-      if (pc.cnt > 0) {
-        // four rows of 16 chunks at a time; rows behind the last drafted token are zeros
-        const int c = qt & 15, last = pc.nodes * a.G;
-        int rr = qt >> 4, u = (pc.r0 + rr) / a.G, g = pc.r0 + rr - u * a.G;
-        const __nv_bfloat16* heads = a.q + ((size_t)pc.t * a.T * a.Hq + (size_t)pc.h * a.G) * kD + c * 8;
-        const uint32_t dst = sm_q + (c >> 3) * (kQBytes / 2);
-#pragma unroll 4
-        for (; rr < kQAll / 256; rr += 4) {
-          cp_async16_or_zero(dst + (rr >> 7) * kQBytes + (rr & 127) * 128 + (((c ^ rr) & 7) << 4),
-                             heads + ((size_t)u * a.Hq + g) * kD, pc.r0 + rr < last);
-          for (g += 4; g >= a.G; g -= a.G) ++u;
+      if (lane == 0) {
+        s_piece[par] = pc;
+        if (pc.cnt > 0) {
+          // (rows of tokens that the trace does not have may come along: a row of the products depends on its own query only)
+          const int tiles = kTwoRows && pc.u0 + a.tokens < pc.nodes ? 2 : 1, box = min(a.tokens, a.T) * a.G * 128;
+          mbar_expect_tx(bar_q, 2 * tiles * box);
+          for (int x = 0; x < 2 * tiles; ++x)
+            tma_load_3d(sm_q + (x >> 1) * kQBytes + (x & 1) * (kQBytes / 2), &map_q, (x & 1) * 64, pc.h * a.G, pc.t * a.T + pc.u0 + (x >> 1) * a.tokens, bar_q);
+        } else {
+          mbar_arrive(bar_q);
         }
       }
-      if (qt == 0) s_piece[par] = pc;
-      cp_async_arrive_when_done(bar_q);
-      mbar_arrive(bar_q);
+      __syncwarp();
       if (pc.cnt == 0) break;
     }
-    cp_async_wait_all();
+    if (*s_abort && lane == 0) { mbar_wait_bounded(bar_q, 0, kDrainNs); mbar_wait_bounded(bar_q, 1, kDrainNs); }
     // out rows behind a trace's last drafted token
     for (int t = blockIdx.x; t < a.n; t += gridDim.x) {
       const int nodes = nodes_of(a, t, false);
       uint4* dst = reinterpret_cast<uint4*>(a.out + ((size_t)t * a.T + nodes) * a.Hq * kD);
       const int chunks = (a.T - nodes) * a.Hq * (kD / 8);
-      for (int x = qt; x < chunks; x += 64) dst[x] = make_uint4(0, 0, 0, 0);
+      for (int x = lane; x < chunks; x += 32) dst[x] = make_uint4(0, 0, 0, 0);
     }
   } else if (warp == kWarpMma && lane == 0) {
     // ------------------------------------------------ products
     const uint32_t id_qk = umma_idesc_bf16(kTile), id_pv = umma_idesc_bf16(kD) | (1u << 16);   // B of the second is MN-major
-    int slot = 0;
-    uint32_t ph = 0, ph_q = 0, ph_p[2] = {0, 0};
+    int at[2] = {0, 0};
+    uint32_t ph[2] = {0, 0}, ph_q = 0, ph_p[2] = {0, 0};
     bool ok = true;
-    // waits for the next slot of the ring; its index
-    auto next = [&]() -> int {
-      if (!ok || !wait(bar_full + 8 * slot, ph)) { ok = false; return 0; }
+    // waits for the next tile of K (0) or V (1); its slot
+    auto next = [&](int kv) -> int {
+      const int s = (kv ? kKSlots : 0) + at[kv];
+      if (!ok || !wait(bar_full + 8 * s, ph[kv])) { ok = false; return 0; }
       fence_async_smem();                                              // rows copied by cp.async came through the generic proxy
-      const int s = slot;
-      if (++slot == kSlots) { slot = 0; ph ^= 1; }
+      if (++at[kv] == (kv ? kVSlots : kKSlots)) { at[kv] = 0; ph[kv] ^= 1; }
       return s;
     };
     auto scores = [&](int ln, int s) {
@@ -649,20 +644,19 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       auto steps = [&](int i) { return min(8, (keys - i * kTile + 15) / 16); };
       ph_q ^= 1;
       if (cnt == 0) break;
-      fence_async_smem();                                              // (the query rows too)
       auto last_scores = [&]() { if (ok) tc_commit(bar_qfree); };
       if constexpr (kTwoRows) {
-        int k = next();
+        int k = next(0);
         scores(0, k);
         scores(1, k);
         release(k);
         if (cnt == 1) last_scores();
         for (int i = 0; i < cnt && ok; ++i) {
-          const int v = next();
+          const int v = next(1);
           const bool more = i + 1 < cnt;
           values(0, v, i == 0, steps(i));
           if (ok && !more) tc_commit(bar_o);
-          if (more) { k = next(); scores(0, k); }
+          if (more) { k = next(0); scores(0, k); }
           values(1, v, i == 0, steps(i));
           if (ok && !more) tc_commit(bar_o + 8);
           release(v);
@@ -670,16 +664,16 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
           if (i + 2 == cnt) last_scores();
         }
       } else {
-        int k = next();
+        int k = next(0);
         scores(0, k);
         release(k);
-        if (cnt > 1) { k = next(); scores(1, k); release(k); }
+        if (cnt > 1) { k = next(0); scores(1, k); release(k); }
         if (cnt <= 2) last_scores();
         for (int i = 0; i < cnt && ok; ++i) {
-          const int v = next();
+          const int v = next(1);
           values(i & 1, v, i < 2, steps(i));
           release(v);
-          if (i + 2 < cnt) { k = next(); scores(i & 1, k); release(k); }
+          if (i + 2 < cnt) { k = next(0); scores(i & 1, k); release(k); }
           if (i + 3 == cnt) last_scores();
         }
         if (ok) { tc_commit(bar_o); tc_commit(bar_o + 8); }
@@ -721,10 +715,11 @@ __global__ void __launch_bounds__(kMergeWarps * 32) tree_merge_kernel(TreeArgs a
   const Place p = s_place;
   const long long W = s_W, start = (w0 + 1) * W - p.tile;              // where the sequence begins
   if (p.t < 0 || p.tile == 0 || start < w0 * W) return;                // no border, no cut, or not the first cut of the sequence
-  const int h = p.hr / p.x.groups, r0 = (p.hr - h * p.x.groups) * a.group_rows;
+  const int h = p.hr / p.x.groups, u0 = (p.hr - h * p.x.groups) * a.tokens * a.lanes;
   const int w1 = (int)((start + p.x.tiles - 1) / W);
-  const int rows = min(a.group_rows, p.x.nodes * a.G - r0);
-  for (int rr = blockIdx.y * kMergeRows + warp; rr < min(rows, (int)(blockIdx.y + 1) * kMergeRows); rr += kMergeWarps) {
+  for (int rr = blockIdx.y * kMergeRows + warp; rr < (int)(blockIdx.y + 1) * kMergeRows; rr += kMergeWarps) {
+    const int row = rr % kHalfRows, u = u0 + rr / kHalfRows * a.tokens + row / a.G;
+    if (row >= a.tokens * a.G || u >= p.x.nodes) continue;
     float M = -INFINITY, den = 0.f;
     float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
@@ -740,8 +735,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) tree_merge_kernel(TreeArgs a
       M = Mb;
     }
     const float inv = 1.f / den;
-    const int r = r0 + rr;
-    reinterpret_cast<uint2*>(a.out + (((size_t)p.t * a.T + r / a.G) * a.Hq + (size_t)h * a.G + r % a.G) * kD)[lane] =
+    reinterpret_cast<uint2*>(a.out + (((size_t)p.t * a.T + u) * a.Hq + (size_t)h * a.G + row % a.G) * kD)[lane] =
         make_uint2(pack2(num.x * inv, num.y * inv), pack2(num.z * inv, num.w * inv));
   }
 }
@@ -762,7 +756,7 @@ bool tree_tc_supported(const step_pool* pool, int n) {
 }
 
 size_t tree_tc_workspace(const step_pool* pool, int T) {
-  const size_t rows = T * pool->G > kHalfRows ? 2 * kHalfRows : kHalfRows;
+  const size_t rows = T > kHalfRows / pool->G ? 2 * kHalfRows : kHalfRows;
   return (size_t)pool->num_sms * 2 * rows * (kD + 2) * sizeof(float);
 }
 
@@ -789,16 +783,25 @@ int tree_tc_launch(step_pool* pool, int layer, const void* q, const void* k_draf
   a.out = (__nv_bfloat16*)out;
   a.counters = pool->v.counters;
   a.n = n; a.T = T; a.Hq = g.Hq; a.Hkv = g.Hkv; a.G = g.G; a.L = g.L; a.layer = layer; a.max_pages = g.max_pages; a.num_blocks = g.num_blocks;
-  a.rows = T * g.G;
-  a.group_rows = a.rows > kHalfRows ? 2 * kHalfRows : kHalfRows;
+  a.tokens = kHalfRows / g.G;
+  a.lanes = T > a.tokens ? 2 : 1;
+  a.group_rows = a.lanes * kHalfRows;
   a.shares = pool->num_sms;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)kD);
   a.ws_o = (float*)workspace;
   a.ws_ml = a.ws_o + (size_t)a.shares * 2 * a.group_rows * kD;
-  const size_t smem = smem_bytes(a.group_rows > kHalfRows);
-  auto kern = a.group_rows > kHalfRows ? tree_tc_kernel<true> : tree_tc_kernel<false>;
+  const size_t smem = smem_bytes(a.lanes == 2);
+  auto kern = a.lanes == 2 ? tree_tc_kernel<true> : tree_tc_kernel<false>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return STEP_ERR_CUDA;
-  kern<<<a.shares, kThreads, smem, s>>>(map, a);
+  // queries: a box is one half of the dims of the G heads of a group, for as many tokens as make a tile of rows
+  CUtensorMap map_q;
+  const cuuint64_t q_dims[3] = {kD, (cuuint64_t)g.Hq, (cuuint64_t)n * T};
+  const cuuint64_t q_strides[2] = {kD * 2, (cuuint64_t)g.Hq * kD * 2};
+  const cuuint32_t q_box[3] = {64, (cuuint32_t)g.G, (cuuint32_t)(a.tokens < T ? a.tokens : T)};
+  if (enc(&map_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), q_dims, q_strides, q_box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return STEP_ERR_CUDA;
+  kern<<<a.shares, kThreads, smem, s>>>(map, map_q, a);
   if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
   if (a.shares > 1 &&
       launch_dependent(tree_merge_kernel, dim3(a.shares - 1, a.group_rows / kMergeRows), dim3(kMergeWarps * 32), 0, s, a) != cudaSuccess) return STEP_ERR_CUDA;
