@@ -144,6 +144,13 @@ __device__ inline void next_sequence(const TreeArgs& a, Place& p) {
 struct Piece { int t, h, u0, tile0, cnt, tiles, S, nodes; };
 
 // ---- instructions
+// One thread of a warp that is together (the same one every time).
+__device__ inline bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
+__device__ inline void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 __device__ inline void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
@@ -248,8 +255,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   const uint32_t bar_q = bars + 16 * kSlots, bar_s = bar_q + 8, bar_p = bar_s + 16, bar_o = bar_p + 16,
                  bar_both = bar_o + 16, bar_qfree = bar_both + 8, bar_drain = bar_qfree + 8;
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
+    prefetch_map(&map);
+    prefetch_map(&map_q);
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(bar_full + 8 * s, 33);              // a fetching warp's threads, and its announcement of bytes
       mbar_init(bar_empty + 8 * s, 1);              // tcgen05.commit
@@ -283,6 +292,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   };
 
   auto wait = [&](uint32_t bar, uint32_t parity) {
+    if (mbar_try_wait(bar, parity)) return true;
     if (*s_abort) return false;
     if (mbar_wait_bounded(bar, parity)) return true;
     flag_error(a.counters, STEP_ERR_TIMEOUT);
@@ -603,84 +613,119 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       const int chunks = (a.T - nodes) * a.Hq * (kD / 8);
       for (int x = lane; x < chunks; x += 32) dst[x] = make_uint4(0, 0, 0, 0);
     }
-  } else if (warp == kWarpMma && lane == 0) {
-    // ------------------------------------------------ products
+  } else {
+    // ------------------------------------------------ products.  The tensor cores take the next few instructions only, so
+    // every cycle this warp spends between them is idle time there once they are what limits the kernel (more than 128
+    // rows).  Hence: the warp stays together and one thread is elected for the instructions (a wait in a single thread's
+    // branch costs twice the cycles), and what is likely there long since is waited for before what is not.
     const uint32_t id_qk = umma_idesc_bf16(kTile), id_pv = umma_idesc_bf16(kD) | (1u << 16);   // B of the second is MN-major
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
     int at[2] = {0, 0};
     uint32_t ph[2] = {0, 0}, ph_q = 0, ph_p[2] = {0, 0};
     bool ok = true;
-    // waits for the next tile of K (0) or V (1); its slot
-    auto next = [&](int kv) -> int {
+    // waits for the next tile of K (0) or V (1); its slot.  Rows copied by cp.async came through the generic proxy.
+    auto next = [&](int kv, bool copied) -> int {
       const int s = (kv ? kKSlots : 0) + at[kv];
-      if (!ok || !wait(bar_full + 8 * s, ph[kv])) { ok = false; return 0; }
-      fence_async_smem();                                              // rows copied by cp.async came through the generic proxy
+      ok = ok && wait_warp(bar_full + 8 * s, ph[kv]);
+      if (copied) fence_async_smem();
       if (++at[kv] == (kv ? kVSlots : kKSlots)) { at[kv] = 0; ph[kv] ^= 1; }
       return s;
     };
-    auto scores = [&](int ln, int s) {
-      if (!ok) return;
+    auto probabilities = [&](int ln) {
+      ok = ok && wait_warp(bar_p + 8 * ln, ph_p[ln]);
+      ph_p[ln] ^= 1;
       tc_fence_after();
+    };
+    // (the elected thread's part of it)
+    auto scores = [&](int ln, int s) {
       const uint32_t qa = sm_q + (kTwoRows ? ln * kQBytes : 0), kb = sm_ring + s * kSlotBytes;
 #pragma unroll
       for (int x = 0; x < 8; ++x)
-        tc_mma_bf16(tmem + ln * 128, umma_desc_sw128(qa + (x >> 2) * (kQBytes / 2) + (x & 3) * 32),
+        tc_mma_bf16(tm + ln * 128, umma_desc_sw128(qa + (x >> 2) * (kQBytes / 2) + (x & 3) * 32),
                     umma_desc_k(kb + (x >> 2) * 1024 + (x & 3) * 32), id_qk, x != 0);
       tc_commit(bar_s + 8 * ln);
     };
     // steps of 16 keys; those of a tile behind the last key are left out, so nothing that lies there matters
     auto values = [&](int ln, int s, bool first, int steps) {
-      if (!ok || !wait(bar_p + 8 * ln, ph_p[ln])) { ok = false; return; }
-      ph_p[ln] ^= 1;
-      tc_fence_after();
       const uint32_t vb = sm_ring + s * kSlotBytes;
 #pragma unroll
       for (int x = 0; x < 8; ++x)
-        if (x < steps) tc_mma_bf16_ta(tmem + 256 + ln * 128, tmem + ln * 128 + x * 8, umma_desc_v(vb + x * 4096), id_pv, !(first && x == 0));
+        if (x < steps) tc_mma_bf16_ta(tm + 256 + ln * 128, tm + ln * 128 + x * 8, umma_desc_v(vb + x * 4096), id_pv, !(first && x == 0));
     };
-    auto release = [&](int s) { if (ok) tc_commit(bar_empty + 8 * s); };
-    for (;;) {
-      if (!wait(bar_q, ph_q)) { ok = false; break; }
-      const int cnt = s_piece[ph_q].cnt, keys = s_piece[ph_q].S + s_piece[ph_q].nodes - s_piece[ph_q].tile0 * kTile;
+    while (ok) {
+      ok = wait_warp(bar_q, ph_q);
+      const int cnt = s_piece[ph_q].cnt, S = s_piece[ph_q].S - s_piece[ph_q].tile0 * kTile, keys = S + s_piece[ph_q].nodes;
+      auto copied = [&](int i) { return (i + 1) * kTile > S; };
       auto steps = [&](int i) { return min(8, (keys - i * kTile + 15) / 16); };
       ph_q ^= 1;
-      if (cnt == 0) break;
-      auto last_scores = [&]() { if (ok) tc_commit(bar_qfree); };
+      if (!ok || cnt == 0) break;
+      tc_fence_after();
       if constexpr (kTwoRows) {
-        int k = next(0);
-        scores(0, k);
-        scores(1, k);
-        release(k);
-        if (cnt == 1) last_scores();
+        int k = next(0, copied(0));
+        if (ok && elect_one()) {
+          scores(0, k);
+          scores(1, k);
+          tc_commit(bar_empty + 8 * k);
+          if (cnt == 1) tc_commit(bar_qfree);
+        }
         for (int i = 0; i < cnt && ok; ++i) {
-          const int v = next(1);
+          const int v = next(1, copied(i));
           const bool more = i + 1 < cnt;
-          values(0, v, i == 0, steps(i));
-          if (ok && !more) tc_commit(bar_o);
-          if (more) { k = next(0); scores(0, k); }
-          values(1, v, i == 0, steps(i));
-          if (ok && !more) tc_commit(bar_o + 8);
-          release(v);
-          if (more) { scores(1, k); release(k); }
-          if (i + 2 == cnt) last_scores();
+          if (more) k = next(0, copied(i + 1));
+          probabilities(0);
+          if (ok && elect_one()) {
+            values(0, v, i == 0, steps(i));
+            if (more) scores(0, k); else tc_commit(bar_o);
+          }
+          __syncwarp();
+          probabilities(1);
+          if (ok && elect_one()) {
+            values(1, v, i == 0, steps(i));
+            tc_commit(bar_empty + 8 * v);
+            if (more) { scores(1, k); tc_commit(bar_empty + 8 * k); } else tc_commit(bar_o + 8);
+            if (i + 2 == cnt) tc_commit(bar_qfree);
+          }
+          __syncwarp();
         }
       } else {
-        int k = next(0);
-        scores(0, k);
-        release(k);
-        if (cnt > 1) { k = next(0); scores(1, k); release(k); }
-        if (cnt <= 2) last_scores();
-        for (int i = 0; i < cnt && ok; ++i) {
-          const int v = next(1);
-          values(i & 1, v, i < 2, steps(i));
-          release(v);
-          if (i + 2 < cnt) { k = next(0); scores(i & 1, k); release(k); }
-          if (i + 3 == cnt) last_scores();
+        // (bound by the stream of tiles: the second product does not wait for a tile of K)
+        for (int i = 0; i < min(cnt, 2); ++i) {
+          const int k = next(0, copied(i));
+          if (ok && elect_one()) {
+            scores(i, k);
+            tc_commit(bar_empty + 8 * k);
+            if (i + 1 == cnt) tc_commit(bar_qfree);
+          }
+          __syncwarp();
         }
-        if (ok) { tc_commit(bar_o); tc_commit(bar_o + 8); }
+        for (int i = 0; i < cnt && ok; ++i) {
+          const int v = next(1, copied(i));
+          probabilities(i & 1);
+          if (ok && elect_one()) {
+            values(i & 1, v, i < 2, steps(i));
+            tc_commit(bar_empty + 8 * v);
+            if (i + 2 >= cnt) tc_commit(bar_o + 8 * (i & 1));
+            if (cnt == 1) tc_commit(bar_o + 8);                        // lane 1 has nothing to do
+          }
+          __syncwarp();
+          if (i + 2 < cnt) {
+            const int k = next(0, copied(i + 2));
+            if (ok && elect_one()) {
+              scores(i & 1, k);
+              tc_commit(bar_empty + 8 * k);
+              if (i + 3 == cnt) tc_commit(bar_qfree);
+            }
+            __syncwarp();
+          }
+        }
       }
     }
-    tc_commit(bar_drain);                                              // no product is in flight when the tensor memory goes back
-    mbar_wait_bounded(bar_drain, 0);
+    __syncwarp();
+    if (elect_one()) {
+      tc_commit(bar_drain);                                            // no product is in flight when the tensor memory goes back
+      mbar_wait_bounded(bar_drain, 0);
+    }
+    __syncwarp();
   }
   }
   __syncwarp();
