@@ -37,6 +37,7 @@ struct EvictArgs {
   int2* drop;                                 // workspace [n * max_pages]: (entry, page) of every reference dropped, in order
   int cpr;
   int cache_keys;                             // positions whose keys evict_move_kernel keeps in shared memory
+  int shift;                                  // log2 of the page size, -1 if it is no power of two
 };
 
 // Pages are examined by a warp per entry, spread over the cluster: a kept page's reference count is a scattered 4-byte
@@ -170,6 +171,7 @@ constexpr int kMoveThreads = 256, kMoveWarps = kMoveThreads / 32;
 constexpr int kBins = 2048;                   // selection by digits of 11, 11 and 10 bits
 constexpr int kMostCachedKeys = 12288;        // 48 KiB of keys: three CTAs per SM still fit
 constexpr int kBatch = 8;                     // rows a warp has in flight
+constexpr int kPageCache = 1024;              // block ids kept in shared memory
 
 // Larger weight -> larger key; NaN below everything; the two zeros are equal.
 __device__ inline uint32_t weight_key(float w) {
@@ -179,14 +181,16 @@ __device__ inline uint32_t weight_key(float w) {
 }
 
 // What bounds it: for a cut of a few positions the passes over the weights (each a read of shared memory, or of L2 for
-// long caches) and the copies' latency; the positions are split into one contiguous run per warp, so that ranks need one
+// long caches) and the copies' latency, so four CTAs per SM matter more than rows in flight per warp; the positions are split into one contiguous run per warp, so that ranks need one
 // exchange of counts between the warps and none per step.
-__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(EvictArgs a) {
+__global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(EvictArgs a) {
   extern __shared__ uint32_t s_key[];                   // [cache_keys]
-  __shared__ int s_hist[kBins];                         // the histogram, then the list of positions that move
+  __shared__ int s_hist[kBins];                         // the histogram, then the positions that move
+  __shared__ int s_slot[kBins];                         // and the slots that take them
   __shared__ int s_cnt[kMoveWarps][4];                  // per warp: above and equal in [0, m), above and equal in [m, first)
   __shared__ int s_scan[kMoveWarps];
   __shared__ int s_digit, s_left;
+  __shared__ int s_page[kPageCache];
   const Geo& g = a.g;
   const int h = blockIdx.x, i = blockIdx.y, l = blockIdx.z;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -207,9 +211,18 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(EvictArgs a) {
   // ---- the m-th largest key of [0, first), and how many of the positions that have it are chosen (`want`): position j is
   // chosen if its key is above the threshold, or equal to it and among the first `want` such positions
   const bool in_smem = first <= a.cache_keys;
-  if (in_smem) {
-#pragma unroll 4
-    for (int j = tid; j < first; j += kMoveThreads) s_key[j] = weight_key(w[j]);
+  const int32_t* old_row = a.v.block_table + (size_t)a.ids[i] * g.max_pages;
+  const int pages = (S + g.P - 1) / g.P;
+  for (int p = tid; p < min(pages, kPageCache); p += kMoveThreads) s_page[p] = old_row[p];
+  // (two buffers: a position below m most likely stays, and those that do not are written again further down)
+  const bool copy_weights = w_out != w;
+  if (in_smem || copy_weights) {
+#pragma unroll 8
+    for (int j = tid; j < first; j += kMoveThreads) {
+      const float x = w[j];
+      if (in_smem) s_key[j] = weight_key(x);
+      if (copy_weights && j < m) w_out[j] = x;
+    }
   }
   auto key = [&](int j) { return in_smem ? s_key[j] : weight_key(w[j]); };
   uint32_t limit = 0;
@@ -219,6 +232,7 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(EvictArgs a) {
     const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bits = pass == 2 ? 10 : 11;
     for (int b = tid; b < kBins; b += kMoveThreads) s_hist[b] = 0;
     __syncthreads();
+#pragma unroll 4
     for (int j = tid; j < first; j += kMoveThreads) {
       const uint32_t k = key(j);
       if (pass == 0 || (k >> (shift + bits)) == limit) atomicAdd(&s_hist[(k >> shift) & ((1u << bits) - 1)], 1);
@@ -256,6 +270,7 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(EvictArgs a) {
   const int a1 = min(first, m + warp * run1), b1 = min(first, a1 + run1);
   auto count = [&](int lo, int hi, int& above, int& equal) {
     above = equal = 0;
+#pragma unroll 4
     for (int j = lo + lane; j < hi; j += 32) {
       const uint32_t k = key(j);
       above += k > limit;
@@ -292,22 +307,47 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(EvictArgs a) {
 
   // ---- rows: a row of K (or V) is cpr chunks of 16 bytes; both rows of a position are one warp's work
   const int nbp = (a.budget + g.P - 1) / g.P;
-  const int32_t* old_row = a.v.block_table + (size_t)a.ids[i] * g.max_pages;
   const int32_t* new_row = a.new_row + (size_t)i * nbp;
   const bool fresh_pages = a.need[i] > 0;               // some kept pages are shared: all that they hold is copied
   const size_t page_chunks = (size_t)g.P * a.cpr;
   uint4* base = a.kv + (size_t)l * g.num_blocks * g.Hkv * 2 * page_chunks + (size_t)h * 2 * page_chunks;
   const size_t block_chunks = (size_t)g.Hkv * 2 * page_chunks;
   const int row_chunks = 2 * a.cpr;
-  // chunk c of the row pair (K, then V) of slot j, as stored
-  auto place = [&](const int32_t* table, int j, int c) {
-    const int kv = c >= a.cpr, slot = j % g.P;
-    const int cc = c - kv * a.cpr;
-    return base + (size_t)table[j / g.P] * block_chunks + (size_t)slot * a.cpr + (size_t)kv * page_chunks +
-           (g.swizzle ? ((cc & ~7) | ((cc ^ slot) & 7)) : cc);
+  auto old_block = [&](int p) { return p < kPageCache ? s_page[p] : old_row[p]; };
+  auto new_block = [&](int p) { return fresh_pages ? new_row[p] : old_block(p); };
+  auto page_of = [&](int j) { return a.shift >= 0 ? j >> a.shift : j / g.P; };
+  // Where slot j's K row starts (in chunks from `base`) in block b, and what its chunk numbers are XORed with: worked out by
+  // one lane per row and handed round, since the arithmetic of every lane for every row cost more than the copies.
+  auto row_of = [&](int b, int j) { return (unsigned long long)b * block_chunks + (unsigned long long)(j - page_of(j) * g.P) * a.cpr; };
+  auto twist_of = [&](int j) { return g.swizzle ? (j - page_of(j) * g.P) & 7 : 0; };
+  // kBatch rows of one warp: lane x < kBatch knows the source of row x, lane kBatch + x its slot; n of them exist
+  auto copy_rows = [&](int j, int n, bool all_read_first) {
+    const bool is_slot = lane >= kBatch;
+    const bool real = lane < 2 * kBatch && lane % kBatch < n;
+    const unsigned long long at = real ? row_of(is_slot ? new_block(page_of(j)) : old_block(page_of(j)), j) : 0ull;
+    const int twist = real ? twist_of(j) : 0;
+    for (int c0 = 0; c0 < row_chunks; c0 += 32) {
+      const int c = c0 + lane, kv = c >= a.cpr, cc = c - kv * a.cpr;
+      uint4* mine = base + (kv ? page_chunks : 0);
+      uint4 x[kBatch];
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r) {
+        const unsigned long long from = __shfl_sync(0xffffffffu, at, r);
+        const int tw = __shfl_sync(0xffffffffu, twist, r);
+        if (r < n && c < row_chunks) x[r] = mine[from + (cc ^ tw)];
+      }
+      if (all_read_first) __syncthreads();
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r) {
+        const unsigned long long to = __shfl_sync(0xffffffffu, at, kBatch + r);
+        const int tw = __shfl_sync(0xffffffffu, twist, kBatch + r);
+        if (r < n && c < row_chunks) mine[to + (cc ^ tw)] = x[r];
+      }
+    }
   };
-  // Slots [0, m), kBins moving positions a round: they are listed in shared memory, then the free slots take them.  The
-  // sources are positions from m on, or the same slot of a page that was shared: nothing written here is read here.
+  // Slots [0, m), kBins moving positions a round: positions and slots are listed in shared memory, then their rows are
+  // copied, all at once.  The sources are positions from m on: nothing written here is read here.  (Copying a slot's row
+  // where the slot is found, one after another, took four times as long.)
   for (int round = 0; round == 0 || round * kBins < moving; ++round) {
     const int lo = round * kBins, hi = lo + kBins;
     __syncthreads();
@@ -338,39 +378,33 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(EvictArgs a) {
       const int r = at + __popc(fr & below);
       eq += __popc(eqs);
       at += __popc(fr);
-      // a free slot belongs to the round that lists its position, everything else to the first
-      const bool mine = j < b0 && (is_free ? r >= lo && r < hi : round == 0);
-      int from = j;
-      if (mine) {
-        if (is_free) from = s_hist[r - lo];
-        kept[j] = from;
-        if (w_out != w) w_out[j] = w[from];
-      }
-      unsigned todo = __ballot_sync(0xffffffffu, mine && (is_free || (fresh_pages && new_row[j / g.P] != old_row[j / g.P])));
-      while (todo) {
-        int slot[kBatch], src[kBatch], cnt = 0;
-#pragma unroll
-        for (int x = 0; x < kBatch; ++x) {
-          const int b = todo ? __ffs(todo) - 1 : 0;
-          slot[x] = j0 + b;
-          src[x] = __shfl_sync(0xffffffffu, from, b);
-          if (todo) { ++cnt; todo &= todo - 1; }
-        }
-        for (int c = lane; c < row_chunks; c += 32) {
-          uint4 v[kBatch];
-#pragma unroll
-          for (int x = 0; x < kBatch; ++x)
-            if (x < cnt) v[x] = *place(old_row, src[x], c);
-#pragma unroll
-          for (int x = 0; x < kBatch; ++x)
-            if (x < cnt) *place(new_row, slot[x], c) = v[x];
-        }
+      if (is_free) {
+        if (r >= lo && r < hi) { s_slot[r - lo] = j; kept[j] = s_hist[r - lo]; }
+      } else if (j < b0 && round == 0) {
+        kept[j] = j;
       }
     }
+    __syncthreads();
+    const int cnt = min(kBins, moving - lo);
+    if (copy_weights || in_smem)                        // (else the weights still say which slots are free)
+      for (int r = tid; r < cnt; r += kMoveThreads) w_out[s_slot[r]] = w[s_hist[r]];
+    for (int r0 = warp * kBatch; r0 < cnt; r0 += kMoveWarps * kBatch) {
+      const int r = r0 + lane % kBatch;
+      copy_rows(r < cnt ? (lane < kBatch ? s_hist[r] : s_slot[r]) : 0, min(kBatch, cnt - r0), false);
+    }
   }
-  // in place, the weights follow only now: until here they say which slots are free
-  if (w_out == w)
-    for (int j = a0 + lane; j < b0; j += 32) {
+  // what stays on a page that was shared goes along to the block that replaces it
+  if (fresh_pages)
+    for (int j0 = warp * kBatch; j0 < m; j0 += kMoveWarps * kBatch) {
+      // (the rows that do not stay are passed over by letting the warp's batch shrink to those that do)
+      const int j = j0 + lane;
+      const bool stays = lane < kBatch && j < m && new_block(page_of(j)) != old_block(page_of(j)) && kept[j] == j;
+      const unsigned who = __ballot_sync(0xffffffffu, stays);
+      const int n = __popc(who), r = lane % kBatch;
+      copy_rows(r < n ? j0 + (int)__fns(who, 0, r + 1) : 0, n, false);
+    }
+  if (!copy_weights && !in_smem)
+    for (int j = tid; j < m; j += kMoveThreads) {
       const int from = kept[j];
       if (from != j) w_out[j] = w[from];
     }
@@ -386,21 +420,8 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(EvictArgs a) {
     __syncthreads();
   }
   for (int r0 = 0; r0 < a.recent; r0 += kMoveWarps * kBatch) {
-    for (int c0 = 0; c0 < row_chunks; c0 += 32) {
-      const int c = c0 + lane;
-      uint4 x[kBatch];
-#pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        const int r = r0 + b * kMoveWarps + warp;
-        if (r < a.recent && c < row_chunks) x[b] = *place(old_row, first + r, c);
-      }
-      __syncthreads();
-#pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        const int r = r0 + b * kMoveWarps + warp;
-        if (r < a.recent && c < row_chunks) *place(new_row, m + r, c) = x[b];
-      }
-    }
+    const int r1 = r0 + warp * kBatch, r = r1 + lane % kBatch;
+    copy_rows(r < a.recent ? (lane < kBatch ? first : m) + r : 0, max(0, min(kBatch, a.recent - r1)), true);
   }
   for (int j = a.budget + tid; j < a.stride; j += kMoveThreads) w_out[j] = 0.f;
 }
@@ -516,6 +537,9 @@ int kv_pool_evict_positions(step_pool* pool, const int32_t* trace_ids, int n, co
   a.old_len = (int32_t*)(a.drop + (size_t)n * a.g.max_pages);
   a.need = a.old_len + n; a.base = a.need + n; a.off = a.base + n + 1; a.new_row = a.off + n + 1;
   a.cpr = a.g.d * pool->elem_bytes / 16;
+  a.shift = -1;
+  for (int b = 0; b < 30; ++b)
+    if (a.g.P == 1 << b) a.shift = b;
   a.cache_keys = weight_stride <= kMostCachedKeys ? weight_stride : 0;
   evict_plan_kernel<<<kClusterCtas, kPruneThreads, 0, s>>>(a);
   if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;

@@ -449,7 +449,7 @@ append_fused_kernel(DevViews v, Geo g, uint4* __restrict__ kv, const uint4* __re
 // Two launches.  Phase 1 (one CTA): as append_alloc_kernel, with per-entry counts; an entry whose count or path is out of
 // range is flagged and skipped.  Leaves every entry's old length in v.append_base (-1: nothing to store) and the prefix
 // sum of the new positions in v.prune_off (scratch of max_traces + 1 ints), by which phase 2 finds its rows.
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
 path_alloc_kernel(DevViews v, Geo g, const int32_t* __restrict__ ids, int n, const int32_t* __restrict__ path,
                   const int32_t* __restrict__ path_len, int max_path, int T) {
   extern __shared__ int sm[];
@@ -539,8 +539,11 @@ __global__ void __launch_bounds__(256)
 path_write_kernel(DevViews v, Geo g, uint4* __restrict__ kv, const uint4* __restrict__ kd, const uint4* __restrict__ vd,
                   const int32_t* __restrict__ ids, int n, const int32_t* __restrict__ path, int max_path, int T, int cpr,
                   int layers_per_cta) {
+  extern __shared__ int s_rows[];                        // [n + 1] rows of the entries before each
   wait_for_primary();
-  const int total = v.prune_off[n];
+  for (int i = threadIdx.x; i <= n; i += blockDim.x) s_rows[i] = v.prune_off[i];
+  __syncthreads();
+  const int total = s_rows[n];
   const int l0 = blockIdx.y * layers_per_cta, l1 = min(g.L, l0 + layers_per_cta);
   const int per_kv = g.Hkv * cpr;
   const size_t page_chunks = (size_t)g.P * cpr;
@@ -549,9 +552,9 @@ path_write_kernel(DevViews v, Geo g, uint4* __restrict__ kv, const uint4* __rest
     int lo = 0, hi = n - 1;                              // the last entry whose rows start at or before e
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (v.prune_off[mid] <= e) lo = mid; else hi = mid - 1;
+      if (s_rows[mid] <= e) lo = mid; else hi = mid - 1;
     }
-    const int j = e - v.prune_off[lo];
+    const int j = e - s_rows[lo];
     const int pos = v.append_base[lo] + j, page = pos / g.P, slot = pos % g.P;
     const int b = v.block_table[(size_t)ids[lo] * g.max_pages + page];
     const int node = path[(size_t)lo * max_path + j];
@@ -734,7 +737,7 @@ int append_kv_path(step_pool* pool, const int32_t* trace_ids, int n, int T, cons
   Geo g = geo_of(pool);
   cudaStream_t s = (cudaStream_t)stream;
   const int cpe = 16 / pool->elem_bytes, cpr = g.d / cpe;
-  path_alloc_kernel<<<1, 256, (size_t)n * 5 * sizeof(int), s>>>(pool->v, g, trace_ids, n, path, path_len, max_path, T);
+  path_alloc_kernel<<<1, 1024, (size_t)n * 5 * sizeof(int), s>>>(pool->v, g, trace_ids, n, path, path_len, max_path, T);
   if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
   // CTAs for every pair there may be, up to eight per SM; the layer range is split when there are few pairs
   const long long pairs = (long long)n * max_path, most = 8ll * pool->num_sms;
@@ -744,7 +747,7 @@ int append_kv_path(step_pool* pool, const int32_t* trace_ids, int n, int T, cons
   if (splits < 1) splits = 1;
   const int layers_per_cta = (g.L + splits - 1) / splits;
   splits = (g.L + layers_per_cta - 1) / layers_per_cta;
-  if (launch_dependent(path_write_kernel, dim3((unsigned)grid, (unsigned)splits), dim3(256), 0, s, pool->v, g,
+  if (launch_dependent(path_write_kernel, dim3((unsigned)grid, (unsigned)splits), dim3(256), (size_t)(n + 1) * sizeof(int), s, pool->v, g,
                        (uint4*)pool->cfg.kv_storage, (const uint4*)k_draft, (const uint4*)v_draft, trace_ids, n, path,
                        max_path, T, cpr, layers_per_cta) != cudaSuccess) return STEP_ERR_CUDA;
   return launch_ok();
