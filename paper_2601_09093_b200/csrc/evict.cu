@@ -224,6 +224,8 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(EvictArgs a
       if (copy_weights && j < m) w_out[j] = x;
     }
   }
+  for (int j = tid; j < m; j += kMoveThreads) kept[j] = j;               // (most slots; the others are written again further down)
+  for (int r = tid; r < a.recent; r += kMoveThreads) kept[m + r] = first + r;
   auto key = [&](int j) { return in_smem ? s_key[j] : weight_key(w[j]); };
   uint32_t limit = 0;
   int want = m;                                         // still to be found among the keys that share the prefix
@@ -378,11 +380,7 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(EvictArgs a
       const int r = at + __popc(fr & below);
       eq += __popc(eqs);
       at += __popc(fr);
-      if (is_free) {
-        if (r >= lo && r < hi) { s_slot[r - lo] = j; kept[j] = s_hist[r - lo]; }
-      } else if (j < b0 && round == 0) {
-        kept[j] = j;
-      }
+      if (is_free && r >= lo && r < hi) { s_slot[r - lo] = j; kept[j] = s_hist[r - lo]; }
     }
     __syncthreads();
     const int cnt = min(kBins, moving - lo);
@@ -411,7 +409,6 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(EvictArgs a
   __syncthreads();
   // the most recent positions, in order: a batch is read whole before it is written (a slot may be the source of an
   // earlier one, never of a later one)
-  for (int r = tid; r < a.recent; r += kMoveThreads) kept[m + r] = first + r;
   for (int r0 = 0; r0 < a.recent; r0 += kMoveThreads) {
     const int r = r0 + tid;
     const float x = r < a.recent ? w[first + r] : 0.f;
