@@ -143,6 +143,7 @@ struct AttnArgs {
   float* scores;                   // [n][Hq][score_stride] log2-scaled scores
   long long score_stride;          // a multiple of the page size; positions behind it are not recorded
   float* row_ml;                   // [n][Hq][2] (max, sum) of every row
+  int merge_wide;                  // 1: the launch that combines the pieces gives a row to a whole CTA, not to a warp
 };
 
 // kMode of attn_mma_kernel: the plain kernel; the pass over the shared pages, whose 16 query rows are the G heads of
@@ -814,7 +815,11 @@ __global__ void __launch_bounds__(kMergeWarps * 32, 5) attn_merge_kernel(AttnArg
   if (blockIdx.x == 0 && threadIdx.x == 0 && a.sched) a.sched[0] = 0;   // the chunk counter, for the next launch
 
   const int n_items = n * Hkv * rows;
-  for (int item = blockIdx.x * kMergeWarps + warp; item < n_items; item += gridDim.x * kMergeWarps) {
+  // few rows with many pieces each (kCount: long caches of few traces): the CTA's warps share a row's pieces, eight in turn
+  const bool wide = kCount && a.merge_wide;
+  __shared__ float2 s_wide_ml[kCount ? kMergeWarps : 1];
+  __shared__ float4 s_wide_o[kCount ? kMergeWarps : 1][32];
+  for (int item = wide ? blockIdx.x : blockIdx.x * kMergeWarps + warp; item < n_items; item += wide ? gridDim.x : gridDim.x * kMergeWarps) {
     const int g = item % rows, th = item / rows;
     const int t = th / Hkv, h = th - t * Hkv;
     const int np_static = s_cum[t + 1] - s_cum[t];
@@ -847,7 +852,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32, 5) attn_merge_kernel(AttnArg
 
     float M = -INFINITY, den = 0.f;
     float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k0 = 0; k0 < n_pieces; k0 += kMergeBatch) {
+    for (int k0 = wide ? warp * kMergeBatch : 0; k0 < n_pieces; k0 += wide ? kMergeWarps * kMergeBatch : kMergeBatch) {
       float2 ml[kMergeBatch];
       float4 o4[kMergeBatch];
 #pragma unroll
@@ -871,6 +876,25 @@ __global__ void __launch_bounds__(kMergeWarps * 32, 5) attn_merge_kernel(AttnArg
           const float wgt = exp2f(ml[j].x - M);
           den += wgt * ml[j].y;
           num.x += wgt * o4[j].x; num.y += wgt * o4[j].y; num.z += wgt * o4[j].z; num.w += wgt * o4[j].w;
+        }
+      }
+    }
+    if constexpr (kCount) {
+      if (wide) {
+        __syncthreads();                                          // the row before has been put together
+        if (lane == 0) s_wide_ml[warp] = make_float2(M, den);
+        s_wide_o[warp][lane] = num;
+        __syncthreads();
+        if (warp > 0) continue;
+        for (int x = 1; x < kMergeWarps; ++x) {                   // (a warp without pieces has a maximum of -inf and counts nothing)
+          const float2 ml = s_wide_ml[x];
+          if (ml.x == -INFINITY) continue;
+          const float4 o4 = s_wide_o[x][lane];
+          const float Mb = fmaxf(M, ml.x), keep = exp2f(M - Mb), wgt = exp2f(ml.x - Mb);
+          den = den * keep + wgt * ml.y;
+          num.x = num.x * keep + wgt * o4.x; num.y = num.y * keep + wgt * o4.y;
+          num.z = num.z * keep + wgt * o4.z; num.w = num.w * keep + wgt * o4.w;
+          M = Mb;
         }
       }
     }
@@ -915,7 +939,8 @@ int launch_one(AttnArgs a, int grid, cudaStream_t s, bool dependent = false) {
     if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
   }
   const int rows = kMode == kPrefixPass ? a.tpb * a.G : a.G;
-  long long mgrid = ((long long)n_seq * a.Hkv * rows + kMergeWarps - 1) / kMergeWarps;
+  a.merge_wide = kCount && (long long)n_seq * a.Hkv * rows <= 2ll * a.merge_ctas;
+  long long mgrid = a.merge_wide ? (long long)n_seq * a.Hkv * rows : ((long long)n_seq * a.Hkv * rows + kMergeWarps - 1) / kMergeWarps;
   if (mgrid > a.merge_ctas) mgrid = a.merge_ctas;
   if (launch_dependent(attn_merge_kernel<kMode, kCount>, dim3((int)mgrid), dim3(kMergeWarps * 32), (size_t)(3 * n_seq + 3) * 4, s, a) != cudaSuccess) return STEP_ERR_CUDA;
   return launch_ok();
@@ -945,7 +970,7 @@ void fill_args(AttnArgs& a, const step_pool* pool, const Geo& g, int layer, cons
   a.n_static = 0;                                      // set by the launcher
   a.merge_ctas = pool->num_sms;
   a.wait_ns = pool->wait_limit_ns;
-  a.scores = nullptr; a.score_stride = 0; a.row_ml = nullptr;
+  a.scores = nullptr; a.score_stride = 0; a.row_ml = nullptr; a.merge_wide = 0;
 }
 
 bool mma_shape(const step_pool* pool, const Geo& g, int n) {

@@ -94,25 +94,35 @@ __device__ inline Shape shape_of(const TreeArgs& a, int t, bool flag) {
 }
 // The stream: for every trace, for every KV head, for every row group, the sequence's tiles.  A warp's place in it:
 struct Place { int t, hr, tile; Shape x; };
-// One warp: how many tiles there are in all.
-__device__ inline long long stream_total(const TreeArgs& a, int lane, bool flag) {
+// (64-bit divisions take hundreds of cycles and stand in front of a small call's first copies)
+__device__ inline long long div_up(long long x, int by) {
+  return x + by <= 0x7fffffffll ? (long long)((unsigned)(x + by - 1) / (unsigned)by) : (x + by - 1) / by;
+}
+// One warp: `total` tiles in all, W tiles per share; the place of position pos_of(W) if that lies inside the stream (else
+// t = -1).  The first 32 traces' shapes are read once.
+template <typename PosOf>
+__device__ inline Place locate(const TreeArgs& a, int lane, bool flag, PosOf pos_of, long long& total, long long& W) {
+  Shape x0 = {};
   long long sum = 0;
   for (int t = lane; t < a.n; t += 32) {
     const Shape x = shape_of(a, t, flag);
+    if (t < 32) x0 = x;
     sum += (long long)x.tiles * x.groups;
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  return sum * a.Hkv;
-}
-// One warp: the place of position pos (inside the stream).
-__device__ inline Place seek(const TreeArgs& a, int lane, long long pos) {
-  long long run = 0;
+  total = sum * a.Hkv;
+  W = div_up(total, a.shares);
+  const long long pos = pos_of(W);
   Place p = {};
+  p.t = -1;
+  if (pos >= total) return p;
+  long long run = 0;
   for (int base = 0; base < a.n; base += 32) {
     const int t = base + lane;
-    long long mine = 0;
-    if (t < a.n) { const Shape x = shape_of(a, t, false); mine = (long long)x.tiles * x.groups * a.Hkv; }
+    Shape x = x0;
+    if (base > 0) x = t < a.n ? shape_of(a, t, false) : Shape{};
+    const long long mine = t < a.n ? (long long)x.tiles * x.groups * a.Hkv : 0;
     long long incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -122,11 +132,14 @@ __device__ inline Place seek(const TreeArgs& a, int lane, long long pos) {
     const unsigned past = __ballot_sync(0xffffffffu, run + incl > pos);      // (lanes behind the last trace count nothing)
     if (past) {
       const int who = __ffs(past) - 1;
-      const long long start = run + __shfl_sync(0xffffffffu, incl - mine, who);
+      const long long r = pos - (run + __shfl_sync(0xffffffffu, incl - mine, who));
       p.t = base + who;
-      p.x = shape_of(a, p.t, false);
-      p.hr = (int)((pos - start) / p.x.tiles);
-      p.tile = (int)((pos - start) % p.x.tiles);
+      p.x.S = __shfl_sync(0xffffffffu, x.S, who);
+      p.x.nodes = __shfl_sync(0xffffffffu, x.nodes, who);
+      p.x.tiles = __shfl_sync(0xffffffffu, x.tiles, who);
+      p.x.groups = __shfl_sync(0xffffffffu, x.groups, who);
+      p.hr = r <= 0x7fffffffll ? (int)((unsigned)r / (unsigned)p.x.tiles) : (int)(r / p.x.tiles);
+      p.tile = (int)(r - (long long)p.hr * p.x.tiles);
       return p;
     }
     run += __shfl_sync(0xffffffffu, incl, 31);
@@ -284,11 +297,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   tc_fence_after();
   dependents_may_launch();
   const uint32_t tmem = *s_tmem;
-  // this CTA's share of the stream: every warp that walks it asks
+  // this CTA's share of the stream and the place it begins at: every warp that walks it asks
   auto my_share = [&](bool flag, long long& pos0, long long& end) {
-    const long long total = stream_total(a, lane, flag), W = (total + a.shares - 1) / a.shares;
+    long long total, W;
+    const Place p = locate(a, lane, flag, [](long long w) { return (long long)blockIdx.x * w; }, total, W);
     pos0 = min(total, (long long)blockIdx.x * W);
     end = min(total, pos0 + W);
+    return p;
   };
 
   auto wait = [&](uint32_t bar, uint32_t parity) {
@@ -489,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     int win = 0, ids0 = 0, ids1 = 0;
     auto load_ids = [&](const Place& of, int first) {
       const int page = first + lane;
-      return of.t < a.n && (long long)page * kP < of.x.S ? a.block_table[(size_t)of.t * a.max_pages + page] : 0;
+      return of.t >= 0 && of.t < a.n && (long long)page * kP < of.x.S ? a.block_table[(size_t)of.t * a.max_pages + page] : 0;
     };
     // tile i of the piece into the next slot
     auto fetch = [&](int i) {
@@ -537,8 +552,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       if (++slot == ring_n) { slot = 0; ph ^= 1; }
     };
     long long pos, end;
-    my_share(kv == 0 && blockIdx.x == 0, pos, end);
-    if (pos < end) pl = seek(a, lane, pos);
+    pl = my_share(kv == 0 && blockIdx.x == 0, pos, end);
     int next0 = load_ids(pl, (pl.tile * (kTile / kP)) & ~31), next1 = load_ids(pl, ((pl.tile * (kTile / kP)) & ~31) + 32);
     while (pos < end && ok) {
       const int cnt = (int)min((long long)(pl.x.tiles - pl.tile), end - pos);
@@ -564,9 +578,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     // ------------------------------------------------ query rows and ancestor masks of one piece after another
     uint32_t par = 0;
     long long pos, end;
-    my_share(false, pos, end);
-    Place pl = {};
-    if (pos < end) pl = seek(a, lane, pos);
+    Place pl = my_share(false, pos, end);
     for (;; par ^= 1) {
       Piece pc = {};
       if (pos < end) {
@@ -749,10 +761,8 @@ __global__ void __launch_bounds__(kMergeWarps * 32) tree_merge_kernel(TreeArgs a
   __shared__ long long s_W;
   const int w0 = blockIdx.x;                                           // the share in front of the border
   if (warp == 0) {
-    const long long total = stream_total(a, lane, false), W = (total + a.shares - 1) / a.shares, border = (w0 + 1) * W;
-    Place p = {};
-    p.t = -1;
-    if (border < total) p = seek(a, lane, border);
+    long long total, W;
+    const Place p = locate(a, lane, false, [&](long long w) { return (w0 + 1) * w; }, total, W);
     if (lane == 0) { s_place = p; s_W = W; }
   }
   __syncthreads();
