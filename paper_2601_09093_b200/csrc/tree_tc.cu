@@ -18,8 +18,9 @@
 //   * two such chains ("lanes") run side by side in a CTA, so that the tensor cores work on one while the other is at
 //     its softmax.  Up to 128 rows: the lanes take even and odd tiles of the same rows and are combined at the end.
 //     More: the lanes take 128 rows each of the same tile, and 256 rows are one row group;
-//   * the tiles of all (trace, KV head, row group) sequences form one stream that is cut into one equal contiguous
-//     share per CTA; what a share holds of a sequence is a piece.  A piece that is not a whole sequence leaves its
+//   * the tiles of all (trace, KV head, row group) sequences form one stream - a sequence counts kSetup tiles more than it
+//     has, which is about what beginning and ending one costs - that is cut into one equal contiguous share per CTA;
+//     what a share holds of a sequence is a piece.  A piece that is not a whole sequence leaves its
 //     (m, l, O) in the share's first or last slot, and tree_merge_kernel - a programmatic dependent - combines the pieces of
 //     every sequence in stream order.  Row groups without a drafted token of theirs (a short tree) are not in the stream;
 //   * query rows come by TMA too (a box: the group's heads of as many tokens as fit 128 rows), the next piece's as soon as 
@@ -38,6 +39,7 @@ namespace {
 
 constexpr int kP = 16, kD = 128;
 constexpr int kTile = 128;                        // keys per tile
+constexpr int kSetup = 4;                         // tiles' worth of time that a sequence takes besides its tiles (see above)
 constexpr int kSlotBytes = kTile * kD * 2;        // K or V of one tile
 constexpr int kQBytes = kHalfRows * kD * 2;       // 128 query rows, same arrangement
 constexpr int kKSlots = 2, kVSlots = 3, kSlots = kKSlots + kVSlots;   // rings of K and of V tiles, 160 KiB: a V tile waits for its softmax
@@ -93,7 +95,7 @@ __device__ inline Shape shape_of(const TreeArgs& a, int t, bool flag) {
   return x;
 }
 // The stream: for every trace, for every KV head, for every row group, the sequence's tiles.  A warp's place in it:
-struct Place { int t, hr, tile; Shape x; };
+struct Place { int t, hr, at; Shape x; };   // at: how far into the sequence, its kSetup counted first
 // (64-bit divisions take hundreds of cycles and stand in front of a small call's first copies)
 __device__ inline long long div_up(long long x, int by) {
   return x + by <= 0x7fffffffll ? (long long)((unsigned)(x + by - 1) / (unsigned)by) : (x + by - 1) / by;
@@ -107,7 +109,7 @@ __device__ inline Place locate(const TreeArgs& a, int lane, bool flag, PosOf pos
   for (int t = lane; t < a.n; t += 32) {
     const Shape x = shape_of(a, t, flag);
     if (t < 32) x0 = x;
-    sum += (long long)x.tiles * x.groups;
+    sum += (long long)(x.tiles + kSetup) * x.groups;
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -122,7 +124,7 @@ __device__ inline Place locate(const TreeArgs& a, int lane, bool flag, PosOf pos
     const int t = base + lane;
     Shape x = x0;
     if (base > 0) x = t < a.n ? shape_of(a, t, false) : Shape{};
-    const long long mine = t < a.n ? (long long)x.tiles * x.groups * a.Hkv : 0;
+    const long long mine = t < a.n ? (long long)(x.tiles + kSetup) * x.groups * a.Hkv : 0;
     long long incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -138,17 +140,27 @@ __device__ inline Place locate(const TreeArgs& a, int lane, bool flag, PosOf pos
       p.x.nodes = __shfl_sync(0xffffffffu, x.nodes, who);
       p.x.tiles = __shfl_sync(0xffffffffu, x.tiles, who);
       p.x.groups = __shfl_sync(0xffffffffu, x.groups, who);
-      p.hr = r <= 0x7fffffffll ? (int)((unsigned)r / (unsigned)p.x.tiles) : (int)(r / p.x.tiles);
-      p.tile = (int)(r - (long long)p.hr * p.x.tiles);
+      p.hr = r <= 0x7fffffffll ? (int)((unsigned)r / (unsigned)(p.x.tiles + kSetup)) : (int)(r / (p.x.tiles + kSetup));
+      p.at = (int)(r - (long long)p.hr * (p.x.tiles + kSetup));
       return p;
     }
     run += __shfl_sync(0xffffffffu, incl, 31);
   }
   return p;
 }
+// What a share that ends at `end` holds of the sequence at place p (stream position pos): tiles [tile0, tile0 + cnt) of it,
+// `len` of the stream.  (No tile at all only at the share's end, in front of a sequence's first.)
+struct Part { int tile0, cnt; long long len; };
+__device__ inline Part part_of(const Place& p, long long pos, long long end) {
+  Part x;
+  x.len = min((long long)(p.x.tiles + kSetup - p.at), end - pos);
+  x.tile0 = max(0, p.at - kSetup);
+  x.cnt = max(0, (int)(p.at + x.len) - kSetup) - x.tile0;
+  return x;
+}
 // The place behind a whole rest of a sequence.
 __device__ inline void next_sequence(const TreeArgs& a, Place& p) {
-  p.tile = 0;
+  p.at = 0;
   if (++p.hr < a.Hkv * p.x.groups) return;
   p.hr = 0;
   if (++p.t < a.n) p.x = shape_of(a, p.t, false);
@@ -409,7 +421,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
 
       // ---- the piece is done
       const bool whole = pc.cnt == pc.tiles;
-      const size_t slot = (size_t)blockIdx.x * 2 + (pc.tile0 > 0 || first ? 0 : 1);
+      const size_t slot = (size_t)blockIdx.x * 2 + (first ? 0 : 1);
       first = false;
       float2* ml_out = reinterpret_cast<float2*>(a.ws_ml) + slot * a.group_rows + (kTwoRows ? ln * 128 : 0) + row;
       float* o_out = a.ws_o + (slot * a.group_rows + (kTwoRows ? ln * 128 : 0) + row) * kD;
@@ -502,6 +514,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     // for when the first is entered, four tiles before it is needed: with a read of the table in front of every tile, the read's
     // latency set the pace of the whole kernel (1,800 cycles a tile and operand).
     int win = 0, ids0 = 0, ids1 = 0;
+    Part part = {};
     auto load_ids = [&](const Place& of, int first) {
       const int page = first + lane;
       return of.t >= 0 && of.t < a.n && (long long)page * kP < of.x.S ? a.block_table[(size_t)of.t * a.max_pages + page] : 0;
@@ -511,7 +524,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       if (!ok) return;
       if (!wait_warp(bar_empty + 8 * (ring0 + slot), ph)) { ok = false; return; }
       const uint32_t bar = bar_full + 8 * (ring0 + slot), dst = sm_ring + (ring0 + slot) * kSlotBytes;
-      const int j0 = (pl.tile + i) * kTile;
+      const int j0 = (part.tile0 + i) * kTile;
       const int S = pl.x.S, nodes = pl.x.nodes;
       if (j0 / kP >= win + 32) { win += 32; ids0 = ids1; ids1 = load_ids(pl, win + 32); }
       const int in_win = j0 / kP - win;
@@ -553,19 +566,21 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     };
     long long pos, end;
     pl = my_share(kv == 0 && blockIdx.x == 0, pos, end);
-    int next0 = load_ids(pl, (pl.tile * (kTile / kP)) & ~31), next1 = load_ids(pl, ((pl.tile * (kTile / kP)) & ~31) + 32);
+    part = part_of(pl, pos, end);
+    const int win0 = (part.tile0 * (kTile / kP)) & ~31;
+    int next0 = load_ids(pl, win0), next1 = load_ids(pl, win0 + 32);
     while (pos < end && ok) {
-      const int cnt = (int)min((long long)(pl.x.tiles - pl.tile), end - pos);
+      part = part_of(pl, pos, end);
       h = pl.hr / pl.x.groups;
-      win = (pl.tile * (kTile / kP)) & ~31;
+      win = (part.tile0 * (kTile / kP)) & ~31;
       ids0 = next0;
       ids1 = next1;
       Place nx = pl;                                                   // the sequence behind this one, its block ids too
       next_sequence(a, nx);
       next0 = load_ids(nx, 0);
       next1 = load_ids(nx, 32);
-      for (int i = 0; i < cnt; ++i) fetch(i);
-      pos += cnt;
+      for (int i = 0; i < part.cnt; ++i) fetch(i);
+      pos += part.len;
       pl = nx;
     }
     cp_async_wait_all();
@@ -581,10 +596,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     Place pl = my_share(false, pos, end);
     for (;; par ^= 1) {
       Piece pc = {};
-      if (pos < end) {
+      Part part = {};
+      if (pos < end) part = part_of(pl, pos, end);
+      if (part.cnt > 0) {
         pc.t = pl.t; pc.h = pl.hr / pl.x.groups; pc.u0 = (pl.hr - pc.h * pl.x.groups) * a.tokens * a.lanes;
-        pc.tile0 = pl.tile; pc.tiles = pl.x.tiles; pc.S = pl.x.S; pc.nodes = pl.x.nodes;
-        pc.cnt = (int)min((long long)(pl.x.tiles - pl.tile), end - pos);
+        pc.tile0 = part.tile0; pc.cnt = part.cnt; pc.tiles = pl.x.tiles; pc.S = pl.x.S; pc.nodes = pl.x.nodes;
         for (int u = lane; u < pc.nodes; u += 32) {                    // (the other piece's masks are the ones in use)
           int p = a.parents[(size_t)pc.t * a.T + u];
           if (p >= u || p < -1) { flag_error(a.counters, STEP_ERR_INVALID_ARG); p = -1; }
@@ -597,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
           s_mask[par * 64 + u] = m;
         }
         __syncwarp();
-        pos += pc.cnt;
+        pos += part.len;
         next_sequence(a, pl);
       }
       // the scores of the piece before are made, and its announcement has been read (the very first wait passes at once)
@@ -768,10 +784,11 @@ __global__ void __launch_bounds__(kMergeWarps * 32) tree_merge_kernel(TreeArgs a
   __syncthreads();
   wait_for_primary();
   const Place p = s_place;
-  const long long W = s_W, start = (w0 + 1) * W - p.tile;              // where the sequence begins
-  if (p.t < 0 || p.tile == 0 || start < w0 * W) return;                // no border, no cut, or not the first cut of the sequence
+  const long long W = s_W, start = (w0 + 1) * W - p.at;                // where the sequence begins
+  // no border, no cut, or not the sequence's first cut
+  if (p.t < 0 || p.at <= kSetup || start + kSetup < w0 * W) return;
   const int h = p.hr / p.x.groups, u0 = (p.hr - h * p.x.groups) * a.tokens * a.lanes;
-  const int w1 = (int)((start + p.x.tiles - 1) / W);
+  const int w1 = (int)((start + kSetup + p.x.tiles - 1) / W);
   for (int rr = blockIdx.y * kMergeRows + warp; rr < (int)(blockIdx.y + 1) * kMergeRows; rr += kMergeWarps) {
     const int row = rr % kHalfRows, u = u0 + rr / kHalfRows * a.tokens + row / a.G;
     if (row >= a.tokens * a.G || u >= p.x.nodes) continue;
