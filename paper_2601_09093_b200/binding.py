@@ -143,6 +143,18 @@ def _stream(stream=None):
     return C.c_void_p(s.cuda_stream)
 
 
+def _raw_stream(device):
+    return torch.cuda.current_stream(device).cuda_stream if _current_raw_stream is None else _current_raw_stream(device.index)
+
+
+# (the stream's number without the Stream object around it, where this torch has it)
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _at(t):
+    return 0 if t is None else t.data_ptr()
+
+
 def _ptr(t):
     return C.c_void_p(0 if t is None else t.data_ptr())
 
@@ -150,7 +162,7 @@ def _ptr(t):
 def _expect(fn, device, *wanted):
     """Every (tensor, shape, dtype) of `wanted` is a contiguous tensor of that shape and type on `device`; None passes."""
     for t, shape, dtype in wanted:
-        if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous()):
+        if t is not None and (t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous()):
             raise StepError(fn, 1)
 
 
@@ -185,6 +197,7 @@ class KVPool:
         for k, v in self.geometry.items():
             setattr(self, k, v)
         self._views = None
+        self._sizes = {}                                 # workspace bytes of the calls that take one
         self.pruned_ids = torch.empty(max_traces, dtype=torch.int32, device=self.device)
         self.n_pruned = torch.zeros(1, dtype=torch.int32, device=self.device)
 
@@ -281,26 +294,29 @@ class KVPool:
         return out
 
     # ---- drafted tokens and a bounded cache
-    def _run(self, fn, stream, workspace, size_args, call):
-        """call(workspace pointer, bytes, stream) with the pool's device current; without a `workspace` (uint8 tensor) one
-        is taken from torch's allocator on the call's stream."""
-        if stream is not None or torch.cuda.current_device() != self._device().index:
-            with torch.cuda.device(self._device()), torch.cuda.stream(stream):
-                return self._run(fn, None, workspace, size_args, call)
-        nbytes = 0
-        if size_args is not None:
-            if workspace is None:
-                need = C.c_size_t()
-                _check(size_args[0], getattr(lib(), size_args[0])(self.handle, *size_args[1:], C.byref(need)))
-                workspace, nbytes = torch.empty(max(1, need.value), dtype=torch.uint8, device=self._device()), need.value
-            elif workspace.device != self._device() or not workspace.is_contiguous():
-                raise StepError(fn, 1)
-            else:
-                nbytes = workspace.numel() * workspace.element_size()
-        _check(fn, call(_ptr(workspace), nbytes, _stream()))
-
-    def _like_table(self, fn, n, block_table, seq_lens):
-        _expect(fn, self._device(), (block_table, (n, self.max_pages_per_trace), torch.int32), (seq_lens, (n,), torch.int32))
+    # (these are called once per layer and step: what a call costs on the host shows in short ones)
+    def _call(self, name, args, size=None, workspace=None, stream=None):
+        """name(pool, *args, [workspace, bytes,] stream) with the pool's device current.  `size`: (function, its arguments) that
+        says how much workspace it takes; without a `workspace` (uint8 tensor) one comes from torch's allocator on the
+        call's stream."""
+        dev = self._device()
+        if stream is not None or torch.cuda.current_device() != dev.index:
+            with torch.cuda.device(dev), torch.cuda.stream(stream):
+                return self._call(name, args, size, workspace)
+        if size is None:
+            _check(name, getattr(lib(), name)(self.handle, *args, _raw_stream(dev)))
+            return
+        need = self._sizes.get(size)
+        if need is None:
+            c = C.c_size_t()
+            _check(size[0], getattr(lib(), size[0])(self.handle, *size[1:], C.byref(c)))
+            need = self._sizes[size] = c.value
+        if workspace is None:
+            workspace = torch.empty(max(1, need), dtype=torch.uint8, device=dev)
+        elif workspace.device != dev or not workspace.is_contiguous():
+            raise StepError(name, 1)
+        _check(name, getattr(lib(), name)(self.handle, *args, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                          _raw_stream(dev)))
 
     def _device(self):
         return self.kv_storage.device
@@ -315,66 +331,66 @@ class KVPool:
     def decode_attention_tree(self, layer, q, k_draft, v_draft, parents, block_table, seq_lens, n_nodes=None, out=None,
                               workspace=None, stream=None):
         """q: [n, T, Hq, d] -> out [n, T, Hq, d] in the pool's type; k_draft, v_draft: [n, T, L, Hkv, d]; parents: [n, T]."""
-        fn, dev, dt = "decode_attention_tree", self._device(), self.torch_dtype
+        fn, dt = "decode_attention_tree", self.torch_dtype
         if q.dim() != 4:
             raise StepError(fn, 1)
         n, T = q.shape[:2]
         draft, rows = (n, T, self.num_layers, self.num_kv_heads, self.head_dim), (n, T, self.num_q_heads, self.head_dim)
-        self._like_table(fn, n, block_table, seq_lens)
-        _expect(fn, dev, (q, rows, dt), (k_draft, draft, dt), (v_draft, draft, dt), (parents, (n, T), torch.int32),
-                (n_nodes, (n,), torch.int32), (out, rows, dt))
+        _expect(fn, self._device(), (q, rows, dt), (k_draft, draft, dt), (v_draft, draft, dt), (parents, (n, T), torch.int32),
+                (n_nodes, (n,), torch.int32), (out, rows, dt), (block_table, (n, self.max_pages_per_trace), torch.int32),
+                (seq_lens, (n,), torch.int32))
         if out is None:
             out = self._empty(rows, dt, stream)
-        self._run(fn, stream, workspace, (fn + "_workspace_bytes", n, T), lambda ws, nb, st: lib().decode_attention_tree(
-            self.handle, layer, _ptr(q), _ptr(k_draft), _ptr(v_draft), _ptr(parents), _ptr(n_nodes), T, _ptr(block_table),
-            _ptr(seq_lens), n, _ptr(out), ws, nb, st))
+        self._call(fn, (layer, q.data_ptr(), k_draft.data_ptr(), v_draft.data_ptr(), parents.data_ptr(), _at(n_nodes), T,
+                        block_table.data_ptr(), seq_lens.data_ptr(), n, out.data_ptr()),
+                   ("decode_attention_tree_workspace_bytes", n, T), workspace, stream)
         return out
 
     def append_kv_path(self, trace_ids, k_draft, v_draft, path, path_len, stream=None):
         """Stores rows path[i, :path_len[i]] of the drafts [n, T, L, Hkv, d] behind trace trace_ids[i]."""
-        fn, dev = "append_kv_path", self._device()
+        fn, dt = "append_kv_path", self.torch_dtype
         if k_draft.dim() != 5 or path.dim() != 2:
             raise StepError(fn, 1)
         n, T = k_draft.shape[:2]
-        draft = (n, T, self.num_layers, self.num_kv_heads, self.head_dim)
-        _expect(fn, dev, (trace_ids, (n,), torch.int32), (k_draft, draft, self.torch_dtype), (v_draft, draft, self.torch_dtype),
-                (path, (n, path.shape[1]), torch.int32), (path_len, (n,), torch.int32))
-        self._run(fn, stream, None, None, lambda ws, nb, st: lib().append_kv_path(
-            self.handle, _ptr(trace_ids), n, T, _ptr(k_draft), _ptr(v_draft), _ptr(path), _ptr(path_len), path.shape[1], st))
+        draft, most = (n, T, self.num_layers, self.num_kv_heads, self.head_dim), path.shape[1]
+        _expect(fn, self._device(), (trace_ids, (n,), torch.int32), (k_draft, draft, dt), (v_draft, draft, dt),
+                (path, (n, most), torch.int32), (path_len, (n,), torch.int32))
+        self._call(fn, (trace_ids.data_ptr(), n, T, k_draft.data_ptr(), v_draft.data_ptr(), path.data_ptr(), path_len.data_ptr(),
+                        most), stream=stream)
 
     def decode_attention_weights(self, layer, q, block_table, seq_lens, weight_sum, out=None, workspace=None, stream=None):
         """q: [n, Hq, d] -> out [n, Hq, d] fp32; adds to weight_sum [n, Hkv, stride] fp32."""
-        fn, dev = "decode_attention_weights", self._device()
+        fn = "decode_attention_weights"
         if q.dim() != 3 or weight_sum.dim() != 3:
             raise StepError(fn, 1)
         n, stride = q.shape[0], weight_sum.shape[2]
         rows = (n, self.num_q_heads, self.head_dim)
-        self._like_table(fn, n, block_table, seq_lens)
-        _expect(fn, dev, (q, rows, self.torch_dtype), (weight_sum, (n, self.num_kv_heads, stride), torch.float32),
-                (out, rows, torch.float32))
+        _expect(fn, self._device(), (q, rows, self.torch_dtype), (weight_sum, (n, self.num_kv_heads, stride), torch.float32),
+                (out, rows, torch.float32), (block_table, (n, self.max_pages_per_trace), torch.int32), (seq_lens, (n,), torch.int32))
         if out is None:
             out = self._empty(rows, torch.float32, stream)
-        self._run(fn, stream, workspace, (fn + "_workspace_bytes", n, stride), lambda ws, nb, st: lib().decode_attention_weights(
-            self.handle, layer, _ptr(q), _ptr(block_table), _ptr(seq_lens), n, _ptr(out), _ptr(weight_sum), stride, ws, nb, st))
+        self._call(fn, (layer, q.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), n, out.data_ptr(), weight_sum.data_ptr(),
+                        stride), ("decode_attention_weights_workspace_bytes", n, stride), workspace, stream)
         return out
 
     def evict_positions(self, trace_ids, weights, budget, recent, weights_out=None, kept_out=None, workspace=None, stream=None):
         """weights: [L, n, Hkv, stride] fp32, in place unless weights_out is given.  Returns kept_out [L, n, Hkv, budget]
         (rows of entries that are left alone are not written: -1 in a tensor made here)."""
-        fn, dev = "kv_pool_evict_positions", self._device()
+        fn = "kv_pool_evict_positions"
         if weights.dim() != 4:
             raise StepError(fn, 1)
         n, stride = weights.shape[1], weights.shape[3]
         shape = (self.num_layers, n, self.num_kv_heads)
-        _expect(fn, dev, (trace_ids, (n,), torch.int32), (weights, shape + (stride,), torch.float32),
+        _expect(fn, self._device(), (trace_ids, (n,), torch.int32), (weights, shape + (stride,), torch.float32),
                 (weights_out, shape + (stride,), torch.float32), (kept_out, shape + (budget,), torch.int32))
         if weights_out is None:
             weights_out = weights
         if kept_out is None:
+            kept_out = self._empty(shape + (max(budget, 0),), torch.int32, stream)
             with torch.cuda.stream(stream):
-                kept_out = torch.full(shape + (max(budget, 0),), -1, dtype=torch.int32, device=dev)
-        self._run(fn, stream, workspace, ("kv_pool_evict_workspace_bytes", n, budget), lambda ws, nb, st: lib().kv_pool_evict_positions(
-            self.handle, _ptr(trace_ids), n, _ptr(weights), _ptr(weights_out), stride, budget, recent, _ptr(kept_out), ws, nb, st))
+                kept_out.fill_(-1)
+        self._call(fn, (trace_ids.data_ptr(), n, weights.data_ptr(), weights_out.data_ptr(), stride, budget, recent,
+                        kept_out.data_ptr()), ("kv_pool_evict_workspace_bytes", n, budget), workspace, stream)
         return kept_out
 
     def score_steps(self, hidden, boundary_mask, row_trace, weights, step_scores_out=None, stream=None):
@@ -495,6 +511,7 @@ class KVPool:
 
     def set_attention_config(self, grid_ctas=0, fast_path=0):
         _check("kv_pool_set_attention_config", lib().kv_pool_set_attention_config(self.handle, grid_ctas, fast_path))
+        self._sizes.clear()
 
     def set_attention_balance(self, dynamic_sixteenths, min_chunk_pages=0):
         _check("kv_pool_set_attention_balance",
