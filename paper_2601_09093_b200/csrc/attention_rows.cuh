@@ -78,7 +78,7 @@ struct RowsArgs {
   int32_t* counters;
 };
 
-constexpr int kRows = 16, kKeys = 32, kRowsThreads = 128;
+constexpr int kRows = 16, kKeys = 32, kRowsThreads = 128, kAhead = 8;
 
 // Ranges of keys per (row block, KV head, trace): enough that about four CTAs per SM have work, each at least two tiles.
 // (8 traces of up to 256 tokens, 4 heads of 64 in fp32, one new token: 229 us with one range and the products of the first
@@ -153,6 +153,7 @@ __global__ void __launch_bounds__(kRowsThreads) attn_rows_kernel(RowsArgs a) {
     }
   };
   locate(it0);
+#pragma unroll 2
   for (int i = tid; i < kRows * cpr; i += kRowsThreads) {
     const int rr = i / cpr, c = i - rr * cpr, r = r0 + rr;
     uint4 raw = make_uint4(0, 0, 0, 0);
@@ -181,21 +182,37 @@ __global__ void __launch_bounds__(kRowsThreads) attn_rows_kernel(RowsArgs a) {
 
   for (int it = it0; it < it1; ++it) {
     const int j0 = it * kKeys;
-    for (int i = tid; i < 2 * kKeys * cpr; i += kRowsThreads) {
-      const int which = i >= kKeys * cpr, r = which ? i - kKeys * cpr : i;
-      const int key = r / cpr, c = r - key * cpr;
-      const T* src = s_src[it & 1][which][key];
-      uint4 raw = make_uint4(0, 0, 0, 0);
-      if (src) {
-        const int j = j0 + key;
-        const int cc = g.swizzle && j < S ? ((c & ~7) | ((c ^ (j % g.P)) & 7)) : c;     // (drafts are stored as they come)
-        raw = *reinterpret_cast<const uint4*>(src + cc * cpe);
-      }
-      const T* e = reinterpret_cast<const T*>(&raw);
-      float* dst = which ? s_v + key * d + c * cpe : s_k + key * ld + c * cpe;
+    // (kAhead loads of a thread are under way before the first of them is used)
+    for (int i0 = tid; i0 < 2 * kKeys * cpr; i0 += kAhead * kRowsThreads) {
+      uint4 raw[kAhead];
 #pragma unroll
-      for (int x = 0; x < cpe; x += 4)
-        *reinterpret_cast<float4*>(dst + x) = make_float4(to_f32(e[x]), to_f32(e[x + 1]), to_f32(e[x + 2]), to_f32(e[x + 3]));
+      for (int y = 0; y < kAhead; ++y) {
+        const int i = i0 + y * kRowsThreads;
+        raw[y] = make_uint4(0, 0, 0, 0);
+        if (i < 2 * kKeys * cpr) {
+          const int which = i >= kKeys * cpr, r = which ? i - kKeys * cpr : i;
+          const int key = r / cpr, c = r - key * cpr;
+          const T* src = s_src[it & 1][which][key];
+          if (src) {
+            const int j = j0 + key;
+            const int cc = g.swizzle && j < S ? ((c & ~7) | ((c ^ (j % g.P)) & 7)) : c;   // (drafts are stored as they come)
+            raw[y] = *reinterpret_cast<const uint4*>(src + cc * cpe);
+          }
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < kAhead; ++y) {
+        const int i = i0 + y * kRowsThreads;
+        if (i < 2 * kKeys * cpr) {
+          const int which = i >= kKeys * cpr, r = which ? i - kKeys * cpr : i;
+          const int key = r / cpr, c = r - key * cpr;
+          const T* e = reinterpret_cast<const T*>(&raw[y]);
+          float* dst = which ? s_v + key * d + c * cpe : s_k + key * ld + c * cpe;
+#pragma unroll
+          for (int x = 0; x < cpe; x += 4)
+            *reinterpret_cast<float4*>(dst + x) = make_float4(to_f32(e[x]), to_f32(e[x + 1]), to_f32(e[x + 2]), to_f32(e[x + 3]));
+        }
+      }
     }
     locate(it + 1);
     __syncthreads();

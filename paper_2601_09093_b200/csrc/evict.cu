@@ -41,8 +41,9 @@ struct EvictArgs {
 };
 
 // Pages are examined by a warp per entry, spread over the cluster: a kept page's reference count is a scattered 4-byte
-// read, and one SM alone takes 10 us for the 16,000 of them that 64 traces of 4,096 positions have.
-__global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kPruneThreads, 1) evict_plan_kernel(EvictArgs a) {
+// read, and one SM alone takes 10 us for the 16,000 of them that 64 traces of 4,096 positions have.  (A call that has few
+// pages to look at is a cluster of one: its barriers cost nothing then.)
+__global__ void __launch_bounds__(kPruneThreads, 1) evict_plan_kernel(EvictArgs a) {
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
   __shared__ int s_warp[33];
@@ -50,8 +51,8 @@ __global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kPruneThr
   dependents_may_launch();
   const DevViews& v = a.v;
   const Geo& g = a.g;
-  const int rank = (int)cluster.block_rank(), lane = threadIdx.x & 31;
-  const int warp = (threadIdx.x >> 5) * kClusterCtas + rank, nwarps = kPruneThreads / 32 * kClusterCtas;
+  const int rank = (int)cluster.block_rank(), C = (int)cluster.num_blocks(), lane = threadIdx.x & 31;
+  const int warp = (threadIdx.x >> 5) * C + rank, nwarps = kPruneThreads / 32 * C;
   const int nbp = (a.budget + g.P - 1) / g.P;
   // first place of every listed trace (a repeat is flagged and left alone)
   if (rank == 0) {
@@ -426,7 +427,7 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(EvictArgs a
 // ---------------------------------------------------------------- bookkeeping
 // The listed (entry, page) pairs drop one reference each.  A block whose count reaches zero is pushed on the free list at
 // the place of the last pair that names it, as a serial walk would (see release.cuh).
-__global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kPruneThreads, 1) evict_finish_kernel(EvictArgs a) {
+__global__ void __launch_bounds__(kPruneThreads, 1) evict_finish_kernel(EvictArgs a) {
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
   __shared__ int s_warp[33], s_count, s_base;
@@ -494,6 +495,19 @@ __global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kPruneThr
   cluster.sync();                        // no CTA leaves while its count may still be read
 }
 
+// A cluster of `ctas` CTAs; dependent: a programmatic dependent of the launch before it.
+cudaError_t launch_cluster(void (*kernel)(EvictArgs), int ctas, bool dependent, cudaStream_t s, const EvictArgs& a) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas); cfg.blockDim = dim3(kPruneThreads); cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = dependent ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
 bool evict_sizes_ok(const step_pool* pool, int n, int budget) {
   return n >= 0 && n <= pool->cfg.max_traces && n <= kMaxTracesFast && budget >= 1 &&
          budget <= (long long)pool->cfg.max_pages_per_trace * pool->cfg.page_size;
@@ -538,12 +552,13 @@ int kv_pool_evict_positions(step_pool* pool, const int32_t* trace_ids, int n, co
   for (int b = 0; b < 30; ++b)
     if (a.g.P == 1 << b) a.shift = b;
   a.cache_keys = weight_stride <= kMostCachedKeys ? weight_stride : 0;
-  evict_plan_kernel<<<kClusterCtas, kPruneThreads, 0, s>>>(a);
-  if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
+  // pages there may be to look at: below 4096 (four rounds of one CTA's threads) one CTA is faster than a cluster of eight
+  const int ctas = (long long)n * a.g.max_pages < 4096 ? 1 : kClusterCtas;
+  if (launch_cluster(evict_plan_kernel, ctas, false, s, a) != cudaSuccess) return STEP_ERR_CUDA;
   const size_t smem = (size_t)a.cache_keys * sizeof(uint32_t);
   if (cudaFuncSetAttribute(evict_move_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostCachedKeys * 4) != cudaSuccess) return STEP_ERR_CUDA;
   if (launch_dependent(evict_move_kernel, dim3(a.g.Hkv, n, a.g.L), dim3(kMoveThreads), smem, s, a) != cudaSuccess) return STEP_ERR_CUDA;
-  if (launch_dependent(evict_finish_kernel, dim3(kClusterCtas), dim3(kPruneThreads), 0, s, a) != cudaSuccess) return STEP_ERR_CUDA;
+  if (launch_cluster(evict_finish_kernel, ctas, true, s, a) != cudaSuccess) return STEP_ERR_CUDA;
   return launch_ok();
 }
 

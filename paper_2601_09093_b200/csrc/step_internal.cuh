@@ -88,6 +88,9 @@ struct step_pool {
   alignas(64) unsigned char tmap_h_bytes[128];
   const void* tmap_h_ptr; int tmap_h_D, tmap_h_M;
   bool tc_smem_set;   // the scorer kernel's dynamic shared memory limit has been raised on this pool's device
+  // the tensor map of the whole pool (tree attention), and whether its kernels' shared memory limits have been raised
+  alignas(64) unsigned char tmap_kv_bytes[128];
+  bool tree_ready;
   int device;
   stepk::MetaLayout lay;
   stepk::DevViews v;

@@ -838,16 +838,26 @@ int tree_tc_launch(step_pool* pool, int layer, const void* q, const void* k_draf
   const Geo g = geo_of(pool);
   EncodeTiledFn enc = encode_tiled_fn();
   if (!enc) return STEP_ERR_CUDA;
-  // the pool as groups of 8 rows of 128 dims, seen as [group][half of the dims][row][64 dims]; a box is the two groups of a
-  // page's K or V
-  CUtensorMap map;
-  const cuuint64_t dims[4] = {64, 8, 2, (cuuint64_t)g.L * g.num_blocks * g.Hkv * 2 * (kP / 8)};
-  const cuuint64_t strides[3] = {256, 128, 2048};
-  const cuuint32_t box[4] = {64, 8, 2, kP / 8};
   const cuuint32_t estr[4] = {1, 1, 1, 1};
-  if (enc(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, pool->cfg.kv_storage, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-          CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-    return STEP_ERR_CUDA;
+  if (!pool->tree_ready) {
+    // the pool as groups of 8 rows of 128 dims, seen as [group][half of the dims][row][64 dims]; a box is the two groups of a
+    // page's K or V
+    CUtensorMap fresh;
+    static_assert(sizeof(fresh) <= sizeof(pool->tmap_kv_bytes), "tensor map");
+    const cuuint64_t dims[4] = {64, 8, 2, (cuuint64_t)g.L * g.num_blocks * g.Hkv * 2 * (kP / 8)};
+    const cuuint64_t strides[3] = {256, 128, 2048};
+    const cuuint32_t box[4] = {64, 8, 2, kP / 8};
+    if (enc(&fresh, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, pool->cfg.kv_storage, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return STEP_ERR_CUDA;
+    memcpy(pool->tmap_kv_bytes, &fresh, sizeof(fresh));
+    if (cudaFuncSetAttribute(tree_tc_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(true)) != cudaSuccess ||
+        cudaFuncSetAttribute(tree_tc_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(false)) != cudaSuccess)
+      return STEP_ERR_CUDA;
+    pool->tree_ready = true;
+  }
+  CUtensorMap map;
+  memcpy(&map, pool->tmap_kv_bytes, sizeof(map));
   TreeArgs a;
   a.kv = (const __nv_bfloat16*)pool->cfg.kv_storage;
   a.q = (const __nv_bfloat16*)q; a.k_draft = (const __nv_bfloat16*)k_draft; a.v_draft = (const __nv_bfloat16*)v_draft;
@@ -864,7 +874,6 @@ int tree_tc_launch(step_pool* pool, int layer, const void* q, const void* k_draf
   a.ws_ml = a.ws_o + (size_t)a.shares * 2 * a.group_rows * kD;
   const size_t smem = smem_bytes(a.lanes == 2);
   auto kern = a.lanes == 2 ? tree_tc_kernel<true> : tree_tc_kernel<false>;
-  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return STEP_ERR_CUDA;
   // queries: a box is one half of the dims of the G heads of a group, for as many tokens as make a tile of rows
   CUtensorMap map_q;
   const cuuint64_t q_dims[3] = {kD, (cuuint64_t)g.Hq, (cuuint64_t)n * T};
