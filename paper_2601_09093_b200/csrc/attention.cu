@@ -939,9 +939,11 @@ int launch_one(AttnArgs a, int grid, cudaStream_t s, bool dependent = false) {
     if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
   }
   const int rows = kMode == kPrefixPass ? a.tpb * a.G : a.G;
-  a.merge_wide = kCount && (long long)n_seq * a.Hkv * rows <= 2ll * a.merge_ctas;
+  a.merge_wide = kCount && (long long)n_seq * a.Hkv * rows <= 4ll * a.merge_ctas;
   long long mgrid = a.merge_wide ? (long long)n_seq * a.Hkv * rows : ((long long)n_seq * a.Hkv * rows + kMergeWarps - 1) / kMergeWarps;
-  if (mgrid > a.merge_ctas) mgrid = a.merge_ctas;
+  // (kCount: the attention kernel's registers leave no room for it beside one of its CTAs, so it may as well fill the SMs)
+  const long long most = kCount ? 4ll * a.merge_ctas : a.merge_ctas;
+  if (mgrid > most) mgrid = most;
   if (launch_dependent(attn_merge_kernel<kMode, kCount>, dim3((int)mgrid), dim3(kMergeWarps * 32), (size_t)(3 * n_seq + 3) * 4, s, a) != cudaSuccess) return STEP_ERR_CUDA;
   return launch_ok();
 }
