@@ -209,8 +209,8 @@ int decode_attention_static(step_pool* pool, int layer, const void* q,
  * itself.  A parent outside [-1, u) is read as -1 and sets the STEP_ERR_INVALID_ARG bit of the device status word.
  * n_nodes: [n] int32 or NULL: row i has n_nodes[i] <= T drafted tokens (NULL: T); out rows behind them are zeros, and
  * their q, k_draft, v_draft and parents are not read.  A count outside [0, T] is clamped and flagged likewise.
- * out: [n, T, num_q_heads, head_dim] in POOL DTYPE (what the output projection behind it reads), rounded once; it must
- * not overlap the inputs.  1 <= T <= 64, n <= 65535.
+ * out: [n, T, num_q_heads, head_dim] in POOL DTYPE (what the output projection behind it reads), rounded once, 32-byte
+ * aligned; it must not overlap the inputs.  1 <= T <= 64, n <= 65535.
  * decode_attention_tree_workspace_bytes (host-only) says how large the workspace has to be; NULL is fine for 0. */
 int decode_attention_tree_workspace_bytes(const step_pool* pool, int n, int T, size_t* bytes);
 int decode_attention_tree(step_pool* pool, int layer, const void* q, const void* k_draft, const void* v_draft,

@@ -23,7 +23,7 @@ int decode_attention_tree(step_pool* pool, int layer, const void* q, const void*
   if (layer < 0 || layer >= pool->cfg.num_layers) return STEP_ERR_INVALID_ARG;
   if (n == 0) return STEP_OK;
   if (!q || !k_draft || !v_draft || !parents || !block_table || !seq_lens || !out || n > 65535) return STEP_ERR_INVALID_ARG;
-  if (((uintptr_t)q | (uintptr_t)k_draft | (uintptr_t)v_draft | (uintptr_t)out) & 15) return STEP_ERR_INVALID_ARG;
+  if (((uintptr_t)q | (uintptr_t)k_draft | (uintptr_t)v_draft) & 15 || (uintptr_t)out & 31) return STEP_ERR_INVALID_ARG;
   int st = on_pool_device(pool);
   if (st != STEP_OK) return st;
   cudaStream_t s = (cudaStream_t)stream;

@@ -187,6 +187,73 @@ def test_a_bad_block_is_flagged():
         assert tw.gpu.last_error() == (7, 1 << 7)
 
 
+def test_the_general_kernel_gives_the_same_within_the_same_bounds():
+    cfg = config((8, 2, 128), "bf16", n=len(LENS))
+    tw = twin(cfg, LENS)
+    tw.gpu.set_attention_config(fast_path=-1)
+    run_tree(tw, 1, 9)
+    tw.gpu.set_attention_config(fast_path=1)
+    run_tree(tw, 1, 9, poison=False)
+
+
+@pytest.mark.parametrize("n", [2048, 2049])
+def test_at_and_beyond_the_tensor_core_kernels_trace_limit(n):
+    lens = np.random.default_rng(n).integers(0, 20, size=n)
+    cfg = config((2, 1, 128), "bf16", n=n, layers=1)
+    run_tree(twin(cfg, lens, max_pages=3), 0, 2, poison=False)
+
+
+def test_a_pool_beyond_32_bit_offsets():
+    """Blocks at the far end of a pool of 2.5e9 elements: tree attention, path append, counting attention and eviction
+    against plain fp64 arithmetic on the rows that went in."""
+    Hq, Hkv, d, P, n, S, T = 4, 2, 128, 16, 2, 83, 3
+    blocks = 2_500_000_000 // (Hkv * 2 * P * d)
+    pool = B.KVPool(1, Hq, Hkv, d, P, num_blocks=blocks, max_traces=n, max_pages_per_trace=8)
+    v = pool.views()
+    v["free_list"].copy_(torch.arange(blocks, dtype=torch.int32, device="cuda"))        # pops from the end: the highest first
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    draw_ = lambda *shape: torch.randn(shape, generator=gen, device="cuda").bfloat16()   # noqa: E731
+    pool.fork_prefix(n, 0, None, None)
+    ids = torch.arange(n, dtype=torch.int32, device="cuda")
+    k, w, kd, vd, q = draw_(n, S, 1, Hkv, d), draw_(n, S, 1, Hkv, d), draw_(n, T, 1, Hkv, d), draw_(n, T, 1, Hkv, d), draw_(n, T, Hq, d)
+    pool.append_kv(ids, S, k, w)
+    assert int(v["block_table"][:, 0].min()) > blocks - 16
+    parents = torch.tensor([[-1, 0, 0]] * n, dtype=torch.int32, device="cuda")
+    out = pool.decode_attention_tree(0, q, kd, vd, parents, v["block_table"], v["seq_lens"]).double()
+    see = torch.tensor([[1, 0, 0], [1, 1, 0], [1, 0, 1]], device="cuda").bool()
+
+    def attend(q, k, v, mask=None):                      # q [n, T, Hq, d]; k, v [n, S, Hkv, d]
+        a = torch.einsum("nthd,nshd->nths", q.double(), k.double().repeat_interleave(2, 2)) / d ** 0.5
+        if mask is not None:
+            a = a.masked_fill(~mask[None, :, None], -torch.inf)
+        p = a.softmax(-1)
+        return torch.einsum("nths,nshd->nthd", p, v.double().repeat_interleave(2, 2)), p
+
+    kk, vv = torch.cat((k, kd), 1)[:, :, 0], torch.cat((w, vd), 1)[:, :, 0]
+    want, p = attend(q, kk, vv, torch.cat((torch.ones((T, S), device="cuda").bool(), see), 1))
+    # probabilities rounded to bf16, fp32 sums of scores below 8, one rounding of the output; values below 6
+    assert (out - want).abs().max().item() <= 2 * BF16_HALF_STEP * 6
+    path = torch.tensor([[0, 2], [1, 0]], dtype=torch.int32, device="cuda")
+    pool.append_kv_path(ids, kd, vd, path, torch.tensor([2, 1], dtype=torch.int32, device="cuda"))
+    sums = torch.zeros((n, Hkv, S + 2), device="cuda")
+    one = q[:, :1]
+    out = pool.decode_attention_weights(0, one[:, 0].contiguous(), v["block_table"], v["seq_lens"], sums)
+    for t, rows in ((0, [0, 2]), (1, [1])):
+        kk, vv = torch.cat((k[t], kd[t, rows]))[None, :, 0], torch.cat((w[t], vd[t, rows]))[None, :, 0]
+        want, p = attend(one[t:t + 1], kk, vv)
+        rel = max(relative_bound(exact_f32(one[t, 0, 2 * h:2 * h + 2]), exact_f32(kk[0, :, h])) for h in range(Hkv))
+        assert (out[t] - want[0, 0]).abs().max().item() <= rel * 6                   # sums of values below 6, weighted by 1 in all
+        weights = p[0, 0].view(Hkv, 2, -1).sum(1)
+        assert ((sums[t, :, :kk.shape[1]] - weights).abs() <= (rel + 2.0 ** -22) * weights).all()
+    kept = pool.evict_positions(ids, sums[None].contiguous(), 40, 7)[0].long()
+    for t, rows in ((0, [0, 2]), (1, [1])):
+        whole = torch.cat((k[t], kd[t, rows]))[:, 0]
+        for h in range(Hkv):
+            got, _ = pool.read_kv(0, h, v["block_table"][t], 40)
+            assert torch.equal(got, whole[kept[t, h], h])
+    assert pool.last_error() == (0, 0)
+
+
 # ---------------------------------------------------------------- append_kv_path
 def same_payload(tw):
     for l in range(tw.cfg.num_layers):
@@ -267,6 +334,8 @@ def test_refusals():
            dict(out=q.float()), dict(q=q.transpose(0, 1).contiguous().transpose(0, 1)),
            dict(q=wide, k_draft=torch.zeros((2, 65, 1, 2, 128), dtype=torch.bfloat16, device=dev),
                 v_draft=torch.zeros((2, 65, 1, 2, 128), dtype=torch.bfloat16, device=dev), parents=torch.full((2, 65), -1, dtype=torch.int32, device=dev))]
+    off = torch.zeros(q.numel() + 8, dtype=torch.bfloat16, device=dev)
+    bad += [dict(out=off[8:].view(q.shape)), dict(q=off[4:-4].view(q.shape))]        # 16 and 8 bytes behind an aligned address
     for change in bad:
         with pytest.raises(B.StepError) as e:
             p.decode_attention_tree(**{**ok, **change})
