@@ -253,6 +253,24 @@ __device__ inline void st_global32(void* dst, const uint32_t* r) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                ::"l"(dst), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
+// Two fp32 operations in one instruction.
+__device__ inline void fma2(float& x, float& y, float ax, float ay, float b, float c) {
+  asm("{\n\t.reg .b64 a, b, c, d;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %5};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(x), "=f"(y) : "f"(ax), "f"(ay), "f"(b), "f"(c));
+}
+__device__ inline void add2(float& x, float& y, float ax, float ay) {
+  asm("{\n\t.reg .b64 a, b, d;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%0, %1};\n\t"
+      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "+f"(x), "+f"(y) : "f"(ax), "f"(ay));
+}
+__device__ inline float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 __device__ inline uint32_t pack2(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
@@ -372,11 +390,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         }
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int c = 0; c < kTile; c += 4) {
+        for (int c = 0; c < kTile; c += 8) {
 #pragma unroll
-          for (int x = 0; x < 4; ++x) mx[x] = fmaxf(mx[x], __uint_as_float(s[c + x]));
+          for (int x = 0; x < 4; ++x) mx[x] = max3(mx[x], __uint_as_float(s[c + 2 * x]), __uint_as_float(s[c + 2 * x + 1]));
         }
-        const float m_new = fmaxf(m_ref, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2);
+        const float m_new = fmaxf(m_ref, fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * a.scale_log2);
         if (!started) {
           m_ref = m_new;
           started = true;
@@ -402,10 +420,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < kTile; c += 2) {
-          const float p0 = exp2f(fmaf(__uint_as_float(s[c]), a.scale_log2, -off));
-          const float p1 = exp2f(fmaf(__uint_as_float(s[c + 1]), a.scale_log2, -off));
-          sum[c & 2] += p0;
-          sum[(c & 2) + 1] += p1;
+          float p0, p1;
+          fma2(p0, p1, __uint_as_float(s[c]), __uint_as_float(s[c + 1]), a.scale_log2, -off);
+          p0 = exp2f(p0);
+          p1 = exp2f(p1);
+          add2(sum[c & 2], sum[(c & 2) + 1], p0, p1);
           s[c / 2] = pack2(p0, p1);
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
