@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   float* s_ml = reinterpret_cast<float*>(s_tmem + 4);                  // [2][128][2] (below 128 rows)
   const uint32_t bars = smem_u32(s_bar);
   const uint32_t bar_full = bars, bar_empty = bars + 8 * kSlots;
-  const uint32_t bar_q = bars + 16 * kSlots, bar_s = bar_q + 8, bar_p = bar_s + 16, bar_o = bar_p + 16,
+  const uint32_t bar_q = bars + 16 * kSlots, bar_s = bar_q + 8, bar_p = bar_s + 16, bar_o = bar_p + 32,
                  bar_both = bar_o + 16, bar_qfree = bar_both + 8, bar_drain = bar_qfree + 8;
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
@@ -311,6 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     for (int s = 0; s < 2; ++s) {
       mbar_init(bar_s + 8 * s, 1);                  // tcgen05.commit: scores made (and the products before them done)
       mbar_init(bar_p + 8 * s, 4);                  // (one arrival per warp: arrivals at one barrier queue up)
+      mbar_init(bar_p + 16 + 8 * s, 4);             // the first half of the probabilities (above 128 rows)
       mbar_init(bar_o + 8 * s, 1);                  // tcgen05.commit: a piece's last product
     }
     mbar_init(bar_both, 8);
@@ -418,21 +419,27 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         }
         const float off = m_ref == -INFINITY ? 0.f : m_ref;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        // (in halves where the tensor cores wait for it: the second product of the first 64 keys runs while the others'
+        // probabilities are made)
 #pragma unroll
-        for (int c = 0; c < kTile; c += 2) {
-          float p0, p1;
-          fma2(p0, p1, __uint_as_float(s[c]), __uint_as_float(s[c + 1]), a.scale_log2, -off);
-          p0 = exp2f(p0);
-          p1 = exp2f(p1);
-          add2(sum[c & 2], sum[(c & 2) + 1], p0, p1);
-          s[c / 2] = pack2(p0, p1);
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+          for (int c = half * 64; c < half * 64 + 64; c += 2) {
+            float p0, p1;
+            fma2(p0, p1, __uint_as_float(s[c]), __uint_as_float(s[c + 1]), a.scale_log2, -off);
+            p0 = exp2f(p0);
+            p1 = exp2f(p1);
+            add2(sum[c & 2], sum[(c & 2) + 1], p0, p1);
+            s[c / 2] = pack2(p0, p1);
+          }
+          tc_st32(t_s + half * 32, s + half * 32);
+          if (kTwoRows || half == 1) {
+            tc_wait_st();
+            tc_fence_before();
+            arrive_warp(bar_p + 8 * (half == 0 ? 2 + ln : ln));
+          }
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        tc_st32(t_s, s);
-        tc_st32(t_s + 32, s + 32);
-        tc_wait_st();
-        tc_fence_before();
-        arrive_warp(bar_p + 8 * ln);
       }
       if (!ok || !wait_warp(bar_o + 8 * ln, ph_piece)) { ok = false; break; }
       tc_fence_after();
@@ -678,9 +685,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       if (++at[kv] == (kv ? kVSlots : kKSlots)) { at[kv] = 0; ph[kv] ^= 1; }
       return s;
     };
-    auto probabilities = [&](int ln) {
-      ok = ok && wait_warp(bar_p + 8 * ln, ph_p[ln]);
-      ph_p[ln] ^= 1;
+    auto probabilities = [&](int ln, bool first_half) {
+      ok = ok && wait_warp(bar_p + 8 * (first_half ? 2 + ln : ln), ph_p[ln]);
+      if (!first_half) ph_p[ln] ^= 1;
       tc_fence_after();
     };
     // (the elected thread's part of it)
@@ -693,11 +700,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       tc_commit(bar_s + 8 * ln);
     };
     // steps of 16 keys; those of a tile behind the last key are left out, so nothing that lies there matters
-    auto values = [&](int ln, int s, bool first, int steps) {
+    auto values = [&](int ln, int s, bool first, int from, int steps) {
       const uint32_t vb = sm_ring + s * kSlotBytes;
 #pragma unroll
       for (int x = 0; x < 8; ++x)
-        if (x < steps) tc_mma_bf16_ta(tm + 256 + ln * 128, tm + ln * 128 + x * 8, umma_desc_v(vb + x * 4096), id_pv, !(first && x == 0));
+        if (x >= from && x < steps) tc_mma_bf16_ta(tm + 256 + ln * 128, tm + ln * 128 + x * 8, umma_desc_v(vb + x * 4096), id_pv, !(first && x == 0));
     };
     while (ok) {
       ok = wait_warp(bar_q, ph_q);
@@ -719,15 +726,21 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
           const int v = next(1, copied(i));
           const bool more = i + 1 < cnt;
           if (more) k = next(0, copied(i + 1));
-          probabilities(0);
+          probabilities(0, true);
+          if (ok && elect_one()) values(0, v, i == 0, 0, min(4, steps(i)));
+          __syncwarp();
+          probabilities(0, false);
           if (ok && elect_one()) {
-            values(0, v, i == 0, steps(i));
+            values(0, v, i == 0, 4, steps(i));
             if (more) scores(0, k); else tc_commit(bar_o);
           }
           __syncwarp();
-          probabilities(1);
+          probabilities(1, true);
+          if (ok && elect_one()) values(1, v, i == 0, 0, min(4, steps(i)));
+          __syncwarp();
+          probabilities(1, false);
           if (ok && elect_one()) {
-            values(1, v, i == 0, steps(i));
+            values(1, v, i == 0, 4, steps(i));
             tc_commit(bar_empty + 8 * v);
             if (more) { scores(1, k); tc_commit(bar_empty + 8 * k); } else tc_commit(bar_o + 8);
             if (i + 2 == cnt) tc_commit(bar_qfree);
@@ -747,9 +760,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         }
         for (int i = 0; i < cnt && ok; ++i) {
           const int v = next(1, copied(i));
-          probabilities(i & 1);
+          probabilities(i & 1, false);
           if (ok && elect_one()) {
-            values(i & 1, v, i < 2, steps(i));
+            values(i & 1, v, i < 2, 0, steps(i));
             tc_commit(bar_empty + 8 * v);
             if (i + 2 >= cnt) tc_commit(bar_o + 8 * (i & 1));
             if (cnt == 1) tc_commit(bar_o + 8);                        // lane 1 has nothing to do
