@@ -294,7 +294,7 @@ __device__ inline void build_partition(const AttnArgs& a, int n, int lane, bool 
 // enter the second product as three bf16 terms (high, middle and low bits: 24 bits in all) instead of one, so that out
 // is accurate to fp32.  Up to eight query heads a KV head occupy the tile's upper eight rows only; the middle terms then
 // ride in its lower eight, and the low terms cost one more product per page: 48 instead of 32 instructions, which the
-// stream of pages still hides (64 traces of 4.6k to 16.9k tokens, 32 / 8 heads: see weights.cu).
+// stream of pages still hides (64 traces of 4.6k to 16.9k tokens, 32 / 8 heads: 438 us for 2.86 GB, 6.5 TB/s).
 
 // How a launch's pages are spread over the SMs.
 //
@@ -613,8 +613,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_mma_kernel(AttnArgs a) {
       ldsm_x4_t(addr, b0, b1, b2, b3);
       if constexpr (kCount) {
         // a page's products start from zero and are added to the running sums in fp32: the tensor cores' own
-        // accumulation cuts low bits off, always downwards, and over a thousand pages that adds up (out 5.6e-6 off where
-        // it is 1e-6 this way)
+        // accumulation cuts low bits off, always downwards, and over a thousand pages that adds up (out 5.6e-6 off, in the
+        // 2-norm, where it is 4.8e-7 this way)
         float t0[4] = {0.f, 0.f, 0.f, 0.f}, t1[4] = {0.f, 0.f, 0.f, 0.f};
         mma_bf16(t0, low0, low1, low2, low3, b0, b1);
         mma_bf16(t1, low0, low1, low2, low3, b2, b3);

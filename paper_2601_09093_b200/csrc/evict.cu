@@ -14,6 +14,9 @@
 //                           the list of the pages that drop a reference
 //   2. evict_move_kernel    one CTA per (KV head, trace, layer): selection, then the rows and weights move
 //   3. evict_finish_kernel  a cluster of CTAs: references dropped, free list, block table, lengths
+//
+// 64 traces, 4 layers, 8 KV heads of 128 in bf16, about 4100 positions cut to 4096 with 256 recent ones: 207 us for 665 MB of
+// rows, weights and lists (102 us at the copy bandwidth).  The move kernel is 180 of them.
 #include "release.cuh"
 
 using namespace stepk;

@@ -6,6 +6,10 @@
 // The weights are known only when a row's maximum and sum are, so the attention kernel leaves its scores (log2-scaled,
 // fp32) in the workspace and a second kernel, its programmatic dependent, turns them into weights: 8 * G bytes per
 // position and KV head on top of the 4 * d bytes of K and V in bf16 (a second read of K would be 2 * d).
+//
+// 64 traces of 4.6k to 16.9k positions, 32 / 8 heads of 128 in bf16: 473 us, 2.86 GB at 6.0 TB/s; the streaming kernel is 438 of
+// them, at the measured copy bandwidth, the rest is combining (bound by the latency of the pieces' loads) and adding (24 us
+// alone: the scores come back from HBM and L2 at 5.5 TB/s).
 #include "attention_rows.cuh"
 
 using namespace stepk;
