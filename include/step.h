@@ -145,7 +145,7 @@ int decode_attention_layers(step_pool* pool, int layer0, int n_layers, const voi
  * out their shares from seq_lens, start their first page copies through block_table, and wait for that kernel's
  * completion (and with it for everything earlier in the stream) only in front of their first read of q.
  * Requirement: the kernel directly before this call in the stream must not write seq_lens, block_table or this
- * layer's cache (do not issue it directly after append_kv or a prune), and it must itself be ordered after
+ * layer's cache (do not issue it directly after append_kv, append_kv_path, kv_pool_evict_positions or a prune), and it must itself be ordered after
  * everything before it, as any kernel launched the ordinary way is.  Shapes the tensor-core kernel does not cover
  * are launched the ordinary way. */
 int decode_attention_dependent(step_pool* pool, int layer, const void* q,

@@ -267,6 +267,43 @@ def test_a_bounded_cache_with_drafts(heads, dtype):
     assert int(tw.ora.seq_lens.max()) == budget
 
 
+def test_calls_take_a_stream_and_two_pools_may_run_side_by_side():
+    """The same steps on two pools: one after the other, and at the same time on two streams that the calls are given."""
+    results = []
+    for together in (False, True):
+        outs = []
+        twins = [twin(config((8, 2, 128), "bf16", layers=1, n=3, seed=50 + k), [600, 77, 130]) for k in range(2)]
+        inputs = []
+        for k, tw in enumerate(twins):
+            c = tw.cfg
+            q, _ = draw(c, W.TID_Q, (3, 4, 8, 128), 1)
+            kd, _ = draw(c, W.TID_K, (3, 4, 1, 2, 128), 2)
+            vd, _ = draw(c, W.TID_V, (3, 4, 1, 2, 128), 3)
+            parents = torch.tensor([[-1, 0, 1, 0]] * 3, dtype=torch.int32, device="cuda")
+            path = torch.tensor([[0, 1, 2]] * 3, dtype=torch.int32, device="cuda")
+            inputs.append((q, kd, vd, parents, path, torch.tensor([3, 0, 2], dtype=torch.int32, device="cuda"),
+                           torch.zeros((3, 2, 640), device="cuda"), torch.arange(3, dtype=torch.int32, device="cuda")))
+        torch.cuda.synchronize()
+        streams = [torch.cuda.Stream() for _ in twins] if together else [None, None]
+        for _ in range(3):
+            for tw, (q, kd, vd, parents, path, lens, sums, ids), s in zip(twins, inputs, streams):
+                v = tw.gpu.views()
+                tree = tw.gpu.decode_attention_tree(0, q, kd, vd, parents, v["block_table"], v["seq_lens"], stream=s)
+                tw.gpu.append_kv_path(ids, kd, vd, path, lens, stream=s)
+                with torch.cuda.stream(s):
+                    last = q[:, 0].contiguous()
+                out = tw.gpu.decode_attention_weights(0, last, v["block_table"], v["seq_lens"], sums, stream=s)
+                with torch.cuda.stream(s):
+                    w = sums[None].clone()
+                kept = tw.gpu.evict_positions(ids, w, 70, 9, stream=s)
+                outs += [tree, out, w, kept]
+        torch.cuda.synchronize()
+        results.append(outs)
+        assert all(tw.gpu.last_error() == (0, 0) for tw in twins)
+    for x, y in zip(*results):
+        assert torch.equal(x, y)
+
+
 # ---------------------------------------------------------------- refusals
 def test_refusals():
     cfg = config((8, 2, 128), "bf16", n=2, layers=1)
