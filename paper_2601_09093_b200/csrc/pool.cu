@@ -534,12 +534,19 @@ path_alloc_kernel(DevViews v, Geo g, const int32_t* __restrict__ ids, int n, con
   }
 }
 
-// Phase 2: CTAs walk over the (entry, new position) pairs that phase 1 admitted and move their rows, a range of layers each.
+// Phase 2: CTAs walk over the (entry, new position) pairs that phase 1 admitted, kPathBatch at most at a time: where their
+// rows come from and go to is worked out by a thread per pair, then every thread moves its chunk of four rows at once (one
+// pair after another left the loads' latency open: the call took 83 us for 16,000 rows of 2 layers, 262 MB; 59 us this
+// way, 4.4 TB/s).  A CTA moves a range of layers.
+constexpr int kPathBatch = 32, kPathAhead = 4;
+
 __global__ void __launch_bounds__(256)
 path_write_kernel(DevViews v, Geo g, uint4* __restrict__ kv, const uint4* __restrict__ kd, const uint4* __restrict__ vd,
                   const int32_t* __restrict__ ids, int n, const int32_t* __restrict__ path, int max_path, int T, int cpr,
                   int layers_per_cta) {
   extern __shared__ int s_rows[];                        // [n + 1] rows of the entries before each
+  __shared__ size_t s_src[kPathBatch], s_dst[kPathBatch];   // first chunk of the draft's row; of the slot's K row, KV head 0, layer 0
+  __shared__ int s_slot[kPathBatch];
   wait_for_primary();
   for (int i = threadIdx.x; i <= n; i += blockDim.x) s_rows[i] = v.prune_off[i];
   __syncthreads();
@@ -548,26 +555,47 @@ path_write_kernel(DevViews v, Geo g, uint4* __restrict__ kv, const uint4* __rest
   const int per_kv = g.Hkv * cpr;
   const size_t page_chunks = (size_t)g.P * cpr;
   const size_t layer_stride = (size_t)g.num_blocks * g.Hkv * 2 * page_chunks;
-  for (int e = blockIdx.x; e < total; e += gridDim.x) {
-    int lo = 0, hi = n - 1;                              // the last entry whose rows start at or before e
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (s_rows[mid] <= e) lo = mid; else hi = mid - 1;
+  const int batch = min(kPathBatch, max(1, (total + (int)gridDim.x - 1) / (int)gridDim.x));
+  for (long long e0 = (long long)blockIdx.x * batch; e0 < total; e0 += (long long)gridDim.x * batch) {
+    const int cnt = (int)min((long long)batch, total - e0);
+    if (threadIdx.x < cnt) {
+      const int e = (int)e0 + threadIdx.x;
+      int lo = 0, hi = n - 1;                            // the last entry whose rows start at or before e
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (s_rows[mid] <= e) lo = mid; else hi = mid - 1;
+      }
+      const int j = e - s_rows[lo];
+      const int pos = v.append_base[lo] + j, page = pos / g.P, slot = pos % g.P;
+      const int b = v.block_table[(size_t)ids[lo] * g.max_pages + page];
+      s_src[threadIdx.x] = ((size_t)lo * T + path[(size_t)lo * max_path + j]) * (size_t)g.L * per_kv;
+      s_dst[threadIdx.x] = (size_t)b * g.Hkv * 2 * page_chunks + (size_t)slot * cpr;
+      s_slot[threadIdx.x] = slot;
     }
-    const int j = e - s_rows[lo];
-    const int pos = v.append_base[lo] + j, page = pos / g.P, slot = pos % g.P;
-    const int b = v.block_table[(size_t)ids[lo] * g.max_pages + page];
-    const int node = path[(size_t)lo * max_path + j];
-    const size_t src_token = ((size_t)lo * T + node) * (size_t)g.L * per_kv;
+    __syncthreads();
     for (int i = threadIdx.x; i < 2 * per_kv; i += blockDim.x) {
       const int which = i >= per_kv;
       const int r = which ? i - per_kv : i;
       const int head = r / cpr, c = r - head * cpr;
-      const int cdst = g.swizzle ? ((c & ~7) | ((c ^ slot) & 7)) : c;
-      const uint4* src = (which ? vd : kd) + src_token + r;
-      const size_t dst0 = (((size_t)b * g.Hkv + head) * 2 + which) * page_chunks + (size_t)slot * cpr + cdst;
-      for (int l = l0; l < l1; ++l) kv[(size_t)l * layer_stride + dst0] = src[(size_t)l * per_kv];
+      const uint4* from = (which ? vd : kd) + r;
+      uint4* to = kv + ((size_t)head * 2 + which) * page_chunks;
+      const int moves = (l1 - l0) * cnt;                 // (layer, pair), pairs fastest
+      for (int m0 = 0; m0 < moves; m0 += kPathAhead) {
+        uint4 x[kPathAhead];
+#pragma unroll
+        for (int y = 0; y < kPathAhead; ++y) {
+          const int l = (m0 + y) / cnt, e = m0 + y - l * cnt;
+          if (m0 + y < moves) x[y] = from[s_src[e] + (size_t)(l0 + l) * per_kv];
+        }
+#pragma unroll
+        for (int y = 0; y < kPathAhead; ++y) {
+          const int l = (m0 + y) / cnt, e = m0 + y - l * cnt;
+          if (m0 + y < moves)
+            to[(size_t)(l0 + l) * layer_stride + s_dst[e] + (g.swizzle ? ((c & ~7) | ((c ^ s_slot[e]) & 7)) : c)] = x[y];
+        }
+      }
     }
+    __syncthreads();
   }
 }
 
