@@ -264,8 +264,27 @@ __global__ void __launch_bounds__(kRowsThreads) attn_rows_kernel(RowsArgs a) {
 #pragma unroll
           for (int z = 0; z < 4; ++z) acc[i][y][z] *= c;
         }
+        // (a drafted token that a row does not see is passed over: its v may hold an infinity or a NaN, and 0 times that is NaN)
+        unsigned long long see[kRpt];
+        if constexpr (kTree) {
+#pragma unroll
+          for (int y = 0; y < kRpt; ++y) see[y] = r0 + rg + y < nodes * G ? s_mask[(r0 + rg + y) / G] : 0ull;
+        }
 #pragma unroll 8
         for (int key = 0; key < kKeys; ++key) {
+          if (kTree && j0 + key >= S) {
+            const int u = j0 + key - S;
+            if (u >= nodes) break;
+            const float4 v = *reinterpret_cast<const float4*>(s_v + key * d + k);
+#pragma unroll
+            for (int y = 0; y < kRpt; ++y)
+              if ((see[y] >> u) & 1) {
+                const float p = s_p[key][rg + y];
+                acc[i][y][0] = fmaf(p, v.x, acc[i][y][0]); acc[i][y][1] = fmaf(p, v.y, acc[i][y][1]);
+                acc[i][y][2] = fmaf(p, v.z, acc[i][y][2]); acc[i][y][3] = fmaf(p, v.w, acc[i][y][3]);
+              }
+            continue;
+          }
           const float4 v = *reinterpret_cast<const float4*>(s_v + key * d + k);
           float p[kRpt];
 #pragma unroll

@@ -10,7 +10,9 @@
 //     the tensor cores read (rows of 128 bytes, 128-byte swizzle), K as a K-major operand of the first product, V as an
 //     MN-major operand of the second.  What lies behind the last whole page - the end of the cache, drafted tokens - is
 //     copied row by row (cp.async), with zeros up to a multiple of 16 keys, where the second product stops: what a page
-//     holds behind a trace's end never reaches it;
+//     holds behind a trace's end never reaches it.  A row's probability of a drafted token that it does not see is 0, and 0
+//     times an infinity or a NaN is NaN: the tile gets zeros for such elements of v (the fetching warp looks for them while
+//     it waits for a slot), and the rows that do see the token get them added at the end;
 //   * scores S (128 x 128, fp32) are made in tensor memory; 128 threads, a row each, read them, keep the running maximum
 //     and sum in fp32, and write the probabilities back as bf16 (one rounding, half a step of 2^-8 at most) over the
 //     same columns, from where they are the A operand of the second product, which adds to O (128 x 128, fp32) in tensor
@@ -56,6 +58,9 @@ constexpr int kThreads = 384;                      // three warpgroups
 constexpr int kRegsSoftmax = 208, kRegsOther = 88; // 2 x 128 x 208 + 128 x 88 = 384 x 168, what the launch has
 constexpr int kTmemCols = 512;                    // S of both lanes (P over them), then O of both
 constexpr float kRescale = 8.f;                   // log2 of how far a row's maximum may run ahead of its reference
+// Drafted tokens of a piece whose v holds an infinity or a NaN: the fetching warp of V is kVSlots pieces ahead of the softmax
+// warps at most, and these are done with a piece when the products of the one after the next begin.
+constexpr int kOddPieces = 8;
 constexpr unsigned long long kDrainNs = 100000000ull;
 
 struct TreeArgs {
@@ -282,6 +287,35 @@ __device__ inline uint32_t pack2(float lo, float hi) {
   return *reinterpret_cast<uint32_t*>(&v);
 }
 
+// Whether one of a pair of bf16 values is an infinity or a NaN.
+__device__ inline bool not_finite(uint32_t pair) { return ((pair & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+
+// What a softmax thread adds to its row at the end of piece pc, where the tile of V had zeros: the infinities and NaN of
+// the drafted tokens in `odd` that the row sees, columns [from, to).  Token pc.u0 + token0 + row / G; row `group_row` of slot
+// `slot` of this share if the piece is not a whole sequence.
+__device__ inline void add_odd(const TreeArgs& a, const Piece& pc, unsigned long long odd, int token0, int row, int group_row, int slot,
+                               int from, int to) {
+  const int u = pc.u0 + token0 + row / a.G;
+  if (row >= a.tokens * a.G || u >= pc.nodes) return;
+  __nv_bfloat16* out = a.out + (((size_t)pc.t * a.T + u) * a.Hq + (size_t)pc.h * a.G + row % a.G) * kD;
+  float* o_out = a.ws_o + (((size_t)blockIdx.x * 2 + slot) * a.group_rows + group_row) * kD;
+  const bool whole = pc.cnt == pc.tiles;
+#pragma unroll 1
+  for (int w = u; w >= 0;) {
+    const __nv_bfloat16* v = a.v_draft + ((((size_t)pc.t * a.T + w) * a.L + a.layer) * a.Hkv + pc.h) * kD;
+    if ((odd >> w) & 1)
+#pragma unroll 1
+      for (int c = from; c < to; ++c) {
+        const __nv_bfloat16 x = v[c];
+        if ((__bfloat16_as_ushort(x) & 0x7f80) != 0x7f80) continue;
+        if (whole) out[c] = __float2bfloat16(__bfloat162float(out[c]) + __bfloat162float(x));
+        else o_out[c] += __bfloat162float(x);
+      }
+    const int up = a.parents[(size_t)pc.t * a.T + w];
+    w = up < w ? up : -1;
+  }
+}
+
 template <bool kTwoRows>   // the lanes take 128 rows each of a 256-row group; else even and odd tiles of the same 128 rows
 __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap map_q, TreeArgs a) {
   extern __shared__ unsigned char smem_raw[];
@@ -295,7 +329,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   uint64_t* s_bar = reinterpret_cast<uint64_t*>(tail);
   unsigned long long* s_mask = reinterpret_cast<unsigned long long*>(s_bar + 32);   // [2][64] by piece parity
   Piece* s_piece = reinterpret_cast<Piece*>(s_mask + 128);             // [2]
-  int* s_up = reinterpret_cast<int*>(s_piece + 2);                     // [64]
+  unsigned long long* s_odd = reinterpret_cast<unsigned long long*>(s_piece + 2);   // [kOddPieces] (see kOddPieces)
+  int* s_up = reinterpret_cast<int*>(s_odd + kOddPieces);              // [64]
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_up + 64);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
   float* s_ml = reinterpret_cast<float*>(s_tmem + 4);                  // [2][128][2] (below 128 rows)
@@ -364,7 +399,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     const int ln = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t t_s = t_row + ln * 128, t_o = t_row + 256 + ln * 128;
-    uint32_t ph_s = 0, ph_piece = 0, ph_both = 0;
+    uint32_t ph_s = 0, ph_piece = 0, ph_both = 0, piece = 0;
     bool ok = true, first = true;
     for (;;) {
       if (!wait_warp(bar_q, ph_piece)) { ok = false; break; }
@@ -454,7 +489,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       // ---- the piece is done
       const bool whole = pc.cnt == pc.tiles;
       const size_t slot = (size_t)blockIdx.x * 2 + (first ? 0 : 1);
-      first = false;
       float2* ml_out = reinterpret_cast<float2*>(a.ws_ml) + slot * a.group_rows + (kTwoRows ? ln * 128 : 0) + row;
       float* o_out = a.ws_o + (slot * a.group_rows + (kTwoRows ? ln * 128 : 0) + row) * kD;
       __nv_bfloat16* out = a.out + (((size_t)pc.t * a.T + (mine ? u : 0)) * a.Hq + (size_t)pc.h * a.G + (mine ? row % a.G : 0)) * kD;
@@ -531,6 +565,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         }
         if (!ok) break;
       }
+      // (read again, not kept: the announcement stays until this warp has begun the next piece)
+      const unsigned long long odd = s_odd[piece++ % kOddPieces];
+      if (odd) add_odd(a, s_piece[ph_piece ^ 1], odd, kTwoRows ? ln * a.tokens : 0, row, (kTwoRows ? ln * 128 : 0) + row, first ? 0 : 1,
+                       kTwoRows || ln == 0 ? 0 : 64, kTwoRows || ln == 1 ? kD : 64);
+      first = false;
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
@@ -538,7 +577,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     // ------------------------------------------------ K or V tiles into their ring
     const int kv = warp == kWarpV, ring0 = kv ? kKSlots : 0, ring_n = kv ? kVSlots : kKSlots;
     int slot = 0;
-    uint32_t ph = 1;
+    uint32_t ph = 1, piece = 0;
+    unsigned long long odd = 0;                                        // (V) drafted tokens of the piece with an infinity or NaN so far
     bool ok = true;
     Place pl = {};
     int h = 0;
@@ -551,13 +591,34 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       const int page = first + lane;
       return of.t >= 0 && of.t < a.n && (long long)page * kP < of.x.S ? a.block_table[(size_t)of.t * a.max_pages + page] : 0;
     };
+    // those of drafted tokens [u0, u1) whose v holds an infinity or a NaN
+    auto look = [&](int u0, int u1) -> unsigned long long {
+      const __nv_bfloat16* v = a.v_draft + ((((size_t)pl.t * a.T) * a.L + a.layer) * a.Hkv + h) * kD + (lane & 15) * 8;
+      uint32_t lo = 0u, hi = 0u;
+      for (int u = u0 + (lane >> 4); u < u1; u += 16) {
+        uint4 x[8];
+#pragma unroll
+        for (int y = 0; y < 8; ++y)
+          x[y] = u + 2 * y < u1 ? *reinterpret_cast<const uint4*>(v + (size_t)(u + 2 * y) * a.L * a.Hkv * kD) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int y = 0; y < 8; ++y)
+          if (not_finite(x[y].x) || not_finite(x[y].y) || not_finite(x[y].z) || not_finite(x[y].w)) {
+            const uint32_t bit = 1u << ((u + 2 * y) & 31);
+            if (u + 2 * y < 32) lo |= bit; else hi |= bit;
+          }
+      }
+      return (unsigned long long)__reduce_or_sync(0xffffffffu, hi) << 32 | __reduce_or_sync(0xffffffffu, lo);
+    };
     // tile i of the piece into the next slot
     auto fetch = [&](int i) {
       if (!ok) return;
-      if (!wait_warp(bar_empty + 8 * (ring0 + slot), ph)) { ok = false; return; }
       const uint32_t bar = bar_full + 8 * (ring0 + slot), dst = sm_ring + (ring0 + slot) * kSlotBytes;
       const int j0 = (part.tile0 + i) * kTile;
       const int S = pl.x.S, nodes = pl.x.nodes;
+      if (i == 0) odd = 0;
+      if (kv && j0 + kTile > S) odd |= look(max(0, j0 - S), min(nodes, j0 + kTile - S));
+      if (!wait_warp(bar_empty + 8 * (ring0 + slot), ph)) { ok = false; return; }
+      if (kv && lane == 0 && (i == 0 || odd)) s_odd[piece % kOddPieces] = odd;   // (an arrival of lane 0 at `bar` follows)
       if (j0 / kP >= win + 32) { win += 32; ids0 = ids1; ids1 = load_ids(pl, win + 32); }
       const int in_win = j0 / kP - win;
       // block of page pg (0 .. 7) of this tile; one out of range is flagged and read as block 0
@@ -590,7 +651,25 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
           const __nv_bfloat16* src = j < S ? tail + (rr % kP) * kD : (real ? draft + (size_t)(j - S) * draft_row : a.kv);
           cp_async16_or_zero(dst + tile_chunk(rr, j < S ? c : (c & 8) | ((c ^ rr) & 7)), src, real);
         }
-        cp_async_arrive_when_done(bar);
+        if (kv && odd) {                                               // this thread's copies, without what is not finite
+          cp_async_wait_all();
+#pragma unroll 1
+          for (int rr = pages * kP + (lane >> 4); rr < rows; rr += 2) {
+            const int u = j0 + rr - S;
+            if (u < 0 || u >= nodes || !((odd >> u) & 1)) continue;
+            uint32_t* at = reinterpret_cast<uint32_t*>(sm + (dst - base) + tile_chunk(rr, (c & 8) | ((c ^ rr) & 7)));
+            for (int x = 0; x < 4; ++x) {
+              uint32_t e = at[x];
+              if ((e & 0x7f80u) == 0x7f80u) e &= 0xffff0000u;
+              if ((e & 0x7f800000u) == 0x7f800000u) e &= 0xffffu;
+              at[x] = e;
+            }
+          }
+          fence_async_smem();
+          mbar_arrive(bar);
+        } else {
+          cp_async_arrive_when_done(bar);
+        }
         if (lane == 0 && pages == 0) mbar_arrive(bar);                 // (the announcement of bytes is the other form of this arrival)
       }
       __syncwarp();
@@ -612,6 +691,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       next0 = load_ids(nx, 0);
       next1 = load_ids(nx, 32);
       for (int i = 0; i < part.cnt; ++i) fetch(i);
+      ++piece;
       pos += part.len;
       pl = nx;
     }
@@ -851,9 +931,9 @@ __global__ void __launch_bounds__(kMergeWarps * 32) tree_merge_kernel(TreeArgs a
 }
 
 size_t smem_bytes(bool two_rows) {
-  return 1024 + (two_rows ? 2 * kQBytes : kQBytes + kXBytes + 512 * 4) + kSlots * kSlotBytes + 32 * 8 + 128 * 8 + 2 * sizeof(Piece) + 64 * 4 + 16;
+  return 1024 + (two_rows ? 2 * kQBytes : kQBytes + kXBytes + 512 * 4) + kSlots * kSlotBytes + 32 * 8 + 128 * 8 + 2 * sizeof(Piece) + kOddPieces * 8 + 64 * 4 + 16;
 }
-static_assert(1024 + 2 * kQBytes + kSlots * kSlotBytes + 32 * 8 + 128 * 8 + 2 * sizeof(Piece) + 64 * 4 + 16 <= 232448, "shared memory of one CTA");
+static_assert(1024 + 2 * kQBytes + kSlots * kSlotBytes + 32 * 8 + 128 * 8 + 2 * sizeof(Piece) + kOddPieces * 8 + 64 * 4 + 16 <= 232448, "shared memory of one CTA");
 
 }  // namespace
 

@@ -174,6 +174,49 @@ def test_a_bad_parent_counts_as_none_and_is_flagged():
         assert tw.gpu.last_error() == (1, 1 << 1)
 
 
+@pytest.mark.parametrize("heads,dtype,T", [((8, 2, 128), "bf16", 13), ((8, 1, 128), "bf16", 64), ((16, 1, 128), "bf16", 20),
+                                           ((4, 1, 64), "fp32", 13), ((4, 2, 256), "bf16", 40)])
+def test_infinities_and_nan_reach_only_the_nodes_that_see_them(heads, dtype, T):
+    """Also the padded batch without n_nodes: what stands in nodes that nobody continues stays there."""
+    cfg = config(heads, dtype, layers=2, n=len(LENS))
+    tw = twin(cfg, LENS)
+    poison_unused(tw)
+    n, layer = len(LENS), 1
+    q, qx = draw(cfg, W.TID_Q, (n, T, cfg.num_q_heads, cfg.head_dim), 3)
+    shape = (n, T, cfg.num_layers, cfg.num_kv_heads, cfg.head_dim)
+    kd, kx = draw(cfg, W.TID_K, shape, 3)
+    vd, vx = draw(cfg, W.TID_V, shape, 3)
+    parents = random_parents(np.random.default_rng(3), n, T, "random")
+    odd = {1: (np.inf, 0), T // 2: (-np.inf, 5), T - 3: (np.nan, cfg.head_dim - 1)}          # node: value and dim of its v
+    for u, (x, c) in odd.items():
+        vd[:, u, :, :, c], vx[:, u, :, :, c] = x, x
+    for x, dev in ((kx, kd), (vx, vd), (qx, q)):                                             # a node of padding
+        x[:, T - 2], dev[:, T - 2] = np.nan, float("nan")
+    parents[:, T - 1][parents[:, T - 1] == T - 2] = -1
+    v = tw.gpu.views()
+    got = exact_f32(tw.gpu.decode_attention_tree(layer, q, kd, vd, torch.from_numpy(parents).cuda(), v["block_table"], v["seq_lens"]))
+    tame = np.where(np.isfinite(vx), vx, 0.0)
+    for t in range(n):
+        K, V = trace_kv(tw, layer, t)
+        with np.errstate(invalid="ignore"):
+            want, _ = OD.tree_attention(qx[t], K, V, kx[t, :, layer], vx[t, :, layer], parents[t], T)
+        assert np.array_equal(np.isnan(got[t]), np.isnan(want)), t
+        assert np.array_equal(got[t][np.isinf(want)], want[np.isinf(want)]), t
+        assert not np.isinf(got[t][np.isfinite(want)]).any()
+        # elsewhere the bound of finite values (the node of padding aside: it is NaN throughout)
+        live = np.arange(T) != T - 2
+        fin, mag = OD.tree_attention(np.nan_to_num(qx[t]), K, V, np.nan_to_num(kx[t, :, layer]), tame[t, :, layer], parents[t], T)
+        keys = np.concatenate([K, np.nan_to_num(kx[t, :, layer])])
+        rel = max(relative_bound(qx[t][live].reshape(-1, cfg.head_dim), keys[:, h]) for h in range(cfg.num_kv_heads))
+        half = BF16_HALF_STEP if dtype == "bf16" else 0.0
+        tol = (half + rel) * mag
+        tol = tol + half * (np.abs(fin) + tol) + 1e-30
+        ok = live[:, None, None] & np.isfinite(want)
+        assert np.all(np.abs(got[t] - fin)[ok] <= tol[ok]), t
+        assert np.isnan(got[t][~live]).all()
+    assert tw.gpu.last_error() == (0, 0)
+
+
 def test_a_bad_block_is_flagged():
     for heads, dtype in (((8, 2, 128), "bf16"), ((4, 1, 64), "fp32")):
         cfg = config(heads, dtype, n=2, layers=1)
