@@ -171,13 +171,20 @@ __global__ void __launch_bounds__(kRowsThreads) attn_rows_kernel(RowsArgs a) {
   if constexpr (kTree) sees = real ? s_mask[my_u] : 0ull;
   float m_run = -INFINITY, l_run = 0.f;
   // second product: thread x of the (row group, dims) tiles owns rows kRpt * (x % groups) .. and dims 4 * (x / groups) ..
-  constexpr int kGroups = kRows / kRpt;
+  constexpr int kGroups = kRows / kRpt;                 // (divides the threads: a thread's rows are the same in all of its tiles)
+  static_assert(kRowsThreads % kGroups == 0, "rows of a thread");
   const int tiles_o = kGroups * (d / 4);
   float acc[kNi][kRpt][4];
 #pragma unroll
   for (int i = 0; i < kNi; ++i)
 #pragma unroll
     for (int x = 0; x < kRpt; ++x) { acc[i][x][0] = acc[i][x][1] = acc[i][x][2] = acc[i][x][3] = 0.f; }
+  unsigned long long see[kRpt];                          // the drafted tokens that these rows see
+#pragma unroll
+  for (int y = 0; y < kRpt; ++y) {
+    const int r = r0 + tid % kGroups * kRpt + y;
+    see[y] = kTree && r < nodes * G ? s_mask[r / G] : 0ull;
+  }
   __syncthreads();
 
   for (int it = it0; it < it1; ++it) {
@@ -264,27 +271,25 @@ __global__ void __launch_bounds__(kRowsThreads) attn_rows_kernel(RowsArgs a) {
 #pragma unroll
           for (int z = 0; z < 4; ++z) acc[i][y][z] *= c;
         }
-        // (a drafted token that a row does not see is passed over: its v may hold an infinity or a NaN, and 0 times that is NaN)
-        unsigned long long see[kRpt];
-        if constexpr (kTree) {
-#pragma unroll
-          for (int y = 0; y < kRpt; ++y) see[y] = r0 + rg + y < nodes * G ? s_mask[(r0 + rg + y) / G] : 0ull;
-        }
-#pragma unroll 8
-        for (int key = 0; key < kKeys; ++key) {
-          if (kTree && j0 + key >= S) {
-            const int u = j0 + key - S;
-            if (u >= nodes) break;
+        if (kTree && j0 + kKeys > S) {
+          // a drafted token that a row does not see is passed over: its v may hold an infinity or a NaN, and 0 times that is NaN
+#pragma unroll 4
+          for (int key = 0; key < min(kKeys, n_keys - j0); ++key) {
             const float4 v = *reinterpret_cast<const float4*>(s_v + key * d + k);
+            const int u = j0 + key - S;
 #pragma unroll
-            for (int y = 0; y < kRpt; ++y)
-              if ((see[y] >> u) & 1) {
-                const float p = s_p[key][rg + y];
+            for (int y = 0; y < kRpt; ++y) {
+              const float p = s_p[key][rg + y];
+              if (u < 0 || ((see[y] >> (u & 63)) & 1)) {
                 acc[i][y][0] = fmaf(p, v.x, acc[i][y][0]); acc[i][y][1] = fmaf(p, v.y, acc[i][y][1]);
                 acc[i][y][2] = fmaf(p, v.z, acc[i][y][2]); acc[i][y][3] = fmaf(p, v.w, acc[i][y][3]);
               }
-            continue;
+            }
           }
+          continue;
+        }
+#pragma unroll 8
+        for (int key = 0; key < kKeys; ++key) {
           const float4 v = *reinterpret_cast<const float4*>(s_v + key * d + k);
           float p[kRpt];
 #pragma unroll

@@ -11,8 +11,8 @@
 //     MN-major operand of the second.  What lies behind the last whole page - the end of the cache, drafted tokens - is
 //     copied row by row (cp.async), with zeros up to a multiple of 16 keys, where the second product stops: what a page
 //     holds behind a trace's end never reaches it.  A row's probability of a drafted token that it does not see is 0, and 0
-//     times an infinity or a NaN is NaN: the tile gets zeros for such elements of v (the fetching warp looks for them while
-//     it waits for a slot), and the rows that do see the token get them added at the end;
+//     times an infinity or a NaN is NaN: the query warp looks at v of a piece's drafted tokens ahead of time, such elements
+//     become zeros in the tile, and the rows that do see the token get them added behind the piece's output;
 //   * scores S (128 x 128, fp32) are made in tensor memory; 128 threads, a row each, read them, keep the running maximum
 //     and sum in fp32, and write the probabilities back as bf16 (one rounding, half a step of 2^-8 at most) over the
 //     same columns, from where they are the A operand of the second product, which adds to O (128 x 128, fp32) in tensor
@@ -58,9 +58,6 @@ constexpr int kThreads = 384;                      // three warpgroups
 constexpr int kRegsSoftmax = 208, kRegsOther = 88; // 2 x 128 x 208 + 128 x 88 = 384 x 168, what the launch has
 constexpr int kTmemCols = 512;                    // S of both lanes (P over them), then O of both
 constexpr float kRescale = 8.f;                   // log2 of how far a row's maximum may run ahead of its reference
-// Drafted tokens of a piece whose v holds an infinity or a NaN: the fetching warp of V is kVSlots pieces ahead of the softmax
-// warps at most, and these are done with a piece when the products of the one after the next begin.
-constexpr int kOddPieces = 8;
 constexpr unsigned long long kDrainNs = 100000000ull;
 
 struct TreeArgs {
@@ -177,7 +174,10 @@ __device__ inline void next_sequence(const TreeArgs& a, Place& p) {
   if (++p.t < a.n) p.x = shape_of(a, p.t, false);
 }
 // A piece, as the query warps announce it: tiles [tile0, tile0 + cnt) of the sequence's `tiles`.
-struct Piece { int t, h, u0, tile0, cnt, tiles, S, nodes; };
+struct Piece {
+  int t, h, u0, tile0, cnt, tiles, S, nodes;
+  unsigned long long odd;         // its drafted tokens whose v holds an infinity or a NaN
+};
 
 // ---- instructions
 // One thread of a warp that is together (the same one every time).
@@ -287,37 +287,57 @@ __device__ inline uint32_t pack2(float lo, float hi) {
   return *reinterpret_cast<uint32_t*>(&v);
 }
 
-// Whether one of a pair of bf16 values is an infinity or a NaN.
+// Whether one of a pair of bf16 values is an infinity or a NaN; the pair with zeros for those.
 __device__ inline bool not_finite(uint32_t pair) { return ((pair & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
-
-// What a softmax thread adds to its row at the end of piece pc, where the tile of V had zeros: the infinities and NaN of
-// the drafted tokens in `odd` that the row sees, columns [from, to).  Token pc.u0 + token0 + row / G; row `group_row` of slot
-// `slot` of this share if the piece is not a whole sequence.
-__device__ inline void add_odd(const TreeArgs& a, const Piece& pc, unsigned long long odd, int token0, int row, int group_row, int slot,
-                               int from, int to) {
-  const int u = pc.u0 + token0 + row / a.G;
-  if (row >= a.tokens * a.G || u >= pc.nodes) return;
-  __nv_bfloat16* out = a.out + (((size_t)pc.t * a.T + u) * a.Hq + (size_t)pc.h * a.G + row % a.G) * kD;
-  float* o_out = a.ws_o + (((size_t)blockIdx.x * 2 + slot) * a.group_rows + group_row) * kD;
-  const bool whole = pc.cnt == pc.tiles;
-#pragma unroll 1
-  for (int w = u; w >= 0;) {
-    const __nv_bfloat16* v = a.v_draft + ((((size_t)pc.t * a.T + w) * a.L + a.layer) * a.Hkv + pc.h) * kD;
-    if ((odd >> w) & 1)
-#pragma unroll 1
-      for (int c = from; c < to; ++c) {
-        const __nv_bfloat16 x = v[c];
-        if ((__bfloat16_as_ushort(x) & 0x7f80) != 0x7f80) continue;
-        if (whole) out[c] = __float2bfloat16(__bfloat162float(out[c]) + __bfloat162float(x));
-        else o_out[c] += __bfloat162float(x);
+__device__ inline uint32_t only_finite(uint32_t pair) {
+  return pair & ((pair & 0x7f80u) == 0x7f80u ? 0xffff0000u : ~0u) & ((pair & 0x7f800000u) == 0x7f800000u ? 0xffffu : ~0u);
+}
+// One warp: those of drafted tokens [u0, u1) of trace t whose v holds an infinity or a NaN.
+__device__ inline unsigned long long odd_tokens(const TreeArgs& a, int t, int h, int u0, int u1, int lane) {
+  const __nv_bfloat16* v = a.v_draft + (((size_t)t * a.T * a.L + a.layer) * a.Hkv + h) * kD + (lane & 15) * 8;
+  uint32_t lo = 0u, hi = 0u;
+  for (int u = u0 + (lane >> 4); u < u1; u += 16) {
+    uint4 x[8];
+#pragma unroll
+    for (int y = 0; y < 8; ++y)
+      x[y] = u + 2 * y < u1 ? *reinterpret_cast<const uint4*>(v + (size_t)(u + 2 * y) * a.L * a.Hkv * kD) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int y = 0; y < 8; ++y)
+      if (not_finite(x[y].x) || not_finite(x[y].y) || not_finite(x[y].z) || not_finite(x[y].w)) {
+        const uint32_t bit = 1u << ((u + 2 * y) & 31);
+        if (u + 2 * y < 32) lo |= bit; else hi |= bit;
       }
-    const int up = a.parents[(size_t)pc.t * a.T + w];
-    w = up < w ? up : -1;
+  }
+  return (unsigned long long)__reduce_or_sync(0xffffffffu, hi) << 32 | __reduce_or_sync(0xffffffffu, lo);
+}
+// One warp, when the rows of piece pc have been written (slot: of this share, if the piece is not a whole sequence): what is
+// not finite in v of its odd tokens is added to the rows that see them.
+__device__ inline void add_odd(const TreeArgs& a, const Piece& pc, int slot, int lane) {
+#pragma unroll 1
+  for (int r = 0; r < a.group_rows; ++r) {
+    const int row = r % kHalfRows, u = pc.u0 + r / kHalfRows * a.tokens + row / a.G;
+    if (row >= a.tokens * a.G || u >= pc.nodes) continue;
+    __nv_bfloat16* out = a.out + (((size_t)pc.t * a.T + u) * a.Hq + (size_t)pc.h * a.G + row % a.G) * kD;
+    float* o_out = a.ws_o + (((size_t)blockIdx.x * 2 + slot) * a.group_rows + r) * kD;
+#pragma unroll 1
+    for (int w = u; w >= 0;) {
+      const __nv_bfloat16* v = a.v_draft + ((((size_t)pc.t * a.T + w) * a.L + a.layer) * a.Hkv + pc.h) * kD;
+      if ((pc.odd >> w) & 1)
+#pragma unroll 1
+        for (int c = lane; c < kD; c += 32) {
+          const float x = __bfloat162float(v[c]);
+          if ((__float_as_uint(x) & 0x7f800000u) != 0x7f800000u) continue;
+          if (pc.cnt == pc.tiles) out[c] = __float2bfloat16(__bfloat162float(out[c]) + x);
+          else o_out[c] += x;
+        }
+      const int up = a.parents[(size_t)pc.t * a.T + w];
+      w = up < w ? up : -1;
+    }
   }
 }
 
 template <bool kTwoRows>   // the lanes take 128 rows each of a 256-row group; else even and odd tiles of the same 128 rows
-__global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap map_q, TreeArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ TreeArgs a) {
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -329,8 +349,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   uint64_t* s_bar = reinterpret_cast<uint64_t*>(tail);
   unsigned long long* s_mask = reinterpret_cast<unsigned long long*>(s_bar + 32);   // [2][64] by piece parity
   Piece* s_piece = reinterpret_cast<Piece*>(s_mask + 128);             // [2]
-  unsigned long long* s_odd = reinterpret_cast<unsigned long long*>(s_piece + 2);   // [kOddPieces] (see kOddPieces)
-  int* s_up = reinterpret_cast<int*>(s_odd + kOddPieces);              // [64]
+  int* s_up = reinterpret_cast<int*>(s_piece + 2);                     // [64]
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_up + 64);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
   float* s_ml = reinterpret_cast<float*>(s_tmem + 4);                  // [2][128][2] (below 128 rows)
@@ -393,13 +412,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   // one arrival for all of the warp's threads
   auto arrive_warp = [&](uint32_t bar) { __syncwarp(); if (lane == 0) mbar_arrive(bar); };
 
+  int last_piece = -1, last_slot = 0;                                  // (query warp) whose rows are written when all is done
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
     // ------------------------------------------------ softmax: lane `ln` of the CTA, row `row` of its 128
     const int ln = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t t_s = t_row + ln * 128, t_o = t_row + 256 + ln * 128;
-    uint32_t ph_s = 0, ph_piece = 0, ph_both = 0, piece = 0;
+    uint32_t ph_s = 0, ph_piece = 0, ph_both = 0;
     bool ok = true, first = true;
     for (;;) {
       if (!wait_warp(bar_q, ph_piece)) { ok = false; break; }
@@ -489,6 +509,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       // ---- the piece is done
       const bool whole = pc.cnt == pc.tiles;
       const size_t slot = (size_t)blockIdx.x * 2 + (first ? 0 : 1);
+      first = false;
       float2* ml_out = reinterpret_cast<float2*>(a.ws_ml) + slot * a.group_rows + (kTwoRows ? ln * 128 : 0) + row;
       float* o_out = a.ws_o + (slot * a.group_rows + (kTwoRows ? ln * 128 : 0) + row) * kD;
       __nv_bfloat16* out = a.out + (((size_t)pc.t * a.T + (mine ? u : 0)) * a.Hq + (size_t)pc.h * a.G + (mine ? row % a.G : 0)) * kD;
@@ -565,11 +586,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         }
         if (!ok) break;
       }
-      // (read again, not kept: the announcement stays until this warp has begun the next piece)
-      const unsigned long long odd = s_odd[piece++ % kOddPieces];
-      if (odd) add_odd(a, s_piece[ph_piece ^ 1], odd, kTwoRows ? ln * a.tokens : 0, row, (kTwoRows ? ln * 128 : 0) + row, first ? 0 : 1,
-                       kTwoRows || ln == 0 ? 0 : 64, kTwoRows || ln == 1 ? kD : 64);
-      first = false;
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
@@ -577,8 +593,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     // ------------------------------------------------ K or V tiles into their ring
     const int kv = warp == kWarpV, ring0 = kv ? kKSlots : 0, ring_n = kv ? kVSlots : kKSlots;
     int slot = 0;
-    uint32_t ph = 1, piece = 0;
-    unsigned long long odd = 0;                                        // (V) drafted tokens of the piece with an infinity or NaN so far
+    uint32_t ph = 1;
     bool ok = true;
     Place pl = {};
     int h = 0;
@@ -591,34 +606,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       const int page = first + lane;
       return of.t >= 0 && of.t < a.n && (long long)page * kP < of.x.S ? a.block_table[(size_t)of.t * a.max_pages + page] : 0;
     };
-    // those of drafted tokens [u0, u1) whose v holds an infinity or a NaN
-    auto look = [&](int u0, int u1) -> unsigned long long {
-      const __nv_bfloat16* v = a.v_draft + ((((size_t)pl.t * a.T) * a.L + a.layer) * a.Hkv + h) * kD + (lane & 15) * 8;
-      uint32_t lo = 0u, hi = 0u;
-      for (int u = u0 + (lane >> 4); u < u1; u += 16) {
-        uint4 x[8];
-#pragma unroll
-        for (int y = 0; y < 8; ++y)
-          x[y] = u + 2 * y < u1 ? *reinterpret_cast<const uint4*>(v + (size_t)(u + 2 * y) * a.L * a.Hkv * kD) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int y = 0; y < 8; ++y)
-          if (not_finite(x[y].x) || not_finite(x[y].y) || not_finite(x[y].z) || not_finite(x[y].w)) {
-            const uint32_t bit = 1u << ((u + 2 * y) & 31);
-            if (u + 2 * y < 32) lo |= bit; else hi |= bit;
-          }
-      }
-      return (unsigned long long)__reduce_or_sync(0xffffffffu, hi) << 32 | __reduce_or_sync(0xffffffffu, lo);
-    };
     // tile i of the piece into the next slot
     auto fetch = [&](int i) {
       if (!ok) return;
+      if (!wait_warp(bar_empty + 8 * (ring0 + slot), ph)) { ok = false; return; }
       const uint32_t bar = bar_full + 8 * (ring0 + slot), dst = sm_ring + (ring0 + slot) * kSlotBytes;
       const int j0 = (part.tile0 + i) * kTile;
       const int S = pl.x.S, nodes = pl.x.nodes;
-      if (i == 0) odd = 0;
-      if (kv && j0 + kTile > S) odd |= look(max(0, j0 - S), min(nodes, j0 + kTile - S));
-      if (!wait_warp(bar_empty + 8 * (ring0 + slot), ph)) { ok = false; return; }
-      if (kv && lane == 0 && (i == 0 || odd)) s_odd[piece % kOddPieces] = odd;   // (an arrival of lane 0 at `bar` follows)
       if (j0 / kP >= win + 32) { win += 32; ids0 = ids1; ids1 = load_ids(pl, win + 32); }
       const int in_win = j0 / kP - win;
       // block of page pg (0 .. 7) of this tile; one out of range is flagged and read as block 0
@@ -651,25 +645,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
           const __nv_bfloat16* src = j < S ? tail + (rr % kP) * kD : (real ? draft + (size_t)(j - S) * draft_row : a.kv);
           cp_async16_or_zero(dst + tile_chunk(rr, j < S ? c : (c & 8) | ((c ^ rr) & 7)), src, real);
         }
-        if (kv && odd) {                                               // this thread's copies, without what is not finite
-          cp_async_wait_all();
-#pragma unroll 1
-          for (int rr = pages * kP + (lane >> 4); rr < rows; rr += 2) {
-            const int u = j0 + rr - S;
-            if (u < 0 || u >= nodes || !((odd >> u) & 1)) continue;
-            uint32_t* at = reinterpret_cast<uint32_t*>(sm + (dst - base) + tile_chunk(rr, (c & 8) | ((c ^ rr) & 7)));
-            for (int x = 0; x < 4; ++x) {
-              uint32_t e = at[x];
-              if ((e & 0x7f80u) == 0x7f80u) e &= 0xffff0000u;
-              if ((e & 0x7f800000u) == 0x7f800000u) e &= 0xffffu;
-              at[x] = e;
-            }
-          }
-          fence_async_smem();
-          mbar_arrive(bar);
-        } else {
-          cp_async_arrive_when_done(bar);
-        }
+        cp_async_arrive_when_done(bar);
         if (lane == 0 && pages == 0) mbar_arrive(bar);                 // (the announcement of bytes is the other form of this arrival)
       }
       __syncwarp();
@@ -691,7 +667,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       next0 = load_ids(nx, 0);
       next1 = load_ids(nx, 32);
       for (int i = 0; i < part.cnt; ++i) fetch(i);
-      ++piece;
       pos += part.len;
       pl = nx;
     }
@@ -704,6 +679,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   } else if (warp == kWarpQ) {
     // ------------------------------------------------ query rows and ancestor masks of one piece after another
     uint32_t par = 0;
+    int made = 0;                                                      // pieces announced
     long long pos, end;
     Place pl = my_share(false, pos, end);
     for (;; par ^= 1) {
@@ -713,8 +689,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       if (part.cnt > 0) {
         pc.t = pl.t; pc.h = pl.hr / pl.x.groups; pc.u0 = (pl.hr - pc.h * pl.x.groups) * a.tokens * a.lanes;
         pc.tile0 = part.tile0; pc.cnt = part.cnt; pc.tiles = pl.x.tiles; pc.S = pl.x.S; pc.nodes = pl.x.nodes;
-        for (int u = lane; u < pc.nodes; u += 32) {                    // (the other piece's masks are the ones in use)
-          int p = a.parents[(size_t)pc.t * a.T + u];
+        int up[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) up[x] = lane + 32 * x < pc.nodes ? a.parents[(size_t)pc.t * a.T + lane + 32 * x] : -1;
+        pc.odd = odd_tokens(a, pc.t, pc.h, max(0, pc.tile0 * kTile - pc.S), min(pc.nodes, (pc.tile0 + pc.cnt) * kTile - pc.S), lane);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {                                  // (the other piece's masks are the ones in use)
+          const int u = lane + 32 * x;
+          int p = up[x];
+          if (u >= pc.nodes) break;
           if (p >= u || p < -1) { flag_error(a.counters, STEP_ERR_INVALID_ARG); p = -1; }
           s_up[u] = p;
         }
@@ -730,6 +713,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       }
       // the scores of the piece before are made, and its announcement has been read (the very first wait passes at once)
       if (!wait_warp(bar_qfree, par ^ 1)) break;
+      // all softmax warps have begun that piece, so the one before it is written
+      if (made >= 2 && s_piece[par].odd) add_odd(a, s_piece[par], made == 2 ? 0 : 1, lane);
+      __syncwarp();
+      if (pc.cnt > 0) ++made;
       if (lane == 0) {
         s_piece[par] = pc;
         if (pc.cnt > 0) {
@@ -745,6 +732,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       __syncwarp();
       if (pc.cnt == 0) break;
     }
+    last_piece = made > 0 ? (int)(par ^ 1) : -1;
+    last_slot = made > 1;
     if (*s_abort && lane == 0) { mbar_wait_bounded(bar_q, 0, kDrainNs); mbar_wait_bounded(bar_q, 1, kDrainNs); }
     // out rows behind a trace's last drafted token
     for (int t = blockIdx.x; t < a.n; t += gridDim.x) {
@@ -795,7 +784,20 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     while (ok) {
       ok = wait_warp(bar_q, ph_q);
       const int cnt = s_piece[ph_q].cnt, S = s_piece[ph_q].S - s_piece[ph_q].tile0 * kTile, keys = S + s_piece[ph_q].nodes;
+      const unsigned long long odd = s_piece[ph_q].odd;
       auto copied = [&](int i) { return (i + 1) * kTile > S; };
+      // zeros for what is not finite in v of drafted tokens (tile i of the piece, in slot s)
+      auto tame = [&](int i, int s) {
+        if (odd == 0 || !copied(i)) return;
+        for (int rr = lane >> 4; rr < kTile; rr += 2) {
+          const int u = i * kTile + rr - S, c = lane & 15;
+          if (u < 0 || u >= keys - S || !((odd >> u) & 1)) continue;
+          uint4* x = reinterpret_cast<uint4*>(sm + (sm_ring - base) + s * kSlotBytes + tile_chunk(rr, c));
+          *x = make_uint4(only_finite(x->x), only_finite(x->y), only_finite(x->z), only_finite(x->w));
+        }
+        fence_async_smem();
+        __syncwarp();
+      };
       auto steps = [&](int i) { return min(8, (keys - i * kTile + 15) / 16); };
       ph_q ^= 1;
       if (!ok || cnt == 0) break;
@@ -810,6 +812,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         }
         for (int i = 0; i < cnt && ok; ++i) {
           const int v = next(1, copied(i));
+          if (ok) tame(i, v);
           const bool more = i + 1 < cnt;
           if (more) k = next(0, copied(i + 1));
           probabilities(0, true);
@@ -846,6 +849,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         }
         for (int i = 0; i < cnt && ok; ++i) {
           const int v = next(1, copied(i));
+          if (ok) tame(i, v);
           probabilities(i & 1, false);
           if (ok && elect_one()) {
             values(i & 1, v, i < 2, 0, steps(i));
@@ -877,6 +881,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   __syncwarp();
   tc_fence_before();
   __syncthreads();
+  if (warp == kWarpQ && last_piece >= 0 && !*s_abort && s_piece[last_piece].odd) add_odd(a, s_piece[last_piece], last_slot, lane);
   if (warp == kWarpMma) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
@@ -931,9 +936,9 @@ __global__ void __launch_bounds__(kMergeWarps * 32) tree_merge_kernel(TreeArgs a
 }
 
 size_t smem_bytes(bool two_rows) {
-  return 1024 + (two_rows ? 2 * kQBytes : kQBytes + kXBytes + 512 * 4) + kSlots * kSlotBytes + 32 * 8 + 128 * 8 + 2 * sizeof(Piece) + kOddPieces * 8 + 64 * 4 + 16;
+  return 1024 + (two_rows ? 2 * kQBytes : kQBytes + kXBytes + 512 * 4) + kSlots * kSlotBytes + 32 * 8 + 128 * 8 + 2 * sizeof(Piece) + 64 * 4 + 16;
 }
-static_assert(1024 + 2 * kQBytes + kSlots * kSlotBytes + 32 * 8 + 128 * 8 + 2 * sizeof(Piece) + kOddPieces * 8 + 64 * 4 + 16 <= 232448, "shared memory of one CTA");
+static_assert(1024 + 2 * kQBytes + kSlots * kSlotBytes + 32 * 8 + 128 * 8 + 2 * sizeof(Piece) + 64 * 4 + 16 <= 232448, "shared memory of one CTA");
 
 }  // namespace
 
