@@ -145,9 +145,9 @@ int decode_attention_layers(step_pool* pool, int layer0, int n_layers, const voi
  * out their shares from seq_lens, start their first page copies through block_table, and wait for that kernel's
  * completion (and with it for everything earlier in the stream) only in front of their first read of q.
  * Requirement: the kernel directly before this call in the stream must not write seq_lens, block_table or this
- * layer's cache (do not issue it directly after append_kv, append_kv_path, kv_pool_evict_positions or a prune), and it must itself be ordered after
- * everything before it, as any kernel launched the ordinary way is.  Shapes the tensor-core kernel does not cover
- * are launched the ordinary way. */
+ * layer's cache (do not issue it directly after append_kv, append_kv_path, kv_pool_evict_positions or a prune), and it
+ * must itself be ordered after everything before it, as any kernel launched the ordinary way is.  Shapes the
+ * tensor-core kernel does not cover are launched the ordinary way. */
 int decode_attention_dependent(step_pool* pool, int layer, const void* q,
                                const int32_t* block_table, const int32_t* seq_lens, int n,
                                void* out, void* stream);
@@ -198,7 +198,7 @@ int decode_attention_static(step_pool* pool, int layer, const void* q,
  * continuations of a trace and verify them in one pass, and for those that bound a trace's cache instead of, or before,
  * giving the trace up).  All of them want the pool's device to be current (else STEP_ERR_INVALID_ARG), take their
  * scratch from the caller (`workspace`: device, 256-byte aligned, in use from the call until its work on the stream is
- * done; two calls that may overlap in time need two of them), and can be captured into a CUDA graph. */
+ * done; calls of different pools that may overlap in time need one each), and can be captured into a CUDA graph. */
 
 /* Attention of one layer for a tree of drafted tokens per trace:
  *   out[i][u][h] = sum_j softmax_j(q[i][u][h] . k[j] / sqrt(d)) v[j],  j over the seq_lens[i] cached positions of row i (as
@@ -211,6 +211,7 @@ int decode_attention_static(step_pool* pool, int layer, const void* q,
  * their q, k_draft, v_draft and parents are not read.  A count outside [0, T] is clamped and flagged likewise.
  * out: [n, T, num_q_heads, head_dim] in POOL DTYPE (what the output projection behind it reads), rounded once, 32-byte
  * aligned; it must not overlap the inputs.  1 <= T <= 64, n <= 65535.
+ * What a row does not see has no part in its result, whatever it holds (infinities and NaN included).
  * decode_attention_tree_workspace_bytes (host-only) says how large the workspace has to be; NULL is fine for 0. */
 int decode_attention_tree_workspace_bytes(const step_pool* pool, int n, int T, size_t* bytes);
 int decode_attention_tree(step_pool* pool, int layer, const void* q, const void* k_draft, const void* v_draft,

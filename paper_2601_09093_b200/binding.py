@@ -300,6 +300,8 @@ class KVPool:
         says how much workspace it takes; without a `workspace` (uint8 tensor) one comes from torch's allocator on the
         call's stream."""
         dev = self._device()
+        if stream is not None and stream.device != dev:
+            raise StepError(name, 1)
         if stream is not None or torch.cuda.current_device() != dev.index:
             with torch.cuda.device(dev), torch.cuda.stream(stream):
                 return self._call(name, args, size, workspace)

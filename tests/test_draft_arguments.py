@@ -1,7 +1,10 @@
 """Argument checks of the draft and bounded-cache calls that need no GPU."""
 import ctypes as C
 
+import types
+
 import pytest
+import torch
 
 from paper_2601_09093_b200 import binding as B
 
@@ -20,3 +23,11 @@ def test_no_pool_is_refused(lib):
     assert lib.append_kv_path(None, None, 1, 1, None, None, None, None, 1, None) == 1
     assert lib.decode_attention_weights(None, 0, None, None, None, 1, None, None, 1, None, 0, None) == 1
     assert lib.kv_pool_evict_positions(None, None, 1, None, None, 1, 1, 0, None, None, 0, None) == 1
+
+
+def test_a_stream_of_another_device_is_refused():
+    """Work on it would not be ordered by it: the call's kernels run on the pool's device."""
+    pool = types.SimpleNamespace(_device=lambda: torch.device("cuda", 0))
+    with pytest.raises(B.StepError) as e:
+        B.KVPool._call(pool, "append_kv_path", (), stream=types.SimpleNamespace(device=torch.device("cuda", 1)))
+    assert e.value.code == 1
