@@ -235,6 +235,7 @@ int append_kv_path(step_pool* pool, const int32_t* trace_ids, int n, int T, cons
  * head_dim] fp32, here accurate to fp32 (the probabilities are not rounded to bf16 on their way into the second product,
  * so the results differ from decode_attention's in the last bits that call has).  weight_sum: [n, num_kv_heads,
  * weight_stride] fp32; positions from weight_stride on are not counted and set the STEP_ERR_CAPACITY bit.
+ * (A probability enters as a sum of terms, some of them 0 or negative: an infinity in a cached v may come out as a NaN.)
  * q and out 16-byte aligned; n <= 65535; no two of q, out, weight_sum and workspace may overlap. */
 int decode_attention_weights_workspace_bytes(const step_pool* pool, int n, int weight_stride, size_t* bytes);
 int decode_attention_weights(step_pool* pool, int layer, const void* q, const int32_t* block_table,
