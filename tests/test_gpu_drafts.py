@@ -176,12 +176,15 @@ def test_a_bad_parent_counts_as_none_and_is_flagged():
 
 @pytest.mark.parametrize("heads,dtype,T", [((8, 2, 128), "bf16", 13), ((8, 1, 128), "bf16", 64), ((16, 1, 128), "bf16", 20),
                                            ((4, 1, 64), "fp32", 13), ((4, 2, 256), "bf16", 40)])
-def test_infinities_and_nan_reach_only_the_nodes_that_see_them(heads, dtype, T):
-    """Also the padded batch without n_nodes: what stands in nodes that nobody continues stays there."""
-    cfg = config(heads, dtype, layers=2, n=len(LENS))
-    tw = twin(cfg, LENS)
+@pytest.mark.parametrize("many", [False, True])
+def test_infinities_and_nan_reach_only_the_nodes_that_see_them(heads, dtype, T, many):
+    """Also the padded batch without n_nodes: what stands in nodes that nobody continues stays there.  `many`: several short
+    sequences for every CTA, where a few longer ones are cut in pieces."""
+    lens = np.random.default_rng(8).integers(0, 40, 2600 // T) if many else LENS
+    cfg = config(heads, dtype, layers=2, n=len(lens))
+    tw = twin(cfg, lens)
     poison_unused(tw)
-    n, layer = len(LENS), 1
+    n, layer = len(lens), 1
     q, qx = draw(cfg, W.TID_Q, (n, T, cfg.num_q_heads, cfg.head_dim), 3)
     shape = (n, T, cfg.num_layers, cfg.num_kv_heads, cfg.head_dim)
     kd, kx = draw(cfg, W.TID_K, shape, 3)
