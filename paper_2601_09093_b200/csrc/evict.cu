@@ -177,11 +177,13 @@ constexpr int kMostCachedKeys = 12288;        // 48 KiB of keys: three CTAs per 
 constexpr int kBatch = 8;                     // rows a warp has in flight
 constexpr int kPageCache = 1024;              // block ids kept in shared memory
 
-// Larger weight -> larger key; NaN below everything; the two zeros are equal.
-__device__ inline uint32_t weight_key(float w) {
-  if (isnan(w)) return 0u;
-  const uint32_t u = __float_as_uint(w == 0.f ? 0.f : w);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+// Bits of a weight -> key.  Larger weight -> larger key; NaN below everything; the two zeros are equal.  The kernel reads and
+// writes weights as integers throughout: this library's arithmetic and comparisons take subnormal numbers for zeros, and
+// the compiler turns a test of a float's bits against zero back into such a comparison.
+__device__ inline uint32_t weight_key(uint32_t u) {
+  const uint32_t magnitude = u & 0x7fffffffu;
+  if (magnitude > 0x7f800000u) return 0u;
+  return magnitude == 0u ? 0x80000000u : ((u & 0x80000000u) ? ~u : (u | 0x80000000u));
 }
 
 // What bounds it: for a cut of a few positions the passes over the weights (each a read of shared memory, or of L2 for
@@ -199,8 +201,8 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(EvictArgs a
   const int h = blockIdx.x, i = blockIdx.y, l = blockIdx.z;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const size_t head = ((size_t)l * a.n + i) * g.Hkv + h;
-  const float* w = a.weights + head * a.stride;
-  float* w_out = a.weights_out + head * a.stride;
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(a.weights) + head * a.stride;
+  uint32_t* w_out = reinterpret_cast<uint32_t*>(a.weights_out) + head * a.stride;
   int32_t* kept = a.kept + head * a.budget;
   dependents_may_launch();
   wait_for_primary();
@@ -223,7 +225,7 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(EvictArgs a
   if (in_smem || copy_weights) {
 #pragma unroll 8
     for (int j = tid; j < first; j += kMoveThreads) {
-      const float x = w[j];
+      const uint32_t x = w[j];
       if (in_smem) s_key[j] = weight_key(x);
       if (copy_weights && j < m) w_out[j] = x;
     }
@@ -415,7 +417,7 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(EvictArgs a
   // earlier one, never of a later one)
   for (int r0 = 0; r0 < a.recent; r0 += kMoveThreads) {
     const int r = r0 + tid;
-    const float x = r < a.recent ? w[first + r] : 0.f;
+    const uint32_t x = r < a.recent ? w[first + r] : 0u;
     __syncthreads();
     if (r < a.recent) w_out[m + r] = x;
     __syncthreads();
@@ -424,7 +426,7 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(EvictArgs a
     const int r1 = r0 + warp * kBatch, r = r1 + lane % kBatch;
     copy_rows(r < a.recent ? (lane < kBatch ? first : m) + r : 0, max(0, min(kBatch, a.recent - r1)), true);
   }
-  for (int j = a.budget + tid; j < a.stride; j += kMoveThreads) w_out[j] = 0.f;
+  for (int j = a.budget + tid; j < a.stride; j += kMoveThreads) w_out[j] = 0u;
 }
 
 // ---------------------------------------------------------------- bookkeeping

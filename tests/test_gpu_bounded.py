@@ -332,3 +332,32 @@ def test_refusals():
     L = B.lib()
     assert L.decode_attention_weights(p.handle, 0, None, None, None, 2, None, None, 5, None, 0, None) == 1
     assert L.kv_pool_evict_positions(p.handle, None, 2, None, None, 50, 45, 4, None, None, 0, None) == 1
+
+
+# ---------------------------------------------------------------- values below the smallest normal number
+def tiny_weights(rng, shape):
+    """Zeros of both signs, subnormals of both signs and the smallest normal numbers, each about as often."""
+    bits = rng.integers(1, 0x00800000, size=shape, dtype=np.uint32)              # subnormals
+    pick = rng.integers(0, 5, size=shape)
+    bits[pick == 0] = 0
+    bits[pick == 1] = rng.integers(1, 5, size=int((pick == 1).sum()))            # the smallest ones, with ties
+    bits[pick == 2] |= 0x00800000                                                # 2^-126 and just above
+    sign = rng.random(shape) < 0.3
+    return (bits | (sign.astype(np.uint32) << 31)).view(np.float32)
+
+
+@pytest.mark.parametrize("heads,dtype,page,layers", POOLS[:2])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_evict_tells_subnormal_weights_apart(heads, dtype, page, layers, in_place):
+    """Only the two zeros are equal: a caller whose sums decay ends up with weights this small."""
+    cfg = config(heads, dtype, page=page, layers=layers, n=3)
+    tw = twin(cfg, [333, 200, 97])
+    w = tiny_weights(np.random.default_rng(9), (layers, 3, heads[1], 340))
+    assert run_evict(tw, [0, 1, 2], w, 96, 20, in_place) == 0
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_evict_tells_subnormal_weights_of_a_long_cache_apart(in_place):
+    cfg = config((2, 1, 128), "bf16", layers=1, n=1)
+    tw = twin(cfg, [14000])
+    run_evict(tw, [0], tiny_weights(np.random.default_rng(10), (1, 1, 1, 14000)), 5000, 100, in_place)

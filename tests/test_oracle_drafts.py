@@ -73,3 +73,13 @@ def test_append_path_is_append_of_the_named_rows():
     assert list(a.seq_lens) == [3, 2] and a.status == 0
     OD.append_path(a, [1, 1, 0], 5, np.array([[0], [0], [7]]), [1, 1, 1], np.concatenate([kd, kd[:1]]), np.concatenate([vd, vd[:1]]))
     assert a.status == (1 << 3) | (1 << 1) and list(a.seq_lens) == [3, 3]
+
+
+def test_slots_of_subnormal_weights_and_of_nan_by_hand():
+    w = np.array([1e-40, 2e-40, 5e-39, 0.0, -0.0, -1e-45, 1e-45], dtype=np.float32)
+    assert OB.slots(w, 7, 1, 0) == [2]
+    assert OB.slots(w, 7, 4, 0) == [0, 1, 2, 6]
+    assert OB.slots(w, 7, 6, 0) == [0, 1, 2, 3, 4, 6]
+    # 0, 1, 3 and 4 stay where they are, and the free slot takes 5
+    nan = np.array([np.nan, -1.0, np.nan, -np.inf, 0.0, -0.0])
+    assert OB.slots(nan, 6, 5, 0) == [0, 1, 5, 3, 4]
