@@ -18,6 +18,14 @@ namespace {
 
 constexpr int kAccThreads = 256, kAccKeys = 4 * kAccThreads;
 
+// x + y with subnormal numbers kept (this library's own arithmetic flushes them): a sum that a caller has let decay that far
+// stays what it is where a weight is nothing.
+__device__ inline float add_kept(float x, float y) {
+  float z;
+  asm("add.rn.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
+  return z;
+}
+
 // weight_sum[t][h][j] += sum_g exp2(scores[t][h G + g][j] - m_g) / l_g.  grid (chunks of kAccKeys positions, Hkv, n), a thread
 // takes four positions; the heads are added in ascending order, so the sums do not depend on the launch.
 __global__ void __launch_bounds__(kAccThreads)
@@ -47,13 +55,14 @@ weights_add_kernel(Geo g, const float* __restrict__ scores, long long score_stri
   }
   if (j + 4 <= S && ((uintptr_t)w & 15) == 0) {
     float4 old = *reinterpret_cast<float4*>(w);
-    old.x += sum.x; old.y += sum.y; old.z += sum.z; old.w += sum.w;
+    old.x = add_kept(old.x, sum.x); old.y = add_kept(old.y, sum.y);
+    old.z = add_kept(old.z, sum.z); old.w = add_kept(old.w, sum.w);
     *reinterpret_cast<float4*>(w) = old;
   } else {
-    w[0] += sum.x;
-    if (j + 1 < S) w[1] += sum.y;
-    if (j + 2 < S) w[2] += sum.z;
-    if (j + 3 < S) w[3] += sum.w;
+    w[0] = add_kept(w[0], sum.x);
+    if (j + 1 < S) w[1] = add_kept(w[1], sum.y);
+    if (j + 2 < S) w[2] = add_kept(w[2], sum.z);
+    if (j + 3 < S) w[3] = add_kept(w[3], sum.w);
   }
 }
 

@@ -361,3 +361,29 @@ def test_evict_tells_subnormal_weights_of_a_long_cache_apart(in_place):
     cfg = config((2, 1, 128), "bf16", layers=1, n=1)
     tw = twin(cfg, [14000])
     run_evict(tw, [0], tiny_weights(np.random.default_rng(10), (1, 1, 1, 14000)), 5000, 100, in_place)
+
+
+@pytest.mark.parametrize("heads,dtype", [((8, 2, 128), "bf16"), ((4, 1, 64), "fp32")])
+def test_a_subnormal_sum_survives_a_weight_of_zero(heads, dtype):
+    """weight_sum += p leaves the sum as it is where p is nothing, however small the sum."""
+    lens = [200, 385]
+    cfg = config(heads, dtype, layers=1, n=2)
+    tw = twin(cfg, lens)
+    shape = (2, cfg.num_q_heads, cfg.head_dim)
+    _, qx = draw(cfg, W.TID_Q, shape, 11)
+    qx = qx * 256                                                               # (exact in both types)
+    q = torch.from_numpy(qx).to(tw.gpu.torch_dtype).cuda()
+    start = np.abs(tiny_weights(np.random.default_rng(11), (2, cfg.num_kv_heads, 386)))
+    sums = torch.from_numpy(start.copy()).cuda()
+    v = tw.gpu.views()
+    tw.gpu.decode_attention_weights(0, q, v["block_table"], v["seq_lens"], sums)
+    got = sums.cpu().numpy()
+    for t in range(2):
+        K, V = trace_kv(tw, 0, t)
+        _, w, _ = OB.decode_weights(qx[t], K, V)
+        # scores spread over hundreds: most weights are far below half of the smallest subnormal, 2^-150
+        none = w < 2.0 ** -400
+        assert none.sum() > none.size // 3
+        k = none.shape[1]
+        np.testing.assert_array_equal(got[t, :, :k].view(np.uint32)[none], start[t, :, :k].view(np.uint32)[none])
+    assert tw.gpu.last_error() == (0, 0)
