@@ -464,7 +464,9 @@ int kv_pool_set_attention_balance(step_pool* pool, int dynamic_sixteenths, int m
  * up: the warp then sets the STEP_ERR_TIMEOUT bit of the status word, waits (with
  * the full limit) for the copies it still has in flight, and leaves; outputs of such a launch are undefined (the
  * launches after it are unaffected: no state of the kernel outlives a launch).  Default 2,000,000,000 ns.
- * 0 = no waiting at all: a page that has not landed by the time it is first looked at counts as timed out - for testing this path, which no healthy device otherwise reaches. */
+ * 0 = no waiting at all: a page that has not landed by the time it is first looked at counts as timed out - for testing this path, which no healthy device otherwise reaches.
+ * The same limit holds for decode_attention_weights where that kernel serves it (out and weight_sum of such a call are
+ * undefined) and for every wait of decode_attention_tree's tensor-core kernel, which winds down likewise. */
 int kv_pool_set_wait_limit_ns(step_pool* pool, unsigned long long ns);
 /* Which first-layer kernel score_steps uses for bf16 scorers whose shape the tensor-core kernel covers
  * (D a multiple of 64, m a multiple of 64 and <= 1024, 16-byte aligned W1 and hidden): mode 0 (default)

@@ -78,7 +78,7 @@ struct step_pool {
   int attn_dyn16;     // sixteenths of every sequence's pages handed out at run time (0: equal shares only)
   int attn_dyn_chunk; // smallest chunk handed out, in pages
   int fast_path;      // 1 allowed, -1 forced off
-  unsigned long long wait_limit_ns;   // limit of decode_attention's wait for a page copy (kv_pool_set_wait_limit_ns)
+  unsigned long long wait_limit_ns;   // limit of decode_attention's wait for a page copy and of the tree kernel's waits (kv_pool_set_wait_limit_ns)
   int scorer_mode;    // 0: tensor-core MLP for launches with >= scorer_tc_min_rows boundary rows; 1: always; -1: never
   int scorer_tc_min_rows;
   // the tensor map of the last W1 the tensor-core scorer was given (encoding it costs a few host microseconds)

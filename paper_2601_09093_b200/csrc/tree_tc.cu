@@ -34,7 +34,9 @@
 // 64 traces x 16 nodes over 4.6k to 16.9k positions, 32 / 8 heads: 458 us, 2.83 GB at 6.2 TB/s (0.94 of the measured copy).  32
 // traces x 64 nodes over 2k to 25.6k positions, 64 / 8 heads: 947 us, 0.70 PFLOP at 0.74 PFLOP/s; there each lane's chain from
 // its scores through the softmax to the second product is what takes the time, the tensor pipe is busy half of it.
-// Every wait is bounded; one that runs out raises STEP_ERR_TIMEOUT and the CTA winds down.
+// Every wait is bounded (kv_pool_set_wait_limit_ns); one that runs out raises STEP_ERR_TIMEOUT and the CTA winds down: no warp
+// begins anything more, the products in flight are waited for, and when all warps are through and nothing new can start, so
+// is every copy that was begun (each with a limit of its own).  Only then is the shared memory given up.
 #include "attention_rows.cuh"
 #include "async_copy.cuh"
 #include "tensor_core.cuh"
@@ -75,6 +77,7 @@ struct TreeArgs {
   int group_rows;                   // 128 or 256
   int shares;                       // CTAs of the attention launch
   float scale_log2;
+  unsigned long long wait_ns;       // limit of every wait for a barrier
 };
 
 // ---- the stream of tiles
@@ -352,7 +355,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   int* s_up = reinterpret_cast<int*>(s_piece + 2);                     // [64]
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_up + 64);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
-  float* s_ml = reinterpret_cast<float*>(s_tmem + 4);                  // [2][128][2] (below 128 rows)
+  int* s_begun = reinterpret_cast<int*>(s_tmem + 4);                   // [3] how many fills of their buffers the K, V and query warps have begun
+  float* s_ml = reinterpret_cast<float*>(s_tmem + 8);                  // [2][128][2] (below 128 rows)
   const uint32_t bars = smem_u32(s_bar);
   const uint32_t bar_full = bars, bar_empty = bars + 8 * kSlots;
   const uint32_t bar_q = bars + 16 * kSlots, bar_s = bar_q + 8, bar_p = bar_s + 16, bar_o = bar_p + 32,
@@ -398,9 +402,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   };
 
   auto wait = [&](uint32_t bar, uint32_t parity) {
-    if (mbar_try_wait(bar, parity)) return true;
+    if (mbar_test_wait(bar, parity)) return true;                      // (a limit of zero: this is all)
     if (*s_abort) return false;
-    if (mbar_wait_bounded(bar, parity)) return true;
+    if (mbar_wait_bounded(bar, parity, a.wait_ns)) return true;
     flag_error(a.counters, STEP_ERR_TIMEOUT);
     *s_abort = 1;
     return false;
@@ -592,7 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
    if (warp == kWarpK || warp == kWarpV) {
     // ------------------------------------------------ K or V tiles into their ring
     const int kv = warp == kWarpV, ring0 = kv ? kKSlots : 0, ring_n = kv ? kVSlots : kKSlots;
-    int slot = 0;
+    int slot = 0, begun = 0;                                           // (fills begun)
     uint32_t ph = 1;
     bool ok = true;
     Place pl = {};
@@ -649,6 +653,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         if (lane == 0 && pages == 0) mbar_arrive(bar);                 // (the announcement of bytes is the other form of this arrival)
       }
       __syncwarp();
+      ++begun;
       if (++slot == ring_n) { slot = 0; ph ^= 1; }
     };
     long long pos, end;
@@ -671,15 +676,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       pl = nx;
     }
     cp_async_wait_all();
-    if (*s_abort)                                                      // copies in flight still target this CTA's shared memory
-      for (int s = ring0; s < ring0 + ring_n; ++s) {
-        mbar_wait_bounded(bar_full + 8 * s, 0, kDrainNs);
-        mbar_wait_bounded(bar_full + 8 * s, 1, kDrainNs);
-      }
+    if (lane == 0) s_begun[kv] = begun;
   } else if (warp == kWarpQ) {
     // ------------------------------------------------ query rows and ancestor masks of one piece after another
     uint32_t par = 0;
-    int made = 0;                                                      // pieces announced
+    int made = 0, begun = 0;                                           // pieces announced; those and the end of the share
+    if (lane == 0) s_begun[2] = 0;
     long long pos, end;
     Place pl = my_share(false, pos, end);
     for (;; par ^= 1) {
@@ -730,11 +732,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         }
       }
       __syncwarp();
+      if (lane == 0) s_begun[2] = ++begun;
       if (pc.cnt == 0) break;
     }
     last_piece = made > 0 ? (int)(par ^ 1) : -1;
     last_slot = made > 1;
-    if (*s_abort && lane == 0) { mbar_wait_bounded(bar_q, 0, kDrainNs); mbar_wait_bounded(bar_q, 1, kDrainNs); }
     // out rows behind a trace's last drafted token
     for (int t = blockIdx.x; t < a.n; t += gridDim.x) {
       const int nodes = nodes_of(a, t, false);
@@ -881,6 +883,19 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   __syncwarp();
   tc_fence_before();
   __syncthreads();
+  // A wait has run out: copies in flight still write this CTA's shared memory.  (Decided here, where no warp can begin one any
+  // more and *s_abort is final: a fetching warp may be through with its share before another warp's wait runs out.)
+  if (*s_abort) {
+    // fills 0, 1, 2, .. of a barrier complete its phases in that order: the last one's parity
+    auto landed = [&](uint32_t bar, int fills) { if (fills > 0) mbar_wait_bounded(bar, (fills - 1) & 1, kDrainNs); };
+    const int begun = warp == kWarpK ? s_begun[0] : (warp == kWarpV ? s_begun[1] : s_begun[2]);
+    if (lane == 0 && warp == kWarpK)
+      for (int s = 0; s < kKSlots; ++s) landed(bar_full + 8 * s, (begun - s + kKSlots - 1) / kKSlots);
+    if (lane == 0 && warp == kWarpV)
+      for (int s = 0; s < kVSlots; ++s) landed(bar_full + 8 * (kKSlots + s), (begun - s + kVSlots - 1) / kVSlots);
+    if (lane == 0 && warp == kWarpQ) landed(bar_q, begun);
+    __syncthreads();
+  }
   if (warp == kWarpQ && last_piece >= 0 && !*s_abort && s_piece[last_piece].odd) add_odd(a, s_piece[last_piece], last_slot, lane);
   if (warp == kWarpMma) {
     tc_fence_after();
@@ -936,9 +951,9 @@ __global__ void __launch_bounds__(kMergeWarps * 32) tree_merge_kernel(TreeArgs a
 }
 
 size_t smem_bytes(bool two_rows) {
-  return 1024 + (two_rows ? 2 * kQBytes : kQBytes + kXBytes + 512 * 4) + kSlots * kSlotBytes + 32 * 8 + 128 * 8 + 2 * sizeof(Piece) + 64 * 4 + 16;
+  return 1024 + (two_rows ? 2 * kQBytes : kQBytes + kXBytes + 512 * 4) + kSlots * kSlotBytes + 32 * 8 + 128 * 8 + 2 * sizeof(Piece) + 64 * 4 + 32;
 }
-static_assert(1024 + 2 * kQBytes + kSlots * kSlotBytes + 32 * 8 + 128 * 8 + 2 * sizeof(Piece) + 64 * 4 + 16 <= 232448, "shared memory of one CTA");
+static_assert(1024 + 2 * kQBytes + kSlots * kSlotBytes + 32 * 8 + 128 * 8 + 2 * sizeof(Piece) + 64 * 4 + 32 <= 232448, "shared memory of one CTA");
 
 }  // namespace
 
@@ -993,6 +1008,7 @@ int tree_tc_launch(step_pool* pool, int layer, const void* q, const void* k_draf
   a.group_rows = a.lanes * kHalfRows;
   a.shares = pool->num_sms;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)kD);
+  a.wait_ns = pool->wait_limit_ns;
   a.ws_o = (float*)workspace;
   a.ws_ml = a.ws_o + (size_t)a.shares * 2 * a.group_rows * kD;
   const size_t smem = smem_bytes(a.lanes == 2);

@@ -300,6 +300,38 @@ def test_a_pool_beyond_32_bit_offsets():
     assert pool.last_error() == (0, 0)
 
 
+@pytest.mark.parametrize("heads,T", [((8, 2, 128), 9), ((8, 1, 128), 64), ((2, 2, 128), 1)])
+def test_a_wait_that_runs_out_is_flagged_and_leaves_nothing_behind(heads, T):
+    """A limit of zero takes whatever has not landed at the first look for lost: query rows are fetched while the softmax warps
+    look for them, so every CTA gives up with copies of K, V and q under way.  (Healthy copies, which land a microsecond later.)
+    Longer limits run out somewhere or not at all.  Between such calls, on the same pool and without a reset, results are as ever."""
+    cfg = config(heads, "bf16", n=7, layers=1)
+    tw = twin(cfg, [9000, 130, 0, 2000, 77, 16, 511])
+    first = run_tree(tw, 0, T, seed=4)
+    v = tw.gpu.views()
+    n, d = 7, cfg.head_dim
+    q, _ = draw(cfg, W.TID_Q, (n, T, cfg.num_q_heads, d), 4)
+    kd, _ = draw(cfg, W.TID_K, (n, T, 1, cfg.num_kv_heads, d), 4)
+    vd, _ = draw(cfg, W.TID_V, (n, T, 1, cfg.num_kv_heads, d), 4)
+    parents = torch.from_numpy(random_parents(np.random.default_rng(4), n, T, "random")).cuda()
+
+    def call():
+        return tw.gpu.decode_attention_tree(0, q, kd, vd, parents, v["block_table"], v["seq_lens"])
+
+    for limit in (0, 1, 500, 5_000, 0):
+        tw.gpu.set_wait_limit_ns(limit)
+        for _ in range(8):
+            out = call()
+        torch.cuda.synchronize()
+        code, mask = tw.gpu.last_error()
+        assert mask == 1 << 6 if limit == 0 else mask in (0, 1 << 6), (limit, mask)      # STEP_ERR_TIMEOUT
+        if mask == 0:
+            assert torch.equal(out, first), limit
+        tw.gpu.set_wait_limit_ns(2_000_000_000)
+        assert torch.equal(call(), first), limit
+        assert tw.gpu.last_error() == (0, 0)
+
+
 # ---------------------------------------------------------------- append_kv_path
 def same_payload(tw):
     for l in range(tw.cfg.num_layers):
