@@ -159,6 +159,9 @@ def _ptr(t):
     return C.c_void_p(0 if t is None else t.data_ptr())
 
 
+_INT_MAX = 0x7fffffff       # (ctypes cuts larger numbers down to 32 bits without a word)
+
+
 def _expect(fn, device, *wanted):
     """Every (tensor, shape, dtype) of `wanted` is a contiguous tensor of that shape and type on `device`; None passes."""
     for t, shape, dtype in wanted:
@@ -334,7 +337,7 @@ class KVPool:
                               workspace=None, stream=None):
         """q: [n, T, Hq, d] -> out [n, T, Hq, d] in the pool's type; k_draft, v_draft: [n, T, L, Hkv, d]; parents: [n, T]."""
         fn, dt = "decode_attention_tree", self.torch_dtype
-        if q.dim() != 4:
+        if q.dim() != 4 or not 0 <= layer < self.num_layers:
             raise StepError(fn, 1)
         n, T = q.shape[:2]
         draft, rows = (n, T, self.num_layers, self.num_kv_heads, self.head_dim), (n, T, self.num_q_heads, self.head_dim)
@@ -351,7 +354,7 @@ class KVPool:
     def append_kv_path(self, trace_ids, k_draft, v_draft, path, path_len, stream=None):
         """Stores rows path[i, :path_len[i]] of the drafts [n, T, L, Hkv, d] behind trace trace_ids[i]."""
         fn, dt = "append_kv_path", self.torch_dtype
-        if k_draft.dim() != 5 or path.dim() != 2:
+        if k_draft.dim() != 5 or path.dim() != 2 or k_draft.shape[1] > _INT_MAX or path.shape[1] > _INT_MAX:
             raise StepError(fn, 1)
         n, T = k_draft.shape[:2]
         draft, most = (n, T, self.num_layers, self.num_kv_heads, self.head_dim), path.shape[1]
@@ -363,7 +366,7 @@ class KVPool:
     def decode_attention_weights(self, layer, q, block_table, seq_lens, weight_sum, out=None, workspace=None, stream=None):
         """q: [n, Hq, d] -> out [n, Hq, d] fp32; adds to weight_sum [n, Hkv, stride] fp32."""
         fn = "decode_attention_weights"
-        if q.dim() != 3 or weight_sum.dim() != 3:
+        if q.dim() != 3 or weight_sum.dim() != 3 or weight_sum.shape[2] > _INT_MAX or not 0 <= layer < self.num_layers:
             raise StepError(fn, 1)
         n, stride = q.shape[0], weight_sum.shape[2]
         rows = (n, self.num_q_heads, self.head_dim)
@@ -379,7 +382,9 @@ class KVPool:
         """weights: [L, n, Hkv, stride] fp32, in place unless weights_out is given.  Returns kept_out [L, n, Hkv, budget]
         (rows of entries that are left alone are not written: -1 in a tensor made here)."""
         fn = "kv_pool_evict_positions"
-        if weights.dim() != 4:
+        if weights.dim() != 4 or weights.shape[3] > _INT_MAX:
+            raise StepError(fn, 1)
+        if not (1 <= budget <= self.max_pages_per_trace * self.page_size and 0 <= recent <= budget):
             raise StepError(fn, 1)
         n, stride = weights.shape[1], weights.shape[3]
         shape = (self.num_layers, n, self.num_kv_heads)
