@@ -55,3 +55,10 @@ def test_ragged_append_plan_gives_every_trace_its_length():
 def test_scorer_shapes_are_the_papers_model_widths():
     got = {name: (bench.scorer_shape(name).scorer_D, bench.scorer_shape(name).scorer_m) for name in ("c1", "c4", "d2560", "d5120")}
     assert got == {"c1": (4096, 512), "c4": (5120, 1024), "d2560": (2560, 512), "d5120": (5120, 512)}
+
+
+def test_the_counters_on_file_are_those_of_the_present_kernel():
+    """profiles/attn_mma_kernel_dram_traffic.txt names the sources it was taken from; every byte is read about once."""
+    ratio, source = bench.attention_dram_traffic_ratio()
+    assert ratio is not None, source
+    assert 1.0 <= ratio < 1.1
