@@ -22,13 +22,13 @@
  *    affected trace, ORs (1 << code) into a sticky device status word and carries on;
  *    kv_pool_last_error reads and clears that word.
  *  - The library allocates no device memory.  KV storage, metadata (which includes all
- *    kernel scratch) and every input/output buffer belong to the caller and must outlive
- *    the pool / the call.  Pointers are DEVICE pointers unless marked "host".
+ *    kernel scratch but the workspaces that some calls take) and every input/output buffer
+ *    belong to the caller and must outlive the pool / the call.  Pointers are DEVICE pointers unless marked "host".
  *  - `stream` is a cudaStream_t passed as void*.  Calls are asynchronous on it and ordered
  *    by it, except those documented as synchronising.  One pool must not be used from two
  *    streams at once.
  *  - dtype: STEP_BF16 (0) or STEP_FP32 (1) is the storage type of K/V, q, hidden states and
- *    scorer weights.  Accumulation and all outputs are fp32.
+ *    scorer weights.  Accumulation is fp32, and so are all outputs but decode_attention_tree's.
  *  - Query head h reads KV head h / G, G = num_q_heads / num_kv_heads.
  *  - Decode order: append_kv for the new token comes BEFORE decode_attention; the query
  *    attends to all S_t stored positions including its own; there is no mask.
@@ -198,7 +198,9 @@ int decode_attention_static(step_pool* pool, int layer, const void* q,
  * continuations of a trace and verify them in one pass, and for those that bound a trace's cache instead of, or before,
  * giving the trace up).  All of them want the pool's device to be current (else STEP_ERR_INVALID_ARG), take their
  * scratch from the caller (`workspace`: device, 256-byte aligned, in use from the call until its work on the stream is
- * done; calls of different pools that may overlap in time need one each), and can be captured into a CUDA graph. */
+ * done; calls of different pools that may overlap in time need one each), and can be captured into a CUDA graph.  They also
+ * use scratch in the pool's metadata, as its other calls do: calls of ONE pool, and replays of graphs that hold them, stay
+ * ordered one behind the other even with workspaces of their own. */
 
 /* Attention of one layer for a tree of drafted tokens per trace:
  *   out[i][u][h] = sum_j softmax_j(q[i][u][h] . k[j] / sqrt(d)) v[j],  j over the seq_lens[i] cached positions of row i (as
@@ -208,10 +210,14 @@ int decode_attention_static(step_pool* pool, int layer, const void* q,
  * parents: [n, T] int32, the node that node u continues, which comes before u, or -1 if it continues the cached text
  * itself.  A parent outside [-1, u) is read as -1 and sets the STEP_ERR_INVALID_ARG bit of the device status word.
  * n_nodes: [n] int32 or NULL: row i has n_nodes[i] <= T drafted tokens (NULL: T); out rows behind them are zeros, and
- * their q, k_draft, v_draft and parents are not read.  A count outside [0, T] is clamped and flagged likewise.
+ * their q, k_draft, v_draft and parents have no effect.  A count outside [0, T] is clamped and flagged likewise.
  * out: [n, T, num_q_heads, head_dim] in POOL DTYPE (what the output projection behind it reads), rounded once, 32-byte
  * aligned; it must not overlap the inputs.  1 <= T <= 64, n <= 65535.
  * What a row does not see has no part in its result, whatever it holds (infinities and NaN included).
+ * Scores, maxima, sums and accumulators are fp32.  The probabilities are rounded to bf16 on their way into the second product
+ * where the tensor-core kernel serves the call (bf16 pools, head_dim 128, page_size 16, n <= 2048, kv_pool_set_attention_config
+ * not -1), as decode_attention's are: 2.3e-3 off in the 2-norm, where rounding the output alone makes 1.7e-3.  Elsewhere they
+ * stay fp32.
  * decode_attention_tree_workspace_bytes (host-only) says how large the workspace has to be; NULL is fine for 0. */
 int decode_attention_tree_workspace_bytes(const step_pool* pool, int n, int T, size_t* bytes);
 int decode_attention_tree(step_pool* pool, int layer, const void* q, const void* k_draft, const void* v_draft,
@@ -225,7 +231,8 @@ int decode_attention_tree(step_pool* pool, int layer, const void* q, const void*
  * of the draft in the order they are to be stored (repeats are allowed); path_len: [n] int32, 0 .. max_path.  T has no
  * upper bound here.  Allocation, and what is flagged, as append_kv: traces in the order listed, an entry that cannot be
  * served is skipped whole; a path_len out of range or a path that names a row outside [0, T) skips its entry and sets the
- * STEP_ERR_INVALID_ARG bit.  n <= min(max_traces, 2048).  Needs no workspace. */
+ * STEP_ERR_INVALID_ARG bit.  With n = 0 or max_path = 0 the call returns at once and looks at nothing, as append_kv does
+ * without tokens.  n <= min(max_traces, 2048).  Needs no workspace. */
 int append_kv_path(step_pool* pool, const int32_t* trace_ids, int n, int T, const void* k_draft, const void* v_draft,
                    const int32_t* path, const int32_t* path_len, int max_path, void* stream);
 
@@ -451,7 +458,8 @@ int kv_pool_last_error(step_pool* pool, unsigned* mask_out, void* stream);
 int kv_pool_read_kv(step_pool* pool, int layer, int kv_head, const int32_t* block_row,
                     int seq_len, void* k_out, void* v_out, void* stream);
 /* Tuning knobs of decode_attention (0 keeps the current value): CTAs per launch, and whether
- * the tensor-core bf16 path may be used (1) or the scalar kernel is forced (-1). */
+ * the tensor-core bf16 path may be used (1) or the scalar kernel is forced (-1).  The second also holds for
+ * decode_attention_tree and decode_attention_weights, whose workspace sizes depend on it. */
 int kv_pool_set_attention_config(step_pool* pool, int grid_ctas, int fast_path);
 /* How decode_attention's tensor-core launch spreads the KV pages over the SMs.  Of every (trace, KV head)
  * sequence the last dynamic_sixteenths / 16 of its pages (0 .. 12; default 4) are cut into chunks of at least
