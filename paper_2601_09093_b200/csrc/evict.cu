@@ -15,8 +15,8 @@
 //   2. evict_move_kernel    one CTA per (KV head, trace, layer): selection, then the rows and weights move
 //   3. evict_finish_kernel  a cluster of CTAs: references dropped, free list, block table, lengths
 //
-// 64 traces, 4 layers, 8 KV heads of 128 in bf16, about 4100 positions cut to 4096 with 256 recent ones: 207 us for 665 MB of
-// rows, weights and lists (102 us at the copy bandwidth).  The move kernel is 180 of them.
+// 64 traces, 4 layers, 8 KV heads of 128 in bf16, about 4100 positions cut to 4096 with 256 recent ones: 207 to 212 us for 665 MB
+// of rows, weights and lists (102 us at the copy bandwidth).  The move kernel is 180 of them.
 #include "release.cuh"
 
 using namespace stepk;
@@ -187,8 +187,11 @@ __device__ inline uint32_t weight_key(uint32_t u) {
 }
 
 // What bounds it: for a cut of a few positions the passes over the weights (each a read of shared memory, or of L2 for
-// long caches) and the copies' latency, so four CTAs per SM matter more than rows in flight per warp; the positions are split into one contiguous run per warp, so that ranks need one
-// exchange of counts between the warps and none per step.
+// long caches) and the copies' latency, so four CTAs per SM matter more than rows in flight per warp, and more than the 52
+// bytes of registers that a thread spills for them; all CTAs go through the same phases at the same time, and the memory
+// system idles while they select.  The positions are split into one contiguous run per warp, so that ranks need one exchange
+// of counts between the warps and none per step.  Keys are kept in shared memory where weight_stride says that those of any
+// trace fit; with a wider stride every pass reads the weights, of short traces too.
 __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(EvictArgs a) {
   extern __shared__ uint32_t s_key[];                   // [cache_keys]
   __shared__ int s_hist[kBins];                         // the histogram, then the positions that move

@@ -14,10 +14,13 @@
 //     times an infinity or a NaN is NaN: the query warp looks at v of a piece's drafted tokens ahead of time, such elements
 //     become zeros in the tile, and the rows that do see the token get them added behind the piece's output;
 //   * scores S (128 x 128, fp32) are made in tensor memory; 128 threads, a row each, read them, keep the running maximum
-//     and sum in fp32, and write the probabilities back as bf16 (one rounding, half a step of 2^-8 at most) over the
-//     same columns, from where they are the A operand of the second product, which adds to O (128 x 128, fp32) in tensor
-//     memory.  O is rescaled only when a row's maximum has grown by more than 2^8 (the probabilities are relative to an
-//     older maximum until then), so the accumulators are almost never touched;
+//     and sum in fp32, and write the probabilities back as bf16 (one rounding, half a step of 2^-8 at most; the sum takes
+//     them unrounded) over the same columns, from where they are the A operand of the second product, which adds to O
+//     (128 x 128, fp32) in tensor memory.  bf16 because both operands of a product have one type and V's is bf16; the output
+//     is rounded to it anyway, and the two roundings together are 2.3e-3 off in the 2-norm where the second alone makes
+//     1.7e-3 (a second term of the probabilities would be half as many products again, in a kernel that above 128 rows waits
+//     for them).  O is rescaled only when a row's maximum has grown by more than 2^8 (the probabilities are relative to an older
+//     maximum until then; a published method), so the accumulators are almost never touched;
 //   * two such chains ("lanes") run side by side in a CTA, so that the tensor cores work on one while the other is at
 //     its softmax.  Up to 128 rows: the lanes take even and odd tiles of the same rows and are combined at the end.
 //     More: the lanes take 128 rows each of the same tile, and 256 rows are one row group;
@@ -31,9 +34,13 @@
 //     softmax and its output.
 // Warps: 4 + 4 softmax (lane 0, lane 1), one that fetches K, one for V (a TMA instruction takes its thread some 70 cycles:
 // with both in one warp that warp set the pace), one that issues the products, one for the query rows.
-// 64 traces x 16 nodes over 4.6k to 16.9k positions, 32 / 8 heads: 458 us, 2.83 GB at 6.2 TB/s (0.94 of the measured copy).  32
-// traces x 64 nodes over 2k to 25.6k positions, 64 / 8 heads: 947 us, 0.70 PFLOP at 0.74 PFLOP/s; there each lane's chain from
-// its scores through the softmax to the second product is what takes the time, the tensor pipe is busy half of it.
+// 64 traces x 16 nodes over 4.6k to 16.9k positions, 32 / 8 heads: 457 to 522 us from device to device, 2.83 GB at 5.4 to 6.2 TB/s
+// (0.83 to 0.95 of the measured copy).  32 traces x 64 nodes over 2k to 25.6k positions, 64 / 8 heads: 854 to 1080 us (the
+// power cap), 0.70 PFLOP at 0.65 to 0.82 PFLOP/s.  There a lane has one buffer for scores and probabilities, so that its softmax
+// waits for the second product of this tile and the first of the next, and the other lane does not fill the gap: the tensor
+// pipe is busy half of the time.  Also, in a trace's last row group whose drafted tokens fit the first 128 rows, the second
+// lane works on rows that are not there (the number of lanes is one per launch): an eighth of all that case's work.
+// A trace without drafted tokens has its tiles read all the same, for nothing.
 // Every wait is bounded (kv_pool_set_wait_limit_ns); one that runs out raises STEP_ERR_TIMEOUT and the CTA winds down: no warp
 // begins anything more, the products in flight are waited for, and when all warps are through and nothing new can start, so
 // is every copy that was begun (each with a limit of its own).  Only then is the shared memory given up.
@@ -906,7 +913,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
 // Combines the pieces of every sequence that more than one share holds.  A CTA takes one border between two shares (and 32
 // of the rows): if the sequence it cuts has no border before it, the CTA combines all of that sequence's pieces, a warp per
 // query row, lanes over the 128 dims, in stream order with a running (max, sum, weighted values).  The same bits whatever
-// ran when.  The search runs while the attention kernel is still at work.
+// ran when.  The search stands in front of the wait for the attention kernel: it runs early on SMs that have no CTA of that
+// kernel left (beside one there are no registers for it).
 constexpr int kMergeWarps = 8, kMergeRows = 32;
 
 __global__ void __launch_bounds__(kMergeWarps * 32) tree_merge_kernel(TreeArgs a) {

@@ -7,9 +7,10 @@
 // fp32) in the workspace and a second kernel, its programmatic dependent, turns them into weights: 8 * G bytes per
 // position and KV head on top of the 4 * d bytes of K and V in bf16 (a second read of K would be 2 * d).
 //
-// 64 traces of 4.6k to 16.9k positions, 32 / 8 heads of 128 in bf16: 473 us, 2.86 GB at 6.0 TB/s; the streaming kernel is 438 of
-// them, at the measured copy bandwidth, the rest is combining (bound by the latency of the pieces' loads) and adding (24 us
-// alone: the scores come back from HBM and L2 at 5.5 TB/s).
+// 64 traces of 4.6k to 16.9k positions, 32 / 8 heads of 128 in bf16: 464 to 488 us, 2.86 GB at 5.9 to 6.2 TB/s; the streaming kernel
+// is 438 of them, at the measured copy bandwidth, the rest is combining (bound by the latency of the pieces' loads) and adding
+// (24 us alone: the scores come back from HBM and L2 at 5.5 TB/s).  The adding launch and the scores' workspace are sized by
+// weight_stride, not by the lengths, which the host does not know: CTAs behind a trace's end return at once.
 #include "attention_rows.cuh"
 
 using namespace stepk;
