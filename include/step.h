@@ -273,6 +273,84 @@ int kv_pool_evict_positions(step_pool* pool, const int32_t* trace_ids, int n, co
                             int weight_stride, int budget, int recent, int32_t* kept_out, void* workspace,
                             size_t workspace_bytes, void* stream);
 
+/* ---- rotary positions, and a cache that is written layer by layer (the paper has no counterpart: append_kv takes keys that
+ * are rotated already, and those of all layers at once; a model that runs on this cache makes them one layer at a time) ----
+ *
+ * Pair i of the first D = rotary_dim dims of a head - dims i and i + D/2, or 2i and 2i + 1 if interleaved - at position p:
+ *   (y1, y2) = scale * ( x1 cos a - x2 sin a,  x2 cos a + x1 sin a ),   a = p * f_i
+ * Dims behind D are left as they are.  The frequencies f_i enter as a table of turns per position in units of 2^-64, so that
+ * the angle of any int32 position is exact to 1e-9 of a turn; the arithmetic is fp32 with one rounding of the result. */
+enum { STEP_ROTARY_PLAIN = 0, STEP_ROTARY_LINEAR = 1, STEP_ROTARY_BASE = 2, STEP_ROTARY_YARN = 3, STEP_ROTARY_BANDS = 4 };
+
+/* t_i = base^(-2i / D); how far f_i is stretched for contexts `factor` times longer than original_positions:
+ *   PLAIN   f_i = t_i
+ *   LINEAR  f_i = t_i / factor
+ *   BASE    f_i = t_i with base * factor^(D / (D - 2)) for base
+ *   YARN    f_i = t_i (1 - r) + t_i / factor * r,  r = clamp((i - first) / (last - first), 0, 1),
+ *           first = max(floor(c(fast)), 0), last = min(ceil(c(slow)), D - 1), c(n) = D ln(original_positions / (2 pi n)) / (2 ln base)
+ *   BANDS   the same with r = clamp((fast - n_i) / (fast - slow), 0, 1), n_i = original_positions t_i / (2 pi) turns
+ * fast > slow > 0 are turns over original_positions (usually 32 and 1 for YARN, 4 and 1 for BANDS).  divisors (HOST, [D / 2], may
+ * be NULL): f_i is divided by divisors[i] besides.  output_scale: the scale above; 0 = 1, for YARN 0.1 ln(factor) + 1. */
+typedef struct {
+  int rotary_dim;                     /* even */
+  int interleaved;                    /* 0 or 1 */
+  double base;
+  int scaling;
+  double factor, original_positions, fast, slow;
+  const double* divisors;
+  double output_scale;
+} step_rotary_config;
+
+typedef struct {
+  const uint64_t* table;              /* [rotary_dim / 2], DEVICE */
+  int rotary_dim, interleaved;
+  float scale;
+} step_rotary;
+
+/* Fills table_out (HOST, [rotary_dim / 2]) and the other members of *rotary_out; the caller copies the table to the device and
+ * sets rotary_out->table.  Needs no GPU. */
+int step_rotary_table(const step_rotary_config* cfg, uint64_t* table_out, step_rotary* rotary_out);
+
+typedef struct {
+  const void* x; void* out;           /* [batch][rows][heads][head_dim], head_dim contiguous, the rest by strides; element-aligned */
+  int dtype;
+  int batch, rows, heads, head_dim;
+  long long x_batch, x_row, x_head, out_batch, out_row, out_head;   /* strides in elements */
+  const int32_t* positions;           /* [batch][rows], rows contiguous; NULL: a row's position is its number */
+  long long position_batch;           /* elements from one batch entry's positions to the next's; 0: all have the same */
+  int transpose;                      /* 1: the transposed rotation (angles negated), which turns dL/dy into dL/dx */
+} rotate_args;
+
+/* Rotates queries or keys.  out may be x with the same strides (in place); otherwise they must not overlap, and no two
+ * elements of out may share a place.  The members of `a` are read during the call.  Device pointers; the current device's. */
+int rotate_positions(const rotate_args* a, const step_rotary* rotary, void* stream);
+
+/* Makes room for n_tokens new positions of each of the n listed traces, as append_kv does (order, what is skipped and
+ * flagged), without storing anything: start_out[i] = the length of trace trace_ids[i] before the call, or -1 for an entry
+ * that was skipped.  What the new positions hold is undefined until it is stored: attend to a layer when it is.
+ * trace_ids, start_out: [n] device.  n <= min(max_traces, 2048). */
+int kv_pool_extend(step_pool* pool, const int32_t* trace_ids, int n, int n_tokens, int32_t* start_out, void* stream);
+
+/* Row r = i * n_tokens + s of k, v and q belongs to token s of entry i. */
+typedef struct {
+  int layer0, n_layers, n, n_tokens;
+  const int32_t* trace_ids;           /* [n] */
+  const int32_t* start;               /* [n] cache position of an entry's first token (kv_pool_extend); negative: passed over */
+  const int32_t* positions;           /* [n] rotary position of an entry's first token; NULL: start */
+  const void* k; const void* v;       /* [rows][n_layers][num_kv_heads][head_dim]; rows k_row, v_row elements apart */
+  long long k_row, v_row;
+  const void* q; void* q_out;         /* [n_layers][rows][num_q_heads][head_dim] by strides; both NULL: no queries.  q_out may be q */
+  long long q_row, q_layer, q_out_row, q_out_layer;
+} kv_store_args;
+
+/* Layers layer0 .. layer0 + n_layers - 1 of positions start[i] + s, s < n_tokens, of trace trace_ids[i]: k rotated by
+ * positions[i] + s (or start[i] + s) and v as it is go into the cache; the rotated q goes to q_out.  Pool dtype; all
+ * rows 16-byte aligned.  Positions have to exist (kv_pool_extend): an entry that reaches beyond its trace's length is
+ * skipped whole (STEP_ERR_INVALID_ARG in the status word), as is one whose trace is not live (STEP_ERR_BAD_TRACE); q_out rows
+ * of entries that are skipped or passed over are left as they are.  No two entries of a call may name the same position.
+ * A page that several traces share is written for all of them.  Wants the pool's device to be current. */
+int store_kv_rotated(step_pool* pool, const kv_store_args* a, const step_rotary* rotary, void* stream);
+
 /* Step scorer at step boundaries (Sec. 3.1) and running-mean update (Sec. 3.3):
  * for every row i with boundary_mask[i] != 0:
  *   y = sigmoid(w2 . ReLU(W1 hidden[i] + b1) + b2);  step_scores_out[i] = y;

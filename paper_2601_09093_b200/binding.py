@@ -18,7 +18,9 @@ STEP_OK = 0
 STATUS_NAMES = {0: "STEP_OK", 1: "STEP_ERR_INVALID_ARG", 2: "STEP_ERR_NO_BLOCKS", 3: "STEP_ERR_BAD_TRACE",
                 4: "STEP_ERR_CAPACITY", 5: "STEP_ERR_CUDA", 6: "STEP_ERR_TIMEOUT", 7: "STEP_ERR_BAD_BLOCK"}
 STEP_BF16, STEP_FP32 = 0, 1
+ROTARY_SCALINGS = {None: 0, "linear": 1, "base": 2, "yarn": 3, "bands": 4}
 _TORCH_DTYPE = {STEP_BF16: torch.bfloat16, STEP_FP32: torch.float32}
+_STEP_DTYPE = {t: c for c, t in _TORCH_DTYPE.items()}
 
 
 class StepError(RuntimeError):
@@ -71,6 +73,30 @@ class scorer_train_hyper(C.Structure):
                 ("weight_decay", C.c_float), ("pos_weight", C.c_float), ("step", C.c_int)]
 
 
+class step_rotary_config(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int), ("interleaved", C.c_int), ("base", C.c_double), ("scaling", C.c_int),
+                ("factor", C.c_double), ("original_positions", C.c_double), ("fast", C.c_double), ("slow", C.c_double),
+                ("divisors", C.c_void_p), ("output_scale", C.c_double)]
+
+
+class step_rotary(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("rotary_dim", C.c_int), ("interleaved", C.c_int), ("scale", C.c_float)]
+
+
+class rotate_args(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("out", C.c_void_p), ("dtype", C.c_int), ("batch", C.c_int), ("rows", C.c_int),
+                ("heads", C.c_int), ("head_dim", C.c_int), ("x_batch", C.c_longlong), ("x_row", C.c_longlong),
+                ("x_head", C.c_longlong), ("out_batch", C.c_longlong), ("out_row", C.c_longlong), ("out_head", C.c_longlong),
+                ("positions", C.c_void_p), ("position_batch", C.c_longlong), ("transpose", C.c_int)]
+
+
+class kv_store_args(C.Structure):
+    _fields_ = [("layer0", C.c_int), ("n_layers", C.c_int), ("n", C.c_int), ("n_tokens", C.c_int), ("trace_ids", C.c_void_p),
+                ("start", C.c_void_p), ("positions", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_row", C.c_longlong), ("v_row", C.c_longlong), ("q", C.c_void_p), ("q_out", C.c_void_p),
+                ("q_row", C.c_longlong), ("q_layer", C.c_longlong), ("q_out_row", C.c_longlong), ("q_out_layer", C.c_longlong)]
+
+
 _lib = None
 
 
@@ -105,6 +131,10 @@ def lib():
     L.decode_attention_weights.argtypes = [vp, i, vp, vp, vp, i, vp, vp, i, vp, sz, vp]
     L.kv_pool_evict_workspace_bytes.argtypes = [vp, i, i, szp]
     L.kv_pool_evict_positions.argtypes = [vp, vp, i, vp, vp, i, i, i, vp, vp, sz, vp]
+    L.step_rotary_table.argtypes = [C.POINTER(step_rotary_config), vp, C.POINTER(step_rotary)]
+    L.rotate_positions.argtypes = [C.POINTER(rotate_args), C.POINTER(step_rotary), vp]
+    L.kv_pool_extend.argtypes = [vp, vp, i, i, vp, vp]
+    L.store_kv_rotated.argtypes = [vp, C.POINTER(kv_store_args), C.POINTER(step_rotary), vp]
     L.score_steps.argtypes = [vp, vp, vp, vp, i, C.POINTER(scorer_weights), vp, vp]
     L.score_steps_tokens.argtypes = [vp, vp, vp, vp, i, vp, i, C.POINTER(scorer_weights), vp, vp, vp]
     L.detect_step_ends.argtypes = [vp, vp, i, vp, i, vp, vp]
@@ -400,6 +430,46 @@ class KVPool:
                         kept_out.data_ptr()), ("kv_pool_evict_workspace_bytes", n, budget), workspace, stream)
         return kept_out
 
+    # ---- rotary positions, a cache written layer by layer
+    def extend(self, trace_ids, n_tokens, start_out=None, stream=None):
+        """Room for n_tokens new positions of every listed trace.  Returns their lengths before (-1: skipped), [n] int32."""
+        fn = "kv_pool_extend"
+        if trace_ids.dim() != 1 or not 0 <= n_tokens <= _INT_MAX:
+            raise StepError(fn, 1)
+        n = trace_ids.shape[0]
+        _expect(fn, self._device(), (trace_ids, (n,), torch.int32), (start_out, (n,), torch.int32))
+        if start_out is None:
+            start_out = self._empty((n,), torch.int32, stream)
+        self._call(fn, (trace_ids.data_ptr(), n, n_tokens, start_out.data_ptr()), stream=stream)
+        return start_out
+
+    def store_kv_rotated(self, layer0, trace_ids, start, k, v, rotary, q=None, q_out=None, positions=None, stream=None):
+        """Stores k (rotated) and v [n, T, layers, Hkv, d] at positions start[i] + s of layers layer0 ..; returns the rotated
+        queries q [layers, n, T, Hq, d] (q_out; it may be q), or None.  Rows may be strided (slices of a projection's output)."""
+        fn, dt, dev = "store_kv_rotated", self.torch_dtype, self._device()
+        if k.dim() != 5 or not 0 <= layer0 < self.num_layers:
+            raise StepError(fn, 1)
+        n, T, layers = k.shape[:3]
+        rows = (n, T, layers, self.num_kv_heads, self.head_dim)
+        heads = (layers, n, T, self.num_q_heads, self.head_dim)
+        _expect(fn, dev, (trace_ids, (n,), torch.int32), (start, (n,), torch.int32), (positions, (n,), torch.int32))
+        if layer0 + layers > self.num_layers or layers < 1 or n * T > _INT_MAX or (q is None and q_out is not None):
+            raise StepError(fn, 1)
+        if rotary.device != dev or rotary.struct.rotary_dim > self.head_dim:
+            raise StepError(fn, 1)
+        for t, shape in ((k, rows), (v, rows), (q, heads), (q_out, heads)):
+            if t is not None and (t.dtype != dt or t.shape != shape or t.device != dev):
+                raise StepError(fn, 1)
+        if q is not None and q_out is None:
+            q_out = self._empty(heads, dt, stream)
+        k_row, v_row = (_row_stride(fn, t.stride(), rows, 0, 2) for t in (k, v))
+        q_row, qo_row = (0 if t is None else _row_stride(fn, t.stride(), heads, 1, 3) for t in (q, q_out))
+        args = kv_store_args(layer0, layers, n, T, trace_ids.data_ptr(), start.data_ptr(), _at(positions), k.data_ptr(), v.data_ptr(),
+                             k_row, v_row, _at(q), _at(q_out), q_row, 0 if q is None else q.stride(0), qo_row,
+                             0 if q is None else q_out.stride(0))
+        self._call(fn, (C.byref(args), C.byref(rotary.struct)), stream=stream)
+        return q_out
+
     def score_steps(self, hidden, boundary_mask, row_trace, weights, step_scores_out=None, stream=None):
         M = hidden.shape[0]
         if step_scores_out is None:
@@ -534,6 +604,78 @@ class KVPool:
         n, u = C.c_int(), C.c_int()
         _check("kv_pool_score_launch_info", lib().kv_pool_score_launch_info(self.handle, C.byref(n), C.byref(u), _stream(stream)))
         return dict(n_rows=n.value, tc_units=u.value)
+
+
+def _row_stride(fn, strides, shape, row_dim, inner):
+    """Elements from one (entry, token) row to the next, where dims row_dim, row_dim + 1 are entries and tokens and those from
+    `inner` on make up a row without gaps."""
+    size = 1
+    for i in range(len(shape) - 1, inner - 1, -1):
+        if shape[i] != 1 and strides[i] != size:
+            raise StepError(fn, 1)
+        size *= shape[i]
+    n, T = shape[row_dim], shape[row_dim + 1]
+    if n > 1 and T > 1 and strides[row_dim] != T * strides[row_dim + 1]:
+        raise StepError(fn, 1)
+    return strides[row_dim + 1] if T > 1 else strides[row_dim]
+
+
+class Rotary:
+    """How positions turn queries and keys: the table of frequencies on the device plus the C struct that points at it.
+    scaling: None, "linear", "base", "yarn" or "bands"; fast, slow: turns over original_positions between which "yarn"
+    (usually 32, 1) and "bands" (4, 1) stretch; divisors: a further divisor of every pair's frequency."""
+
+    def __init__(self, rotary_dim, base=10000.0, interleaved=False, scaling=None, factor=1.0, original_positions=0, fast=None,
+                 slow=1.0, divisors=None, output_scale=0.0, device="cuda:0"):
+        if scaling not in ROTARY_SCALINGS or not 2 <= rotary_dim <= _INT_MAX:
+            raise StepError("step_rotary_table", 1)
+        if fast is None:
+            fast = 4.0 if scaling == "bands" else 32.0
+        if divisors is not None:
+            divisors = torch.as_tensor(divisors, dtype=torch.float64, device="cpu").contiguous()
+            if divisors.shape != (rotary_dim // 2,):
+                raise StepError("step_rotary_table", 1)
+        cfg = step_rotary_config(rotary_dim, int(interleaved), base, ROTARY_SCALINGS[scaling], factor, original_positions, fast, slow,
+                                 _at(divisors), output_scale)
+        table = torch.empty(rotary_dim // 2, dtype=torch.int64)
+        self.struct = step_rotary()
+        _check("step_rotary_table", lib().step_rotary_table(C.byref(cfg), table.data_ptr(), C.byref(self.struct)))
+        self.table = table.to(device)
+        self.device = self.table.device
+        self.struct.table = self.table.data_ptr()
+
+
+def rotate_positions(x, rotary, positions=None, out=None, transpose=False, stream=None):
+    """x [batch, rows, heads, d] or [rows, heads, d], any strides but the last dim's, turned by positions ([rows] or
+    [batch, rows] int32; None: the row's number) -> out (a new contiguous tensor; it may be x).  transpose: the transposed
+    rotation, which takes the gradient of the result to the gradient of x."""
+    fn, dev = "rotate_positions", x.device
+    if x.dim() not in (3, 4) or x.dtype not in _STEP_DTYPE or dev != rotary.device or rotary.struct.rotary_dim > x.shape[-1]:
+        raise StepError(fn, 1)
+    if stream is not None and stream.device != dev:
+        raise StepError(fn, 1)
+    if stream is not None or torch.cuda.current_device() != dev.index:
+        with torch.cuda.device(dev), torch.cuda.stream(stream):
+            return rotate_positions(x, rotary, positions, out, transpose)
+    shape = x.shape if x.dim() == 4 else (1,) + tuple(x.shape)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    if out.shape != x.shape or out.dtype != x.dtype or out.device != dev or max(shape) > _INT_MAX:
+        raise StepError(fn, 1)
+    xs, os = ((t.stride() if t.dim() == 4 else (0,) + t.stride()) for t in (x, out))
+    if shape[3] > 1 and (xs[3] != 1 or os[3] != 1):
+        raise StepError(fn, 1)
+    step = 0
+    if positions is not None:
+        if positions.dtype != torch.int32 or positions.device != dev or positions.shape not in ((shape[1],), (shape[0], shape[1])):
+            raise StepError(fn, 1)
+        if shape[1] > 1 and positions.stride(-1) != 1:
+            raise StepError(fn, 1)
+        step = positions.stride(0) if positions.dim() == 2 else 0
+    args = rotate_args(x.data_ptr(), out.data_ptr(), _STEP_DTYPE[x.dtype], *shape, *xs[:3], *os[:3], _at(positions), step,
+                       int(bool(transpose)))
+    _check(fn, lib().rotate_positions(C.byref(args), C.byref(rotary.struct), _raw_stream(dev)))
+    return out
 
 
 class ScorerTrainer:

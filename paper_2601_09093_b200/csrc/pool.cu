@@ -752,6 +752,19 @@ int append_kv(step_pool* pool, const int32_t* trace_ids, int n, int n_tokens, co
   return stepk::append_kv_impl(pool, trace_ids, n, n_tokens, k_new, v_new, nullptr, 0, (cudaStream_t)stream, nullptr, 0);
 }
 
+int kv_pool_extend(step_pool* pool, const int32_t* trace_ids, int n, int n_tokens, int32_t* start_out, void* stream) {
+  if (!pool || n < 0 || n_tokens < 0) return STEP_ERR_INVALID_ARG;
+  if (n == 0) return STEP_OK;
+  // ids must be distinct; the list is served by one CTA from shared memory (12 bytes per entry)
+  if (!trace_ids || !start_out || n > pool->cfg.max_traces || n > kMaxTracesFast) return STEP_ERR_INVALID_ARG;
+  const int st = on_pool_device(pool);
+  if (st != STEP_OK) return st;
+  DevViews v = pool->v;
+  v.append_base = start_out;                             // where append_alloc_kernel leaves every entry's old length, or -1
+  append_alloc_kernel<<<1, 256, (size_t)n * 3 * sizeof(int), (cudaStream_t)stream>>>(v, geo_of(pool), trace_ids, n, n_tokens, nullptr);
+  return launch_ok();
+}
+
 int append_kv_path(step_pool* pool, const int32_t* trace_ids, int n, int T, const void* k_draft, const void* v_draft,
                    const int32_t* path, const int32_t* path_len, int max_path, void* stream) {
   if (!pool || n < 0 || T < 1 || max_path < 0) return STEP_ERR_INVALID_ARG;

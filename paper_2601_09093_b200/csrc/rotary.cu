@@ -1,0 +1,459 @@
+// Rotary positions: rotate_positions turns queries or keys by their positions, store_kv_rotated turns keys on their way into
+// the paged cache (and the queries of the same tokens along with them).
+//
+//   pair i of a head's first D = rotary_dim dims (i and i + D/2, or 2i and 2i + 1), at position p:
+//   (y1, y2) = scale * ( x1 cos a - x2 sin a,  x2 cos a + x1 sin a ),  a = p * f_i;      transposed: a = -p * f_i
+//
+// Angles.  f_i enters as turns per position in units of 2^-64 (a 64-bit integer, made once on the host): p times that, modulo
+// 2^64, IS the angle modulo a turn, with an error of p * 2^-65 turns - 1e-13 at a position of a million, where a 32-bit
+// product p * f would be off by 0.03.  The two top bits are the quadrant (rounded to nearest), what is left - at most an
+// eighth of a turn - becomes a float and goes through sincospif.  One 64-bit multiplication per pair and position, shared
+// by all heads of the token.
+//
+// Both kernels are bound by memory: every element is read once and written once.  A thread owns kU = 16 bytes worth of
+// pairs ("unit"): two 16-byte chunks of a head - one in each half, or two neighbours - so that it reads and writes whole
+// chunks and both members of its pairs, in place as well.  Values are turned in fp32 and rounded once.
+#include "step_internal.cuh"
+
+#include <math.h>
+
+using namespace stepk;
+
+namespace {
+
+// Cosine and sine (times scale) of p * step turns, step in units of 2^-64.
+__device__ inline void angle_of(long long p, unsigned long long step, float scale, float& c, float& s) {
+  const unsigned long long phase = (unsigned long long)p * step;
+  const unsigned quadrant = (unsigned)((phase + (1ull << 61)) >> 62);
+  const long long rest = (long long)(phase - ((unsigned long long)quadrant << 62));    // in [-2^61, 2^61)
+  float sn, cs;
+  sincospif((float)rest * 0x1p-63f, &sn, &cs);
+  c = (quadrant & 1) ? sn : cs;
+  s = (quadrant & 1) ? cs : sn;
+  if (quadrant == 1 || quadrant == 2) c = -c;
+  if (quadrant & 2) s = -s;
+  c *= scale;
+  s *= scale;
+}
+
+__device__ inline float to_float(float x) { return x; }
+__device__ inline float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T> __device__ inline T from_float(float x);
+template <> __device__ inline float from_float<float>(float x) { return x; }
+template <> __device__ inline __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16(x); }
+
+// The two chunks of a unit, turned.
+template <typename T, bool kPairs>
+__device__ inline void turn_unit(uint4& a, uint4& b, const float* c, const float* s) {
+  constexpr int kU = 16 / (int)sizeof(T);
+  T x[2 * kU];
+  *reinterpret_cast<uint4*>(x) = a;
+  *reinterpret_cast<uint4*>(x + kU) = b;
+#pragma unroll
+  for (int i = 0; i < kU; ++i) {
+    const int i1 = kPairs ? 2 * i : i, i2 = kPairs ? 2 * i + 1 : i + kU;
+    const float x1 = to_float(x[i1]), x2 = to_float(x[i2]);
+    x[i1] = from_float<T>(x1 * c[i] - x2 * s[i]);
+    x[i2] = from_float<T>(x2 * c[i] + x1 * s[i]);
+  }
+  a = *reinterpret_cast<uint4*>(x);
+  b = *reinterpret_cast<uint4*>(x + kU);
+}
+// Chunks of unit u in a head of D rotated dims.
+template <typename T, bool kPairs>
+__device__ inline void chunks_of(int u, int D, int& a, int& b) {
+  constexpr int kU = 16 / (int)sizeof(T);
+  a = kPairs ? 2 * u : u;
+  b = kPairs ? 2 * u + 1 : u + D / (2 * kU);
+}
+
+// ---------------------------------------------------------------- rotate_positions
+struct RotateDev {
+  const void* x; void* out;
+  const int32_t* positions; long long position_batch;
+  const unsigned long long* table;
+  long long x_batch, x_row, x_head, out_batch, out_row, out_head;      // elements
+  int batch, rows, heads, d, D;
+  float scale, sign;
+  int heads_per_task, tasks_per_row;
+  int copy_tail;                    // dims behind D are copied (not in place)
+};
+
+constexpr int kRotateWarps = 8, kRotateAhead = 4;
+
+// A warp takes one row and a range of its heads.  Lanes: a unit each, as many heads at once as there is room for.
+template <typename T, bool kPairs>
+__global__ void __launch_bounds__(kRotateWarps * 32) rotate_kernel(const RotateDev a) {
+  constexpr int kU = 16 / (int)sizeof(T);
+  const int lane = threadIdx.x & 31;
+  const long long task = (long long)blockIdx.x * kRotateWarps + (threadIdx.x >> 5);
+  const long long row = task / a.tasks_per_row;
+  if (row >= (long long)a.batch * a.rows) return;
+  const int h0 = (int)(task - row * a.tasks_per_row) * a.heads_per_task, h1 = min(a.heads, h0 + a.heads_per_task);
+  const int bi = (int)(row / a.rows), ri = (int)(row - (long long)bi * a.rows);
+  const int p = a.positions ? a.positions[bi * a.position_batch + ri] : ri;
+  const T* x = (const T*)a.x + bi * a.x_batch + ri * a.x_row;
+  T* out = (T*)a.out + bi * a.out_batch + ri * a.out_row;
+  const int units = a.D / (2 * kU), across = min(units, 32), together = 32 / across;
+  const int sub = lane / across;
+  for (int u0 = 0; u0 < units; u0 += across) {
+    const int u = u0 + lane - sub * across;
+    if (sub >= together || u >= units) continue;
+    float c[kU], s[kU];
+#pragma unroll
+    for (int i = 0; i < kU; ++i) {
+      angle_of(p, a.table[u * kU + i], a.scale, c[i], s[i]);
+      s[i] *= a.sign;
+    }
+    int ca, cb;
+    chunks_of<T, kPairs>(u, a.D, ca, cb);
+    for (int h = h0 + sub; h < h1; h += kRotateAhead * together) {
+      uint4 va[kRotateAhead], vb[kRotateAhead];
+#pragma unroll
+      for (int y = 0; y < kRotateAhead; ++y) {
+        const int hy = h + y * together;
+        if (hy < h1) {
+          const uint4* src = reinterpret_cast<const uint4*>(x + hy * a.x_head);
+          va[y] = src[ca];
+          vb[y] = src[cb];
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < kRotateAhead; ++y) {
+        const int hy = h + y * together;
+        if (hy < h1) {
+          turn_unit<T, kPairs>(va[y], vb[y], c, s);
+          uint4* dst = reinterpret_cast<uint4*>(out + hy * a.out_head);
+          dst[ca] = va[y];
+          dst[cb] = vb[y];
+        }
+      }
+    }
+  }
+  if (a.copy_tail) {
+    const int first = a.D / kU, tail = a.d / kU - first;
+    for (int i = lane; i < (h1 - h0) * tail; i += 32) {
+      const int h = h0 + i / tail, ch = first + i % tail;
+      reinterpret_cast<uint4*>(out + h * a.out_head)[ch] = reinterpret_cast<const uint4*>(x + h * a.x_head)[ch];
+    }
+  }
+}
+
+// Any alignment, any even D: a thread takes one pair, or one dim behind D, at a time.
+template <typename T, bool kPairs>
+__global__ void __launch_bounds__(256) rotate_any_kernel(const RotateDev a) {
+  const int half = a.D / 2, items = half + (a.copy_tail ? a.d - a.D : 0);
+  const long long all = (long long)a.batch * a.rows * a.heads * items;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
+    const int e = (int)(i % items);
+    long long r = i / items;
+    const int h = (int)(r % a.heads);
+    r /= a.heads;
+    const int bi = (int)(r / a.rows), ri = (int)(r - (long long)bi * a.rows);
+    const T* x = (const T*)a.x + bi * a.x_batch + ri * a.x_row + h * a.x_head;
+    T* out = (T*)a.out + bi * a.out_batch + ri * a.out_row + h * a.out_head;
+    if (e >= half) { out[e + half] = x[e + half]; continue; }
+    const int p = a.positions ? a.positions[bi * a.position_batch + ri] : ri;
+    float c, s;
+    angle_of(p, a.table[e], a.scale, c, s);
+    s *= a.sign;
+    const int i1 = kPairs ? 2 * e : e, i2 = kPairs ? 2 * e + 1 : e + half;
+    const float x1 = to_float(x[i1]), x2 = to_float(x[i2]);
+    out[i1] = from_float<T>(x1 * c - x2 * s);
+    out[i2] = from_float<T>(x2 * c + x1 * s);
+  }
+}
+
+// ---------------------------------------------------------------- store_kv_rotated
+struct StoreDev {
+  Geo g;
+  const int32_t* block_table; const int32_t* seq_lens; const uint8_t* live; int32_t* counters;
+  void* kv;
+  const int32_t* ids; const int32_t* start; const int32_t* positions;
+  const void* k; const void* v; const void* q; void* q_out;
+  long long k_row, v_row, q_row, q_layer, q_out_row, q_out_layer;       // elements
+  const unsigned long long* table;
+  int D; float scale;
+  int layer0, n_layers, n_tokens;
+  int layers_per_cta;
+};
+
+constexpr int kMaxPairs = 256;                                           // head_dim <= 512
+constexpr int kStoreAhead = 2;
+
+// A CTA takes one (entry, token) row and a range of layers: cosines and sines of its position once, into shared memory;
+// where the row goes (block and slot, the same for every layer and head) once; then its warps share the heads.
+// kChunks: whole units (D a multiple of two chunks); else pair by pair.
+template <typename T, bool kPairs, bool kChunks>
+__global__ void __launch_bounds__(256) store_kernel(const StoreDev a) {
+  constexpr int kU = 16 / (int)sizeof(T);
+  __shared__ float s_c[kMaxPairs], s_s[kMaxPairs];
+  const Geo& g = a.g;
+  const int i = blockIdx.x / a.n_tokens, tok = blockIdx.x - i * a.n_tokens;
+  const int st = a.start[i], t = a.ids[i];
+  if (st < 0) return;                                                    // no room was made for this entry
+  const bool reporter = threadIdx.x == 0 && tok == 0 && blockIdx.y == 0;
+  if (t < 0 || t >= g.max_traces) { if (reporter) flag_error(a.counters, STEP_ERR_BAD_TRACE); return; }
+  const long long p = (long long)(a.positions ? a.positions[i] : st) + tok;
+  const int half = a.D / 2;
+  for (int x = threadIdx.x; x < half; x += 256) angle_of(p, a.table[x], a.scale, s_c[x], s_s[x]);
+  const bool live = a.live[t];
+  const int S = a.seq_lens[t];
+  if (!live) { if (reporter) flag_error(a.counters, STEP_ERR_BAD_TRACE); return; }
+  if ((long long)st + a.n_tokens > S || (long long)S > (long long)g.max_pages * g.P) {
+    if (reporter) flag_error(a.counters, STEP_ERR_INVALID_ARG);
+    return;
+  }
+  const int pos = st + tok, page = pos / g.P, slot = pos - page * g.P;
+  const int b = a.block_table[(size_t)t * g.max_pages + page];
+  if (b < 0 || b >= g.num_blocks) { if (threadIdx.x == 0 && blockIdx.y == 0) flag_error(a.counters, STEP_ERR_BAD_BLOCK); return; }
+  __syncthreads();
+  const int l0 = blockIdx.y * a.layers_per_cta, l1 = min(a.n_layers, l0 + a.layers_per_cta);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = 256 / 32;
+  const int cpr = g.d / kU;                                              // chunks of a head's row
+  const size_t head_stride = (size_t)2 * g.P * g.d, layer_stride = (size_t)g.num_blocks * g.Hkv * head_stride;
+  // K row of (layer l of this call, head 0); V's is P * d further
+  T* const kv0 = (T*)a.kv + (size_t)a.layer0 * layer_stride + (size_t)b * g.Hkv * head_stride + (size_t)slot * g.d;
+  const T* const k0 = (const T*)a.k + (long long)blockIdx.x * a.k_row;
+  const T* const v0 = (const T*)a.v + (long long)blockIdx.x * a.v_row;
+  const T* const q0 = (const T*)a.q + (long long)blockIdx.x * a.q_row;
+  T* const qo0 = (T*)a.q_out + (long long)blockIdx.x * a.q_out_row;
+  auto stored = [&](int c) { return g.swizzle ? ((c & ~7) | ((c ^ slot) & 7)) : c; };   // where a row's chunk c stands
+
+  // ---- values: as they are
+  const int kv_heads = (l1 - l0) * g.Hkv;
+  for (int x = threadIdx.x; x < kv_heads * cpr; x += 256) {
+    const int hh = x / cpr, c = x - hh * cpr, l = l0 + hh / g.Hkv, h = hh % g.Hkv;
+    reinterpret_cast<uint4*>(kv0 + (size_t)l * layer_stride + h * head_stride + (size_t)g.P * g.d)[stored(c)] =
+        reinterpret_cast<const uint4*>(v0 + ((size_t)l * g.Hkv + h) * g.d)[c];
+  }
+  // ---- keys and queries: heads hh of [0, total) are turned; from(hh) and to(hh) say where a head's row is
+  const int units = kChunks ? a.D / (2 * kU) : 1, across = min(units, 32), together = 32 / across;
+  const int sub = lane / across;
+  auto turn_heads = [&](int total, auto from, auto to, auto at) {
+    if constexpr (kChunks) {
+      for (int u0 = 0; u0 < units; u0 += across) {
+        const int u = u0 + lane - sub * across;
+        if (sub >= together || u >= units) continue;
+        float c[kU], s[kU];
+#pragma unroll
+        for (int x = 0; x < kU; ++x) { c[x] = s_c[u * kU + x]; s[x] = s_s[u * kU + x]; }
+        int ca, cb;
+        chunks_of<T, kPairs>(u, a.D, ca, cb);
+        for (int hh = warp * together + sub; hh < total; hh += kStoreAhead * warps * together) {
+          uint4 va[kStoreAhead], vb[kStoreAhead];
+#pragma unroll
+          for (int y = 0; y < kStoreAhead; ++y) {
+            const int hy = hh + y * warps * together;
+            if (hy < total) {
+              const uint4* src = reinterpret_cast<const uint4*>(from(hy));
+              va[y] = src[ca];
+              vb[y] = src[cb];
+            }
+          }
+#pragma unroll
+          for (int y = 0; y < kStoreAhead; ++y) {
+            const int hy = hh + y * warps * together;
+            if (hy < total) {
+              turn_unit<T, kPairs>(va[y], vb[y], c, s);
+              uint4* dst = reinterpret_cast<uint4*>(to(hy));
+              dst[at(ca)] = va[y];
+              dst[at(cb)] = vb[y];
+            }
+          }
+        }
+      }
+    } else {
+      for (int x = threadIdx.x; x < total * half; x += 256) {
+        const int hh = x / half, e = x - hh * half;
+        const T* src = from(hh);
+        T* dst = to(hh);
+        const int i1 = kPairs ? 2 * e : e, i2 = kPairs ? 2 * e + 1 : e + half;
+        const float x1 = to_float(src[i1]), x2 = to_float(src[i2]);
+        dst[at(i1 / kU) * kU + i1 % kU] = from_float<T>(x1 * s_c[e] - x2 * s_s[e]);
+        dst[at(i2 / kU) * kU + i2 % kU] = from_float<T>(x2 * s_c[e] + x1 * s_s[e]);
+      }
+    }
+    const int tail = g.d - a.D;                                          // dims that are not turned
+    if (kChunks) {
+      for (int x = threadIdx.x; x < total * (tail / kU); x += 256) {
+        const int hh = x / (tail / kU), c = a.D / kU + x % (tail / kU);
+        reinterpret_cast<uint4*>(to(hh))[at(c)] = reinterpret_cast<const uint4*>(from(hh))[c];
+      }
+    } else {
+      for (int x = threadIdx.x; x < total * tail; x += 256) {
+        const int hh = x / tail, e = a.D + x % tail;
+        to(hh)[at(e / kU) * kU + e % kU] = from(hh)[e];
+      }
+    }
+  };
+  turn_heads(kv_heads, [&](int hh) { return k0 + ((size_t)l0 * g.Hkv + hh) * g.d; },
+             [&](int hh) { return kv0 + (size_t)(l0 + hh / g.Hkv) * layer_stride + (hh % g.Hkv) * head_stride; }, stored);
+  if (a.q)
+    turn_heads((l1 - l0) * g.Hq, [&](int hh) { return q0 + (long long)(l0 + hh / g.Hq) * a.q_layer + (hh % g.Hq) * g.d; },
+               [&](int hh) { return qo0 + (long long)(l0 + hh / g.Hq) * a.q_out_layer + (hh % g.Hq) * g.d; }, [](int c) { return c; });
+}
+
+bool rotary_valid(const step_rotary* r, int head_dim) {
+  return r && r->table && r->rotary_dim >= 2 && r->rotary_dim % 2 == 0 && r->rotary_dim <= head_dim &&
+         (r->interleaved == 0 || r->interleaved == 1) && isfinite(r->scale) && !((uintptr_t)r->table & 7);
+}
+
+typedef void (*StoreForm)(const StoreDev);
+template <typename T>
+StoreForm store_form(bool pairs, bool chunks) {
+  if (chunks) return pairs ? store_kernel<T, true, true> : store_kernel<T, false, true>;
+  return pairs ? store_kernel<T, true, false> : store_kernel<T, false, false>;
+}
+
+template <typename T>
+int launch_rotate(const RotateDev& a0, int pairs, cudaStream_t s) {
+  constexpr int kU = 16 / (int)sizeof(T);
+  RotateDev a = a0;
+  const long long strides = a.x_batch | a.x_row | a.x_head | a.out_batch | a.out_row | a.out_head;
+  // whole 16-byte chunks wherever the shape allows it
+  const bool chunks = a.D % (2 * kU) == 0 && (!a.copy_tail || a.d % kU == 0) && strides % kU == 0 &&
+                      !(((uintptr_t)a.x | (uintptr_t)a.out) & 15);
+  const long long rows = (long long)a.batch * a.rows;
+  if (chunks) {
+    // a warp takes all heads of a row; where that leaves SMs without work, fewer
+    const int units = a.D / (2 * kU), together = units < 32 ? 32 / units : 1;
+    int per = a.heads;
+    while (per > together && rows * ((a.heads + per - 1) / per) < 148ll * 16) per = (per + 1) / 2;
+    per = (per + together - 1) / together * together;
+    a.heads_per_task = per;
+    a.tasks_per_row = (a.heads + per - 1) / per;
+    const long long ctas = (rows * a.tasks_per_row + kRotateWarps - 1) / kRotateWarps;
+    if (ctas > 0x7fffffffll) return STEP_ERR_INVALID_ARG;
+    if (pairs) rotate_kernel<T, true><<<(unsigned)ctas, kRotateWarps * 32, 0, s>>>(a);
+    else rotate_kernel<T, false><<<(unsigned)ctas, kRotateWarps * 32, 0, s>>>(a);
+  } else {
+    const long long items = rows * a.heads * (a.D / 2 + (a.copy_tail ? a.d - a.D : 0));
+    const long long ctas = (items + 255) / 256 < 148 * 16 ? (items + 255) / 256 : 148 * 16;
+    if (pairs) rotate_any_kernel<T, true><<<(unsigned)ctas, 256, 0, s>>>(a);
+    else rotate_any_kernel<T, false><<<(unsigned)ctas, 256, 0, s>>>(a);
+  }
+  return launch_ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+int step_rotary_table(const step_rotary_config* cfg, uint64_t* table_out, step_rotary* rotary_out) {
+  if (!cfg || !table_out || !rotary_out) return STEP_ERR_INVALID_ARG;
+  const int D = cfg->rotary_dim;
+  if (D < 2 || D % 2 != 0 || (cfg->interleaved != 0 && cfg->interleaved != 1)) return STEP_ERR_INVALID_ARG;
+  if (!(isfinite(cfg->base) && cfg->base > 1.0) || !(isfinite(cfg->output_scale) && cfg->output_scale >= 0.0)) return STEP_ERR_INVALID_ARG;
+  const int kind = cfg->scaling;
+  if (kind < STEP_ROTARY_PLAIN || kind > STEP_ROTARY_BANDS) return STEP_ERR_INVALID_ARG;
+  const long double s = cfg->factor;
+  if (kind != STEP_ROTARY_PLAIN && !(isfinite(cfg->factor) && cfg->factor > 0.0)) return STEP_ERR_INVALID_ARG;
+  if (kind == STEP_ROTARY_BASE && D == 2) return STEP_ERR_INVALID_ARG;
+  const bool ramp = kind == STEP_ROTARY_YARN || kind == STEP_ROTARY_BANDS;
+  if (ramp && (!(isfinite(cfg->original_positions) && cfg->original_positions > 0.0) ||
+               !(isfinite(cfg->fast) && cfg->slow > 0.0 && cfg->fast > cfg->slow))) return STEP_ERR_INVALID_ARG;
+  if (cfg->divisors)
+    for (int i = 0; i < D / 2; ++i)
+      if (!(isfinite(cfg->divisors[i]) && cfg->divisors[i] > 0.0)) return STEP_ERR_INVALID_ARG;
+  const long double turn = 6.283185307179586476925286766559005768L;
+  long double log_base = logl((long double)cfg->base);
+  if (kind == STEP_ROTARY_BASE) log_base += logl(s) * D / (D - 2);
+  long double first = 0.0L, last = 0.0L;                 // YARN: the pairs between which the stretching sets in
+  if (kind == STEP_ROTARY_YARN) {
+    const long double L = cfg->original_positions;
+    first = floorl(D * logl(L / (cfg->fast * turn)) / (2 * log_base));
+    last = ceill(D * logl(L / (cfg->slow * turn)) / (2 * log_base));
+    if (first < 0) first = 0;
+    if (last > D - 1) last = D - 1;
+  }
+  for (int i = 0; i < D / 2; ++i) {
+    long double f = expl(-2.0L * i / D * log_base), stretched = 0.0L;
+    if (kind == STEP_ROTARY_LINEAR) stretched = 1.0L;
+    if (kind == STEP_ROTARY_YARN) stretched = (i - first) / (last - first > 0.001L ? last - first : 0.001L);
+    if (kind == STEP_ROTARY_BANDS) stretched = (cfg->fast - cfg->original_positions * f / turn) / ((long double)cfg->fast - cfg->slow);
+    if (stretched < 0) stretched = 0;
+    if (stretched > 1) stretched = 1;
+    if (stretched > 0) f = f * (1.0L - stretched) + f / s * stretched;
+    if (cfg->divisors) f /= cfg->divisors[i];
+    // turns per position; whole turns do not matter at whole positions
+    long double x = f / turn;
+    x = (x - floorl(x)) * 0x1p64L;
+    if (!(x >= 0.0L)) return STEP_ERR_INVALID_ARG;       // (a frequency beyond what a long double resolves)
+    uint64_t u = x < 0x1p64L ? (uint64_t)x : 0;
+    if (x < 0x1p64L && x - (long double)u >= 0.5L) ++u;
+    table_out[i] = u;
+  }
+  double scale = cfg->output_scale;
+  if (scale == 0.0) scale = kind == STEP_ROTARY_YARN && cfg->factor > 1.0 ? 0.1 * log(cfg->factor) + 1.0 : 1.0;
+  rotary_out->table = nullptr;
+  rotary_out->rotary_dim = D;
+  rotary_out->interleaved = cfg->interleaved;
+  rotary_out->scale = (float)scale;
+  return STEP_OK;
+}
+
+int rotate_positions(const rotate_args* a, const step_rotary* rotary, void* stream) {
+  if (!a || a->batch < 0 || a->rows < 0 || a->heads < 0 || a->head_dim < 1) return STEP_ERR_INVALID_ARG;
+  if (a->dtype != STEP_BF16 && a->dtype != STEP_FP32) return STEP_ERR_INVALID_ARG;
+  if ((a->transpose != 0 && a->transpose != 1) || !rotary_valid(rotary, a->head_dim)) return STEP_ERR_INVALID_ARG;
+  if (a->batch == 0 || a->rows == 0 || a->heads == 0) return STEP_OK;
+  if (!a->x || !a->out) return STEP_ERR_INVALID_ARG;
+  const uintptr_t unit = a->dtype == STEP_BF16 ? 1 : 3;
+  if (((uintptr_t)a->x | (uintptr_t)a->out) & unit || (uintptr_t)a->positions & 3) return STEP_ERR_INVALID_ARG;
+  RotateDev r = {};
+  r.x = a->x; r.out = a->out;
+  r.positions = a->positions; r.position_batch = a->position_batch;
+  r.table = (const unsigned long long*)rotary->table;
+  r.x_batch = a->x_batch; r.x_row = a->x_row; r.x_head = a->x_head;
+  r.out_batch = a->out_batch; r.out_row = a->out_row; r.out_head = a->out_head;
+  r.batch = a->batch; r.rows = a->rows; r.heads = a->heads; r.d = a->head_dim; r.D = rotary->rotary_dim;
+  if (r.batch == 1) r.x_batch = r.out_batch = 0;         // (a stride that is not used may be anything)
+  if (r.rows == 1) r.x_row = r.out_row = 0;
+  if (r.heads == 1) r.x_head = r.out_head = 0;
+  r.scale = rotary->scale; r.sign = a->transpose ? -1.f : 1.f;
+  r.copy_tail = a->x != a->out && r.D < r.d;
+  return a->dtype == STEP_BF16 ? launch_rotate<__nv_bfloat16>(r, rotary->interleaved, (cudaStream_t)stream)
+                               : launch_rotate<float>(r, rotary->interleaved, (cudaStream_t)stream);
+}
+
+int store_kv_rotated(step_pool* pool, const kv_store_args* a, const step_rotary* rotary, void* stream) {
+  if (!pool || !a || a->n < 0 || a->n_tokens < 0) return STEP_ERR_INVALID_ARG;
+  const kv_pool_config& cfg = pool->cfg;
+  if (a->layer0 < 0 || a->n_layers < 1 || a->layer0 > cfg.num_layers - a->n_layers) return STEP_ERR_INVALID_ARG;
+  if (!rotary_valid(rotary, cfg.head_dim)) return STEP_ERR_INVALID_ARG;
+  if (a->n == 0 || a->n_tokens == 0) return STEP_OK;
+  if (!a->trace_ids || !a->start || !a->k || !a->v || !a->q != !a->q_out) return STEP_ERR_INVALID_ARG;
+  const long long rows = (long long)a->n * a->n_tokens;
+  if (rows > 0x7fffffffll) return STEP_ERR_INVALID_ARG;
+  const int cpe = 16 / pool->elem_bytes;
+  const long long k_row = rows > 1 ? a->k_row : 0, v_row = rows > 1 ? a->v_row : 0;      // (a stride that is not used may be anything)
+  const long long q_row = rows > 1 ? a->q_row : 0, q_out_row = rows > 1 ? a->q_out_row : 0;
+  const long long q_layer = a->n_layers > 1 ? a->q_layer : 0, q_out_layer = a->n_layers > 1 ? a->q_out_layer : 0;
+  if (((uintptr_t)a->k | (uintptr_t)a->v | (uintptr_t)a->q | (uintptr_t)a->q_out) & 15) return STEP_ERR_INVALID_ARG;
+  if ((k_row | v_row) % cpe != 0 || (a->q && (q_row | q_layer | q_out_row | q_out_layer) % cpe != 0)) return STEP_ERR_INVALID_ARG;
+  const int st = on_pool_device(pool);
+  if (st != STEP_OK) return st;
+  StoreDev d = {};
+  d.g = geo_of(pool);
+  d.block_table = pool->v.block_table; d.seq_lens = pool->v.seq_lens; d.live = pool->v.live; d.counters = pool->v.counters;
+  d.kv = cfg.kv_storage;
+  d.ids = a->trace_ids; d.start = a->start; d.positions = a->positions;
+  d.k = a->k; d.v = a->v; d.q = a->q; d.q_out = a->q_out;
+  d.k_row = k_row; d.v_row = v_row; d.q_row = q_row; d.q_layer = q_layer; d.q_out_row = q_out_row; d.q_out_layer = q_out_layer;
+  d.table = (const unsigned long long*)rotary->table;
+  d.D = rotary->rotary_dim; d.scale = rotary->scale;
+  d.layer0 = a->layer0; d.n_layers = a->n_layers; d.n_tokens = a->n_tokens;
+  // a CTA takes all layers of a row; where that leaves SMs without work, fewer
+  int splits = (int)((2ll * pool->num_sms + rows - 1) / rows);
+  if (splits > a->n_layers) splits = a->n_layers;
+  d.layers_per_cta = (a->n_layers + splits - 1) / splits;
+  const dim3 grid((unsigned)rows, (unsigned)((a->n_layers + d.layers_per_cta - 1) / d.layers_per_cta));
+  cudaStream_t s = (cudaStream_t)stream;
+  const bool chunks = d.D % (2 * cpe) == 0;
+  auto kernel = cfg.dtype == STEP_BF16 ? store_form<__nv_bfloat16>(rotary->interleaved, chunks) : store_form<float>(rotary->interleaved, chunks);
+  kernel<<<grid, 256, 0, s>>>(d);
+  return launch_ok();
+}
+
+}  // extern "C"
