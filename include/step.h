@@ -351,6 +351,27 @@ typedef struct {
  * A page that several traces share is written for all of them.  Wants the pool's device to be current. */
 int store_kv_rotated(step_pool* pool, const kv_store_args* a, const step_rotary* rotary, void* stream);
 
+/* decode_attention for traces that were forked from several prompts (kv_pool_fork_prefix, once per problem), each prompt's pages
+ * read once for all of its traces.  Rows [group_rows[g], group_rows[g + 1]) of q, block_table and seq_lens are group g,
+ * g < n_groups, whose rows' tables begin with the same group_pages[g] blocks; these are read through the table of the group's
+ * first row that is at least as long (group_pages[g] * page_size positions).  Shorter rows of a group, ended traces (seq_lens 0:
+ * zeros) among them, and rows of no group read their own tables, and so does everyone where fewer than two rows of a group
+ * are that long: the result is decode_attention's whenever the tables do begin alike.
+ * group_rows: [n_groups + 1] int32, ascending, 0 .. n; group_pages: [n_groups] int32, 0 .. max_pages_per_trace; device.  A
+ * description that is not in order sets the STEP_ERR_INVALID_ARG bit of the status word and is not followed: every row reads
+ * its own table.  n_groups = 0: no groups (both may be NULL).
+ * q and out: [n, num_q_heads, head_dim] in POOL DTYPE, 16-byte aligned; out is rounded once and must not overlap the inputs.
+ * n, n_groups <= 65535.  Scores, maxima, sums and accumulators are fp32.  Where the tensor-core kernels serve the call (bf16 pools,
+ * head_dim 128, page_size 16, n <= 2048, kv_pool_set_attention_config not -1) the probabilities are rounded to bf16 on their way
+ * into the second product, as decode_attention_tree's are; elsewhere they stay fp32 and every row reads its own table.
+ * Wants the pool's device to be current and a workspace of decode_attention_groups_workspace_bytes (host-only) bytes, 256-byte
+ * aligned, from the caller, as the calls above; calls of one pool stay ordered one behind the other unless each has a workspace
+ * of its own and nothing writes the pool meanwhile. */
+int decode_attention_groups_workspace_bytes(const step_pool* pool, int n, int n_groups, size_t* bytes);
+int decode_attention_groups(step_pool* pool, int layer, const void* q, const int32_t* block_table, const int32_t* seq_lens,
+                            int n, const int32_t* group_rows, const int32_t* group_pages, int n_groups, void* out,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
 /* Step scorer at step boundaries (Sec. 3.1) and running-mean update (Sec. 3.3):
  * for every row i with boundary_mask[i] != 0:
  *   y = sigmoid(w2 . ReLU(W1 hidden[i] + b1) + b2);  step_scores_out[i] = y;

@@ -135,6 +135,8 @@ def lib():
     L.rotate_positions.argtypes = [C.POINTER(rotate_args), C.POINTER(step_rotary), vp]
     L.kv_pool_extend.argtypes = [vp, vp, i, i, vp, vp]
     L.store_kv_rotated.argtypes = [vp, C.POINTER(kv_store_args), C.POINTER(step_rotary), vp]
+    L.decode_attention_groups_workspace_bytes.argtypes = [vp, i, i, szp]
+    L.decode_attention_groups.argtypes = [vp, i, vp, vp, vp, i, vp, vp, i, vp, vp, sz, vp]
     L.score_steps.argtypes = [vp, vp, vp, vp, i, C.POINTER(scorer_weights), vp, vp]
     L.score_steps_tokens.argtypes = [vp, vp, vp, vp, i, vp, i, C.POINTER(scorer_weights), vp, vp, vp]
     L.detect_step_ends.argtypes = [vp, vp, i, vp, i, vp, vp]
@@ -469,6 +471,22 @@ class KVPool:
                              0 if q is None else q_out.stride(0))
         self._call(fn, (C.byref(args), C.byref(rotary.struct)), stream=stream)
         return q_out
+
+    def decode_attention_groups(self, layer, q, block_table, seq_lens, group_rows, group_pages, out=None, workspace=None, stream=None):
+        """q: [n, Hq, d] -> out [n, Hq, d] in the pool's type; rows group_rows[g] .. group_rows[g + 1] share their first
+        group_pages[g] pages (both None: no groups)."""
+        fn, dt = "decode_attention_groups", self.torch_dtype
+        if q.dim() != 3 or not 0 <= layer < self.num_layers or (group_rows is None) != (group_pages is None):
+            raise StepError(fn, 1)
+        n, n_groups = q.shape[0], 0 if group_pages is None else group_pages.numel()
+        rows = (n, self.num_q_heads, self.head_dim)
+        _expect(fn, self._device(), (q, rows, dt), (out, rows, dt), (block_table, (n, self.max_pages_per_trace), torch.int32),
+                (seq_lens, (n,), torch.int32), (group_rows, (n_groups + 1,), torch.int32), (group_pages, (n_groups,), torch.int32))
+        if out is None:
+            out = self._empty(rows, dt, stream)
+        self._call(fn, (layer, q.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), n, _at(group_rows), _at(group_pages), n_groups,
+                        out.data_ptr()), ("decode_attention_groups_workspace_bytes", n, n_groups), workspace, stream)
+        return out
 
     def score_steps(self, hidden, boundary_mask, row_trace, weights, step_scores_out=None, stream=None):
         M = hidden.shape[0]

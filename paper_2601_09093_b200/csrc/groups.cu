@@ -1,0 +1,63 @@
+// decode_attention_groups: decode attention of traces that were forked from several prompts, each prompt read once for all of
+// its traces.
+//
+//   out[i][h] = sum_j softmax_j(q[i][h] . K_i[j] / sqrt(d)) V_i[j],  j in [0, seq_lens[i]),
+//
+// where the first pages of a group's rows are the same blocks.  bf16 pools of the usual shape run on groups_tc.cu; elsewhere
+// every row reads its own table (attention_rows.cuh).
+#include "attention_rows.cuh"
+
+using namespace stepk;
+
+namespace {
+
+// Raises the flag of a description that is not in order (it changes nothing else here: nothing is shared).
+__global__ void groups_check_kernel(const int32_t* group_rows, const int32_t* group_pages, int n_groups, int n, int max_pages, int32_t* counters) {
+  bool bad = false;
+  for (int g = threadIdx.x; g < n_groups; g += blockDim.x)
+    bad |= group_rows[g] < 0 || group_rows[g + 1] < group_rows[g] || group_rows[g + 1] > n || group_pages[g] < 0 || group_pages[g] > max_pages;
+  if (bad) flag_error(counters, STEP_ERR_INVALID_ARG);
+}
+
+}  // namespace
+
+extern "C" {
+
+int decode_attention_groups_workspace_bytes(const step_pool* pool, int n, int n_groups, size_t* bytes) {
+  if (!pool || !bytes || n < 0 || n_groups < 0 || n > 65535 || n_groups > 65535) return STEP_ERR_INVALID_ARG;
+  *bytes = groups_tc_supported(pool, n) ? groups_tc_workspace(pool, n, n_groups) : attn_rows_workspace(pool, n, 1);
+  return STEP_OK;
+}
+
+int decode_attention_groups(step_pool* pool, int layer, const void* q, const int32_t* block_table, const int32_t* seq_lens, int n,
+                            const int32_t* group_rows, const int32_t* group_pages, int n_groups, void* out, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  if (!pool || n < 0 || n_groups < 0 || layer < 0 || layer >= pool->cfg.num_layers) return STEP_ERR_INVALID_ARG;
+  if (n == 0) return STEP_OK;
+  if (!q || !block_table || !seq_lens || !out || n > 65535 || n_groups > 65535) return STEP_ERR_INVALID_ARG;
+  if (n_groups > 0 && (!group_rows || !group_pages)) return STEP_ERR_INVALID_ARG;
+  if (((uintptr_t)q | (uintptr_t)out) & 15) return STEP_ERR_INVALID_ARG;
+  size_t need = 0;
+  int st = decode_attention_groups_workspace_bytes(pool, n, n_groups, &need);
+  if (st != STEP_OK) return st;
+  if (need > 0 && (!workspace || (uintptr_t)workspace & 255 || workspace_bytes < need)) return STEP_ERR_INVALID_ARG;
+  st = on_pool_device(pool);
+  if (st != STEP_OK) return st;
+  cudaStream_t s = (cudaStream_t)stream;
+  if (groups_tc_supported(pool, n))
+    return groups_tc_launch(pool, layer, q, block_table, seq_lens, n, group_rows, group_pages, n_groups, out, workspace, s);
+  RowsArgs a = {};
+  a.g = geo_of(pool);
+  a.kv = pool->cfg.kv_storage; a.layer = layer;
+  a.q = q; a.T = 1;
+  a.block_table = block_table; a.seq_lens = seq_lens; a.out = out;
+  a.counters = pool->v.counters;
+  if (n_groups > 0) {
+    groups_check_kernel<<<1, 256, 0, s>>>(group_rows, group_pages, n_groups, n, a.g.max_pages, a.counters);
+    if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
+  }
+  if (pool->cfg.dtype == STEP_BF16) return launch_attn_rows<__nv_bfloat16, __nv_bfloat16, false, false>(pool, a, n, (float*)workspace, s);
+  return launch_attn_rows<float, float, false, false>(pool, a, n, (float*)workspace, s);
+}
+
+}  // extern "C"

@@ -1,0 +1,970 @@
+// Tensor-core form of decode_attention_groups (bf16 pools, head_dim 128, page 16).
+//
+// A trace's keys are the pages it shares with its group and the pages of its own.  Both kinds leave partial results
+//   m = max_j s_j,  l = sum_j 2^(s_j - m),  o = sum_j 2^(s_j - m) v_j          (s in units of log 2)
+// which a last kernel combines.  Three launches, each a programmatic dependent of the one before:
+//
+// 1. groups_stream_kernel: the own pages, bound by HBM.  The pages of all (row, KV head) sequences form one stream, cut into one
+//    equal contiguous share per warp; a warp streams its share through a private ring of whole pages (8 KiB, K and V rows of one
+//    head, one bulk copy each) and runs both products on 16 x 8 x 16 tiles, the G heads of the group as rows: with so few
+//    rows a 128-row tensor-core tile would be nearly empty, and beginning a sequence costs such a kernel four tiles' time,
+//    more than a trace's own text often has.  Each CTA works out for itself which rows share what (from the lengths and the
+//    groups' arrays); the first leaves the outcome in the workspace for the other two kernels.
+// 2. groups_prefix_kernel: the shared pages, bound by the tensor cores and the exponentials.  The query rows of a group's traces
+//    - (trace, head of the KV head's group) - are taken 256 at a time against one read of the keys, as decode_attention_tree does
+//    with a trace's drafted tokens: scores by tcgen05 into tensor memory, a thread per row for the softmax, probabilities
+//    rounded to bf16 over the scores, from where they are the second product's A operand.  Two chains ("lanes") run side by
+//    side: 128 rows each of the same tile of 128 keys, or, where a row block has at most 128 rows, even and odd tiles of the same
+//    rows.  The tiles of all (group, KV head, row block) sequences form one stream, cut into one equal share per CTA.
+// 3. groups_merge_kernel: a warp per query row.
+//
+// The partition is a function of lengths and groups alone and pieces are combined in stream order, so a call gives the same
+// bits every time.  Every wait is bounded (kv_pool_set_wait_limit_ns); a kernel whose wait runs out raises STEP_ERR_TIMEOUT and
+// leaves when its copies and products in flight have ended.
+#include "attention_tc.cuh"
+
+#include <string.h>
+
+using namespace stepk;
+
+namespace {
+
+constexpr int kSetup = 4;                         // units that a sequence of the prefix kernel takes besides its tiles (a tile of one lane is one)
+constexpr int kKSlots = 2, kVSlots = 3, kSlots = kKSlots + kVSlots;   // rings of K and of V tiles, 160 KiB: a V tile waits for its softmax
+constexpr int kWarpK = 8, kWarpMma = 9, kWarpQ = 10, kWarpV = 11;
+constexpr int kThreads = 384;                     // three warpgroups
+constexpr int kRegsSoftmax = 208, kRegsOther = 88; // 2 x 128 x 208 + 128 x 88 = 384 x 168, what the launch has
+constexpr int kTmemCols = 512;                    // S of both lanes (P over them), then O of both
+constexpr float kRescale = 8.f;                   // log2 of how far a row's maximum may run ahead of its reference
+constexpr unsigned long long kDrainNs = 100000000ull;
+
+constexpr int kStreamWarps = 8, kStages = 3, kPageBytes = 2 * kP * kD * 2;
+
+struct Header { long long units; int groups; int pad; };   // units of the prefix stream; groups of a valid description, else 0
+
+struct GroupArgs {
+  const __nv_bfloat16* kv; const __nv_bfloat16* q; __nv_bfloat16* out;
+  const int32_t* block_table; const int32_t* seq_lens; const int32_t* group_rows; const int32_t* group_pages;
+  int32_t* counters;
+  int n, n_groups, Hq, Hkv, G, layer, max_pages, num_blocks;
+  int tokens;                       // traces whose heads fill a tile of query rows: 128 / G
+  int box;                          // traces of one copy of query rows
+  int shares, warps;                // CTAs of the prefix launch; warps of the stream launch
+  float scale_log2;
+  unsigned long long wait_ns;
+  // workspace
+  Header* header;
+  int4* groups;                     // [n_groups] first row, rows, first row that is long enough (-1: nothing shared), pages
+  long long* group_at;              // [n_groups] where the group's tiles begin in the prefix stream
+  int* group_of;                    // [n] the group whose pages the row shares, or -1
+  long long* own_at;                // [n + 1] own pages of the rows before
+  float *pre_ml, *pre_o;            // [share][2][lane][128] (m, l) and o of the prefix pieces that are not whole sequences
+  float *row_ml, *row_o;            // [lane][n][Hq] of those that are
+  float *own_ml, *own_o;            // [warp][2][G] of the stream's pieces that are not whole sequences
+  float *all_ml, *all_o;            // [n][Hq] of those that are, where there are shared pages besides
+};
+
+__device__ inline int length_of(const GroupArgs& a, int i, bool flag) {
+  int S = a.seq_lens[i];
+  if (S < 0) S = 0;
+  if ((long long)S > (long long)a.max_pages * kP) { S = a.max_pages * kP; if (flag) flag_error(a.counters, STEP_ERR_CAPACITY); }
+  return S;
+}
+
+// ---- the prefix stream: for every group that shares pages, for every KV head, for every block of 2 * tokens traces
+struct Shape { int tiles, blocks, last; };          // last: units per tile of a head's last block (1: at most `tokens` traces); 2 in the others
+__device__ inline Shape shape_of(const GroupArgs& a, int4 g) {
+  Shape x;
+  x.tiles = (g.w + kTile / kP - 1) / (kTile / kP);
+  x.blocks = (g.y + 2 * a.tokens - 1) / (2 * a.tokens);
+  x.last = g.y - (x.blocks - 1) * 2 * a.tokens <= a.tokens ? 1 : 2;
+  return x;
+}
+__device__ inline long long head_units(const Shape& x) {
+  return (long long)(x.blocks - 1) * (2 * x.tiles + kSetup) + x.last * x.tiles + kSetup;
+}
+
+// ---------------------------------------------------------------- 1. own pages
+__device__ inline void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ inline void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ inline void mma16816(float (&c)[4], const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+constexpr size_t kStreamSmem = 1024 + (size_t)kStreamWarps * kStages * kPageBytes + (kMaxTracesFast + 1) * 8 + kMaxTracesFast * 4 + kStreamWarps * kStages * 8;
+static_assert(kStreamSmem <= 232448 - 1024, "shared memory of one CTA");
+
+__global__ void __launch_bounds__(kStreamWarps * 32, 1) groups_stream_kernel(const __grid_constant__ GroupArgs a) {
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  unsigned char* sm = smem_raw + (base - raw);
+  long long* s_at = reinterpret_cast<long long*>(sm + kStreamWarps * kStages * kPageBytes);   // [n + 1] own pages of the rows before
+  int* s_own = reinterpret_cast<int*>(s_at + kMaxTracesFast + 1);                            // [n] pages that the row shares
+  uint64_t* s_bar = reinterpret_cast<uint64_t*>(s_own + kMaxTracesFast);
+  __shared__ long long s_sum[kStreamWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const bool first = blockIdx.x == 0;
+  dependents_may_launch();
+  const uint32_t bars = smem_u32(s_bar) + warp * kStages * 8;
+  if (lane == 0) {
+    for (int s = 0; s < kStages; ++s) mbar_init(bars + 8 * s, 1);
+    mbar_init_fence();
+  }
+  // ---- who shares what.  A description that is not in order is not followed at all.
+  bool bad = false;
+  for (int g = threadIdx.x; g < a.n_groups; g += kStreamWarps * 32) {
+    const int r0 = a.group_rows[g], r1 = a.group_rows[g + 1], pages = a.group_pages[g];
+    bad |= r0 < 0 || r1 < r0 || r1 > a.n || pages < 0 || pages > a.max_pages;
+  }
+  for (int i = threadIdx.x; i < a.n; i += kStreamWarps * 32) {
+    s_own[i] = 0;
+    if (first) a.group_of[i] = -1;
+  }
+  const int n_groups = __syncthreads_or(bad) ? 0 : a.n_groups;
+  if (first && threadIdx.x == 0 && n_groups != a.n_groups) flag_error(a.counters, STEP_ERR_INVALID_ARG);
+  for (int g = warp; g < n_groups; g += kStreamWarps) {
+    const int r0 = a.group_rows[g], r1 = a.group_rows[g + 1], pages = a.group_pages[g];
+    int members = 0, leader = -1;
+    for (int i0 = r0; i0 < r1; i0 += 32) {
+      const int i = i0 + lane;
+      const unsigned m = __ballot_sync(0xffffffffu, i < r1 && pages > 0 && length_of(a, i, false) >= (long long)pages * kP);
+      if (m && leader < 0) leader = i0 + __ffs(m) - 1;
+      members += __popc(m);
+    }
+    if (members < 2) leader = -1;
+    if (leader >= 0)
+      for (int i = r0 + lane; i < r1; i += 32)
+        if (length_of(a, i, false) >= (long long)pages * kP) {
+          s_own[i] = pages;
+          if (first) a.group_of[i] = g;
+        }
+    if (first && lane == 0) a.groups[g] = make_int4(r0, r1 - r0, leader, pages);
+  }
+  __syncthreads();
+  if (first && warp == 0) {
+    long long run = 0;
+    for (int g0 = 0; g0 < n_groups; g0 += 32) {
+      const int g = g0 + lane;
+      long long mine = 0;
+      if (g < n_groups) {
+        const int4 x = a.groups[g];
+        if (x.z >= 0) mine = head_units(shape_of(a, x)) * a.Hkv;
+      }
+      long long incl = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long u = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += u;
+      }
+      if (g < n_groups) a.group_at[g] = run + incl - mine;
+      run += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (lane == 0) *a.header = Header{run, n_groups, 0};
+  }
+  // ---- own pages of the rows before each: a thread takes `per` rows
+  {
+    const int per = (a.n + kStreamWarps * 32 - 1) / (kStreamWarps * 32), i0 = threadIdx.x * per;
+    auto pages_of = [&](int i) { return (length_of(a, i, first) + kP - 1) / kP - s_own[i]; };
+    long long mine = 0;
+    for (int i = i0; i < min(a.n, i0 + per); ++i) mine += pages_of(i);
+    long long incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long u = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += u;
+    }
+    if (lane == 31) s_sum[warp] = incl;
+    __syncthreads();
+    long long run = incl - mine;
+    for (int w = 0; w < warp; ++w) run += s_sum[w];
+    for (int i = i0; i < min(a.n, i0 + per); ++i) {
+      s_at[i] = run;
+      if (first) a.own_at[i] = run;
+      run += pages_of(i);
+      if (i == a.n - 1) { s_at[a.n] = run; if (first) a.own_at[a.n] = run; }
+    }
+  }
+  __syncthreads();
+
+  // ---- this warp's share
+  const long long total = s_at[a.n] * a.Hkv, W = div_up(total, a.warps);
+  const int me = blockIdx.x * kStreamWarps + warp;
+  const long long begin = min(total, me * W), end = min(total, begin + W);
+  if (begin >= end) return;
+  // the sequence that holds a position of the stream
+  struct Seq { int row, h, pages, own; long long at; };                // at: where it begins
+  auto seq_at = [&](long long pos) {
+    int lo = 0, hi = a.n - 1;                                          // the last row that begins at or before pos: it has pages
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (s_at[mid] * a.Hkv <= pos) lo = mid; else hi = mid - 1;
+    }
+    Seq s;
+    s.row = lo;
+    s.pages = (int)(s_at[lo + 1] - s_at[lo]);
+    s.own = s_own[lo];
+    const long long off = pos - s_at[lo] * a.Hkv;
+    s.h = off <= 0x7fffffffll ? (int)((unsigned)off / (unsigned)s.pages) : (int)(off / s.pages);
+    s.at = pos - off + (long long)s.h * s.pages;
+    return s;
+  };
+  auto next_seq = [&](Seq s) {
+    s.at += s.pages;
+    if (++s.h < a.Hkv) return s;
+    s.h = 0;
+    do ++s.row; while (s.row < a.n && s_at[s.row + 1] == s_at[s.row]);
+    if (s.row < a.n) { s.pages = (int)(s_at[s.row + 1] - s_at[s.row]); s.own = s_own[s.row]; }
+    return s;
+  };
+
+  // ---- the copies: up to kStages pages ahead.  Lane i holds the blocks of pages win + i of the sequence; those of the window
+  // behind are asked for when a window is entered.
+  const uint32_t ring = base + warp * kStages * kPageBytes;
+  Seq ps = seq_at(begin);
+  long long ppos = begin;
+  int win = 0, ids = 0, ids_next = 0, put = 0;
+  auto load_ids = [&](const Seq& s, int w) {
+    return w + lane < s.pages ? a.block_table[(size_t)s.row * a.max_pages + s.own + w + lane] : 0;
+  };
+  auto enter = [&](int page) { win = page; ids = load_ids(ps, win); ids_next = load_ids(ps, win + 32); };
+  enter((int)(ppos - ps.at));
+  auto issue = [&]() {
+    if (ppos >= end) return;
+    int page = (int)(ppos - ps.at);
+    if (page == ps.pages) { ps = next_seq(ps); page = 0; enter(0); }
+    if (page - win >= 32) { win += 32; ids = ids_next; ids_next = load_ids(ps, win + 32); }
+    int b = __shfl_sync(0xffffffffu, ids, page - win);
+    if (b < 0 || b >= a.num_blocks) { if (lane == 0) flag_error(a.counters, STEP_ERR_BAD_BLOCK); b = 0; }
+    if (lane == 0) {
+      mbar_expect_tx(bars + 8 * put, kPageBytes);
+      bulk_load(ring + put * kPageBytes, a.kv + (((size_t)a.layer * a.num_blocks + b) * a.Hkv + ps.h) * (2 * kP * kD), kPageBytes, bars + 8 * put);
+    }
+    if (++put == kStages) put = 0;
+    ++ppos;
+  };
+  for (int s = 0; s < kStages; ++s) issue();
+
+  const int gr = lane >> 2, tq = lane & 3;                             // rows gr, gr + 8 and columns 2 tq, 2 tq + 1 of a tile
+  // where this lane's address of an ldmatrix points, for K (chunk 2 x + kc of key kk) and V (chunk 2 x + vc of key vk)
+  const int kk = (lane >> 4) * 8 + (lane & 7), kc = (lane >> 3) & 1, vk = ((lane >> 3) & 1) * 8 + (lane & 7), vc = lane >> 4;
+  const bool upper = a.G > 8;                                          // (rows from 8 on are heads too)
+  int get = 0;
+  long long used = begin;                                              // pages done with
+  uint32_t ph = 0;
+  Seq s = seq_at(begin);
+  bool ok = true;
+  for (long long pos = begin; pos < end && ok;) {
+    const int page0 = (int)(pos - s.at), cnt = (int)min((long long)(s.pages - page0), end - pos);
+    const int S = length_of(a, s.row, false) - s.own * kP;             // own positions
+    const __nv_bfloat16* q = a.q + ((size_t)s.row * a.Hq + (size_t)s.h * a.G) * kD;
+    uint32_t qf[8][4];
+#pragma unroll
+    for (int x = 0; x < 8; ++x)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const int r = gr + (y & 1) * 8;
+        qf[x][y] = r < a.G ? __ldg(reinterpret_cast<const uint32_t*>(q + (size_t)r * kD + x * 16 + (y >> 1) * 8 + tq * 2)) : 0u;
+      }
+    float o[16][4] = {};
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    for (int p = page0; p < page0 + cnt; ++p) {
+      if (!__all_sync(0xffffffffu, mbar_wait_bounded(bars + 8 * get, ph, a.wait_ns))) { ok = false; break; }
+      const uint32_t pg = ring + get * kPageBytes;
+      const int rows = S - p * kP;                                     // positions in this page and behind
+      if (rows < kP) {                                                 // what a page holds behind the last position takes no part
+        unsigned char* v = sm + (pg - base) + kP * kD * 2;
+        for (int x = rows * 16 + lane; x < kP * 16; x += 32) *reinterpret_cast<uint4*>(v + x * 16) = make_uint4(0, 0, 0, 0);
+        fence_async_smem();                                            // (the slot's next page is written by the copy engine)
+        __syncwarp();
+      }
+      float sc[2][4] = {};
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        uint32_t b[4];
+        const int c = 2 * x + kc;
+        ldsm4(b, pg + kk * 256 + ((c & 8) | ((c ^ kk) & 7)) * 16);
+        mma16816(sc[0], qf[x], b[0], b[1]);
+        mma16816(sc[1], qf[x], b[2], b[3]);
+      }
+      float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          sc[y][z] *= a.scale_log2;
+          if (rows < kP && y * 8 + tq * 2 + (z & 1) >= rows) sc[y][z] = -INFINITY;
+          mx[z >> 1] = fmaxf(mx[z >> 1], sc[y][z]);
+        }
+      uint32_t pf[4];
+      float corr[2];
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        if (z == 1 && !upper) { corr[1] = 1.f; pf[1] = pf[3] = 0u; break; }
+        mx[z] = fmaxf(mx[z], __shfl_xor_sync(0xffffffffu, mx[z], 1));
+        mx[z] = fmaxf(mx[z], __shfl_xor_sync(0xffffffffu, mx[z], 2));
+        const float mn = fmaxf(m[z], mx[z]), off = mn == -INFINITY ? 0.f : mn;
+        corr[z] = exp2f(m[z] - off);
+        m[z] = mn;
+        const float p0 = exp2f(sc[0][2 * z] - off), p1 = exp2f(sc[0][2 * z + 1] - off);
+        const float p2 = exp2f(sc[1][2 * z] - off), p3 = exp2f(sc[1][2 * z + 1] - off);
+        l[z] = l[z] * corr[z] + ((p0 + p1) + (p2 + p3));
+        pf[z] = pack2(p0, p1);                                         // (rounded for the second product, whose V is bf16; the sum is not)
+        pf[2 + z] = pack2(p2, p3);
+      }
+      if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) { o[x][0] *= corr[0]; o[x][1] *= corr[0]; o[x][2] *= corr[1]; o[x][3] *= corr[1]; }
+      }
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        uint32_t b[4];
+        const int c = 2 * x + vc;
+        ldsm4_t(b, pg + kP * kD * 2 + vk * 256 + ((c & 8) | ((c ^ vk) & 7)) * 16);
+        mma16816(o[2 * x], pf, b[0], b[1]);
+        mma16816(o[2 * x + 1], pf, b[2], b[3]);
+      }
+      if (++get == kStages) { get = 0; ph ^= 1; }
+      __syncwarp();                                                    // all lanes have read the page
+      ++used;
+      issue();
+    }
+    if (!ok) break;
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      l[z] += __shfl_xor_sync(0xffffffffu, l[z], 1);
+      l[z] += __shfl_xor_sync(0xffffffffu, l[z], 2);
+    }
+    const bool whole = cnt == s.pages;
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      const int r = gr + z * 8;
+      if (r >= a.G) continue;
+      const size_t row = (size_t)s.row * a.Hq + (size_t)s.h * a.G + r;
+      if (whole && s.own == 0) {
+        const float inv = 1.f / l[z];
+        uint32_t* out = reinterpret_cast<uint32_t*>(a.out + row * kD) + tq;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) out[x * 4] = pack2(o[x][2 * z] * inv, o[x][2 * z + 1] * inv);
+      } else {
+        const size_t slot = whole ? row : ((size_t)me * 2 + (s.at <= begin ? 0 : 1)) * a.G + r;
+        float2* po = reinterpret_cast<float2*>((whole ? a.all_o : a.own_o) + slot * kD) + tq;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) po[x * 4] = make_float2(o[x][2 * z], o[x][2 * z + 1]);
+        if (tq == 0) reinterpret_cast<float2*>(whole ? a.all_ml : a.own_ml)[slot] = make_float2(m[z], l[z]);
+      }
+    }
+    pos += cnt;
+    if (pos < end) s = next_seq(s);
+  }
+  if (!ok) {
+    // a wait has run out: the copies in flight still write this CTA's shared memory
+    flag_error(a.counters, STEP_ERR_TIMEOUT);
+    if (lane == 0)
+      for (; used < ppos; ++used) {
+        mbar_wait_bounded(bars + 8 * get, ph, kDrainNs);
+        if (++get == kStages) { get = 0; ph ^= 1; }
+      }
+    __syncwarp();
+  }
+}
+
+// ---------------------------------------------------------------- 2. shared pages
+struct Place { int g, hb, at; int4 grp; Shape x; };   // sequence hb = head * blocks + block of group g; at: units into it, kSetup counted first
+__device__ inline int width_of(const Place& p) { return p.hb % p.x.blocks == p.x.blocks - 1 ? p.x.last : 2; }
+__device__ inline int units_of(const Place& p) { return width_of(p) * p.x.tiles + kSetup; }
+// What a share that ends at `end` holds of the sequence at place p (stream position pos): the tiles that begin in it.
+struct Part { int tile0, cnt; long long len; };
+__device__ inline Part part_of(const Place& p, long long pos, long long end) {
+  const int w = width_of(p);
+  Part x;
+  x.len = min((long long)(units_of(p) - p.at), end - pos);
+  x.tile0 = (max(0, p.at - kSetup) + w - 1) / w;
+  x.cnt = (max(0, (int)(p.at + x.len) - kSetup) + w - 1) / w - x.tile0;
+  return x;
+}
+__device__ inline long long share_units(const GroupArgs& a, long long total) { return max(2ll, div_up(total, a.shares)); }   // (a wide tile begins in every share)
+// One warp: the group that position pos of the stream (pos < total) lies in.
+__device__ inline Place locate(const GroupArgs& a, int n_groups, long long pos, int lane) {
+  int g = 0;
+  for (int g0 = 0; g0 < n_groups; g0 += 32) {           // the last that begins at or before pos: it has tiles
+    const unsigned m = __ballot_sync(0xffffffffu, g0 + lane < n_groups && a.group_at[g0 + lane] <= pos);
+    if (!m) break;
+    g = g0 + 31 - __clz(m);
+    if (m != 0xffffffffu) break;
+  }
+  Place p;
+  p.g = g;
+  p.grp = a.groups[g];
+  p.x = shape_of(a, p.grp);
+  const long long off = pos - a.group_at[g], head = head_units(p.x);
+  const int h = (int)(off / head), wide = 2 * p.x.tiles + kSetup, in = (int)(off - h * head);
+  const int block = min(in / wide, p.x.blocks - 1);
+  p.hb = h * p.x.blocks + block;
+  p.at = in - block * wide;
+  return p;
+}
+// The place behind a whole rest of a sequence.
+__device__ inline void next_sequence(const GroupArgs& a, int n_groups, Place& p) {
+  p.at = 0;
+  if (++p.hb < a.Hkv * p.x.blocks) return;
+  p.hb = 0;
+  while (++p.g < n_groups) {
+    p.grp = a.groups[p.g];
+    if (p.grp.z >= 0) { p.x = shape_of(a, p.grp); return; }
+  }
+}
+// A piece, as the query warp announces it: tiles [tile0, tile0 + cnt) of the sequence's `tiles`, for rows of traces
+// [row0, row0 + rows).
+struct Piece { int h, row0, rows, two, tile0, cnt, tiles, keys, slot; };
+
+__global__ void __launch_bounds__(kThreads, 1) groups_prefix_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ GroupArgs a) {
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  unsigned char* sm = smem_raw + (base - raw);
+  const uint32_t sm_q = base, sm_ring = base + 2 * kQBytes;
+  uint64_t* s_bar = reinterpret_cast<uint64_t*>(sm + 2 * kQBytes + kSlots * kSlotBytes);
+  Piece* s_piece = reinterpret_cast<Piece*>(s_bar + 32);               // [2]
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_piece + 2);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
+  int* s_begun = reinterpret_cast<int*>(s_tmem + 4);                   // [3] how many fills of their buffers the K, V and query warps have begun
+  const uint32_t bars = smem_u32(s_bar);
+  const uint32_t bar_full = bars, bar_empty = bars + 8 * kSlots;
+  const uint32_t bar_q = bars + 16 * kSlots, bar_s = bar_q + 8, bar_p = bar_s + 16, bar_o = bar_p + 32,
+                 bar_qfree = bar_o + 16, bar_drain = bar_qfree + 8;
+
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+  dependents_may_launch();
+  if (threadIdx.x == 0) {
+    prefetch_map(&map);
+    prefetch_map(&map_q);
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(bar_full + 8 * s, 1);               // the fetching warp's announcement of bytes
+      mbar_init(bar_empty + 8 * s, 1);              // tcgen05.commit
+    }
+    mbar_init(bar_q, 1);                            // the query warp's announcement
+    mbar_init(bar_qfree, 9);                        // tcgen05.commit: a piece's last scores; all softmax warps have begun it
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(bar_s + 8 * s, 1);                  // tcgen05.commit: scores made (and the products before them done)
+      mbar_init(bar_p + 8 * s, 4);                  // the second half of the probabilities (one arrival per warp)
+      mbar_init(bar_p + 16 + 8 * s, 4);             // the first half
+      mbar_init(bar_o + 8 * s, 1);                  // tcgen05.commit: a piece's last product
+    }
+    mbar_init(bar_drain, 1);
+    *s_abort = 0;
+    s_begun[0] = s_begun[1] = s_begun[2] = 0;
+    mbar_init_fence();
+  }
+  if (warp == kWarpMma) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *s_tmem;
+  wait_for_primary();                               // the groups, as the stream kernel found them
+  // this CTA's share of the stream
+  const Header hd = *a.header;
+  const long long W = share_units(a, hd.units), pos0 = min(hd.units, blockIdx.x * W), end = min(hd.units, pos0 + W);
+
+  auto wait = [&](uint32_t bar, uint32_t parity) {
+    if (mbar_test_wait(bar, parity)) return true;                      // (a limit of zero: this is all)
+    if (*s_abort) return false;
+    if (mbar_wait_bounded(bar, parity, a.wait_ns)) return true;
+    flag_error(a.counters, STEP_ERR_TIMEOUT);
+    *s_abort = 1;
+    return false;
+  };
+  // the same, with one answer for the whole warp: what follows has to be executed by all of it
+  auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
+  // one arrival for all of the warp's threads
+  auto arrive_warp = [&](uint32_t bar) { __syncwarp(); if (lane == 0) mbar_arrive(bar); };
+
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+    // ------------------------------------------------ softmax: lane `ln` of the CTA, row `row` of its 128
+    const int ln = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t t_s = t_row + ln * 128, t_o = t_row + 256 + ln * 128;
+    uint32_t ph_s = 0, ph_piece = 0;
+    for (;;) {
+      if (!wait_warp(bar_q, ph_piece)) break;
+      const Piece pc = s_piece[ph_piece];
+      if (pc.cnt == 0) break;                                          // the share is done
+      arrive_warp(bar_qfree);
+      float m_ref = -INFINITY, l = 0.f;
+      bool started = false, ok = true;
+      for (int i = pc.two ? 0 : ln; i < pc.cnt; i += pc.two ? 1 : 2) {
+        if (!wait_warp(bar_s + 8 * ln, ph_s)) { ok = false; break; }
+        ph_s ^= 1;
+        tc_fence_after();
+        uint32_t s[128];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tc_ld32_async(t_s + 32 * c, s + 32 * c);
+        tc_wait_ld();
+        pin<128>(s);
+        const int left = pc.keys - (pc.tile0 + i) * kTile;
+        if (left < kTile) {                                            // behind the last page
+#pragma unroll
+          for (int c = 0; c < kTile; ++c)
+            if (c >= left) s[c] = 0xff800000u;
+        }
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < kTile; c += 8) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) mx[x] = max3(mx[x], __uint_as_float(s[c + 2 * x]), __uint_as_float(s[c + 2 * x + 1]));
+        }
+        const float m_new = fmaxf(m_ref, fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * a.scale_log2);
+        if (!started) {
+          m_ref = m_new;
+          started = true;
+        } else {
+          const bool grow = m_new > m_ref + kRescale;
+          if (__any_sync(0xffffffffu, grow)) {
+            const float corr = grow ? exp2f(m_ref - m_new) : 1.f;
+            if (grow) m_ref = m_new;
+            l *= corr;
+#pragma unroll 1
+            for (int c = 0; c < kD; c += 32) {
+              uint32_t o[32];
+              tc_ld32_async(t_o + c, o);
+              tc_wait_ld();
+              pin<32>(o);
+#pragma unroll
+              for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * corr);
+              tc_st32(t_o + c, o);
+            }
+          }
+        }
+        const float off = m_ref == -INFINITY ? 0.f : m_ref;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        // in halves: the second product of the first 64 keys runs while the others' probabilities are made
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+          for (int c = half * 64; c < half * 64 + 64; c += 2) {
+            float p0, p1;
+            fma2(p0, p1, __uint_as_float(s[c]), __uint_as_float(s[c + 1]), a.scale_log2, -off);
+            p0 = exp2f(p0);
+            p1 = exp2f(p1);
+            add2(sum[c & 2], sum[(c & 2) + 1], p0, p1);
+            s[c / 2] = pack2(p0, p1);
+          }
+          tc_st32(t_s + half * 32, s + half * 32);
+          tc_wait_st();
+          tc_fence_before();
+          arrive_warp(bar_p + 8 * (half == 0 ? 2 + ln : ln));
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      }
+      if (!ok || !wait_warp(bar_o + 8 * ln, ph_piece)) break;
+      tc_fence_after();
+      ph_piece ^= 1;
+
+      // ---- the piece is done: its rows' (m, l) and o
+      const int t = (pc.two ? ln * a.tokens : 0) + row / a.G;           // trace of the block
+      const bool mine = row < a.tokens * a.G && t < pc.rows, some = pc.two || ln < pc.cnt;   // a piece of one tile leaves lane 1 without any
+      const bool whole = pc.cnt == pc.tiles;
+      const size_t at = whole ? ((size_t)(pc.two ? 0 : ln) * a.n + pc.row0 + (mine ? t : 0)) * a.Hq + (size_t)pc.h * a.G + row % a.G
+                              : (((size_t)blockIdx.x * 2 + pc.slot) * 2 + ln) * kHalfRows + row;
+      if (mine) reinterpret_cast<float2*>(whole ? a.row_ml : a.pre_ml)[at] = make_float2(m_ref, l);
+      float* o_out = (whole ? a.row_o : a.pre_o) + at * kD;
+      if (some) {
+#pragma unroll
+        for (int c = 0; c < kD; c += 64) {
+          uint32_t o[64];
+          tc_ld32_async(t_o + c, o);
+          tc_ld32_async(t_o + c + 32, o + 32);
+          tc_wait_ld();
+          pin<64>(o);
+          if (mine) {
+#pragma unroll
+            for (int x = 0; x < 64; x += 8) st_global32(o_out + c + x, o + x);
+          }
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
+    if (warp == kWarpK || warp == kWarpV) {
+      // ------------------------------------------------ K or V tiles into their ring
+      const int kv = warp == kWarpV, ring0 = kv ? kKSlots : 0, ring_n = kv ? kVSlots : kKSlots;
+      int slot = 0, begun = 0;                                         // (fills begun)
+      uint32_t ph = 1;
+      bool ok = true;
+      // Block ids of 64 pages (eight tiles): lane i holds those of pages win + i and win + 32 + i.  The second half is asked
+      // for when the first is entered, four tiles before it is needed.
+      auto load_ids = [&](const Place& of, int first) {
+        const int page = first + lane;
+        return of.g < hd.groups && page < of.grp.w ? a.block_table[(size_t)of.grp.z * a.max_pages + page] : 0;
+      };
+      long long pos = pos0;
+      if (pos < end) {
+        Place pl = locate(a, hd.groups, pos, lane);
+        Part part = part_of(pl, pos, end);
+        int win = (part.tile0 * (kTile / kP)) & ~31;
+        int next0 = load_ids(pl, win), next1 = load_ids(pl, win + 32);
+        while (pos < end && ok) {
+          part = part_of(pl, pos, end);
+          const int h = pl.hb / pl.x.blocks, all = pl.grp.w;
+          win = (part.tile0 * (kTile / kP)) & ~31;
+          int ids0 = next0, ids1 = next1;
+          Place nx = pl;                                               // the sequence behind this one, its block ids too
+          next_sequence(a, hd.groups, nx);
+          next0 = load_ids(nx, 0);
+          next1 = load_ids(nx, 32);
+          for (int i = 0; i < part.cnt; ++i) {
+            const int pg0 = (part.tile0 + i) * (kTile / kP);
+            if (!wait_warp(bar_empty + 8 * (ring0 + slot), ph)) { ok = false; break; }
+            const uint32_t bar = bar_full + 8 * (ring0 + slot), dst = sm_ring + (ring0 + slot) * kSlotBytes;
+            if (pg0 >= win + 32) { win += 32; ids0 = ids1; ids1 = load_ids(pl, win + 32); }
+            const int in_win = pg0 - win, pages = min(kTile / kP, all - pg0);
+            int bb = __shfl_sync(0xffffffffu, ids0, (in_win + (lane & 7)) & 31);
+            if (lane < pages && (bb < 0 || bb >= a.num_blocks)) { flag_error(a.counters, STEP_ERR_BAD_BLOCK); bb = 0; }
+            if (lane == 0) mbar_expect_tx(bar, pages * (kP * kD * 2));
+            __syncwarp();
+            if (lane < pages)                                          // a box is the K or the V of a page
+              tma_load_4d(dst + lane * (kP * kD * 2), &map, 0, 0, 0, ((((a.layer * a.num_blocks) + bb) * a.Hkv + h) * 2 + kv) * (kP / 8), bar);
+            __syncwarp();
+            ++begun;
+            if (++slot == ring_n) { slot = 0; ph ^= 1; }
+          }
+          pos += part.len;
+          pl = nx;
+        }
+      }
+      if (lane == 0) s_begun[kv] = begun;
+    } else if (warp == kWarpQ) {
+      // ------------------------------------------------ query rows of one piece after another
+      uint32_t par = 0;
+      int begun = 0;
+      long long pos = pos0;
+      Place pl = {};
+      if (pos < end) pl = locate(a, hd.groups, pos, lane);
+      for (;; par ^= 1) {
+        Piece pc = {};
+        while (pos < end && pc.cnt == 0) {
+          const Part part = part_of(pl, pos, end);
+          if (part.cnt > 0) {
+            const int block = pl.hb % pl.x.blocks, t0 = block * 2 * a.tokens;
+            pc.h = pl.hb / pl.x.blocks;
+            pc.row0 = pl.grp.x + t0; pc.rows = min(2 * a.tokens, pl.grp.y - t0);
+            pc.two = width_of(pl) == 2;
+            pc.tile0 = part.tile0; pc.cnt = part.cnt; pc.tiles = pl.x.tiles; pc.keys = pl.grp.w * kP;
+            pc.slot = pos - pl.at <= pos0 ? 0 : 1;                     // of the share: does the sequence begin inside it?
+          }
+          pos += part.len;
+          next_sequence(a, hd.groups, pl);
+        }
+        // the scores of the piece before are made, and its announcement has been read (the very first wait passes at once)
+        if (!wait_warp(bar_qfree, par ^ 1)) break;
+        if (lane == 0) {
+          s_piece[par] = pc;
+          if (pc.cnt > 0) {
+            // (rows of other groups may come along: a row of the products depends on its own query only)
+            const int halves = pc.two ? 4 : 2;
+            mbar_expect_tx(bar_q, halves * a.box * a.G * 128);
+            for (int x = 0; x < halves; ++x)
+              tma_load_3d(sm_q + (x >> 1) * kQBytes + (x & 1) * (kQBytes / 2), &map_q, (x & 1) * 64, pc.h * a.G, pc.row0 + (x >> 1) * a.tokens, bar_q);
+          } else {
+            mbar_arrive(bar_q);
+          }
+        }
+        __syncwarp();
+        if (lane == 0) s_begun[2] = ++begun;
+        if (pc.cnt == 0) break;
+      }
+    } else {
+      // ------------------------------------------------ products.  The tensor cores take the next few instructions only, so
+      // every cycle this warp spends between them is idle time there.  Hence: the warp stays together and one thread is
+      // elected for the instructions, and what is likely there long since is waited for before what is not.
+      const uint32_t id_qk = umma_idesc_bf16(kTile), id_pv = umma_idesc_bf16(kD) | (1u << 16);   // B of the second is MN-major
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+      int at[2] = {0, 0};
+      uint32_t ph[2] = {0, 0}, ph_q = 0, ph_p[2] = {0, 0};
+      bool ok = true;
+      // waits for the next tile of K (0) or V (1); its slot
+      auto next = [&](int kv) -> int {
+        const int s = (kv ? kKSlots : 0) + at[kv];
+        ok = ok && wait_warp(bar_full + 8 * s, ph[kv]);
+        if (++at[kv] == (kv ? kVSlots : kKSlots)) { at[kv] = 0; ph[kv] ^= 1; }
+        return s;
+      };
+      auto probabilities = [&](int ln, bool first_half) {
+        ok = ok && wait_warp(bar_p + 8 * (first_half ? 2 + ln : ln), ph_p[ln]);
+        if (!first_half) ph_p[ln] ^= 1;
+        tc_fence_after();
+      };
+      // (the elected thread's part of it)
+      auto scores = [&](int ln, int q, int s) {
+        const uint32_t qa = sm_q + q * kQBytes, kb = sm_ring + s * kSlotBytes;
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+          tc_mma_bf16(tm + ln * 128, umma_desc_sw128(qa + (x >> 2) * (kQBytes / 2) + (x & 3) * 32),
+                      umma_desc_k(kb + (x >> 2) * 1024 + (x & 3) * 32), id_qk, x != 0);
+        tc_commit(bar_s + 8 * ln);
+      };
+      // steps of 16 keys; those of a tile behind the last page are left out, so nothing that lies there matters
+      auto values = [&](int ln, int s, bool first, int from, int steps) {
+        const uint32_t vb = sm_ring + s * kSlotBytes;
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+          if (x >= from && x < steps) tc_mma_bf16_ta(tm + 256 + ln * 128, tm + ln * 128 + x * 8, umma_desc_v(vb + x * 4096), id_pv, !(first && x == 0));
+      };
+      while (ok) {
+        ok = wait_warp(bar_q, ph_q);
+        const Piece pc = s_piece[ph_q];
+        const int cnt = pc.cnt, keys = pc.keys - pc.tile0 * kTile;
+        auto steps = [&](int i) { return min(8, (keys - i * kTile) / 16); };
+        ph_q ^= 1;
+        if (!ok || cnt == 0) break;
+        tc_fence_after();
+        if (pc.two) {
+          int k = next(0);
+          if (ok && elect_one()) {
+            scores(0, 0, k);
+            scores(1, 1, k);
+            tc_commit(bar_empty + 8 * k);
+            if (cnt == 1) tc_commit(bar_qfree);
+          }
+          __syncwarp();
+          for (int i = 0; i < cnt && ok; ++i) {
+            const int v = next(1);
+            const bool more = i + 1 < cnt;
+            if (more) k = next(0);
+            probabilities(0, true);
+            if (ok && elect_one()) values(0, v, i == 0, 0, min(4, steps(i)));
+            __syncwarp();
+            probabilities(0, false);
+            if (ok && elect_one()) {
+              values(0, v, i == 0, 4, steps(i));
+              if (more) scores(0, 0, k); else tc_commit(bar_o);
+            }
+            __syncwarp();
+            probabilities(1, true);
+            if (ok && elect_one()) values(1, v, i == 0, 0, min(4, steps(i)));
+            __syncwarp();
+            probabilities(1, false);
+            if (ok && elect_one()) {
+              values(1, v, i == 0, 4, steps(i));
+              tc_commit(bar_empty + 8 * v);
+              if (more) { scores(1, 1, k); tc_commit(bar_empty + 8 * k); } else tc_commit(bar_o + 8);
+              if (i + 2 == cnt) tc_commit(bar_qfree);
+            }
+            __syncwarp();
+          }
+        } else {
+          for (int i = 0; i < min(cnt, 2); ++i) {
+            const int k = next(0);
+            if (ok && elect_one()) {
+              scores(i, 0, k);
+              tc_commit(bar_empty + 8 * k);
+              if (i + 1 == cnt) tc_commit(bar_qfree);
+            }
+            __syncwarp();
+          }
+          for (int i = 0; i < cnt && ok; ++i) {
+            const int ln = i & 1, v = next(1);
+            probabilities(ln, true);
+            if (ok && elect_one()) values(ln, v, i < 2, 0, min(4, steps(i)));
+            __syncwarp();
+            probabilities(ln, false);
+            if (ok && elect_one()) {
+              values(ln, v, i < 2, 4, steps(i));
+              tc_commit(bar_empty + 8 * v);
+              if (i + 2 >= cnt) tc_commit(bar_o + 8 * ln);
+              if (cnt == 1) tc_commit(bar_o + 8);                      // lane 1 has nothing to do
+            }
+            __syncwarp();
+            if (i + 2 < cnt) {
+              const int k = next(0);
+              if (ok && elect_one()) {
+                scores(ln, 0, k);
+                tc_commit(bar_empty + 8 * k);
+                if (i + 3 == cnt) tc_commit(bar_qfree);
+              }
+              __syncwarp();
+            }
+          }
+        }
+      }
+      __syncwarp();
+      if (elect_one()) {
+        tc_commit(bar_drain);                                          // no product is in flight when the tensor memory goes back
+        mbar_wait_bounded(bar_drain, 0);
+      }
+      __syncwarp();
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  // A wait has run out: copies in flight still write this CTA's shared memory.  (Decided here, where no warp can begin one any
+  // more and *s_abort is final.)
+  if (*s_abort) {
+    // fills 0, 1, 2, .. of a barrier complete its phases in that order: the last one's parity
+    auto landed = [&](uint32_t bar, int fills) { if (fills > 0) mbar_wait_bounded(bar, (fills - 1) & 1, kDrainNs); };
+    const int begun = warp == kWarpK ? s_begun[0] : (warp == kWarpV ? s_begun[1] : s_begun[2]);
+    if (lane == 0 && warp == kWarpK)
+      for (int s = 0; s < kKSlots; ++s) landed(bar_full + 8 * s, (begun - s + kKSlots - 1) / kKSlots);
+    if (lane == 0 && warp == kWarpV)
+      for (int s = 0; s < kVSlots; ++s) landed(bar_full + 8 * (kKSlots + s), (begun - s + kVSlots - 1) / kVSlots);
+    if (lane == 0 && warp == kWarpQ) landed(bar_q, begun);
+    __syncthreads();
+  }
+  if (warp == kWarpMma) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+constexpr size_t kPrefixSmem = 1024 + 2 * kQBytes + kSlots * kSlotBytes + 32 * 8 + 2 * sizeof(Piece) + 64;
+static_assert(kPrefixSmem <= 232448, "shared memory of one CTA");
+
+// ---------------------------------------------------------------- 3. one result per row
+constexpr int kMergeWarps = 4;
+
+// A warp per query row, lanes over the 128 dims: the shared pages' pieces, then the row's own, in stream order with a running
+// (max, sum, values).
+__global__ void __launch_bounds__(kMergeWarps * 32) groups_merge_kernel(const __grid_constant__ GroupArgs a) {
+  const int lane = threadIdx.x & 31;
+  wait_for_primary();
+  const Header hd = *a.header;
+  const long long total = a.own_at[a.n] * a.Hkv, W = div_up(total, a.warps), Wp = share_units(a, hd.units);
+  for (int r = blockIdx.x * kMergeWarps + (threadIdx.x >> 5); r < a.n * a.Hq; r += gridDim.x * kMergeWarps) {
+    const int i = r / a.Hq, hq = r - i * a.Hq, h = hq / a.G, sub = hq - h * a.G;
+    const int g = a.group_of[i];
+    const long long pages = a.own_at[i + 1] - a.own_at[i], at = a.own_at[i] * a.Hkv + h * pages;
+    const int w0 = pages > 0 ? (int)(at / W) : 0, w1 = pages > 0 ? (int)((at + pages - 1) / W) : -1;
+    if (g < 0 && w0 == w1) continue;                                   // written by the stream kernel
+    float M = -INFINITY, den = 0.f;
+    float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto take = [&](const float* mls, const float* os, size_t slot) {
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(mls) + slot);
+      const float4 o = __ldcg(reinterpret_cast<const float4*>(os + slot * kD) + lane);
+      if (ml.y == 0.f) return;                                         // a lane that had no tile: nothing stands there
+      const float Mb = fmaxf(M, ml.x), off = Mb == -INFINITY ? 0.f : Mb;
+      const float keep = exp2f(M - off), wgt = exp2f(ml.x - off);
+      den = den * keep + wgt * ml.y;
+      num.x = num.x * keep + wgt * o.x; num.y = num.y * keep + wgt * o.y;
+      num.z = num.z * keep + wgt * o.z; num.w = num.w * keep + wgt * o.w;
+      M = Mb;
+    };
+    if (g >= 0) {
+      const int4 grp = a.groups[g];
+      const Shape x = shape_of(a, grp);
+      const int t = i - grp.x, block = t / (2 * a.tokens), tb = t - block * 2 * a.tokens;
+      const int w = block == x.blocks - 1 ? x.last : 2;
+      const long long tile0 = a.group_at[g] + h * head_units(x) + (long long)block * (2 * x.tiles + kSetup) + kSetup;
+      const int p0 = (int)(tile0 / Wp), p1 = (int)((tile0 + (long long)w * (x.tiles - 1)) / Wp);
+      if (p0 == p1) {
+        take(a.row_ml, a.row_o, r);
+        if (w == 1) take(a.row_ml, a.row_o, (size_t)a.n * a.Hq + r);
+      } else {
+        const int ln = w == 2 ? tb / a.tokens : 0, row = (tb - ln * a.tokens) * a.G + sub;
+#pragma unroll 4
+        for (int s = p0; s <= p1; ++s) {
+          const size_t slot = (((size_t)s * 2 + (tile0 - kSetup <= s * Wp ? 0 : 1)) * 2 + ln) * kHalfRows + row;
+          take(a.pre_ml, a.pre_o, slot);
+          if (w == 1) take(a.pre_ml, a.pre_o, slot + kHalfRows);
+        }
+      }
+    }
+    if (w0 == w1) {
+      take(a.all_ml, a.all_o, r);
+    } else {
+#pragma unroll 2
+      for (int s = w0; s <= w1; ++s) take(a.own_ml, a.own_o, ((size_t)s * 2 + (at <= s * W ? 0 : 1)) * a.G + sub);
+    }
+    const float inv = g < 0 && pages == 0 ? 0.f : 1.f / den;           // a row without any key: zeros
+    reinterpret_cast<uint2*>(a.out + (size_t)r * kD)[lane] = make_uint2(pack2(num.x * inv, num.y * inv), pack2(num.z * inv, num.w * inv));
+  }
+}
+
+// Lays the workspace out (from `ws` on; null: only its size).
+size_t lay_out(const step_pool* pool, int n, int n_groups, char* ws, GroupArgs* a) {
+  const Geo g = geo_of(pool);
+  const size_t shares = pool->num_sms, warps = shares * kStreamWarps, rows = (size_t)n * g.Hq;
+  size_t off = 0;
+  auto take = [&](size_t bytes) { char* p = ws + off; off += (bytes + 255) / 256 * 256; return p; };
+  GroupArgs x = {};
+  x.header = (Header*)take(sizeof(Header));
+  x.groups = (int4*)take((size_t)n_groups * sizeof(int4));
+  x.group_at = (long long*)take((size_t)n_groups * 8);
+  x.group_of = (int*)take((size_t)n * 4);
+  x.own_at = (long long*)take((size_t)(n + 1) * 8);
+  x.own_ml = (float*)take(warps * 2 * g.G * 8);
+  x.own_o = (float*)take(warps * 2 * g.G * kD * 4);
+  if (n_groups > 0) {
+    x.pre_ml = (float*)take(shares * 4 * kHalfRows * 8);
+    x.pre_o = (float*)take(shares * 4 * kHalfRows * kD * 4);
+    x.row_ml = (float*)take(2 * rows * 8);
+    x.row_o = (float*)take(2 * rows * kD * 4);
+    x.all_ml = (float*)take(rows * 8);
+    x.all_o = (float*)take(rows * kD * 4);
+  }
+  if (a) *a = x;
+  return off;
+}
+
+}  // namespace
+
+namespace stepk {
+
+bool groups_tc_supported(const step_pool* pool, int n) { return attention_tc_covers(pool, n); }
+
+size_t groups_tc_workspace(const step_pool* pool, int n, int n_groups) { return lay_out(pool, n, n_groups, nullptr, nullptr); }
+
+int groups_tc_launch(step_pool* pool, int layer, const void* q, const int32_t* block_table, const int32_t* seq_lens, int n,
+                     const int32_t* group_rows, const int32_t* group_pages, int n_groups, void* out, void* workspace, cudaStream_t s) {
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (!enc) return STEP_ERR_CUDA;
+  const Geo g = geo_of(pool);
+  if (!pool->groups_ready) {
+    CUtensorMap fresh;
+    static_assert(sizeof(fresh) <= sizeof(pool->tmap_kv_bytes), "tensor map");
+    if (!encode_pool_map(enc, pool, &fresh)) return STEP_ERR_CUDA;
+    memcpy(pool->tmap_kv_bytes, &fresh, sizeof(fresh));                // (the same for every kernel that uses it)
+    if (cudaFuncSetAttribute(groups_stream_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStreamSmem) != cudaSuccess ||
+        cudaFuncSetAttribute(groups_prefix_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPrefixSmem) != cudaSuccess)
+      return STEP_ERR_CUDA;
+    pool->groups_ready = true;
+  }
+  GroupArgs a;
+  lay_out(pool, n, n_groups, (char*)workspace, &a);
+  a.kv = (const __nv_bfloat16*)pool->cfg.kv_storage; a.q = (const __nv_bfloat16*)q; a.out = (__nv_bfloat16*)out;
+  a.block_table = block_table; a.seq_lens = seq_lens; a.group_rows = group_rows; a.group_pages = group_pages;
+  a.counters = pool->v.counters;
+  a.n = n; a.n_groups = n_groups; a.Hq = g.Hq; a.Hkv = g.Hkv; a.G = g.G; a.layer = layer; a.max_pages = g.max_pages; a.num_blocks = g.num_blocks;
+  a.tokens = kHalfRows / g.G;
+  a.box = a.tokens < n ? a.tokens : n;
+  a.shares = pool->num_sms;
+  a.warps = a.shares * kStreamWarps;
+  a.scale_log2 = 1.4426950408889634f / sqrtf((float)kD);
+  a.wait_ns = pool->wait_limit_ns;
+  groups_stream_kernel<<<a.shares, kStreamWarps * 32, kStreamSmem, s>>>(a);
+  if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
+  if (n_groups > 0) {
+    CUtensorMap map, map_q;
+    memcpy(&map, pool->tmap_kv_bytes, sizeof(map));
+    // queries: a box is one half of the dims of the G heads of a group, for as many traces as make a tile of rows
+    const cuuint64_t q_dims[3] = {kD, (cuuint64_t)g.Hq, (cuuint64_t)n};
+    const cuuint64_t q_strides[2] = {kD * 2, (cuuint64_t)g.Hq * kD * 2};
+    const cuuint32_t q_box[3] = {64, (cuuint32_t)g.G, (cuuint32_t)a.box}, estr[3] = {1, 1, 1};
+    if (enc(&map_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), q_dims, q_strides, q_box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return STEP_ERR_CUDA;
+    if (launch_dependent(groups_prefix_kernel, dim3(a.shares), dim3(kThreads), kPrefixSmem, s, map, map_q, a) != cudaSuccess) return STEP_ERR_CUDA;
+  }
+  const long long rows = (long long)n * g.Hq, most = 4ll * a.shares;
+  const long long ctas = (rows + kMergeWarps - 1) / kMergeWarps;
+  if (launch_dependent(groups_merge_kernel, dim3((unsigned)(ctas < most ? ctas : most)), dim3(kMergeWarps * 32), 0, s, a) != cudaSuccess) return STEP_ERR_CUDA;
+  return launch_ok();
+}
+
+}  // namespace stepk

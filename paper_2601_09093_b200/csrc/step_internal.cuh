@@ -88,9 +88,9 @@ struct step_pool {
   alignas(64) unsigned char tmap_h_bytes[128];
   const void* tmap_h_ptr; int tmap_h_D, tmap_h_M;
   bool tc_smem_set;   // the scorer kernel's dynamic shared memory limit has been raised on this pool's device
-  // the tensor map of the whole pool (tree attention), and whether its kernels' shared memory limits have been raised
+  // the tensor map of the whole pool (tree and group attention), and whether their kernels' shared memory limits have been raised
   alignas(64) unsigned char tmap_kv_bytes[128];
-  bool tree_ready;
+  bool tree_ready, groups_ready;
   int device;
   stepk::MetaLayout lay;
   stepk::DevViews v;
@@ -204,5 +204,11 @@ size_t tree_tc_workspace(const step_pool* pool, int T);
 int tree_tc_launch(step_pool* pool, int layer, const void* q, const void* k_draft, const void* v_draft, const int32_t* parents,
                    const int32_t* n_nodes, int T, const int32_t* block_table, const int32_t* seq_lens, int n, void* out,
                    void* workspace, cudaStream_t s);
+
+// ---- tensor-core attention of groups of traces (groups_tc.cu)
+bool groups_tc_supported(const step_pool* pool, int n);
+size_t groups_tc_workspace(const step_pool* pool, int n, int n_groups);
+int groups_tc_launch(step_pool* pool, int layer, const void* q, const int32_t* block_table, const int32_t* seq_lens, int n,
+                     const int32_t* group_rows, const int32_t* group_pages, int n_groups, void* out, void* workspace, cudaStream_t s);
 
 }  // namespace stepk

@@ -45,8 +45,7 @@
 // begins anything more, the products in flight are waited for, and when all warps are through and nothing new can start, so
 // is every copy that was begun (each with a limit of its own).  Only then is the shared memory given up.
 #include "attention_rows.cuh"
-#include "async_copy.cuh"
-#include "tensor_core.cuh"
+#include "attention_tc.cuh"
 
 #include <string.h>
 
@@ -54,11 +53,7 @@ using namespace stepk;
 
 namespace {
 
-constexpr int kP = 16, kD = 128;
-constexpr int kTile = 128;                        // keys per tile
 constexpr int kSetup = 4;                         // tiles' worth of time that a sequence takes besides its tiles (see above)
-constexpr int kSlotBytes = kTile * kD * 2;        // K or V of one tile
-constexpr int kQBytes = kHalfRows * kD * 2;       // 128 query rows, same arrangement
 constexpr int kKSlots = 2, kVSlots = 3, kSlots = kKSlots + kVSlots;   // rings of K and of V tiles, 160 KiB: a V tile waits for its softmax
 constexpr int kXCols = 16;                        // columns per round in which the lanes exchange their sums (below 128 rows)
 constexpr int kXBytes = 2 * kXCols * kHalfRows * 4;
@@ -114,10 +109,6 @@ __device__ inline Shape shape_of(const TreeArgs& a, int t, bool flag) {
 }
 // The stream: for every trace, for every KV head, for every row group, the sequence's tiles.  A warp's place in it:
 struct Place { int t, hr, at; Shape x; };   // at: how far into the sequence, its kSetup counted first
-// (64-bit divisions take hundreds of cycles and stand in front of a small call's first copies)
-__device__ inline long long div_up(long long x, int by) {
-  return x + by <= 0x7fffffffll ? (long long)((unsigned)(x + by - 1) / (unsigned)by) : (x + by - 1) / by;
-}
 // One warp: `total` tiles in all, W tiles per share; the place of position pos_of(W) if that lies inside the stream (else
 // t = -1).  The first 32 traces' shapes are read once.
 template <typename PosOf>
@@ -189,114 +180,9 @@ struct Piece {
   unsigned long long odd;         // its drafted tokens whose v holds an infinity or a NaN
 };
 
-// ---- instructions
-// One thread of a warp that is together (the same one every time).
-__device__ inline bool elect_one() {
-  uint32_t p;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
-  return p != 0;
-}
-__device__ inline void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
-__device__ inline void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
-}
-__device__ inline void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
-      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
-}
-__device__ inline void mbar_arrive_n(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-// 16 bytes, or 16 zero bytes (src is then not read)
-__device__ inline void cp_async16_or_zero(uint32_t dst, const void* src, bool real) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
-}
-// 32 columns of this thread's TMEM lane, without waiting for them
-__device__ inline void tc_ld32_async(uint32_t taddr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr) : "memory");
-}
-__device__ inline void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-// The values of an asynchronous load may be used only behind the wait: ties them to this place.
-template <int N> __device__ inline void pin(uint32_t* r) {
-#pragma unroll
-  for (int i = 0; i < N; i += 8)
-    asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
-}
-__device__ inline void tc_st32(uint32_t taddr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
-      :: "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-         "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-         "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-         "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]),
-         "r"(taddr) : "memory");
-}
-__device__ inline void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// D[tmem] (+)= A[tmem] * B[smem]
-__device__ inline void tc_mma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
-}
 // A K or V tile in a ring slot: groups of 8 rows (tokens), a group as two halves of 8 rows x 128 bytes with the 128-byte
 // swizzle.  Byte offset of 16-byte chunk `at` (0 .. 15, as stored) of row rr:
 __device__ inline uint32_t tile_chunk(int rr, int at) { return (rr >> 3) * 2048 + (at >> 3) * 1024 + (rr & 7) * 128 + (at & 7) * 16; }
-// K as a K-major operand: the next 8 keys (N) are 2048 bytes further; dims from 64 on start 1024 bytes further.
-__device__ inline uint64_t umma_desc_k(uint32_t smem_addr) {
-  const uint32_t lo = ((smem_addr >> 4) & 0x3FFFu) | (1u << 16);
-  const uint32_t hi = (2048u >> 4) | (1u << 14) | (2u << 29);
-  return ((uint64_t)hi << 32) | lo;
-}
-// V as an MN-major operand: 64 of the N index (dims) are 128 contiguous bytes, the next 64 lie 1024 bytes further (leading
-// byte offset), the next 8 of the K index (tokens) 2048 bytes (stride byte offset).
-__device__ inline uint64_t umma_desc_v(uint32_t smem_addr) {
-  const uint32_t lo = ((smem_addr >> 4) & 0x3FFFu) | ((1024u >> 4) << 16);
-  const uint32_t hi = (2048u >> 4) | (1u << 14) | (2u << 29);
-  return ((uint64_t)hi << 32) | lo;
-}
-// 32 bytes (a whole sector) per thread
-__device__ inline void st_global32(void* dst, const uint32_t* r) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-               ::"l"(dst), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
-}
-// Two fp32 operations in one instruction.
-__device__ inline void fma2(float& x, float& y, float ax, float ay, float b, float c) {
-  asm("{\n\t.reg .b64 a, b, c, d;\n\t"
-      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %5};\n\t"
-      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
-      : "=f"(x), "=f"(y) : "f"(ax), "f"(ay), "f"(b), "f"(c));
-}
-__device__ inline void add2(float& x, float& y, float ax, float ay) {
-  asm("{\n\t.reg .b64 a, b, d;\n\t"
-      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%0, %1};\n\t"
-      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
-      : "+f"(x), "+f"(y) : "f"(ax), "f"(ay));
-}
-__device__ inline float max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-__device__ inline uint32_t pack2(float lo, float hi) {
-  __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<uint32_t*>(&v);
-}
-
 // Whether one of a pair of bf16 values is an infinity or a NaN; the pair with zeros for those.
 __device__ inline bool not_finite(uint32_t pair) { return ((pair & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 __device__ inline uint32_t only_finite(uint32_t pair) {
@@ -967,11 +853,7 @@ static_assert(1024 + 2 * kQBytes + kSlots * kSlotBytes + 32 * 8 + 128 * 8 + 2 * 
 
 namespace stepk {
 
-bool tree_tc_supported(const step_pool* pool, int n) {
-  const kv_pool_config& c = pool->cfg;
-  return c.dtype == STEP_BF16 && c.head_dim == kD && c.page_size == kP && pool->swizzle && n <= kMaxTracesFast && pool->fast_path > 0 &&
-         (long long)c.num_layers * c.num_blocks * c.num_kv_heads * 2 * kP < (1ll << 31) && encode_tiled_fn() != nullptr;
-}
+bool tree_tc_supported(const step_pool* pool, int n) { return attention_tc_covers(pool, n); }
 
 size_t tree_tc_workspace(const step_pool* pool, int T) {
   const size_t rows = T > kHalfRows / pool->G ? 2 * kHalfRows : kHalfRows;
@@ -986,16 +868,9 @@ int tree_tc_launch(step_pool* pool, int layer, const void* q, const void* k_draf
   if (!enc) return STEP_ERR_CUDA;
   const cuuint32_t estr[4] = {1, 1, 1, 1};
   if (!pool->tree_ready) {
-    // the pool as groups of 8 rows of 128 dims, seen as [group][half of the dims][row][64 dims]; a box is the two groups of a
-    // page's K or V
     CUtensorMap fresh;
     static_assert(sizeof(fresh) <= sizeof(pool->tmap_kv_bytes), "tensor map");
-    const cuuint64_t dims[4] = {64, 8, 2, (cuuint64_t)g.L * g.num_blocks * g.Hkv * 2 * (kP / 8)};
-    const cuuint64_t strides[3] = {256, 128, 2048};
-    const cuuint32_t box[4] = {64, 8, 2, kP / 8};
-    if (enc(&fresh, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, pool->cfg.kv_storage, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-      return STEP_ERR_CUDA;
+    if (!encode_pool_map(enc, pool, &fresh)) return STEP_ERR_CUDA;
     memcpy(pool->tmap_kv_bytes, &fresh, sizeof(fresh));
     if (cudaFuncSetAttribute(tree_tc_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(true)) != cudaSuccess ||
         cudaFuncSetAttribute(tree_tc_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(false)) != cudaSuccess)

@@ -162,3 +162,23 @@ def test_the_binding_refuses_what_does_not_fit():
         with pytest.raises(B.StepError) as e:
             B.KVPool.extend(bare_pool(), *args)
         assert e.value.code == 1
+
+
+def test_struct_layouts_match_the_binding(tmp_path):
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    names = ["step_rotary_config", "step_rotary", "rotate_args", "kv_store_args"]
+    lines = ['#include <stdio.h>', '#include <stddef.h>', '#include "step.h"', "int main(void) {"]
+    for s in names:
+        lines.append('  printf("%s %%zu\\n", sizeof(%s));' % (s, s))
+        lines += ['  printf("%s.%s %%zu\\n", offsetof(%s, %s));' % (s, f, s, f) for f, _ in getattr(B, s)._fields_]
+    src, exe = tmp_path / "layout.c", tmp_path / "layout"
+    src.write_text("\n".join(lines + ["  return 0;", "}"]))
+    subprocess.run(["gcc", "-std=c99", "-pedantic", "-Wall", "-Werror", "-I", os.path.join(root, "include"), str(src), "-o", str(exe)], check=True)
+    out = dict(line.split() for line in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.splitlines())
+    for s in names:
+        cls = getattr(B, s)
+        assert int(out[s]) == C.sizeof(cls), s
+        for f, _ in cls._fields_:
+            assert int(out["%s.%s" % (s, f)]) == getattr(cls, f).offset, (s, f)
