@@ -2,24 +2,25 @@
 //
 // A trace's keys are the pages it shares with its group and the pages of its own.  Both kinds leave partial results
 //   m = max_j s_j,  l = sum_j 2^(s_j - m),  o = sum_j 2^(s_j - m) v_j          (s in units of log 2)
-// which a last kernel combines.  Three launches, each a programmatic dependent of the one before:
+// which a last kernel combines.
 //
-// 1. groups_stream_kernel: the own pages, bound by HBM.  The pages of all (row, KV head) sequences form one stream, cut into one
-//    equal contiguous share per warp; a warp streams its share through a private ring of whole pages (8 KiB, K and V rows of one
-//    head, one bulk copy each) and runs both products on 16 x 8 x 16 tiles, the G heads of the group as rows: with so few
-//    rows a 128-row tensor-core tile would be nearly empty, and beginning a sequence costs such a kernel four tiles' time,
-//    more than a trace's own text often has.  Each CTA works out for itself which rows share what (from the lengths and the
-//    groups' arrays); the first leaves the outcome in the workspace for the other two kernels.
-// 2. groups_prefix_kernel: the shared pages, bound by the tensor cores and the exponentials.  The query rows of a group's traces
-//    - (trace, head of the KV head's group) - are taken 256 at a time against one read of the keys, as decode_attention_tree does
-//    with a trace's drafted tokens: scores by tcgen05 into tensor memory, a thread per row for the softmax, probabilities
-//    rounded to bf16 over the scores, from where they are the second product's A operand.  Two chains ("lanes") run side by
-//    side: 128 rows each of the same tile of 128 keys, or, where a row block has at most 128 rows, even and odd tiles of the same
-//    rows.  The tiles of all (group, KV head, row block) sequences form one stream, cut into one equal share per CTA.
-// 3. groups_merge_kernel: a warp per query row.
+// groups_kernel works on both kinds at once, on different SMs: the shared pages are bound by the tensor cores and the
+// exponentials, the own pages by HBM, and the SMs that read own pages get the more of its bandwidth the fewer they are.  Every
+// CTA works out for itself who shares what (from the lengths and the groups' arrays) and how many CTAs each kind gets; the first
+// leaves the outcome in the workspace for groups_merge_kernel, a programmatic dependent.
+//   Own pages: the pages of all (row, KV head) sequences form one stream, cut into one equal contiguous share per warp; a warp
+//   streams its share through a private ring of whole pages (8 KiB, K and V rows of one head, one bulk copy each) and runs both
+//   products on 16 x 8 x 16 tiles, the G heads of the group as rows: with so few rows a 128-row tensor-core tile would be nearly
+//   empty, and beginning a sequence costs such a kernel four tiles' time, more than a trace's own text often has.
+//   Shared pages: the query rows of a group's traces - (trace, head of the KV head's group) - are taken 256 at a time against
+//   one read of the keys, as decode_attention_tree does with a trace's drafted tokens: scores by tcgen05 into tensor memory, a
+//   thread per row for the softmax, probabilities rounded to bf16 over the scores, from where they are the second product's A
+//   operand.  Two chains ("lanes") run side by side: 128 rows each of the same tile of 128 keys, or, where a row block has
+//   at most 128 rows, even and odd tiles of the same rows.  The tiles of all (group, KV head, row block) sequences form one
+//   stream, cut into one equal share per CTA.
 //
 // The partition is a function of lengths and groups alone and pieces are combined in stream order, so a call gives the same
-// bits every time.  Every wait is bounded (kv_pool_set_wait_limit_ns); a kernel whose wait runs out raises STEP_ERR_TIMEOUT and
+// bits every time.  Every wait is bounded (kv_pool_set_wait_limit_ns); a warp whose wait runs out raises STEP_ERR_TIMEOUT and
 // leaves when its copies and products in flight have ended.
 #include "attention_tc.cuh"
 
@@ -40,7 +41,11 @@ constexpr unsigned long long kDrainNs = 100000000ull;
 
 constexpr int kStreamWarps = 8, kStages = 3, kPageBytes = 2 * kP * kD * 2;
 
-struct Header { long long units; int groups; int pad; };   // units of the prefix stream; groups of a valid description, else 0
+constexpr int kTableGroups = 48;                  // groups whose table fits beside the rings; a longer one lies in the workspace
+constexpr int kUnitPages = 10;                    // a unit of the prefix stream takes an SM as long as this many own pages
+
+// Units of the prefix stream, own pages (of all KV heads), groups of a valid description (else 0).
+struct Header { long long units, pages; int groups; };
 
 struct GroupArgs {
   const __nv_bfloat16* kv; const __nv_bfloat16* q; __nv_bfloat16* out;
@@ -49,20 +54,32 @@ struct GroupArgs {
   int n, n_groups, Hq, Hkv, G, layer, max_pages, num_blocks;
   int tokens;                       // traces whose heads fill a tile of query rows: 128 / G
   int box;                          // traces of one copy of query rows
-  int shares, warps;                // CTAs of the prefix launch; warps of the stream launch
+  int ctas;
   float scale_log2;
   unsigned long long wait_ns;
   // workspace
   Header* header;
   int4* groups;                     // [n_groups] first row, rows, first row that is long enough (-1: nothing shared), pages
   long long* group_at;              // [n_groups] where the group's tiles begin in the prefix stream
+  int4* cta_groups;                 // the same for every CTA by itself: [ctas][n_groups] (more than kTableGroups groups)
+  long long* cta_group_at;
   int* group_of;                    // [n] the group whose pages the row shares, or -1
   long long* own_at;                // [n + 1] own pages of the rows before
-  float *pre_ml, *pre_o;            // [share][2][lane][128] (m, l) and o of the prefix pieces that are not whole sequences
+  float *pre_ml, *pre_o;            // [CTA][2][lane][128] (m, l) and o of the prefix pieces that are not whole sequences
   float *row_ml, *row_o;            // [lane][n][Hq] of those that are
-  float *own_ml, *own_o;            // [warp][2][G] of the stream's pieces that are not whole sequences
+  float *own_ml, *own_o;            // [warp][2][G] of the own pages' pieces that are not whole sequences
   float *all_ml, *all_o;            // [n][Hq] of those that are, where there are shared pages besides
 };
+
+// CTAs that take shared pages; the others take own pages.
+__device__ inline int prefix_ctas(const GroupArgs& a, const Header& h) {
+  if (h.units == 0) return 0;
+  if (h.pages == 0) return a.ctas;
+  const long long p = h.units * kUnitPages;
+  return max(1, min(a.ctas - 1, (int)(a.ctas * p / (p + h.pages))));
+}
+__device__ inline long long prefix_share(const Header& h, int ctas) { return max(2ll, div_up(h.units, ctas)); }   // (a wide tile begins in every share)
+__device__ inline long long own_share(const Header& h, int ctas) { return div_up(h.pages, ctas * kStreamWarps); }
 
 __device__ inline int length_of(const GroupArgs& a, int i, bool flag) {
   int S = a.seq_lens[i];
@@ -84,7 +101,7 @@ __device__ inline long long head_units(const Shape& x) {
   return (long long)(x.blocks - 1) * (2 * x.tiles + kSetup) + x.last * x.tiles + kSetup;
 }
 
-// ---------------------------------------------------------------- 1. own pages
+// ---------------------------------------------------------------- own pages
 __device__ inline void ldsm4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
@@ -96,104 +113,19 @@ __device__ inline void mma16816(float (&c)[4], const uint32_t* a, uint32_t b0, u
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-constexpr size_t kStreamSmem = 1024 + (size_t)kStreamWarps * kStages * kPageBytes + (kMaxTracesFast + 1) * 8 + kMaxTracesFast * 4 + kStreamWarps * kStages * 8;
-static_assert(kStreamSmem <= 232448 - 1024, "shared memory of one CTA");
+constexpr size_t kRing = (size_t)kStreamWarps * kStages * kPageBytes;                      // rings of own pages
+constexpr size_t kStreamSmem = 1024 + kRing + (kMaxTracesFast + 1) * 8 + 2 * kMaxTracesFast * 4 + kStreamWarps * kStages * 8;
 
-__global__ void __launch_bounds__(kStreamWarps * 32, 1) groups_stream_kernel(const __grid_constant__ GroupArgs a) {
-  extern __shared__ unsigned char smem_raw[];
-  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  unsigned char* sm = smem_raw + (base - raw);
-  long long* s_at = reinterpret_cast<long long*>(sm + kStreamWarps * kStages * kPageBytes);   // [n + 1] own pages of the rows before
-  int* s_own = reinterpret_cast<int*>(s_at + kMaxTracesFast + 1);                            // [n] pages that the row shares
-  uint64_t* s_bar = reinterpret_cast<uint64_t*>(s_own + kMaxTracesFast);
-  __shared__ long long s_sum[kStreamWarps];
+// What every CTA works out first, in shared memory behind the rings of own pages.
+struct Rows {
+  long long* at;                    // [n + 1] own pages of the rows before
+  int* own;                         // [n] pages that the row shares
+  int* len;                         // [n] its length, at most what the table holds
+};
+
+// This CTA's share of the own pages: `share` of them for each of its warps, this one the me-th of all.
+__device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, unsigned char* sm, uint32_t base, uint32_t bars, int me, long long total, long long W) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const bool first = blockIdx.x == 0;
-  dependents_may_launch();
-  const uint32_t bars = smem_u32(s_bar) + warp * kStages * 8;
-  if (lane == 0) {
-    for (int s = 0; s < kStages; ++s) mbar_init(bars + 8 * s, 1);
-    mbar_init_fence();
-  }
-  // ---- who shares what.  A description that is not in order is not followed at all.
-  bool bad = false;
-  for (int g = threadIdx.x; g < a.n_groups; g += kStreamWarps * 32) {
-    const int r0 = a.group_rows[g], r1 = a.group_rows[g + 1], pages = a.group_pages[g];
-    bad |= r0 < 0 || r1 < r0 || r1 > a.n || pages < 0 || pages > a.max_pages;
-  }
-  for (int i = threadIdx.x; i < a.n; i += kStreamWarps * 32) {
-    s_own[i] = 0;
-    if (first) a.group_of[i] = -1;
-  }
-  const int n_groups = __syncthreads_or(bad) ? 0 : a.n_groups;
-  if (first && threadIdx.x == 0 && n_groups != a.n_groups) flag_error(a.counters, STEP_ERR_INVALID_ARG);
-  for (int g = warp; g < n_groups; g += kStreamWarps) {
-    const int r0 = a.group_rows[g], r1 = a.group_rows[g + 1], pages = a.group_pages[g];
-    int members = 0, leader = -1;
-    for (int i0 = r0; i0 < r1; i0 += 32) {
-      const int i = i0 + lane;
-      const unsigned m = __ballot_sync(0xffffffffu, i < r1 && pages > 0 && length_of(a, i, false) >= (long long)pages * kP);
-      if (m && leader < 0) leader = i0 + __ffs(m) - 1;
-      members += __popc(m);
-    }
-    if (members < 2) leader = -1;
-    if (leader >= 0)
-      for (int i = r0 + lane; i < r1; i += 32)
-        if (length_of(a, i, false) >= (long long)pages * kP) {
-          s_own[i] = pages;
-          if (first) a.group_of[i] = g;
-        }
-    if (first && lane == 0) a.groups[g] = make_int4(r0, r1 - r0, leader, pages);
-  }
-  __syncthreads();
-  if (first && warp == 0) {
-    long long run = 0;
-    for (int g0 = 0; g0 < n_groups; g0 += 32) {
-      const int g = g0 + lane;
-      long long mine = 0;
-      if (g < n_groups) {
-        const int4 x = a.groups[g];
-        if (x.z >= 0) mine = head_units(shape_of(a, x)) * a.Hkv;
-      }
-      long long incl = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long u = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += u;
-      }
-      if (g < n_groups) a.group_at[g] = run + incl - mine;
-      run += __shfl_sync(0xffffffffu, incl, 31);
-    }
-    if (lane == 0) *a.header = Header{run, n_groups, 0};
-  }
-  // ---- own pages of the rows before each: a thread takes `per` rows
-  {
-    const int per = (a.n + kStreamWarps * 32 - 1) / (kStreamWarps * 32), i0 = threadIdx.x * per;
-    auto pages_of = [&](int i) { return (length_of(a, i, first) + kP - 1) / kP - s_own[i]; };
-    long long mine = 0;
-    for (int i = i0; i < min(a.n, i0 + per); ++i) mine += pages_of(i);
-    long long incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long u = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += u;
-    }
-    if (lane == 31) s_sum[warp] = incl;
-    __syncthreads();
-    long long run = incl - mine;
-    for (int w = 0; w < warp; ++w) run += s_sum[w];
-    for (int i = i0; i < min(a.n, i0 + per); ++i) {
-      s_at[i] = run;
-      if (first) a.own_at[i] = run;
-      run += pages_of(i);
-      if (i == a.n - 1) { s_at[a.n] = run; if (first) a.own_at[a.n] = run; }
-    }
-  }
-  __syncthreads();
-
-  // ---- this warp's share
-  const long long total = s_at[a.n] * a.Hkv, W = div_up(total, a.warps);
-  const int me = blockIdx.x * kStreamWarps + warp;
   const long long begin = min(total, me * W), end = min(total, begin + W);
   if (begin >= end) return;
   // the sequence that holds a position of the stream
@@ -202,13 +134,13 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) groups_stream_kernel(con
     int lo = 0, hi = a.n - 1;                                          // the last row that begins at or before pos: it has pages
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (s_at[mid] * a.Hkv <= pos) lo = mid; else hi = mid - 1;
+      if (rw.at[mid] * a.Hkv <= pos) lo = mid; else hi = mid - 1;
     }
     Seq s;
     s.row = lo;
-    s.pages = (int)(s_at[lo + 1] - s_at[lo]);
-    s.own = s_own[lo];
-    const long long off = pos - s_at[lo] * a.Hkv;
+    s.pages = (int)(rw.at[lo + 1] - rw.at[lo]);
+    s.own = rw.own[lo];
+    const long long off = pos - rw.at[lo] * a.Hkv;
     s.h = off <= 0x7fffffffll ? (int)((unsigned)off / (unsigned)s.pages) : (int)(off / s.pages);
     s.at = pos - off + (long long)s.h * s.pages;
     return s;
@@ -217,8 +149,8 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) groups_stream_kernel(con
     s.at += s.pages;
     if (++s.h < a.Hkv) return s;
     s.h = 0;
-    do ++s.row; while (s.row < a.n && s_at[s.row + 1] == s_at[s.row]);
-    if (s.row < a.n) { s.pages = (int)(s_at[s.row + 1] - s_at[s.row]); s.own = s_own[s.row]; }
+    do ++s.row; while (s.row < a.n && rw.at[s.row + 1] == rw.at[s.row]);
+    if (s.row < a.n) { s.pages = (int)(rw.at[s.row + 1] - rw.at[s.row]); s.own = rw.own[s.row]; }
     return s;
   };
 
@@ -260,7 +192,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) groups_stream_kernel(con
   bool ok = true;
   for (long long pos = begin; pos < end && ok;) {
     const int page0 = (int)(pos - s.at), cnt = (int)min((long long)(s.pages - page0), end - pos);
-    const int S = length_of(a, s.row, false) - s.own * kP;             // own positions
+    const int S = rw.len[s.row] - s.own * kP;                          // own positions
     const __nv_bfloat16* q = a.q + ((size_t)s.row * a.Hq + (size_t)s.h * a.G) * kD;
     uint32_t qf[8][4];
 #pragma unroll
@@ -373,7 +305,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) groups_stream_kernel(con
   }
 }
 
-// ---------------------------------------------------------------- 2. shared pages
+// ---------------------------------------------------------------- shared pages
 struct Place { int g, hb, at; int4 grp; Shape x; };   // sequence hb = head * blocks + block of group g; at: units into it, kSetup counted first
 __device__ inline int width_of(const Place& p) { return p.hb % p.x.blocks == p.x.blocks - 1 ? p.x.last : 2; }
 __device__ inline int units_of(const Place& p) { return width_of(p) * p.x.tiles + kSetup; }
@@ -387,34 +319,35 @@ __device__ inline Part part_of(const Place& p, long long pos, long long end) {
   x.cnt = (max(0, (int)(p.at + x.len) - kSetup) + w - 1) / w - x.tile0;
   return x;
 }
-__device__ inline long long share_units(const GroupArgs& a, long long total) { return max(2ll, div_up(total, a.shares)); }   // (a wide tile begins in every share)
+// The groups as this CTA keeps them: in shared memory, or, if they are many, in the workspace.
+struct Table { const int4* groups; const long long* at; int n; };
 // One warp: the group that position pos of the stream (pos < total) lies in.
-__device__ inline Place locate(const GroupArgs& a, int n_groups, long long pos, int lane) {
+__device__ inline Place locate(const GroupArgs& a, const Table& tab, long long pos, int lane) {
   int g = 0;
-  for (int g0 = 0; g0 < n_groups; g0 += 32) {           // the last that begins at or before pos: it has tiles
-    const unsigned m = __ballot_sync(0xffffffffu, g0 + lane < n_groups && a.group_at[g0 + lane] <= pos);
+  for (int g0 = 0; g0 < tab.n; g0 += 32) {              // the last that begins at or before pos: it has tiles
+    const unsigned m = __ballot_sync(0xffffffffu, g0 + lane < tab.n && tab.at[g0 + lane] <= pos);
     if (!m) break;
     g = g0 + 31 - __clz(m);
     if (m != 0xffffffffu) break;
   }
   Place p;
   p.g = g;
-  p.grp = a.groups[g];
+  p.grp = tab.groups[g];
   p.x = shape_of(a, p.grp);
-  const long long off = pos - a.group_at[g], head = head_units(p.x);
-  const int h = (int)(off / head), wide = 2 * p.x.tiles + kSetup, in = (int)(off - h * head);
+  const long long off = pos - tab.at[g], head = head_units(p.x);
+  const int h = off + head <= 0x7fffffffll ? (int)((unsigned)off / (unsigned)head) : (int)(off / head), wide = 2 * p.x.tiles + kSetup, in = (int)(off - h * head);
   const int block = min(in / wide, p.x.blocks - 1);
   p.hb = h * p.x.blocks + block;
   p.at = in - block * wide;
   return p;
 }
 // The place behind a whole rest of a sequence.
-__device__ inline void next_sequence(const GroupArgs& a, int n_groups, Place& p) {
+__device__ inline void next_sequence(const GroupArgs& a, const Table& tab, Place& p) {
   p.at = 0;
   if (++p.hb < a.Hkv * p.x.blocks) return;
   p.hb = 0;
-  while (++p.g < n_groups) {
-    p.grp = a.groups[p.g];
+  while (++p.g < tab.n) {
+    p.grp = tab.groups[p.g];
     if (p.grp.z >= 0) { p.x = shape_of(a, p.grp); return; }
   }
 }
@@ -422,12 +355,142 @@ __device__ inline void next_sequence(const GroupArgs& a, int n_groups, Place& p)
 // [row0, row0 + rows).
 struct Piece { int h, row0, rows, two, tile0, cnt, tiles, keys, slot; };
 
-__global__ void __launch_bounds__(kThreads, 1) groups_prefix_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ GroupArgs a) {
+constexpr size_t kTableAt = 2 * kQBytes + kSlots * kSlotBytes + 16;          // behind the rings and the rows' arrays
+static_assert(kTableAt >= kRing + (kMaxTracesFast + 1) * 8 + 2 * kMaxTracesFast * 4, "rows and groups lie side by side");
+constexpr size_t kPrefixSmem = 1024 + kTableAt + 32 * 8 + 2 * sizeof(Piece) + 64 + kTableGroups * 24;
+constexpr size_t kSmem = kPrefixSmem > kStreamSmem ? kPrefixSmem : kStreamSmem;
+static_assert(kSmem <= 232448 - 256, "shared memory of one CTA");
+
+__global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ GroupArgs a) {
   extern __shared__ unsigned char smem_raw[];
+  __shared__ long long s_sum[kThreads / 32];
+  __shared__ Header s_header;
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   unsigned char* sm = smem_raw + (base - raw);
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+  const bool first = blockIdx.x == 0;
+  dependents_may_launch();
+  if (threadIdx.x == 0) { prefetch_map(&map); prefetch_map(&map_q); }
+
+  // ---- who shares what.  A description that is not in order is not followed at all.
+  Rows rw;
+  rw.at = reinterpret_cast<long long*>(sm + kRing);
+  rw.own = reinterpret_cast<int*>(rw.at + kMaxTracesFast + 1);
+  rw.len = rw.own + kMaxTracesFast;
+  int4* s_grp = reinterpret_cast<int4*>(sm + kTableAt);
+  long long* s_grp_at = reinterpret_cast<long long*>(s_grp + kTableGroups);
+  bool bad = false;
+  for (int g = threadIdx.x; g < a.n_groups; g += kThreads) {
+    const int r0 = a.group_rows[g], r1 = a.group_rows[g + 1], pages = a.group_pages[g];
+    bad |= r0 < 0 || r1 < r0 || r1 > a.n || pages < 0 || pages > a.max_pages;
+  }
+  for (int i = threadIdx.x; i < a.n; i += kThreads) {
+    rw.own[i] = 0;
+    rw.len[i] = length_of(a, i, first);
+    if (first) a.group_of[i] = -1;
+  }
+  Table tab;
+  tab.n = __syncthreads_or(bad) ? 0 : a.n_groups;
+  if (first && threadIdx.x == 0 && tab.n != a.n_groups) flag_error(a.counters, STEP_ERR_INVALID_ARG);
+  int4* grp = a.n_groups <= kTableGroups ? s_grp : a.cta_groups + (size_t)blockIdx.x * a.n_groups;
+  long long* grp_at = a.n_groups <= kTableGroups ? s_grp_at : a.cta_group_at + (size_t)blockIdx.x * a.n_groups;
+  tab.groups = grp;
+  tab.at = grp_at;
+  for (int g = warp; g < tab.n; g += kThreads / 32) {
+    const int r0 = a.group_rows[g], r1 = a.group_rows[g + 1], pages = a.group_pages[g];
+    int members = 0, leader = -1;
+    for (int i0 = r0; i0 < r1; i0 += 32) {
+      const int i = i0 + lane;
+      const unsigned m = __ballot_sync(0xffffffffu, i < r1 && pages > 0 && rw.len[i] >= (long long)pages * kP);
+      if (m && leader < 0) leader = i0 + __ffs(m) - 1;
+      members += __popc(m);
+    }
+    if (members < 2) leader = -1;
+    if (leader >= 0)
+      for (int i = r0 + lane; i < r1; i += 32)
+        if (rw.len[i] >= (long long)pages * kP) {
+          rw.own[i] = pages;
+          if (first) a.group_of[i] = g;
+        }
+    if (lane == 0) {
+      grp[g] = make_int4(r0, r1 - r0, leader, pages);
+      if (first) a.groups[g] = grp[g];
+    }
+  }
+  __syncthreads();
+  // ---- where every group's tiles begin in their stream (one warp), and every row's own pages in theirs (a thread takes `per` rows)
+  if (warp == kThreads / 32 - 1) {
+    long long run = 0;
+    for (int g0 = 0; g0 < tab.n; g0 += 32) {
+      const int g = g0 + lane;
+      long long mine = 0;
+      if (g < tab.n) {
+        const int4 x = grp[g];
+        if (x.z >= 0) mine = head_units(shape_of(a, x)) * a.Hkv;
+      }
+      long long incl = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long u = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += u;
+      }
+      if (g < tab.n) {
+        grp_at[g] = run + incl - mine;
+        if (first) a.group_at[g] = run + incl - mine;
+      }
+      run += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (lane == 0) s_header.units = run;
+  }
+  {
+    const int per = (a.n + kThreads - 1) / kThreads, i0 = threadIdx.x * per;
+    auto pages_of = [&](int i) { return (rw.len[i] + kP - 1) / kP - rw.own[i]; };
+    long long mine = 0;
+    for (int i = i0; i < min(a.n, i0 + per); ++i) mine += pages_of(i);
+    long long incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long u = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += u;
+    }
+    if (lane == 31) s_sum[warp] = incl;
+    __syncthreads();
+    long long run = incl - mine;
+    for (int w = 0; w < warp; ++w) run += s_sum[w];
+    for (int i = i0; i < min(a.n, i0 + per); ++i) {
+      rw.at[i] = run;
+      if (first) a.own_at[i] = run;
+      run += pages_of(i);
+      if (i == a.n - 1) { rw.at[a.n] = run; if (first) a.own_at[a.n] = run; }
+    }
+  }
+  __syncthreads();
+  Header hd;
+  hd.units = s_header.units; hd.pages = rw.at[a.n] * a.Hkv; hd.groups = tab.n;
+  if (first && threadIdx.x == 0) *a.header = hd;
+  const int n_prefix = prefix_ctas(a, hd);
+
+  if ((int)blockIdx.x >= n_prefix) {
+    // ================================================ own pages
+    const int n_own = a.ctas - n_prefix;
+    const uint32_t bars = smem_u32(rw.len + kMaxTracesFast) + warp * kStages * 8;
+    if (warp < kStreamWarps) {
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+      if (lane == 0) {
+        for (int s = 0; s < kStages; ++s) mbar_init(bars + 8 * s, 1);
+        mbar_init_fence();
+      }
+      __syncwarp();
+      own_pages(a, rw, sm, base, bars, ((int)blockIdx.x - n_prefix) * kStreamWarps + warp, hd.pages, own_share(hd, n_own));
+    } else {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
+    }
+    return;
+  }
+
+  // ================================================ shared pages
   const uint32_t sm_q = base, sm_ring = base + 2 * kQBytes;
-  uint64_t* s_bar = reinterpret_cast<uint64_t*>(sm + 2 * kQBytes + kSlots * kSlotBytes);
+  uint64_t* s_bar = reinterpret_cast<uint64_t*>(s_grp_at + kTableGroups);
   Piece* s_piece = reinterpret_cast<Piece*>(s_bar + 32);               // [2]
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_piece + 2);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
@@ -436,12 +499,7 @@ __global__ void __launch_bounds__(kThreads, 1) groups_prefix_kernel(const __grid
   const uint32_t bar_full = bars, bar_empty = bars + 8 * kSlots;
   const uint32_t bar_q = bars + 16 * kSlots, bar_s = bar_q + 8, bar_p = bar_s + 16, bar_o = bar_p + 32,
                  bar_qfree = bar_o + 16, bar_drain = bar_qfree + 8;
-
-  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-  dependents_may_launch();
   if (threadIdx.x == 0) {
-    prefetch_map(&map);
-    prefetch_map(&map_q);
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(bar_full + 8 * s, 1);               // the fetching warp's announcement of bytes
       mbar_init(bar_empty + 8 * s, 1);              // tcgen05.commit
@@ -463,14 +521,13 @@ __global__ void __launch_bounds__(kThreads, 1) groups_prefix_kernel(const __grid
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "r"(kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  fence_async_smem();                               // (the rows' arrays, which everyone has read by now, make way for copies)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
-  wait_for_primary();                               // the groups, as the stream kernel found them
   // this CTA's share of the stream
-  const Header hd = *a.header;
-  const long long W = share_units(a, hd.units), pos0 = min(hd.units, blockIdx.x * W), end = min(hd.units, pos0 + W);
+  const long long W = prefix_share(hd, n_prefix), pos0 = min(hd.units, blockIdx.x * W), end = min(hd.units, pos0 + W);
 
   auto wait = [&](uint32_t bar, uint32_t parity) {
     if (mbar_test_wait(bar, parity)) return true;                      // (a limit of zero: this is all)
@@ -602,11 +659,11 @@ __global__ void __launch_bounds__(kThreads, 1) groups_prefix_kernel(const __grid
       // for when the first is entered, four tiles before it is needed.
       auto load_ids = [&](const Place& of, int first) {
         const int page = first + lane;
-        return of.g < hd.groups && page < of.grp.w ? a.block_table[(size_t)of.grp.z * a.max_pages + page] : 0;
+        return of.g < tab.n && page < of.grp.w ? a.block_table[(size_t)of.grp.z * a.max_pages + page] : 0;
       };
       long long pos = pos0;
       if (pos < end) {
-        Place pl = locate(a, hd.groups, pos, lane);
+        Place pl = locate(a, tab, pos, lane);
         Part part = part_of(pl, pos, end);
         int win = (part.tile0 * (kTile / kP)) & ~31;
         int next0 = load_ids(pl, win), next1 = load_ids(pl, win + 32);
@@ -616,7 +673,7 @@ __global__ void __launch_bounds__(kThreads, 1) groups_prefix_kernel(const __grid
           win = (part.tile0 * (kTile / kP)) & ~31;
           int ids0 = next0, ids1 = next1;
           Place nx = pl;                                               // the sequence behind this one, its block ids too
-          next_sequence(a, hd.groups, nx);
+          next_sequence(a, tab, nx);
           next0 = load_ids(nx, 0);
           next1 = load_ids(nx, 32);
           for (int i = 0; i < part.cnt; ++i) {
@@ -646,7 +703,7 @@ __global__ void __launch_bounds__(kThreads, 1) groups_prefix_kernel(const __grid
       int begun = 0;
       long long pos = pos0;
       Place pl = {};
-      if (pos < end) pl = locate(a, hd.groups, pos, lane);
+      if (pos < end) pl = locate(a, tab, pos, lane);
       for (;; par ^= 1) {
         Piece pc = {};
         while (pos < end && pc.cnt == 0) {
@@ -660,7 +717,7 @@ __global__ void __launch_bounds__(kThreads, 1) groups_prefix_kernel(const __grid
             pc.slot = pos - pl.at <= pos0 ? 0 : 1;                     // of the share: does the sequence begin inside it?
           }
           pos += part.len;
-          next_sequence(a, hd.groups, pl);
+          next_sequence(a, tab, pl);
         }
         // the scores of the piece before are made, and its announcement has been read (the very first wait passes at once)
         if (!wait_warp(bar_qfree, par ^ 1)) break;
@@ -823,65 +880,82 @@ __global__ void __launch_bounds__(kThreads, 1) groups_prefix_kernel(const __grid
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
   }
 }
-constexpr size_t kPrefixSmem = 1024 + 2 * kQBytes + kSlots * kSlotBytes + 32 * 8 + 2 * sizeof(Piece) + 64;
-static_assert(kPrefixSmem <= 232448, "shared memory of one CTA");
-
-// ---------------------------------------------------------------- 3. one result per row
-constexpr int kMergeWarps = 4;
+// ---------------------------------------------------------------- one result per row
+constexpr int kMergeWarps = 4, kMergeAhead = 8;
 
 // A warp per query row, lanes over the 128 dims: the shared pages' pieces, then the row's own, in stream order with a running
-// (max, sum, values).
+// (max, sum, values); the loads of kMergeAhead pieces are under way at once.
 __global__ void __launch_bounds__(kMergeWarps * 32) groups_merge_kernel(const __grid_constant__ GroupArgs a) {
   const int lane = threadIdx.x & 31;
   wait_for_primary();
   const Header hd = *a.header;
-  const long long total = a.own_at[a.n] * a.Hkv, W = div_up(total, a.warps), Wp = share_units(a, hd.units);
+  const int n_prefix = prefix_ctas(a, hd);
+  const long long W = hd.pages > 0 ? own_share(hd, a.ctas - n_prefix) : 1, Wp = hd.units > 0 ? prefix_share(hd, n_prefix) : 1;
+  auto share_of = [](long long x, long long by) { return x <= 0x7fffffffll ? (int)((unsigned)x / (unsigned)by) : (int)(x / by); };
   for (int r = blockIdx.x * kMergeWarps + (threadIdx.x >> 5); r < a.n * a.Hq; r += gridDim.x * kMergeWarps) {
     const int i = r / a.Hq, hq = r - i * a.Hq, h = hq / a.G, sub = hq - h * a.G;
     const int g = a.group_of[i];
-    const long long pages = a.own_at[i + 1] - a.own_at[i], at = a.own_at[i] * a.Hkv + h * pages;
-    const int w0 = pages > 0 ? (int)(at / W) : 0, w1 = pages > 0 ? (int)((at + pages - 1) / W) : -1;
-    if (g < 0 && w0 == w1) continue;                                   // written by the stream kernel
-    float M = -INFINITY, den = 0.f;
-    float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-    auto take = [&](const float* mls, const float* os, size_t slot) {
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(mls) + slot);
-      const float4 o = __ldcg(reinterpret_cast<const float4*>(os + slot * kD) + lane);
-      if (ml.y == 0.f) return;                                         // a lane that had no tile: nothing stands there
-      const float Mb = fmaxf(M, ml.x), off = Mb == -INFINITY ? 0.f : Mb;
-      const float keep = exp2f(M - off), wgt = exp2f(ml.x - off);
-      den = den * keep + wgt * ml.y;
-      num.x = num.x * keep + wgt * o.x; num.y = num.y * keep + wgt * o.y;
-      num.z = num.z * keep + wgt * o.z; num.w = num.w * keep + wgt * o.w;
-      M = Mb;
-    };
+    const long long at0 = a.own_at[i], pages = a.own_at[i + 1] - at0, at = at0 * a.Hkv + h * pages;
+    const int w0 = pages > 0 ? share_of(at, W) : 0, w1 = pages > 0 ? share_of(at + pages - 1, W) : -1;
+    if (g < 0 && w0 == w1) continue;                                   // written already
+    // the pieces of the shared pages: shares p0 .. p1, each with one result or (narrow) one per lane
+    int p0 = 0, pieces = 0, narrow = 0, row = 0;
+    long long begin = 0;
     if (g >= 0) {
       const int4 grp = a.groups[g];
       const Shape x = shape_of(a, grp);
       const int t = i - grp.x, block = t / (2 * a.tokens), tb = t - block * 2 * a.tokens;
-      const int w = block == x.blocks - 1 ? x.last : 2;
-      const long long tile0 = a.group_at[g] + h * head_units(x) + (long long)block * (2 * x.tiles + kSetup) + kSetup;
-      const int p0 = (int)(tile0 / Wp), p1 = (int)((tile0 + (long long)w * (x.tiles - 1)) / Wp);
-      if (p0 == p1) {
-        take(a.row_ml, a.row_o, r);
-        if (w == 1) take(a.row_ml, a.row_o, (size_t)a.n * a.Hq + r);
-      } else {
-        const int ln = w == 2 ? tb / a.tokens : 0, row = (tb - ln * a.tokens) * a.G + sub;
-#pragma unroll 4
-        for (int s = p0; s <= p1; ++s) {
-          const size_t slot = (((size_t)s * 2 + (tile0 - kSetup <= s * Wp ? 0 : 1)) * 2 + ln) * kHalfRows + row;
-          take(a.pre_ml, a.pre_o, slot);
-          if (w == 1) take(a.pre_ml, a.pre_o, slot + kHalfRows);
+      const int w = block == x.blocks - 1 ? x.last : 2, ln = tb / a.tokens;
+      begin = a.group_at[g] + h * head_units(x) + (long long)block * (2 * x.tiles + kSetup);
+      p0 = share_of(begin + kSetup, Wp);
+      narrow = w == 1;
+      pieces = (share_of(begin + kSetup + (long long)w * (x.tiles - 1), Wp) - p0 + 1) << narrow;
+      row = ln * kHalfRows + (tb - ln * a.tokens) * a.G + sub;
+    }
+    const bool whole = pieces == 1 << narrow;                          // one share has all tiles
+    const int all = pieces + (w1 - w0 + 1);
+    float M = -INFINITY, den = 0.f;
+    float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = 0; k0 < all; k0 += kMergeAhead) {
+      float2 ml[kMergeAhead];
+      float4 o[kMergeAhead];
+#pragma unroll
+      for (int y = 0; y < kMergeAhead; ++y) {
+        const int k = k0 + y;
+        ml[y] = make_float2(-INFINITY, 0.f);
+        if (k >= all) continue;
+        const float *mls, *os;
+        size_t slot;
+        if (k < pieces) {
+          const int s = p0 + (k >> narrow), ln = k & narrow;
+          mls = whole ? a.row_ml : a.pre_ml;
+          os = whole ? a.row_o : a.pre_o;
+          slot = whole ? (size_t)ln * a.n * a.Hq + r : ((size_t)s * 2 + (begin <= s * Wp ? 0 : 1)) * 2 * kHalfRows + ln * kHalfRows + row;
+        } else {
+          const int s = w0 + k - pieces;
+          mls = w0 == w1 ? a.all_ml : a.own_ml;
+          os = w0 == w1 ? a.all_o : a.own_o;
+          slot = w0 == w1 ? r : ((size_t)s * 2 + (at <= s * W ? 0 : 1)) * a.G + sub;
         }
+        ml[y] = __ldcg(reinterpret_cast<const float2*>(mls) + slot);
+        o[y] = __ldcg(reinterpret_cast<const float4*>(os + slot * kD) + lane);
       }
+      float Mb = M;
+#pragma unroll
+      for (int y = 0; y < kMergeAhead; ++y)
+        if (ml[y].y != 0.f) Mb = fmaxf(Mb, ml[y].x);
+      const float off = Mb == -INFINITY ? 0.f : Mb, keep = exp2f(M - off);
+      den *= keep; num.x *= keep; num.y *= keep; num.z *= keep; num.w *= keep;
+#pragma unroll
+      for (int y = 0; y < kMergeAhead; ++y) {
+        if (ml[y].y == 0.f) continue;                                  // none, or a lane that had no tile: nothing stands there
+        const float wgt = exp2f(ml[y].x - off);
+        den += wgt * ml[y].y;
+        num.x += wgt * o[y].x; num.y += wgt * o[y].y; num.z += wgt * o[y].z; num.w += wgt * o[y].w;
+      }
+      M = Mb;
     }
-    if (w0 == w1) {
-      take(a.all_ml, a.all_o, r);
-    } else {
-#pragma unroll 2
-      for (int s = w0; s <= w1; ++s) take(a.own_ml, a.own_o, ((size_t)s * 2 + (at <= s * W ? 0 : 1)) * a.G + sub);
-    }
-    const float inv = g < 0 && pages == 0 ? 0.f : 1.f / den;           // a row without any key: zeros
+    const float inv = all == 0 ? 0.f : 1.f / den;                      // a row without any key: zeros
     reinterpret_cast<uint2*>(a.out + (size_t)r * kD)[lane] = make_uint2(pack2(num.x * inv, num.y * inv), pack2(num.z * inv, num.w * inv));
   }
 }
@@ -889,20 +963,24 @@ __global__ void __launch_bounds__(kMergeWarps * 32) groups_merge_kernel(const __
 // Lays the workspace out (from `ws` on; null: only its size).
 size_t lay_out(const step_pool* pool, int n, int n_groups, char* ws, GroupArgs* a) {
   const Geo g = geo_of(pool);
-  const size_t shares = pool->num_sms, warps = shares * kStreamWarps, rows = (size_t)n * g.Hq;
+  const size_t ctas = pool->num_sms, warps = ctas * kStreamWarps, rows = (size_t)n * g.Hq;
   size_t off = 0;
   auto take = [&](size_t bytes) { char* p = ws + off; off += (bytes + 255) / 256 * 256; return p; };
   GroupArgs x = {};
   x.header = (Header*)take(sizeof(Header));
   x.groups = (int4*)take((size_t)n_groups * sizeof(int4));
   x.group_at = (long long*)take((size_t)n_groups * 8);
+  if (n_groups > kTableGroups) {
+    x.cta_groups = (int4*)take(ctas * n_groups * sizeof(int4));
+    x.cta_group_at = (long long*)take(ctas * n_groups * 8);
+  }
   x.group_of = (int*)take((size_t)n * 4);
   x.own_at = (long long*)take((size_t)(n + 1) * 8);
   x.own_ml = (float*)take(warps * 2 * g.G * 8);
   x.own_o = (float*)take(warps * 2 * g.G * kD * 4);
   if (n_groups > 0) {
-    x.pre_ml = (float*)take(shares * 4 * kHalfRows * 8);
-    x.pre_o = (float*)take(shares * 4 * kHalfRows * kD * 4);
+    x.pre_ml = (float*)take(ctas * 4 * kHalfRows * 8);
+    x.pre_o = (float*)take(ctas * 4 * kHalfRows * kD * 4);
     x.row_ml = (float*)take(2 * rows * 8);
     x.row_o = (float*)take(2 * rows * kD * 4);
     x.all_ml = (float*)take(rows * 8);
@@ -930,9 +1008,7 @@ int groups_tc_launch(step_pool* pool, int layer, const void* q, const int32_t* b
     static_assert(sizeof(fresh) <= sizeof(pool->tmap_kv_bytes), "tensor map");
     if (!encode_pool_map(enc, pool, &fresh)) return STEP_ERR_CUDA;
     memcpy(pool->tmap_kv_bytes, &fresh, sizeof(fresh));                // (the same for every kernel that uses it)
-    if (cudaFuncSetAttribute(groups_stream_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStreamSmem) != cudaSuccess ||
-        cudaFuncSetAttribute(groups_prefix_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPrefixSmem) != cudaSuccess)
-      return STEP_ERR_CUDA;
+    if (cudaFuncSetAttribute(groups_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess) return STEP_ERR_CUDA;
     pool->groups_ready = true;
   }
   GroupArgs a;
@@ -943,25 +1019,21 @@ int groups_tc_launch(step_pool* pool, int layer, const void* q, const int32_t* b
   a.n = n; a.n_groups = n_groups; a.Hq = g.Hq; a.Hkv = g.Hkv; a.G = g.G; a.layer = layer; a.max_pages = g.max_pages; a.num_blocks = g.num_blocks;
   a.tokens = kHalfRows / g.G;
   a.box = a.tokens < n ? a.tokens : n;
-  a.shares = pool->num_sms;
-  a.warps = a.shares * kStreamWarps;
+  a.ctas = pool->num_sms;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)kD);
   a.wait_ns = pool->wait_limit_ns;
-  groups_stream_kernel<<<a.shares, kStreamWarps * 32, kStreamSmem, s>>>(a);
+  CUtensorMap map, map_q;
+  memcpy(&map, pool->tmap_kv_bytes, sizeof(map));
+  // queries: a box is one half of the dims of the G heads of a group, for as many traces as make a tile of rows
+  const cuuint64_t q_dims[3] = {kD, (cuuint64_t)g.Hq, (cuuint64_t)n};
+  const cuuint64_t q_strides[2] = {kD * 2, (cuuint64_t)g.Hq * kD * 2};
+  const cuuint32_t q_box[3] = {64, (cuuint32_t)g.G, (cuuint32_t)a.box}, estr[3] = {1, 1, 1};
+  if (enc(&map_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), q_dims, q_strides, q_box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return STEP_ERR_CUDA;
+  groups_kernel<<<a.ctas, kThreads, kSmem, s>>>(map, map_q, a);
   if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
-  if (n_groups > 0) {
-    CUtensorMap map, map_q;
-    memcpy(&map, pool->tmap_kv_bytes, sizeof(map));
-    // queries: a box is one half of the dims of the G heads of a group, for as many traces as make a tile of rows
-    const cuuint64_t q_dims[3] = {kD, (cuuint64_t)g.Hq, (cuuint64_t)n};
-    const cuuint64_t q_strides[2] = {kD * 2, (cuuint64_t)g.Hq * kD * 2};
-    const cuuint32_t q_box[3] = {64, (cuuint32_t)g.G, (cuuint32_t)a.box}, estr[3] = {1, 1, 1};
-    if (enc(&map_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), q_dims, q_strides, q_box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-      return STEP_ERR_CUDA;
-    if (launch_dependent(groups_prefix_kernel, dim3(a.shares), dim3(kThreads), kPrefixSmem, s, map, map_q, a) != cudaSuccess) return STEP_ERR_CUDA;
-  }
-  const long long rows = (long long)n * g.Hq, most = 4ll * a.shares;
+  const long long rows = (long long)n * g.Hq, most = 4ll * a.ctas;
   const long long ctas = (rows + kMergeWarps - 1) / kMergeWarps;
   if (launch_dependent(groups_merge_kernel, dim3((unsigned)(ctas < most ? ctas : most)), dim3(kMergeWarps * 32), 0, s, a) != cudaSuccess) return STEP_ERR_CUDA;
   return launch_ok();
