@@ -30,7 +30,7 @@ using namespace stepk;
 
 namespace {
 
-constexpr int kSetup = 4;                         // units that a sequence of the prefix kernel takes besides its tiles (a tile of one lane is one)
+constexpr int kSetup = 2;                         // tiles' worth of time that a sequence of shared pages takes besides its tiles
 constexpr int kKSlots = 2, kVSlots = 3, kSlots = kKSlots + kVSlots;   // rings of K and of V tiles, 160 KiB: a V tile waits for its softmax
 constexpr int kWarpK = 8, kWarpMma = 9, kWarpQ = 10, kWarpV = 11;
 constexpr int kThreads = 384;                     // three warpgroups
@@ -42,10 +42,24 @@ constexpr unsigned long long kDrainNs = 100000000ull;
 constexpr int kStreamWarps = 8, kStages = 3, kPageBytes = 2 * kP * kD * 2;
 
 constexpr int kTableGroups = 48;                  // groups whose table fits beside the rings; a longer one lies in the workspace
-constexpr int kUnitPages = 10;                    // a unit of the prefix stream takes an SM as long as this many own pages
+// What a CTA takes, in nanoseconds (measured, 32 / 8 and 64 / 8 heads): a tile of shared pages with more than 128 rows (its products
+// and exponentials) and with fewer (1.0 alone, the latency of its copies when all SMs read); a page of a warp's own; what comes
+// before and behind them.
+constexpr int kWideNs = 2150, kNarrowNs = 1600, kPageNs = 1050, kPrefixNs = 9000, kOwnNs = 5000;
+constexpr int kOwnSetup = 2;                      // pages' worth of time that a sequence of own pages takes besides them
 
-// Units of the prefix stream, own pages (of all KV heads), groups of a valid description (else 0).
-struct Header { long long units, pages; int groups; };
+// Tiles in the prefix stream, own pages (of all KV heads; setups counted in both), groups of a valid description (else 0), CTAs that
+// take shared pages (the others take own pages).
+struct Header { long long units, pages; int groups, n_prefix; };
+
+// What a row's result is combined from.
+struct RowPlan {
+  long long at;                     // where the row's own pages begin in their stream, KV head 0: Hkv times this
+  long long begin;                  // where the tiles of the row's block of its group begin in the prefix stream, KV head 0
+  int pages, tiles;                 // own pages; tiles it shares (0: none)
+  int head;                         // from one KV head's tiles to the next's
+  int place;                        // of its heads in the block: trace * 2 + 1 if the block has results of two lanes for a row
+};
 
 struct GroupArgs {
   const __nv_bfloat16* kv; const __nv_bfloat16* q; __nv_bfloat16* out;
@@ -59,26 +73,31 @@ struct GroupArgs {
   unsigned long long wait_ns;
   // workspace
   Header* header;
-  int4* groups;                     // [n_groups] first row, rows, first row that is long enough (-1: nothing shared), pages
-  long long* group_at;              // [n_groups] where the group's tiles begin in the prefix stream
-  int4* cta_groups;                 // the same for every CTA by itself: [ctas][n_groups] (more than kTableGroups groups)
+  RowPlan* plan;                    // [n]
+  int4* cta_groups;                 // [ctas][n_groups] the groups as every CTA finds them for itself (more than kTableGroups)
   long long* cta_group_at;
-  int* group_of;                    // [n] the group whose pages the row shares, or -1
-  long long* own_at;                // [n + 1] own pages of the rows before
   float *pre_ml, *pre_o;            // [CTA][2][lane][128] (m, l) and o of the prefix pieces that are not whole sequences
   float *row_ml, *row_o;            // [lane][n][Hq] of those that are
   float *own_ml, *own_o;            // [warp][2][G] of the own pages' pieces that are not whole sequences
   float *all_ml, *all_o;            // [n][Hq] of those that are, where there are shared pages besides
 };
 
-// CTAs that take shared pages; the others take own pages.
-__device__ inline int prefix_ctas(const GroupArgs& a, const Header& h) {
-  if (h.units == 0) return 0;
-  if (h.pages == 0) return a.ctas;
-  const long long p = h.units * kUnitPages;
-  return max(1, min(a.ctas - 1, (int)(a.ctas * p / (p + h.pages))));
+// One warp: how many CTAs take shared pages, so that the slower kind of CTA is as fast as can be.  (Around the ratio of the work,
+// a candidate per lane: with few tiles a share is a whole number of them.)
+__device__ inline int choose_prefix(const GroupArgs& a, long long units, float unit_ns, long long pages, int lane) {
+  if (units == 0 || pages == 0) return units == 0 ? 0 : a.ctas;
+  const float ratio = (float)units * unit_ns / ((float)units * unit_ns + (float)pages * (kPageNs / (float)kStreamWarps));
+  const int at = (int)(ratio * a.ctas) - 12 + lane;
+  unsigned long long key = ~0ull;
+  if (at >= 1 && at < a.ctas) {
+    const long long t = max(kPrefixNs + (long long)((float)div_up(units, at) * unit_ns), kOwnNs + div_up(pages, (a.ctas - at) * kStreamWarps) * kPageNs);
+    key = (unsigned long long)t << 16 | at;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) key = min(key, __shfl_xor_sync(0xffffffffu, key, o));
+  return (int)(key & 0xffff);
 }
-__device__ inline long long prefix_share(const Header& h, int ctas) { return max(2ll, div_up(h.units, ctas)); }   // (a wide tile begins in every share)
+__device__ inline long long prefix_share(const Header& h, int ctas) { return div_up(h.units, ctas); }
 __device__ inline long long own_share(const Header& h, int ctas) { return div_up(h.pages, ctas * kStreamWarps); }
 
 __device__ inline int length_of(const GroupArgs& a, int i, bool flag) {
@@ -89,16 +108,12 @@ __device__ inline int length_of(const GroupArgs& a, int i, bool flag) {
 }
 
 // ---- the prefix stream: for every group that shares pages, for every KV head, for every block of 2 * tokens traces
-struct Shape { int tiles, blocks, last; };          // last: units per tile of a head's last block (1: at most `tokens` traces); 2 in the others
+struct Shape { int tiles, blocks; };
 __device__ inline Shape shape_of(const GroupArgs& a, int4 g) {
   Shape x;
   x.tiles = (g.w + kTile / kP - 1) / (kTile / kP);
   x.blocks = (g.y + 2 * a.tokens - 1) / (2 * a.tokens);
-  x.last = g.y - (x.blocks - 1) * 2 * a.tokens <= a.tokens ? 1 : 2;
   return x;
-}
-__device__ inline long long head_units(const Shape& x) {
-  return (long long)(x.blocks - 1) * (2 * x.tiles + kSetup) + x.last * x.tiles + kSetup;
 }
 
 // ---------------------------------------------------------------- own pages
@@ -118,7 +133,7 @@ constexpr size_t kStreamSmem = 1024 + kRing + (kMaxTracesFast + 1) * 8 + 2 * kMa
 
 // What every CTA works out first, in shared memory behind the rings of own pages.
 struct Rows {
-  long long* at;                    // [n + 1] own pages of the rows before
+  long long* at;                    // [n + 1] own pages of the rows before, setups counted
   int* own;                         // [n] pages that the row shares
   int* len;                         // [n] its length, at most what the table holds
 };
@@ -130,6 +145,11 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
   if (begin >= end) return;
   // the sequence that holds a position of the stream
   struct Seq { int row, h, pages, own; long long at; };                // at: where it begins
+  auto of_row = [&](Seq& s) { s.pages = (int)(rw.at[s.row + 1] - rw.at[s.row]) - kOwnSetup; s.own = rw.own[s.row]; };
+  auto row_behind = [&](int row) {                                     // that has pages
+    do ++row; while (row < a.n && rw.at[row + 1] == rw.at[row]);
+    return row;
+  };
   auto seq_at = [&](long long pos) {
     int lo = 0, hi = a.n - 1;                                          // the last row that begins at or before pos: it has pages
     while (lo < hi) {
@@ -138,38 +158,48 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
     }
     Seq s;
     s.row = lo;
-    s.pages = (int)(rw.at[lo + 1] - rw.at[lo]);
-    s.own = rw.own[lo];
+    of_row(s);
     const long long off = pos - rw.at[lo] * a.Hkv;
-    s.h = off <= 0x7fffffffll ? (int)((unsigned)off / (unsigned)s.pages) : (int)(off / s.pages);
-    s.at = pos - off + (long long)s.h * s.pages;
+    const int each = s.pages + kOwnSetup;
+    s.h = off <= 0x7fffffffll ? (int)((unsigned)off / (unsigned)each) : (int)(off / each);
+    s.at = pos - off + (long long)s.h * each;
     return s;
   };
   auto next_seq = [&](Seq s) {
-    s.at += s.pages;
+    s.at += s.pages + kOwnSetup;
     if (++s.h < a.Hkv) return s;
     s.h = 0;
-    do ++s.row; while (s.row < a.n && rw.at[s.row + 1] == rw.at[s.row]);
-    if (s.row < a.n) { s.pages = (int)(rw.at[s.row + 1] - rw.at[s.row]); s.own = rw.own[s.row]; }
+    s.row = row_behind(s.row);
+    if (s.row < a.n) of_row(s);
     return s;
   };
+  // pages [first, last) of sequence s are in this share
+  auto first_of = [&](const Seq& s) { return (int)max(0ll, begin - s.at - kOwnSetup); };
+  auto last_of = [&](const Seq& s) { return (int)min((long long)s.pages, max(0ll, end - s.at - kOwnSetup)); };
 
   // ---- the copies: up to kStages pages ahead.  Lane i holds the blocks of pages win + i of the sequence; those of the window
-  // behind are asked for when a window is entered.
+  // behind are asked for when a window is entered, those of the next row when a row is: a read of the table takes a page's time.
   const uint32_t ring = base + warp * kStages * kPageBytes;
-  Seq ps = seq_at(begin);
-  long long ppos = begin;
-  int win = 0, ids = 0, ids_next = 0, put = 0;
-  auto load_ids = [&](const Seq& s, int w) {
-    return w + lane < s.pages ? a.block_table[(size_t)s.row * a.max_pages + s.own + w + lane] : 0;
+  auto load_ids = [&](int row, int w) {
+    if (row >= a.n) return 0;
+    const int own = rw.own[row], pages = (int)(rw.at[row + 1] - rw.at[row]) - kOwnSetup;
+    return w + lane < pages ? a.block_table[(size_t)row * a.max_pages + own + w + lane] : 0;
   };
-  auto enter = [&](int page) { win = page; ids = load_ids(ps, win); ids_next = load_ids(ps, win + 32); };
-  enter((int)(ppos - ps.at));
+  // the next piece's query rows on their way to the L1
+  auto prefetch_q = [&](const Seq& s) {
+    if (s.row < a.n && s.at < end && lane < 2 * a.G)
+      asm volatile("prefetch.global.L1 [%0];" ::"l"(a.q + ((size_t)s.row * a.Hq + (size_t)s.h * a.G) * kD + lane * 64));
+  };
+  Seq s = seq_at(begin), ps = s;
+  int page = first_of(s), plast = last_of(s), win = page, put = 0;
+  int ids = load_ids(s.row, win), ids_next = load_ids(s.row, win + 32), ids_row = win == 0 ? ids : load_ids(s.row, 0);
+  int behind = row_behind(s.row), ids_behind = load_ids(behind, 0);
+  long long copies = 0, used = 0;                                      // begun; done with
+  bool any = page < plast;                                             // pages are left to copy
+  prefetch_q(next_seq(s));
   auto issue = [&]() {
-    if (ppos >= end) return;
-    int page = (int)(ppos - ps.at);
-    if (page == ps.pages) { ps = next_seq(ps); page = 0; enter(0); }
-    if (page - win >= 32) { win += 32; ids = ids_next; ids_next = load_ids(ps, win + 32); }
+    if (!any) return;
+    if (page - win >= 32) { win += 32; ids = ids_next; ids_next = load_ids(ps.row, win + 32); }
     int b = __shfl_sync(0xffffffffu, ids, page - win);
     if (b < 0 || b >= a.num_blocks) { if (lane == 0) flag_error(a.counters, STEP_ERR_BAD_BLOCK); b = 0; }
     if (lane == 0) {
@@ -177,21 +207,29 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
       bulk_load(ring + put * kPageBytes, a.kv + (((size_t)a.layer * a.num_blocks + b) * a.Hkv + ps.h) * (2 * kP * kD), kPageBytes, bars + 8 * put);
     }
     if (++put == kStages) put = 0;
-    ++ppos;
+    ++copies;
+    if (++page < plast) return;
+    const int row = ps.row;
+    ps = next_seq(ps);
+    any = ps.row < a.n && ps.at + kOwnSetup < end;
+    if (!any) return;
+    page = win = 0;
+    plast = last_of(ps);
+    if (ps.row != row) { ids_row = ids_behind; behind = row_behind(behind); ids_behind = load_ids(behind, 0); }
+    ids = ids_row;
+    ids_next = load_ids(ps.row, 32);
   };
-  for (int s = 0; s < kStages; ++s) issue();
+  for (int x = 0; x < kStages; ++x) issue();
 
   const int gr = lane >> 2, tq = lane & 3;                             // rows gr, gr + 8 and columns 2 tq, 2 tq + 1 of a tile
   // where this lane's address of an ldmatrix points, for K (chunk 2 x + kc of key kk) and V (chunk 2 x + vc of key vk)
   const int kk = (lane >> 4) * 8 + (lane & 7), kc = (lane >> 3) & 1, vk = ((lane >> 3) & 1) * 8 + (lane & 7), vc = lane >> 4;
   const bool upper = a.G > 8;                                          // (rows from 8 on are heads too)
   int get = 0;
-  long long used = begin;                                              // pages done with
   uint32_t ph = 0;
-  Seq s = seq_at(begin);
   bool ok = true;
-  for (long long pos = begin; pos < end && ok;) {
-    const int page0 = (int)(pos - s.at), cnt = (int)min((long long)(s.pages - page0), end - pos);
+  for (; s.row < a.n && s.at + kOwnSetup < end; s = next_seq(s)) {
+    const int page0 = first_of(s), cnt = last_of(s) - page0;
     const int S = rw.len[s.row] - s.own * kP;                          // own positions
     const __nv_bfloat16* q = a.q + ((size_t)s.row * a.Hq + (size_t)s.h * a.G) * kD;
     uint32_t qf[8][4];
@@ -290,14 +328,13 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
         if (tq == 0) reinterpret_cast<float2*>(whole ? a.all_ml : a.own_ml)[slot] = make_float2(m[z], l[z]);
       }
     }
-    pos += cnt;
-    if (pos < end) s = next_seq(s);
+    prefetch_q(next_seq(next_seq(s)));
   }
   if (!ok) {
     // a wait has run out: the copies in flight still write this CTA's shared memory
     flag_error(a.counters, STEP_ERR_TIMEOUT);
     if (lane == 0)
-      for (; used < ppos; ++used) {
+      for (; used < copies; ++used) {
         mbar_wait_bounded(bars + 8 * get, ph, kDrainNs);
         if (++get == kStages) { get = 0; ph ^= 1; }
       }
@@ -306,17 +343,15 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
 }
 
 // ---------------------------------------------------------------- shared pages
-struct Place { int g, hb, at; int4 grp; Shape x; };   // sequence hb = head * blocks + block of group g; at: units into it, kSetup counted first
-__device__ inline int width_of(const Place& p) { return p.hb % p.x.blocks == p.x.blocks - 1 ? p.x.last : 2; }
-__device__ inline int units_of(const Place& p) { return width_of(p) * p.x.tiles + kSetup; }
-// What a share that ends at `end` holds of the sequence at place p (stream position pos): the tiles that begin in it.
+struct Place { int g, hb, at; int4 grp; Shape x; };   // sequence hb = head * blocks + block of group g; at: how far into it, kSetup counted first
+// What a share that ends at `end` holds of the sequence at place p (stream position pos).  (No tile at all only at the share's
+// end, in front of a sequence's first.)
 struct Part { int tile0, cnt; long long len; };
 __device__ inline Part part_of(const Place& p, long long pos, long long end) {
-  const int w = width_of(p);
   Part x;
-  x.len = min((long long)(units_of(p) - p.at), end - pos);
-  x.tile0 = (max(0, p.at - kSetup) + w - 1) / w;
-  x.cnt = (max(0, (int)(p.at + x.len) - kSetup) + w - 1) / w - x.tile0;
+  x.len = min((long long)(p.x.tiles + kSetup - p.at), end - pos);
+  x.tile0 = max(0, p.at - kSetup);
+  x.cnt = max(0, (int)(p.at + x.len) - kSetup) - x.tile0;
   return x;
 }
 // The groups as this CTA keeps them: in shared memory, or, if they are many, in the workspace.
@@ -334,11 +369,10 @@ __device__ inline Place locate(const GroupArgs& a, const Table& tab, long long p
   p.g = g;
   p.grp = tab.groups[g];
   p.x = shape_of(a, p.grp);
-  const long long off = pos - tab.at[g], head = head_units(p.x);
-  const int h = off + head <= 0x7fffffffll ? (int)((unsigned)off / (unsigned)head) : (int)(off / head), wide = 2 * p.x.tiles + kSetup, in = (int)(off - h * head);
-  const int block = min(in / wide, p.x.blocks - 1);
-  p.hb = h * p.x.blocks + block;
-  p.at = in - block * wide;
+  const long long off = pos - tab.at[g];
+  const int each = p.x.tiles + kSetup;
+  p.hb = off <= 0x7fffffffll ? (int)((unsigned)off / (unsigned)each) : (int)(off / each);
+  p.at = (int)(off - (long long)p.hb * each);
   return p;
 }
 // The place behind a whole rest of a sequence.
@@ -365,6 +399,7 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
   extern __shared__ unsigned char smem_raw[];
   __shared__ long long s_sum[kThreads / 32];
   __shared__ Header s_header;
+  __shared__ float s_unit_ns;
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   unsigned char* sm = smem_raw + (base - raw);
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
@@ -387,7 +422,6 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
   for (int i = threadIdx.x; i < a.n; i += kThreads) {
     rw.own[i] = 0;
     rw.len[i] = length_of(a, i, first);
-    if (first) a.group_of[i] = -1;
   }
   Table tab;
   tab.n = __syncthreads_or(bad) ? 0 : a.n_groups;
@@ -410,23 +444,26 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
       for (int i = r0 + lane; i < r1; i += 32)
         if (rw.len[i] >= (long long)pages * kP) {
           rw.own[i] = pages;
-          if (first) a.group_of[i] = g;
+          if (first) a.plan[i].tiles = g + 1;                          // (for now: whose pages it shares)
         }
-    if (lane == 0) {
-      grp[g] = make_int4(r0, r1 - r0, leader, pages);
-      if (first) a.groups[g] = grp[g];
-    }
+    if (lane == 0) grp[g] = make_int4(r0, r1 - r0, leader, pages);
   }
   __syncthreads();
   // ---- where every group's tiles begin in their stream (one warp), and every row's own pages in theirs (a thread takes `per` rows)
   if (warp == kThreads / 32 - 1) {
     long long run = 0;
+    float ns = 0.f;
     for (int g0 = 0; g0 < tab.n; g0 += 32) {
       const int g = g0 + lane;
       long long mine = 0;
       if (g < tab.n) {
         const int4 x = grp[g];
-        if (x.z >= 0) mine = head_units(shape_of(a, x)) * a.Hkv;
+        if (x.z >= 0) {
+          const Shape sh = shape_of(a, x);
+          mine = (long long)(sh.tiles + kSetup) * sh.blocks * a.Hkv;
+          const int narrow = x.y - (sh.blocks - 1) * 2 * a.tokens <= a.tokens;
+          ns += (float)mine * (kWideNs - (kWideNs - kNarrowNs) * narrow / (float)sh.blocks);
+        }
       }
       long long incl = mine;
 #pragma unroll
@@ -434,17 +471,19 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
         const long long u = __shfl_up_sync(0xffffffffu, incl, o);
         if (lane >= o) incl += u;
       }
-      if (g < tab.n) {
-        grp_at[g] = run + incl - mine;
-        if (first) a.group_at[g] = run + incl - mine;
-      }
+      if (g < tab.n) grp_at[g] = run + incl - mine;
       run += __shfl_sync(0xffffffffu, incl, 31);
     }
-    if (lane == 0) s_header.units = run;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ns += __shfl_xor_sync(0xffffffffu, ns, o);
+    if (lane == 0) { s_header.units = run; s_unit_ns = ns / (float)max(1ll, run); }
   }
   {
     const int per = (a.n + kThreads - 1) / kThreads, i0 = threadIdx.x * per;
-    auto pages_of = [&](int i) { return (rw.len[i] + kP - 1) / kP - rw.own[i]; };
+    auto pages_of = [&](int i) {
+      const int pages = (rw.len[i] + kP - 1) / kP - rw.own[i];
+      return pages > 0 ? pages + kOwnSetup : 0;
+    };
     long long mine = 0;
     for (int i = i0; i < min(a.n, i0 + per); ++i) mine += pages_of(i);
     long long incl = mine;
@@ -459,16 +498,34 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
     for (int w = 0; w < warp; ++w) run += s_sum[w];
     for (int i = i0; i < min(a.n, i0 + per); ++i) {
       rw.at[i] = run;
-      if (first) a.own_at[i] = run;
       run += pages_of(i);
-      if (i == a.n - 1) { rw.at[a.n] = run; if (first) a.own_at[a.n] = run; }
+      if (i == a.n - 1) rw.at[a.n] = run;
     }
   }
   __syncthreads();
   Header hd;
   hd.units = s_header.units; hd.pages = rw.at[a.n] * a.Hkv; hd.groups = tab.n;
-  if (first && threadIdx.x == 0) *a.header = hd;
-  const int n_prefix = prefix_ctas(a, hd);
+  hd.n_prefix = choose_prefix(a, hd.units, s_unit_ns, hd.pages, lane);
+  const int n_prefix = hd.n_prefix;
+  if (first) {
+    if (threadIdx.x == 0) *a.header = hd;
+    for (int i = threadIdx.x; i < a.n; i += kThreads) {
+      RowPlan p = {};
+      p.at = rw.at[i];
+      p.pages = max(0, (int)(rw.at[i + 1] - rw.at[i]) - kOwnSetup);
+      if (rw.own[i] > 0) {
+        const int g = a.plan[i].tiles - 1;
+        const int4 x = grp[g];
+        const Shape sh = shape_of(a, x);
+        const int t = i - x.x, block = t / (2 * a.tokens);
+        p.tiles = sh.tiles;
+        p.head = sh.blocks * (sh.tiles + kSetup);
+        p.begin = grp_at[g] + (long long)block * (sh.tiles + kSetup);
+        p.place = (t - block * 2 * a.tokens) * 2 + (x.y - block * 2 * a.tokens <= a.tokens);
+      }
+      a.plan[i] = p;
+    }
+  }
 
   if ((int)blockIdx.x >= n_prefix) {
     // ================================================ own pages
@@ -706,16 +763,15 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
       if (pos < end) pl = locate(a, tab, pos, lane);
       for (;; par ^= 1) {
         Piece pc = {};
-        while (pos < end && pc.cnt == 0) {
-          const Part part = part_of(pl, pos, end);
-          if (part.cnt > 0) {
-            const int block = pl.hb % pl.x.blocks, t0 = block * 2 * a.tokens;
-            pc.h = pl.hb / pl.x.blocks;
-            pc.row0 = pl.grp.x + t0; pc.rows = min(2 * a.tokens, pl.grp.y - t0);
-            pc.two = width_of(pl) == 2;
-            pc.tile0 = part.tile0; pc.cnt = part.cnt; pc.tiles = pl.x.tiles; pc.keys = pl.grp.w * kP;
-            pc.slot = pos - pl.at <= pos0 ? 0 : 1;                     // of the share: does the sequence begin inside it?
-          }
+        Part part = {};
+        if (pos < end) part = part_of(pl, pos, end);
+        if (part.cnt > 0) {
+          pc.h = pl.hb / pl.x.blocks;
+          const int t0 = (pl.hb - pc.h * pl.x.blocks) * 2 * a.tokens;
+          pc.row0 = pl.grp.x + t0; pc.rows = min(2 * a.tokens, pl.grp.y - t0);
+          pc.two = pc.rows > a.tokens;
+          pc.tile0 = part.tile0; pc.cnt = part.cnt; pc.tiles = pl.x.tiles; pc.keys = pl.grp.w * kP;
+          pc.slot = pos - pl.at <= pos0 ? 0 : 1;                       // of the share: does the sequence begin inside it?
           pos += part.len;
           next_sequence(a, tab, pl);
         }
@@ -889,29 +945,19 @@ __global__ void __launch_bounds__(kMergeWarps * 32) groups_merge_kernel(const __
   const int lane = threadIdx.x & 31;
   wait_for_primary();
   const Header hd = *a.header;
-  const int n_prefix = prefix_ctas(a, hd);
-  const long long W = hd.pages > 0 ? own_share(hd, a.ctas - n_prefix) : 1, Wp = hd.units > 0 ? prefix_share(hd, n_prefix) : 1;
   auto share_of = [](long long x, long long by) { return x <= 0x7fffffffll ? (int)((unsigned)x / (unsigned)by) : (int)(x / by); };
   for (int r = blockIdx.x * kMergeWarps + (threadIdx.x >> 5); r < a.n * a.Hq; r += gridDim.x * kMergeWarps) {
     const int i = r / a.Hq, hq = r - i * a.Hq, h = hq / a.G, sub = hq - h * a.G;
-    const int g = a.group_of[i];
-    const long long at0 = a.own_at[i], pages = a.own_at[i + 1] - at0, at = at0 * a.Hkv + h * pages;
-    const int w0 = pages > 0 ? share_of(at, W) : 0, w1 = pages > 0 ? share_of(at + pages - 1, W) : -1;
-    if (g < 0 && w0 == w1) continue;                                   // written already
+    const RowPlan pl = a.plan[i];
+    const long long W = hd.pages > 0 ? own_share(hd, a.ctas - hd.n_prefix) : 1, Wp = hd.units > 0 ? prefix_share(hd, hd.n_prefix) : 1;
+    const long long at = pl.at * a.Hkv + (long long)h * (pl.pages + kOwnSetup);
+    const int w0 = pl.pages > 0 ? share_of(at + kOwnSetup, W) : 0, w1 = pl.pages > 0 ? share_of(at + kOwnSetup + pl.pages - 1, W) : -1;
+    if (pl.tiles == 0 && w0 == w1) continue;                           // written already
     // the pieces of the shared pages: shares p0 .. p1, each with one result or (narrow) one per lane
-    int p0 = 0, pieces = 0, narrow = 0, row = 0;
-    long long begin = 0;
-    if (g >= 0) {
-      const int4 grp = a.groups[g];
-      const Shape x = shape_of(a, grp);
-      const int t = i - grp.x, block = t / (2 * a.tokens), tb = t - block * 2 * a.tokens;
-      const int w = block == x.blocks - 1 ? x.last : 2, ln = tb / a.tokens;
-      begin = a.group_at[g] + h * head_units(x) + (long long)block * (2 * x.tiles + kSetup);
-      p0 = share_of(begin + kSetup, Wp);
-      narrow = w == 1;
-      pieces = (share_of(begin + kSetup + (long long)w * (x.tiles - 1), Wp) - p0 + 1) << narrow;
-      row = ln * kHalfRows + (tb - ln * a.tokens) * a.G + sub;
-    }
+    const long long begin = pl.begin + (long long)h * pl.head;
+    const int narrow = pl.place & 1, trace = pl.place >> 1, ln = trace / a.tokens, row = ln * kHalfRows + (trace - ln * a.tokens) * a.G + sub;
+    const int p0 = pl.tiles > 0 ? share_of(begin + kSetup, Wp) : 0;
+    const int pieces = pl.tiles > 0 ? (share_of(begin + kSetup + pl.tiles - 1, Wp) - p0 + 1) << narrow : 0;
     const bool whole = pieces == 1 << narrow;                          // one share has all tiles
     const int all = pieces + (w1 - w0 + 1);
     float M = -INFINITY, den = 0.f;
@@ -927,10 +973,10 @@ __global__ void __launch_bounds__(kMergeWarps * 32) groups_merge_kernel(const __
         const float *mls, *os;
         size_t slot;
         if (k < pieces) {
-          const int s = p0 + (k >> narrow), ln = k & narrow;
+          const int s = p0 + (k >> narrow), by = k & narrow;
           mls = whole ? a.row_ml : a.pre_ml;
           os = whole ? a.row_o : a.pre_o;
-          slot = whole ? (size_t)ln * a.n * a.Hq + r : ((size_t)s * 2 + (begin <= s * Wp ? 0 : 1)) * 2 * kHalfRows + ln * kHalfRows + row;
+          slot = whole ? (size_t)by * a.n * a.Hq + r : ((size_t)s * 2 + (begin <= s * Wp ? 0 : 1)) * 2 * kHalfRows + by * kHalfRows + row;
         } else {
           const int s = w0 + k - pieces;
           mls = w0 == w1 ? a.all_ml : a.own_ml;
@@ -968,14 +1014,11 @@ size_t lay_out(const step_pool* pool, int n, int n_groups, char* ws, GroupArgs* 
   auto take = [&](size_t bytes) { char* p = ws + off; off += (bytes + 255) / 256 * 256; return p; };
   GroupArgs x = {};
   x.header = (Header*)take(sizeof(Header));
-  x.groups = (int4*)take((size_t)n_groups * sizeof(int4));
-  x.group_at = (long long*)take((size_t)n_groups * 8);
+  x.plan = (RowPlan*)take((size_t)n * sizeof(RowPlan));
   if (n_groups > kTableGroups) {
     x.cta_groups = (int4*)take(ctas * n_groups * sizeof(int4));
     x.cta_group_at = (long long*)take(ctas * n_groups * 8);
   }
-  x.group_of = (int*)take((size_t)n * 4);
-  x.own_at = (long long*)take((size_t)(n + 1) * 8);
   x.own_ml = (float*)take(warps * 2 * g.G * 8);
   x.own_o = (float*)take(warps * 2 * g.G * kD * 4);
   if (n_groups > 0) {
@@ -1033,7 +1076,7 @@ int groups_tc_launch(step_pool* pool, int layer, const void* q, const int32_t* b
     return STEP_ERR_CUDA;
   groups_kernel<<<a.ctas, kThreads, kSmem, s>>>(map, map_q, a);
   if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
-  const long long rows = (long long)n * g.Hq, most = 4ll * a.ctas;
+  const long long rows = (long long)n * g.Hq, most = 16ll * a.ctas;
   const long long ctas = (rows + kMergeWarps - 1) / kMergeWarps;
   if (launch_dependent(groups_merge_kernel, dim3((unsigned)(ctas < most ? ctas : most)), dim3(kMergeWarps * 32), 0, s, a) != cudaSuccess) return STEP_ERR_CUDA;
   return launch_ok();
