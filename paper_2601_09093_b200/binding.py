@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -97,6 +98,10 @@ class kv_store_args(C.Structure):
                 ("q_row", C.c_longlong), ("q_layer", C.c_longlong), ("q_out_row", C.c_longlong), ("q_out_layer", C.c_longlong)]
 
 
+# (these two are filled in once per call: packing them takes a fifth of the time that making a Structure does)
+_pack_rotate = struct.Struct("@PP5i6qPqi0q").pack
+_pack_store = struct.Struct("@4i3P2P2q2P4q").pack
+
 _lib = None
 
 
@@ -132,9 +137,9 @@ def lib():
     L.kv_pool_evict_workspace_bytes.argtypes = [vp, i, i, szp]
     L.kv_pool_evict_positions.argtypes = [vp, vp, i, vp, vp, i, i, i, vp, vp, sz, vp]
     L.step_rotary_table.argtypes = [C.POINTER(step_rotary_config), vp, C.POINTER(step_rotary)]
-    L.rotate_positions.argtypes = [C.POINTER(rotate_args), C.POINTER(step_rotary), vp]
+    L.rotate_positions.argtypes = [vp, vp, vp]            # (rotate_args, step_rotary)
     L.kv_pool_extend.argtypes = [vp, vp, i, i, vp, vp]
-    L.store_kv_rotated.argtypes = [vp, C.POINTER(kv_store_args), C.POINTER(step_rotary), vp]
+    L.store_kv_rotated.argtypes = [vp, vp, vp, vp]        # (kv_store_args, step_rotary)
     L.decode_attention_groups_workspace_bytes.argtypes = [vp, i, i, szp]
     L.decode_attention_groups.argtypes = [vp, i, vp, vp, vp, i, vp, vp, i, vp, vp, sz, vp]
     L.score_steps.argtypes = [vp, vp, vp, vp, i, C.POINTER(scorer_weights), vp, vp]
@@ -179,8 +184,10 @@ def _raw_stream(device):
     return torch.cuda.current_stream(device).cuda_stream if _current_raw_stream is None else _current_raw_stream(device.index)
 
 
-# (the stream's number without the Stream object around it, where this torch has it)
+# (the stream's number without the Stream object around it, the device's without a look at whether CUDA is up, where this
+# torch has them)
 _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _at(t):
@@ -337,7 +344,7 @@ class KVPool:
         dev = self._device()
         if stream is not None and stream.device != dev:
             raise StepError(name, 1)
-        if stream is not None or torch.cuda.current_device() != dev.index:
+        if stream is not None or _current_device() != dev.index:
             with torch.cuda.device(dev), torch.cuda.stream(stream):
                 return self._call(name, args, size, workspace)
         if size is None:
@@ -452,24 +459,24 @@ class KVPool:
         if k.dim() != 5 or not 0 <= layer0 < self.num_layers:
             raise StepError(fn, 1)
         n, T, layers = k.shape[:3]
-        rows = (n, T, layers, self.num_kv_heads, self.head_dim)
-        heads = (layers, n, T, self.num_q_heads, self.head_dim)
+        Hq, Hkv, d = self.num_q_heads, self.num_kv_heads, self.head_dim
         _expect(fn, dev, (trace_ids, (n,), torch.int32), (start, (n,), torch.int32), (positions, (n,), torch.int32))
-        if layer0 + layers > self.num_layers or layers < 1 or n * T > _INT_MAX or (q is None and q_out is not None):
+        if layer0 + layers > self.num_layers or layers < 1 or n * T > _INT_MAX or rotary.device != dev or rotary.rotary_dim > d:
             raise StepError(fn, 1)
-        if rotary.device != dev or rotary.struct.rotary_dim > self.head_dim:
+        rows = (n, T, layers, Hkv, d)
+        k_row, v_row = _row_stride(fn, k, rows, dt, dev, 0), _row_stride(fn, v, rows, dt, dev, 0)
+        q_at = out_at = q_row = out_row = q_layer = out_layer = 0
+        if q is not None:
+            heads = (layers, n, T, Hq, d)
+            if q_out is None:
+                q_out = self._empty(heads, dt, stream)
+            q_row, out_row = _row_stride(fn, q, heads, dt, dev, 1), _row_stride(fn, q_out, heads, dt, dev, 1)
+            q_at, out_at, q_layer, out_layer = q.data_ptr(), q_out.data_ptr(), q.stride(0), q_out.stride(0)
+        elif q_out is not None:
             raise StepError(fn, 1)
-        for t, shape in ((k, rows), (v, rows), (q, heads), (q_out, heads)):
-            if t is not None and (t.dtype != dt or t.shape != shape or t.device != dev):
-                raise StepError(fn, 1)
-        if q is not None and q_out is None:
-            q_out = self._empty(heads, dt, stream)
-        k_row, v_row = (_row_stride(fn, t.stride(), rows, 0, 2) for t in (k, v))
-        q_row, qo_row = (0 if t is None else _row_stride(fn, t.stride(), heads, 1, 3) for t in (q, q_out))
-        args = kv_store_args(layer0, layers, n, T, trace_ids.data_ptr(), start.data_ptr(), _at(positions), k.data_ptr(), v.data_ptr(),
-                             k_row, v_row, _at(q), _at(q_out), q_row, 0 if q is None else q.stride(0), qo_row,
-                             0 if q is None else q_out.stride(0))
-        self._call(fn, (C.byref(args), C.byref(rotary.struct)), stream=stream)
+        args = _pack_store(layer0, layers, n, T, trace_ids.data_ptr(), start.data_ptr(), _at(positions), k.data_ptr(), v.data_ptr(),
+                           k_row, v_row, q_at, out_at, q_row, q_layer, out_row, out_layer)
+        self._call(fn, (args, rotary.ref), stream=stream)
         return q_out
 
     def decode_attention_groups(self, layer, q, block_table, seq_lens, group_rows, group_pages, out=None, workspace=None, stream=None):
@@ -624,18 +631,18 @@ class KVPool:
         return dict(n_rows=n.value, tc_units=u.value)
 
 
-def _row_stride(fn, strides, shape, row_dim, inner):
-    """Elements from one (entry, token) row to the next, where dims row_dim, row_dim + 1 are entries and tokens and those from
-    `inner` on make up a row without gaps."""
-    size = 1
-    for i in range(len(shape) - 1, inner - 1, -1):
-        if shape[i] != 1 and strides[i] != size:
-            raise StepError(fn, 1)
-        size *= shape[i]
-    n, T = shape[row_dim], shape[row_dim + 1]
-    if n > 1 and T > 1 and strides[row_dim] != T * strides[row_dim + 1]:
+def _row_stride(fn, t, shape, dtype, device, row_dim):
+    """Elements from one (entry, token) row of t to the next, where dims row_dim, row_dim + 1 are entries and tokens; the last two,
+    and a layer dim right before them, make up a row without gaps."""
+    if t.dtype != dtype or t.shape != shape or t.device != device:
         raise StepError(fn, 1)
-    return strides[row_dim + 1] if T > 1 else strides[row_dim]
+    st = t.stride()
+    n, T, (layers, heads, d) = shape[row_dim], shape[row_dim + 1], shape[2:]
+    if (d > 1 and st[4] != 1) or (heads > 1 and st[3] != d) or (row_dim == 0 and layers > 1 and st[2] != heads * d):
+        raise StepError(fn, 1)
+    if n > 1 and T > 1 and st[row_dim] != T * st[row_dim + 1]:
+        raise StepError(fn, 1)
+    return st[row_dim + 1] if T > 1 else st[row_dim]
 
 
 class Rotary:
@@ -661,38 +668,41 @@ class Rotary:
         self.table = table.to(device)
         self.device = self.table.device
         self.struct.table = self.table.data_ptr()
+        self.rotary_dim, self.ref = rotary_dim, C.byref(self.struct)
 
 
 def rotate_positions(x, rotary, positions=None, out=None, transpose=False, stream=None):
     """x [batch, rows, heads, d] or [rows, heads, d], any strides but the last dim's, turned by positions ([rows] or
     [batch, rows] int32; None: the row's number) -> out (a new contiguous tensor; it may be x).  transpose: the transposed
     rotation, which takes the gradient of the result to the gradient of x."""
-    fn, dev = "rotate_positions", x.device
-    if x.dim() not in (3, 4) or x.dtype not in _STEP_DTYPE or dev != rotary.device or rotary.struct.rotary_dim > x.shape[-1]:
+    fn, dev, shape = "rotate_positions", x.device, x.shape
+    code = _STEP_DTYPE.get(x.dtype)
+    if code is None or len(shape) not in (3, 4) or dev != rotary.device or rotary.rotary_dim > shape[-1]:
         raise StepError(fn, 1)
     if stream is not None and stream.device != dev:
         raise StepError(fn, 1)
-    if stream is not None or torch.cuda.current_device() != dev.index:
+    if stream is not None or _current_device() != dev.index:
         with torch.cuda.device(dev), torch.cuda.stream(stream):
             return rotate_positions(x, rotary, positions, out, transpose)
-    shape = x.shape if x.dim() == 4 else (1,) + tuple(x.shape)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=dev)
-    if out.shape != x.shape or out.dtype != x.dtype or out.device != dev or max(shape) > _INT_MAX:
+        out = torch.empty(shape, dtype=x.dtype, device=dev)
+    elif out.shape != shape or out.dtype != x.dtype or out.device != dev:
         raise StepError(fn, 1)
-    xs, os = ((t.stride() if t.dim() == 4 else (0,) + t.stride()) for t in (x, out))
-    if shape[3] > 1 and (xs[3] != 1 or os[3] != 1):
+    xs, os = x.stride(), out.stride()
+    if len(shape) == 3:
+        shape, xs, os = (1, *shape), (0, *xs), (0, *os)
+    batch, rows, heads, d = shape
+    if (d > 1 and (xs[3] != 1 or os[3] != 1)) or max(shape) > _INT_MAX:
         raise StepError(fn, 1)
-    step = 0
+    at = step = 0
     if positions is not None:
-        if positions.dtype != torch.int32 or positions.device != dev or positions.shape not in ((shape[1],), (shape[0], shape[1])):
+        if positions.dtype != torch.int32 or positions.device != dev or positions.shape not in ((rows,), (batch, rows)):
             raise StepError(fn, 1)
-        if shape[1] > 1 and positions.stride(-1) != 1:
+        if rows > 1 and positions.stride(-1) != 1:
             raise StepError(fn, 1)
-        step = positions.stride(0) if positions.dim() == 2 else 0
-    args = rotate_args(x.data_ptr(), out.data_ptr(), _STEP_DTYPE[x.dtype], *shape, *xs[:3], *os[:3], _at(positions), step,
-                       int(bool(transpose)))
-    _check(fn, lib().rotate_positions(C.byref(args), C.byref(rotary.struct), _raw_stream(dev)))
+        at, step = positions.data_ptr(), positions.stride(0) if positions.dim() == 2 else 0
+    args = _pack_rotate(x.data_ptr(), out.data_ptr(), code, batch, rows, heads, d, *xs[:3], *os[:3], at, step, 1 if transpose else 0)
+    _check(fn, lib().rotate_positions(args, rotary.ref, _raw_stream(dev)))
     return out
 
 

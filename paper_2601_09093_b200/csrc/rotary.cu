@@ -68,6 +68,21 @@ __device__ inline void chunks_of(int u, int D, int& a, int& b) {
 }
 
 // ---------------------------------------------------------------- rotate_positions
+// x / by for 0 <= x < 2^31 and a divisor that the host knows: two instructions instead of twenty.
+struct Quotient {
+  unsigned by, mul, shift;
+};
+inline Quotient quotient(int by) {
+  Quotient q;
+  q.by = (unsigned)by;
+  int log = 0;
+  while ((1ll << log) < by) ++log;
+  q.shift = by == 1 ? 0 : log - 1;
+  q.mul = (unsigned)(((1ull << (31 + log)) + by - 1) / by);            // (not used for 1)
+  return q;
+}
+__device__ inline int over(int x, const Quotient& q) { return q.by == 1 ? x : (int)(__umulhi((unsigned)x, q.mul) >> q.shift); }
+
 struct RotateDev {
   const void* x; void* out;
   const int32_t* positions; long long position_batch;
@@ -75,35 +90,49 @@ struct RotateDev {
   long long x_batch, x_row, x_head, out_batch, out_row, out_head;      // elements
   int batch, rows, heads, d, D;
   float scale, sign;
-  int heads_per_task, tasks_per_row;
   int copy_tail;                    // dims behind D are copied (not in place)
+  int heads_per_task, tasks_per_row;                                   // rotate_rows_kernel
+  int rows_per_cta;                                                    // rotate_flat_kernel
+  Quotient by_rows, by_half, by_units, by_heads, by_tail;
 };
 
-constexpr int kRotateWarps = 8, kRotateAhead = 4;
+constexpr int kRotateThreads = 256, kRotateAhead = 2, kRotateAngles = 2048;   // (ahead 4: 104 registers, 35 us for 8191 rows of 40 heads instead of 31)
+constexpr int kRotateWarps = kRotateThreads / 32;
 
-// A warp takes one row and a range of its heads.  Lanes: a unit each, as many heads at once as there is room for.
+// Rows of many heads: a warp takes one row and a range of its heads.  It makes the cosines and sines of the row's pairs once (in
+// shared memory); a lane keeps those of its unit and goes through the heads with nothing but adds, as many heads at once as there
+// is room for.  64 x 1024 rows of 64 heads of 128 in bf16: 328 us, 6.5 TB/s (the measured copy); numbering the units
+// of all heads and rows, as rotate_flat_kernel does, took 662 us: 60 instructions of indexing per unit.
 template <typename T, bool kPairs>
-__global__ void __launch_bounds__(kRotateWarps * 32) rotate_kernel(const RotateDev a) {
+__global__ void __launch_bounds__(kRotateThreads) rotate_rows_kernel(const __grid_constant__ RotateDev a) {
   constexpr int kU = 16 / (int)sizeof(T);
-  const int lane = threadIdx.x & 31;
-  const long long task = (long long)blockIdx.x * kRotateWarps + (threadIdx.x >> 5);
+  __shared__ float2 s_angle[kRotateAngles];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long task = (long long)blockIdx.x * kRotateWarps + warp;
   const long long row = task / a.tasks_per_row;
   if (row >= (long long)a.batch * a.rows) return;
   const int h0 = (int)(task - row * a.tasks_per_row) * a.heads_per_task, h1 = min(a.heads, h0 + a.heads_per_task);
   const int bi = (int)(row / a.rows), ri = (int)(row - (long long)bi * a.rows);
-  const int p = a.positions ? a.positions[bi * a.position_batch + ri] : ri;
   const T* x = (const T*)a.x + bi * a.x_batch + ri * a.x_row;
   T* out = (T*)a.out + bi * a.out_batch + ri * a.out_row;
-  const int units = a.D / (2 * kU), across = min(units, 32), together = 32 / across;
+  const int half = a.D / 2, units = a.D / (2 * kU), across = min(units, 32), together = 32 / across;
+  float2* angle = s_angle + warp * (kRotateAngles / kRotateWarps);
+  const int p = a.positions ? a.positions[bi * a.position_batch + ri] : ri;
+  for (int i = lane; i < half; i += 32) {
+    float c, s;
+    angle_of(p, a.table[i], a.scale, c, s);
+    angle[i] = make_float2(c, s * a.sign);
+  }
+  __syncwarp();
   const int sub = lane / across;
   for (int u0 = 0; u0 < units; u0 += across) {
     const int u = u0 + lane - sub * across;
     if (sub >= together || u >= units) continue;
     float c[kU], s[kU];
 #pragma unroll
-    for (int i = 0; i < kU; ++i) {
-      angle_of(p, a.table[u * kU + i], a.scale, c[i], s[i]);
-      s[i] *= a.sign;
+    for (int i = 0; i < kU; i += 2) {
+      const float4 v = reinterpret_cast<const float4*>(angle + u * kU)[i / 2];
+      c[i] = v.x; s[i] = v.y; c[i + 1] = v.z; s[i + 1] = v.w;
     }
     int ca, cb;
     chunks_of<T, kPairs>(u, a.D, ca, cb);
@@ -133,15 +162,95 @@ __global__ void __launch_bounds__(kRotateWarps * 32) rotate_kernel(const RotateD
   if (a.copy_tail) {
     const int first = a.D / kU, tail = a.d / kU - first;
     for (int i = lane; i < (h1 - h0) * tail; i += 32) {
-      const int h = h0 + i / tail, ch = first + i % tail;
-      reinterpret_cast<uint4*>(out + h * a.out_head)[ch] = reinterpret_cast<const uint4*>(x + h * a.x_head)[ch];
+      const int hy = over(i, a.by_tail), ch = first + i - hy * tail;
+      reinterpret_cast<uint4*>(out + (h0 + hy) * a.out_head)[ch] = reinterpret_cast<const uint4*>(x + (h0 + hy) * a.x_head)[ch];
+    }
+  }
+}
+
+// Rows of few heads: a CTA takes up to rows_per_cta rows.  Cosines and sines of all pairs of its rows once,
+// into shared memory; then its threads go through the units of all heads of all rows, kRotateAhead of them under way at once.
+// 33 x 1021 rows of 5 heads of 64, fp32, half of each turned: 16.5 us where a warp per row took 37 (most of its lanes idle).
+template <typename T, bool kPairs>
+__global__ void __launch_bounds__(kRotateThreads) rotate_flat_kernel(const __grid_constant__ RotateDev a) {
+  constexpr int kU = 16 / (int)sizeof(T);
+  __shared__ float2 s_angle[kRotateAngles];
+  const int row0 = blockIdx.x * a.rows_per_cta, n_rows = min(a.rows_per_cta, a.batch * a.rows - row0);
+  const int heads = a.heads, half = a.D / 2, units = a.D / (2 * kU);
+  for (int x = threadIdx.x; x < n_rows * half; x += kRotateThreads) {
+    const int r = over(x, a.by_half), pair = x - r * half, bi = over(row0 + r, a.by_rows), ri = row0 + r - bi * a.rows;
+    float c, s;
+    angle_of(a.positions ? a.positions[bi * a.position_batch + ri] : ri, a.table[pair], a.scale, c, s);
+    s_angle[x] = make_float2(c, s * a.sign);
+  }
+  __syncthreads();
+  // (row, head) number x of this CTA: where it lies
+  auto place = [&](int x, int& r, long long& in, long long& out) {
+    r = over(x, a.by_heads);
+    const int h = x - r * heads, bi = over(row0 + r, a.by_rows), ri = row0 + r - bi * a.rows;
+    in = bi * a.x_batch + ri * a.x_row + h * a.x_head;
+    out = bi * a.out_batch + ri * a.out_row + h * a.out_head;
+  };
+  const int items = n_rows * heads * units;
+  for (int i0 = threadIdx.x; i0 < items; i0 += kRotateAhead * kRotateThreads) {
+    uint4 va[kRotateAhead], vb[kRotateAhead];
+    uint4 *da[kRotateAhead], *db[kRotateAhead];
+    const float4* cs[kRotateAhead];
+#pragma unroll
+    for (int y = 0; y < kRotateAhead; ++y) {
+      const int i = i0 + y * kRotateThreads;
+      if (i >= items) continue;
+      const int x = over(i, a.by_units), u = i - x * units;
+      int r, ca, cb;
+      long long in, out;
+      place(x, r, in, out);
+      chunks_of<T, kPairs>(u, a.D, ca, cb);
+      const uint4* src = reinterpret_cast<const uint4*>((const T*)a.x + in);
+      va[y] = src[ca];
+      vb[y] = src[cb];
+      da[y] = reinterpret_cast<uint4*>((T*)a.out + out) + ca;
+      db[y] = reinterpret_cast<uint4*>((T*)a.out + out) + cb;
+      cs[y] = reinterpret_cast<const float4*>(s_angle + r * half + u * kU);
+    }
+#pragma unroll
+    for (int y = 0; y < kRotateAhead; ++y) {
+      if (i0 + y * kRotateThreads >= items) continue;
+      float c[kU], s[kU];
+#pragma unroll
+      for (int x = 0; x < kU; x += 2) {
+        const float4 v = cs[y][x / 2];
+        c[x] = v.x; s[x] = v.y; c[x + 1] = v.z; s[x + 1] = v.w;
+      }
+      turn_unit<T, kPairs>(va[y], vb[y], c, s);
+      *da[y] = va[y];
+      *db[y] = vb[y];
+    }
+  }
+  if (a.copy_tail) {
+    const int first = a.D / kU, tail = a.d / kU - first, chunks = n_rows * heads * tail;
+    for (int i0 = threadIdx.x; i0 < chunks; i0 += kRotateAhead * kRotateThreads) {
+      uint4 v[kRotateAhead], *dst[kRotateAhead];
+#pragma unroll
+      for (int y = 0; y < kRotateAhead; ++y) {
+        const int i = i0 + y * kRotateThreads;
+        if (i >= chunks) continue;
+        const int x = over(i, a.by_tail), c = first + i - x * tail;
+        int r;
+        long long in, out;
+        place(x, r, in, out);
+        v[y] = reinterpret_cast<const uint4*>((const T*)a.x + in)[c];
+        dst[y] = reinterpret_cast<uint4*>((T*)a.out + out) + c;
+      }
+#pragma unroll
+      for (int y = 0; y < kRotateAhead; ++y)
+        if (i0 + y * kRotateThreads < chunks) *dst[y] = v[y];
     }
   }
 }
 
 // Any alignment, any even D: a thread takes one pair, or one dim behind D, at a time.
 template <typename T, bool kPairs>
-__global__ void __launch_bounds__(256) rotate_any_kernel(const RotateDev a) {
+__global__ void __launch_bounds__(256) rotate_any_kernel(const __grid_constant__ RotateDev a) {
   const int half = a.D / 2, items = half + (a.copy_tail ? a.d - a.D : 0);
   const long long all = (long long)a.batch * a.rows * a.heads * items;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
@@ -179,11 +288,11 @@ struct StoreDev {
 };
 
 constexpr int kMaxPairs = 256;                                           // head_dim <= 512
-constexpr int kStoreAhead = 2;
 
 // A CTA takes one (entry, token) row and a range of layers: cosines and sines of its position once, into shared memory;
 // where the row goes (block and slot, the same for every layer and head) once; then its warps share the heads.
-// kChunks: whole units (D a multiple of two chunks); else pair by pair.
+// kChunks: whole units (D a multiple of two chunks); else pair by pair.  32 tokens for 64 traces, 36 layers of 32 / 8 heads of 128 in
+// bf16, with their queries: 290 us, 1.81 GB at 6.3 TB/s; one token, one layer: 4 us, the latency of four dependent reads.
 template <typename T, bool kPairs, bool kChunks>
 __global__ void __launch_bounds__(256) store_kernel(const StoreDev a) {
   constexpr int kU = 16 / (int)sizeof(T);
@@ -240,27 +349,14 @@ __global__ void __launch_bounds__(256) store_kernel(const StoreDev a) {
         for (int x = 0; x < kU; ++x) { c[x] = s_c[u * kU + x]; s[x] = s_s[u * kU + x]; }
         int ca, cb;
         chunks_of<T, kPairs>(u, a.D, ca, cb);
-        for (int hh = warp * together + sub; hh < total; hh += kStoreAhead * warps * together) {
-          uint4 va[kStoreAhead], vb[kStoreAhead];
-#pragma unroll
-          for (int y = 0; y < kStoreAhead; ++y) {
-            const int hy = hh + y * warps * together;
-            if (hy < total) {
-              const uint4* src = reinterpret_cast<const uint4*>(from(hy));
-              va[y] = src[ca];
-              vb[y] = src[cb];
-            }
-          }
-#pragma unroll
-          for (int y = 0; y < kStoreAhead; ++y) {
-            const int hy = hh + y * warps * together;
-            if (hy < total) {
-              turn_unit<T, kPairs>(va[y], vb[y], c, s);
-              uint4* dst = reinterpret_cast<uint4*>(to(hy));
-              dst[at(ca)] = va[y];
-              dst[at(cb)] = vb[y];
-            }
-          }
+        // (a head at a time: with two under way the 32 more registers cost a CTA per SM, and 339 us instead of 308)
+        for (int hh = warp * together + sub; hh < total; hh += warps * together) {
+          const uint4* src = reinterpret_cast<const uint4*>(from(hh));
+          uint4* dst = reinterpret_cast<uint4*>(to(hh));
+          uint4 va = src[ca], vb = src[cb];
+          turn_unit<T, kPairs>(va, vb, c, s);
+          dst[at(ca)] = va;
+          dst[at(cb)] = vb;
         }
       }
     } else {
@@ -312,12 +408,26 @@ int launch_rotate(const RotateDev& a0, int pairs, cudaStream_t s) {
   RotateDev a = a0;
   const long long strides = a.x_batch | a.x_row | a.x_head | a.out_batch | a.out_row | a.out_head;
   // whole 16-byte chunks wherever the shape allows it
-  const bool chunks = a.D % (2 * kU) == 0 && (!a.copy_tail || a.d % kU == 0) && strides % kU == 0 &&
+  const bool chunks = a.D % (2 * kU) == 0 && a.D / 2 <= kRotateAngles / kRotateWarps && (!a.copy_tail || a.d % kU == 0) && strides % kU == 0 &&
                       !(((uintptr_t)a.x | (uintptr_t)a.out) & 15);
   const long long rows = (long long)a.batch * a.rows;
-  if (chunks) {
+  const int half = a.D / 2, units = a.D / (2 * kU);
+  a.by_tail = quotient(a.copy_tail && chunks ? (a.d - a.D) / kU : 1);
+  // (the flat form numbers its rows, and what one CTA goes through, in 31 bits)
+  if (chunks && (long long)a.heads * units < 32 * kRotateAhead && rows <= 0x3fffffffll) {
+    // kRotateAhead units a thread, unless that leaves SMs without work
+    const int most = kRotateAngles / half, row_units = a.heads * units;
+    long long per = (kRotateAhead * kRotateThreads + row_units - 1) / row_units;
+    if (per > most) per = most;
+    if (per > rows / (2 * 148)) per = rows / (2 * 148);
+    a.rows_per_cta = per < 1 ? 1 : (int)per;
+    a.by_rows = quotient(a.rows); a.by_half = quotient(half); a.by_units = quotient(units); a.by_heads = quotient(a.heads);
+    const unsigned ctas = (unsigned)((rows + a.rows_per_cta - 1) / a.rows_per_cta);
+    if (pairs) rotate_flat_kernel<T, true><<<ctas, kRotateThreads, 0, s>>>(a);
+    else rotate_flat_kernel<T, false><<<ctas, kRotateThreads, 0, s>>>(a);
+  } else if (chunks) {
     // a warp takes all heads of a row; where that leaves SMs without work, fewer
-    const int units = a.D / (2 * kU), together = units < 32 ? 32 / units : 1;
+    const int together = units < 32 ? 32 / units : 1;
     int per = a.heads;
     while (per > together && rows * ((a.heads + per - 1) / per) < 148ll * 16) per = (per + 1) / 2;
     per = (per + together - 1) / together * together;
@@ -325,8 +435,8 @@ int launch_rotate(const RotateDev& a0, int pairs, cudaStream_t s) {
     a.tasks_per_row = (a.heads + per - 1) / per;
     const long long ctas = (rows * a.tasks_per_row + kRotateWarps - 1) / kRotateWarps;
     if (ctas > 0x7fffffffll) return STEP_ERR_INVALID_ARG;
-    if (pairs) rotate_kernel<T, true><<<(unsigned)ctas, kRotateWarps * 32, 0, s>>>(a);
-    else rotate_kernel<T, false><<<(unsigned)ctas, kRotateWarps * 32, 0, s>>>(a);
+    if (pairs) rotate_rows_kernel<T, true><<<(unsigned)ctas, kRotateThreads, 0, s>>>(a);
+    else rotate_rows_kernel<T, false><<<(unsigned)ctas, kRotateThreads, 0, s>>>(a);
   } else {
     const long long items = rows * a.heads * (a.D / 2 + (a.copy_tail ? a.d - a.D : 0));
     const long long ctas = (items + 255) / 256 < 148 * 16 ? (items + 255) / 256 : 148 * 16;
