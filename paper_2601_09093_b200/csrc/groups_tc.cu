@@ -50,12 +50,12 @@ constexpr int kOwnSetup = 2;                      // pages' worth of time that a
 
 // Tiles in the prefix stream, own pages (of all KV heads; setups counted in both), groups of a valid description (else 0), CTAs that
 // take shared pages (the others take own pages).
-struct Header { long long units, pages; int groups, n_prefix; };
+struct Header { int units, pages, groups, n_prefix; };
 
 // What a row's result is combined from.
-struct RowPlan {
-  long long at;                     // where the row's own pages begin in their stream, KV head 0: Hkv times this
-  long long begin;                  // where the tiles of the row's block of its group begin in the prefix stream, KV head 0
+struct RowPlan {                     // (positions in both streams fit 32 bits: groups_tc_supported)
+  int at;                           // where the row's own pages begin in their stream, KV head 0: Hkv times this
+  int begin;                        // where the tiles of the row's block of its group begin in the prefix stream, KV head 0
   int pages, tiles;                 // own pages; tiles it shares (0: none)
   int head;                         // from one KV head's tiles to the next's
   int place;                        // of its heads in the block: trace * 2 + 1 if the block has results of two lanes for a row
@@ -75,30 +75,31 @@ struct GroupArgs {
   Header* header;
   RowPlan* plan;                    // [n]
   int4* cta_groups;                 // [ctas][n_groups] the groups as every CTA finds them for itself (more than kTableGroups)
-  long long* cta_group_at;
+  int* cta_group_at;
   float *pre_ml, *pre_o;            // [CTA][2][lane][128] (m, l) and o of the prefix pieces that are not whole sequences
   float *row_ml, *row_o;            // [lane][n][Hq] of those that are
   float *own_ml, *own_o;            // [warp][2][G] of the own pages' pieces that are not whole sequences
   float *all_ml, *all_o;            // [n][Hq] of those that are, where there are shared pages besides
 };
 
+__device__ inline int div_up(int x, int by) { return (int)(((unsigned)x + (unsigned)by - 1) / (unsigned)by); }
+
 // One warp: how many CTAs take shared pages, so that the slower kind of CTA is as fast as can be.  (Around the ratio of the work,
 // a candidate per lane: with few tiles a share is a whole number of them.)
-__device__ inline int choose_prefix(const GroupArgs& a, long long units, float unit_ns, long long pages, int lane) {
+__device__ inline int choose_prefix(const GroupArgs& a, int units, float unit_ns, int pages, int lane) {
   if (units == 0 || pages == 0) return units == 0 ? 0 : a.ctas;
   const float ratio = (float)units * unit_ns / ((float)units * unit_ns + (float)pages * (kPageNs / (float)kStreamWarps));
   const int at = (int)(ratio * a.ctas) - 12 + lane;
-  unsigned long long key = ~0ull;
-  if (at >= 1 && at < a.ctas) {
-    const long long t = max(kPrefixNs + (long long)((float)div_up(units, at) * unit_ns), kOwnNs + div_up(pages, (a.ctas - at) * kStreamWarps) * kPageNs);
-    key = (unsigned long long)t << 16 | at;
-  }
+  float t = INFINITY;
+  if (at >= 1 && at < a.ctas)
+    t = fmaxf(kPrefixNs + (float)div_up(units, at) * unit_ns, kOwnNs + (float)div_up(pages, (a.ctas - at) * kStreamWarps) * kPageNs);
+  float best = t;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) key = min(key, __shfl_xor_sync(0xffffffffu, key, o));
-  return (int)(key & 0xffff);
+  for (int o = 16; o > 0; o >>= 1) best = fminf(best, __shfl_xor_sync(0xffffffffu, best, o));
+  return __shfl_sync(0xffffffffu, at, __ffs(__ballot_sync(0xffffffffu, t == best)) - 1);
 }
-__device__ inline long long prefix_share(const Header& h, int ctas) { return div_up(h.units, ctas); }
-__device__ inline long long own_share(const Header& h, int ctas) { return div_up(h.pages, ctas * kStreamWarps); }
+__device__ inline int prefix_share(const Header& h, int ctas) { return div_up(h.units, ctas); }
+__device__ inline int own_share(const Header& h, int ctas) { return div_up(h.pages, ctas * kStreamWarps); }
 
 __device__ inline int length_of(const GroupArgs& a, int i, bool flag) {
   int S = a.seq_lens[i];
@@ -129,28 +130,28 @@ __device__ inline void mma16816(float (&c)[4], const uint32_t* a, uint32_t b0, u
 }
 
 constexpr size_t kRing = (size_t)kStreamWarps * kStages * kPageBytes;                      // rings of own pages
-constexpr size_t kStreamSmem = 1024 + kRing + (kMaxTracesFast + 1) * 8 + 2 * kMaxTracesFast * 4 + kStreamWarps * kStages * 8;
+constexpr size_t kStreamSmem = 1024 + kRing + (kMaxTracesFast + 2) * 4 + 2 * kMaxTracesFast * 4 + kStreamWarps * kStages * 8;
 
 // What every CTA works out first, in shared memory behind the rings of own pages.
 struct Rows {
-  long long* at;                    // [n + 1] own pages of the rows before, setups counted
+  int* at;                          // [n + 1] own pages of the rows before, setups counted
   int* own;                         // [n] pages that the row shares
   int* len;                         // [n] its length, at most what the table holds
 };
 
 // This CTA's share of the own pages: `share` of them for each of its warps, this one the me-th of all.
-__device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, unsigned char* sm, uint32_t base, uint32_t bars, int me, long long total, long long W) {
+__device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, unsigned char* sm, uint32_t base, uint32_t bars, int me, int total, int W) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long begin = min(total, me * W), end = min(total, begin + W);
+  const int begin = (int)min((long long)total, (long long)me * W), end = min(total - begin, W) + begin;
   if (begin >= end) return;
   // the sequence that holds a position of the stream
-  struct Seq { int row, h, pages, own; long long at; };                // at: where it begins
-  auto of_row = [&](Seq& s) { s.pages = (int)(rw.at[s.row + 1] - rw.at[s.row]) - kOwnSetup; s.own = rw.own[s.row]; };
+  struct Seq { int row, h, pages, own, at; };                          // at: where it begins
+  auto of_row = [&](Seq& s) { s.pages = rw.at[s.row + 1] - rw.at[s.row] - kOwnSetup; s.own = rw.own[s.row]; };
   auto row_behind = [&](int row) {                                     // that has pages
     do ++row; while (row < a.n && rw.at[row + 1] == rw.at[row]);
     return row;
   };
-  auto seq_at = [&](long long pos) {
+  auto seq_at = [&](int pos) {
     int lo = 0, hi = a.n - 1;                                          // the last row that begins at or before pos: it has pages
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -159,10 +160,9 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
     Seq s;
     s.row = lo;
     of_row(s);
-    const long long off = pos - rw.at[lo] * a.Hkv;
-    const int each = s.pages + kOwnSetup;
-    s.h = off <= 0x7fffffffll ? (int)((unsigned)off / (unsigned)each) : (int)(off / each);
-    s.at = pos - off + (long long)s.h * each;
+    const int off = pos - rw.at[lo] * a.Hkv, each = s.pages + kOwnSetup;
+    s.h = (int)((unsigned)off / (unsigned)each);
+    s.at = pos - off + s.h * each;
     return s;
   };
   auto next_seq = [&](Seq s) {
@@ -174,15 +174,15 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
     return s;
   };
   // pages [first, last) of sequence s are in this share
-  auto first_of = [&](const Seq& s) { return (int)max(0ll, begin - s.at - kOwnSetup); };
-  auto last_of = [&](const Seq& s) { return (int)min((long long)s.pages, max(0ll, end - s.at - kOwnSetup)); };
+  auto first_of = [&](const Seq& s) { return max(0, begin - s.at - kOwnSetup); };
+  auto last_of = [&](const Seq& s) { return min(s.pages, max(0, end - s.at - kOwnSetup)); };
 
   // ---- the copies: up to kStages pages ahead.  Lane i holds the blocks of pages win + i of the sequence; those of the window
   // behind are asked for when a window is entered, those of the next row when a row is: a read of the table takes a page's time.
   const uint32_t ring = base + warp * kStages * kPageBytes;
   auto load_ids = [&](int row, int w) {
     if (row >= a.n) return 0;
-    const int own = rw.own[row], pages = (int)(rw.at[row + 1] - rw.at[row]) - kOwnSetup;
+    const int own = rw.own[row], pages = rw.at[row + 1] - rw.at[row] - kOwnSetup;
     return w + lane < pages ? a.block_table[(size_t)row * a.max_pages + own + w + lane] : 0;
   };
   // the next piece's query rows on their way to the L1
@@ -194,7 +194,7 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
   int page = first_of(s), plast = last_of(s), win = page, put = 0;
   int ids = load_ids(s.row, win), ids_next = load_ids(s.row, win + 32), ids_row = win == 0 ? ids : load_ids(s.row, 0);
   int behind = row_behind(s.row), ids_behind = load_ids(behind, 0);
-  long long copies = 0, used = 0;                                      // begun; done with
+  int copies = 0, used = 0;                                      // begun; done with
   bool any = page < plast;                                             // pages are left to copy
   prefetch_q(next_seq(s));
   auto issue = [&]() {
@@ -346,18 +346,18 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
 struct Place { int g, hb, at; int4 grp; Shape x; };   // sequence hb = head * blocks + block of group g; at: how far into it, kSetup counted first
 // What a share that ends at `end` holds of the sequence at place p (stream position pos).  (No tile at all only at the share's
 // end, in front of a sequence's first.)
-struct Part { int tile0, cnt; long long len; };
-__device__ inline Part part_of(const Place& p, long long pos, long long end) {
+struct Part { int tile0, cnt, len; };
+__device__ inline Part part_of(const Place& p, int pos, int end) {
   Part x;
-  x.len = min((long long)(p.x.tiles + kSetup - p.at), end - pos);
+  x.len = min(p.x.tiles + kSetup - p.at, end - pos);
   x.tile0 = max(0, p.at - kSetup);
-  x.cnt = max(0, (int)(p.at + x.len) - kSetup) - x.tile0;
+  x.cnt = max(0, p.at + x.len - kSetup) - x.tile0;
   return x;
 }
 // The groups as this CTA keeps them: in shared memory, or, if they are many, in the workspace.
-struct Table { const int4* groups; const long long* at; int n; };
+struct Table { const int4* groups; const int* at; int n; };
 // One warp: the group that position pos of the stream (pos < total) lies in.
-__device__ inline Place locate(const GroupArgs& a, const Table& tab, long long pos, int lane) {
+__device__ inline Place locate(const GroupArgs& a, const Table& tab, int pos, int lane) {
   int g = 0;
   for (int g0 = 0; g0 < tab.n; g0 += 32) {              // the last that begins at or before pos: it has tiles
     const unsigned m = __ballot_sync(0xffffffffu, g0 + lane < tab.n && tab.at[g0 + lane] <= pos);
@@ -369,10 +369,9 @@ __device__ inline Place locate(const GroupArgs& a, const Table& tab, long long p
   p.g = g;
   p.grp = tab.groups[g];
   p.x = shape_of(a, p.grp);
-  const long long off = pos - tab.at[g];
-  const int each = p.x.tiles + kSetup;
-  p.hb = off <= 0x7fffffffll ? (int)((unsigned)off / (unsigned)each) : (int)(off / each);
-  p.at = (int)(off - (long long)p.hb * each);
+  const int off = pos - tab.at[g], each = p.x.tiles + kSetup;
+  p.hb = (int)((unsigned)off / (unsigned)each);
+  p.at = off - p.hb * each;
   return p;
 }
 // The place behind a whole rest of a sequence.
@@ -389,15 +388,15 @@ __device__ inline void next_sequence(const GroupArgs& a, const Table& tab, Place
 // [row0, row0 + rows).
 struct Piece { int h, row0, rows, two, tile0, cnt, tiles, keys, slot; };
 
-constexpr size_t kTableAt = 2 * kQBytes + kSlots * kSlotBytes + 16;          // behind the rings and the rows' arrays
-static_assert(kTableAt >= kRing + (kMaxTracesFast + 1) * 8 + 2 * kMaxTracesFast * 4, "rows and groups lie side by side");
-constexpr size_t kPrefixSmem = 1024 + kTableAt + 32 * 8 + 2 * sizeof(Piece) + 64 + kTableGroups * 24;
+constexpr size_t kTableAt = 2 * kQBytes + kSlots * kSlotBytes;          // behind the rings and the rows' arrays
+static_assert(kTableAt >= kRing + (kMaxTracesFast + 2) * 4 + 2 * kMaxTracesFast * 4, "rows and groups lie side by side");
+constexpr size_t kPrefixSmem = 1024 + kTableAt + 32 * 8 + 2 * sizeof(Piece) + 64 + kTableGroups * 20;
 constexpr size_t kSmem = kPrefixSmem > kStreamSmem ? kPrefixSmem : kStreamSmem;
 static_assert(kSmem <= 232448 - 256, "shared memory of one CTA");
 
 __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ GroupArgs a) {
   extern __shared__ unsigned char smem_raw[];
-  __shared__ long long s_sum[kThreads / 32];
+  __shared__ int s_sum[kThreads / 32];
   __shared__ Header s_header;
   __shared__ float s_unit_ns;
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -409,11 +408,11 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
 
   // ---- who shares what.  A description that is not in order is not followed at all.
   Rows rw;
-  rw.at = reinterpret_cast<long long*>(sm + kRing);
-  rw.own = reinterpret_cast<int*>(rw.at + kMaxTracesFast + 1);
+  rw.at = reinterpret_cast<int*>(sm + kRing);
+  rw.own = rw.at + kMaxTracesFast + 2;
   rw.len = rw.own + kMaxTracesFast;
   int4* s_grp = reinterpret_cast<int4*>(sm + kTableAt);
-  long long* s_grp_at = reinterpret_cast<long long*>(s_grp + kTableGroups);
+  int* s_grp_at = reinterpret_cast<int*>(s_grp + kTableGroups);
   bool bad = false;
   for (int g = threadIdx.x; g < a.n_groups; g += kThreads) {
     const int r0 = a.group_rows[g], r1 = a.group_rows[g + 1], pages = a.group_pages[g];
@@ -427,7 +426,7 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
   tab.n = __syncthreads_or(bad) ? 0 : a.n_groups;
   if (first && threadIdx.x == 0 && tab.n != a.n_groups) flag_error(a.counters, STEP_ERR_INVALID_ARG);
   int4* grp = a.n_groups <= kTableGroups ? s_grp : a.cta_groups + (size_t)blockIdx.x * a.n_groups;
-  long long* grp_at = a.n_groups <= kTableGroups ? s_grp_at : a.cta_group_at + (size_t)blockIdx.x * a.n_groups;
+  int* grp_at = a.n_groups <= kTableGroups ? s_grp_at : a.cta_group_at + (size_t)blockIdx.x * a.n_groups;
   tab.groups = grp;
   tab.at = grp_at;
   for (int g = warp; g < tab.n; g += kThreads / 32) {
@@ -451,24 +450,24 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
   __syncthreads();
   // ---- where every group's tiles begin in their stream (one warp), and every row's own pages in theirs (a thread takes `per` rows)
   if (warp == kThreads / 32 - 1) {
-    long long run = 0;
+    int run = 0;
     float ns = 0.f;
     for (int g0 = 0; g0 < tab.n; g0 += 32) {
       const int g = g0 + lane;
-      long long mine = 0;
+      int mine = 0;
       if (g < tab.n) {
         const int4 x = grp[g];
         if (x.z >= 0) {
           const Shape sh = shape_of(a, x);
-          mine = (long long)(sh.tiles + kSetup) * sh.blocks * a.Hkv;
+          mine = (sh.tiles + kSetup) * sh.blocks * a.Hkv;
           const int narrow = x.y - (sh.blocks - 1) * 2 * a.tokens <= a.tokens;
           ns += (float)mine * (kWideNs - (kWideNs - kNarrowNs) * narrow / (float)sh.blocks);
         }
       }
-      long long incl = mine;
+      int incl = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const long long u = __shfl_up_sync(0xffffffffu, incl, o);
+        const int u = __shfl_up_sync(0xffffffffu, incl, o);
         if (lane >= o) incl += u;
       }
       if (g < tab.n) grp_at[g] = run + incl - mine;
@@ -476,7 +475,7 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) ns += __shfl_xor_sync(0xffffffffu, ns, o);
-    if (lane == 0) { s_header.units = run; s_unit_ns = ns / (float)max(1ll, run); }
+    if (lane == 0) { s_header.units = run; s_unit_ns = ns / (float)max(1, run); }
   }
   {
     const int per = (a.n + kThreads - 1) / kThreads, i0 = threadIdx.x * per;
@@ -484,18 +483,17 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
       const int pages = (rw.len[i] + kP - 1) / kP - rw.own[i];
       return pages > 0 ? pages + kOwnSetup : 0;
     };
-    long long mine = 0;
+    int mine = 0;
     for (int i = i0; i < min(a.n, i0 + per); ++i) mine += pages_of(i);
-    long long incl = mine;
+    int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long u = __shfl_up_sync(0xffffffffu, incl, o);
+      const int u = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += u;
     }
     if (lane == 31) s_sum[warp] = incl;
     __syncthreads();
-    long long run = incl - mine;
-    for (int w = 0; w < warp; ++w) run += s_sum[w];
+    int run = incl - mine + __reduce_add_sync(0xffffffffu, lane < warp ? s_sum[lane] : 0);
     for (int i = i0; i < min(a.n, i0 + per); ++i) {
       rw.at[i] = run;
       run += pages_of(i);
@@ -512,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
     for (int i = threadIdx.x; i < a.n; i += kThreads) {
       RowPlan p = {};
       p.at = rw.at[i];
-      p.pages = max(0, (int)(rw.at[i + 1] - rw.at[i]) - kOwnSetup);
+      p.pages = max(0, rw.at[i + 1] - rw.at[i] - kOwnSetup);
       if (rw.own[i] > 0) {
         const int g = a.plan[i].tiles - 1;
         const int4 x = grp[g];
@@ -520,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
         const int t = i - x.x, block = t / (2 * a.tokens);
         p.tiles = sh.tiles;
         p.head = sh.blocks * (sh.tiles + kSetup);
-        p.begin = grp_at[g] + (long long)block * (sh.tiles + kSetup);
+        p.begin = grp_at[g] + block * (sh.tiles + kSetup);
         p.place = (t - block * 2 * a.tokens) * 2 + (x.y - block * 2 * a.tokens <= a.tokens);
       }
       a.plan[i] = p;
@@ -584,7 +582,7 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
   // this CTA's share of the stream
-  const long long W = prefix_share(hd, n_prefix), pos0 = min(hd.units, blockIdx.x * W), end = min(hd.units, pos0 + W);
+  const int W = prefix_share(hd, n_prefix), pos0 = (int)min((long long)hd.units, (long long)blockIdx.x * W), end = min(hd.units - pos0, W) + pos0;
 
   auto wait = [&](uint32_t bar, uint32_t parity) {
     if (mbar_test_wait(bar, parity)) return true;                      // (a limit of zero: this is all)
@@ -718,7 +716,7 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
         const int page = first + lane;
         return of.g < tab.n && page < of.grp.w ? a.block_table[(size_t)of.grp.z * a.max_pages + page] : 0;
       };
-      long long pos = pos0;
+      int pos = pos0;
       if (pos < end) {
         Place pl = locate(a, tab, pos, lane);
         Part part = part_of(pl, pos, end);
@@ -758,7 +756,7 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
       // ------------------------------------------------ query rows of one piece after another
       uint32_t par = 0;
       int begun = 0;
-      long long pos = pos0;
+      int pos = pos0;
       Place pl = {};
       if (pos < end) pl = locate(a, tab, pos, lane);
       for (;; par ^= 1) {
@@ -945,19 +943,18 @@ __global__ void __launch_bounds__(kMergeWarps * 32) groups_merge_kernel(const __
   const int lane = threadIdx.x & 31;
   wait_for_primary();
   const Header hd = *a.header;
-  auto share_of = [](long long x, long long by) { return x <= 0x7fffffffll ? (int)((unsigned)x / (unsigned)by) : (int)(x / by); };
+  const int W = max(1, own_share(hd, max(1, a.ctas - hd.n_prefix))), Wp = max(1, prefix_share(hd, max(1, hd.n_prefix)));
   for (int r = blockIdx.x * kMergeWarps + (threadIdx.x >> 5); r < a.n * a.Hq; r += gridDim.x * kMergeWarps) {
     const int i = r / a.Hq, hq = r - i * a.Hq, h = hq / a.G, sub = hq - h * a.G;
     const RowPlan pl = a.plan[i];
-    const long long W = hd.pages > 0 ? own_share(hd, a.ctas - hd.n_prefix) : 1, Wp = hd.units > 0 ? prefix_share(hd, hd.n_prefix) : 1;
-    const long long at = pl.at * a.Hkv + (long long)h * (pl.pages + kOwnSetup);
-    const int w0 = pl.pages > 0 ? share_of(at + kOwnSetup, W) : 0, w1 = pl.pages > 0 ? share_of(at + kOwnSetup + pl.pages - 1, W) : -1;
+    const int at = pl.at * a.Hkv + h * (pl.pages + kOwnSetup);
+    const int w0 = pl.pages > 0 ? (at + kOwnSetup) / W : 0, w1 = pl.pages > 0 ? (at + kOwnSetup + pl.pages - 1) / W : -1;
     if (pl.tiles == 0 && w0 == w1) continue;                           // written already
     // the pieces of the shared pages: shares p0 .. p1, each with one result or (narrow) one per lane
-    const long long begin = pl.begin + (long long)h * pl.head;
+    const int begin = pl.begin + h * pl.head;
     const int narrow = pl.place & 1, trace = pl.place >> 1, ln = trace / a.tokens, row = ln * kHalfRows + (trace - ln * a.tokens) * a.G + sub;
-    const int p0 = pl.tiles > 0 ? share_of(begin + kSetup, Wp) : 0;
-    const int pieces = pl.tiles > 0 ? (share_of(begin + kSetup + pl.tiles - 1, Wp) - p0 + 1) << narrow : 0;
+    const int p0 = pl.tiles > 0 ? (begin + kSetup) / Wp : 0;
+    const int pieces = pl.tiles > 0 ? ((begin + kSetup + pl.tiles - 1) / Wp - p0 + 1) << narrow : 0;
     const bool whole = pieces == 1 << narrow;                          // one share has all tiles
     const int all = pieces + (w1 - w0 + 1);
     float M = -INFINITY, den = 0.f;
@@ -1017,7 +1014,7 @@ size_t lay_out(const step_pool* pool, int n, int n_groups, char* ws, GroupArgs* 
   x.plan = (RowPlan*)take((size_t)n * sizeof(RowPlan));
   if (n_groups > kTableGroups) {
     x.cta_groups = (int4*)take(ctas * n_groups * sizeof(int4));
-    x.cta_group_at = (long long*)take(ctas * n_groups * 8);
+    x.cta_group_at = (int*)take(ctas * n_groups * 4);
   }
   x.own_ml = (float*)take(warps * 2 * g.G * 8);
   x.own_o = (float*)take(warps * 2 * g.G * kD * 4);
@@ -1037,7 +1034,10 @@ size_t lay_out(const step_pool* pool, int n, int n_groups, char* ws, GroupArgs* 
 
 namespace stepk {
 
-bool groups_tc_supported(const step_pool* pool, int n) { return attention_tc_covers(pool, n); }
+// (positions in the streams of own and of shared pages are 32-bit numbers)
+bool groups_tc_supported(const step_pool* pool, int n) {
+  return attention_tc_covers(pool, n) && (long long)n * pool->cfg.num_kv_heads * ((long long)pool->cfg.max_pages_per_trace + 3) < (1ll << 31);
+}
 
 size_t groups_tc_workspace(const step_pool* pool, int n, int n_groups) { return lay_out(pool, n, n_groups, nullptr, nullptr); }
 
