@@ -677,7 +677,7 @@ def rotate_positions(x, rotary, positions=None, out=None, transpose=False, strea
     rotation, which takes the gradient of the result to the gradient of x."""
     fn, dev, shape = "rotate_positions", x.device, x.shape
     code = _STEP_DTYPE.get(x.dtype)
-    if code is None or len(shape) not in (3, 4) or dev != rotary.device or rotary.rotary_dim > shape[-1]:
+    if code is None or len(shape) not in (3, 4) or dev.type != "cuda" or dev != rotary.device or rotary.rotary_dim > shape[-1]:
         raise StepError(fn, 1)
     if stream is not None and stream.device != dev:
         raise StepError(fn, 1)

@@ -937,14 +937,18 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
 // ---------------------------------------------------------------- one result per row
 constexpr int kMergeWarps = 4, kMergeAhead = 8;
 
-// A warp per query row, lanes over the 128 dims: the shared pages' pieces, then the row's own, in stream order with a running
-// (max, sum, values); the loads of kMergeAhead pieces are under way at once.
+// A warp per query row (kTeam: a CTA, whose warps take a run of the pieces each), lanes over the 128 dims: the shared pages' pieces,
+// then the row's own, in stream order with a running (max, sum, values); the loads of kMergeAhead pieces are under way at once.
+// With few rows there are many pieces of each: 16 traces of one prompt of 16,000, 34 pieces a row, took a warp 10 us.
+template <bool kTeam>
 __global__ void __launch_bounds__(kMergeWarps * 32) groups_merge_kernel(const __grid_constant__ GroupArgs a) {
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __shared__ float2 s_ml[kTeam ? kMergeWarps : 1];
+  __shared__ float4 s_o[kTeam ? kMergeWarps : 1][32];
   wait_for_primary();
   const Header hd = *a.header;
   const int W = max(1, own_share(hd, max(1, a.ctas - hd.n_prefix))), Wp = max(1, prefix_share(hd, max(1, hd.n_prefix)));
-  for (int r = blockIdx.x * kMergeWarps + (threadIdx.x >> 5); r < a.n * a.Hq; r += gridDim.x * kMergeWarps) {
+  for (int r = kTeam ? blockIdx.x : blockIdx.x * kMergeWarps + warp; r < a.n * a.Hq; r += gridDim.x * (kTeam ? 1 : kMergeWarps)) {
     const int i = r / a.Hq, hq = r - i * a.Hq, h = hq / a.G, sub = hq - h * a.G;
     const RowPlan pl = a.plan[i];
     const int at = pl.at * a.Hkv + h * (pl.pages + kOwnSetup);
@@ -959,14 +963,15 @@ __global__ void __launch_bounds__(kMergeWarps * 32) groups_merge_kernel(const __
     const int all = pieces + (w1 - w0 + 1);
     float M = -INFINITY, den = 0.f;
     float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k0 = 0; k0 < all; k0 += kMergeAhead) {
+    const int from = kTeam ? all * warp / kMergeWarps : 0, to = kTeam ? all * (warp + 1) / kMergeWarps : all;
+    for (int k0 = from; k0 < to; k0 += kMergeAhead) {
       float2 ml[kMergeAhead];
       float4 o[kMergeAhead];
 #pragma unroll
       for (int y = 0; y < kMergeAhead; ++y) {
         const int k = k0 + y;
         ml[y] = make_float2(-INFINITY, 0.f);
-        if (k >= all) continue;
+        if (k >= to) continue;
         const float *mls, *os;
         size_t slot;
         if (k < pieces) {
@@ -997,6 +1002,26 @@ __global__ void __launch_bounds__(kMergeWarps * 32) groups_merge_kernel(const __
         num.x += wgt * o[y].x; num.y += wgt * o[y].y; num.z += wgt * o[y].z; num.w += wgt * o[y].w;
       }
       M = Mb;
+    }
+    if constexpr (kTeam) {
+      if (lane == 0) s_ml[warp] = make_float2(M, den);
+      s_o[warp][lane] = num;
+      __syncthreads();
+      float Mb = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kMergeWarps; ++w) Mb = fmaxf(Mb, s_ml[w].x);
+      const float off = Mb == -INFINITY ? 0.f : Mb;
+      den = 0.f;
+      num = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kMergeWarps; ++w) {
+        const float wgt = exp2f(s_ml[w].x - off);
+        const float4 o = s_o[w][lane];
+        den += wgt * s_ml[w].y;
+        num.x += wgt * o.x; num.y += wgt * o.y; num.z += wgt * o.z; num.w += wgt * o.w;
+      }
+      __syncthreads();                                                 // (the next row's results go to the same place)
+      if (warp != 0) continue;
     }
     const float inv = all == 0 ? 0.f : 1.f / den;                      // a row without any key: zeros
     reinterpret_cast<uint2*>(a.out + (size_t)r * kD)[lane] = make_uint2(pack2(num.x * inv, num.y * inv), pack2(num.z * inv, num.w * inv));
@@ -1077,8 +1102,10 @@ int groups_tc_launch(step_pool* pool, int layer, const void* q, const int32_t* b
   groups_kernel<<<a.ctas, kThreads, kSmem, s>>>(map, map_q, a);
   if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
   const long long rows = (long long)n * g.Hq, most = 16ll * a.ctas;
-  const long long ctas = (rows + kMergeWarps - 1) / kMergeWarps;
-  if (launch_dependent(groups_merge_kernel, dim3((unsigned)(ctas < most ? ctas : most)), dim3(kMergeWarps * 32), 0, s, a) != cudaSuccess) return STEP_ERR_CUDA;
+  const bool team = rows <= 8ll * a.ctas;
+  const long long ctas = team ? rows : (rows + kMergeWarps - 1) / kMergeWarps;
+  if (launch_dependent(team ? groups_merge_kernel<true> : groups_merge_kernel<false>, dim3((unsigned)(ctas < most ? ctas : most)), dim3(kMergeWarps * 32), 0, s, a) !=
+      cudaSuccess) return STEP_ERR_CUDA;
   return launch_ok();
 }
 

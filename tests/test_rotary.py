@@ -133,6 +133,12 @@ def test_the_library_refuses_without_looking_at_the_device():
     assert L.kv_pool_extend(None, None, 1, 1, None, None) == 1
 
 
+def test_tensors_that_are_not_on_a_gpu_are_refused():
+    with pytest.raises(B.StepError) as e:
+        B.rotate_positions(torch.zeros(2, 3, 8), B.Rotary(8, device="cpu"))
+    assert e.value.code == 1
+
+
 def bare_pool():
     def reached(*args, **kwargs):
         raise AssertionError("the library was called")
