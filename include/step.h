@@ -28,7 +28,8 @@
  *    by it, except those documented as synchronising.  One pool must not be used from two
  *    streams at once.
  *  - dtype: STEP_BF16 (0) or STEP_FP32 (1) is the storage type of K/V, q, hidden states and
- *    scorer weights.  Accumulation is fp32, and so are all outputs but decode_attention_tree's.
+ *    scorer weights.  Accumulation is fp32, and so are all outputs but those of decode_attention_tree,
+ *    decode_attention_groups, rotate_positions and store_kv_rotated, which have the type of their inputs.
  *  - Query head h reads KV head h / G, G = num_q_heads / num_kv_heads.
  *  - Decode order: append_kv for the new token comes BEFORE decode_attention; the query
  *    attends to all S_t stored positions including its own; there is no mask.
@@ -328,7 +329,8 @@ int rotate_positions(const rotate_args* a, const step_rotary* rotary, void* stre
 /* Makes room for n_tokens new positions of each of the n listed traces, as append_kv does (order, what is skipped and
  * flagged), without storing anything: start_out[i] = the length of trace trace_ids[i] before the call, or -1 for an entry
  * that was skipped.  What the new positions hold is undefined until it is stored: attend to a layer when it is.
- * trace_ids, start_out: [n] device.  n <= min(max_traces, 2048). */
+ * trace_ids, start_out: [n] device, not the same place.  n <= min(max_traces, 2048).  It uses scratch in the pool's metadata, as
+ * append_kv does.  Wants the pool's device to be current. */
 int kv_pool_extend(step_pool* pool, const int32_t* trace_ids, int n, int n_tokens, int32_t* start_out, void* stream);
 
 /* Row r = i * n_tokens + s of k, v and q belongs to token s of entry i. */
@@ -362,11 +364,12 @@ int store_kv_rotated(step_pool* pool, const kv_store_args* a, const step_rotary*
  * its own table.  n_groups = 0: no groups (both may be NULL).
  * q and out: [n, num_q_heads, head_dim] in POOL DTYPE, 16-byte aligned; out is rounded once and must not overlap the inputs.
  * n, n_groups <= 65535.  Scores, maxima, sums and accumulators are fp32.  Where the tensor-core kernels serve the call (bf16 pools,
- * head_dim 128, page_size 16, n <= 2048, kv_pool_set_attention_config not -1) the probabilities are rounded to bf16 on their way
- * into the second product, as decode_attention_tree's are; elsewhere they stay fp32 and every row reads its own table.
+ * head_dim 128, page_size 16, n <= 2048, n * num_kv_heads * (max_pages_per_trace + 3) < 2^31, kv_pool_set_attention_config not -1)
+ * the probabilities are rounded to bf16 on their way into the second product, as decode_attention_tree's are (2.3e-3 off in the
+ * 2-norm, where rounding the output alone makes 1.7e-3); elsewhere they stay fp32 and every row reads its own table.
  * Wants the pool's device to be current and a workspace of decode_attention_groups_workspace_bytes (host-only) bytes, 256-byte
- * aligned, from the caller, as the calls above; calls of one pool stay ordered one behind the other unless each has a workspace
- * of its own and nothing writes the pool meanwhile. */
+ * aligned, in use from the call until its work on the stream is done; can be captured into a CUDA graph.  It keeps nothing in the
+ * pool's metadata: calls that only read one pool may overlap if each has a workspace of its own. */
 int decode_attention_groups_workspace_bytes(const step_pool* pool, int n, int n_groups, size_t* bytes);
 int decode_attention_groups(step_pool* pool, int layer, const void* q, const int32_t* block_table, const int32_t* seq_lens,
                             int n, const int32_t* group_rows, const int32_t* group_pages, int n_groups, void* out,
@@ -558,7 +561,7 @@ int kv_pool_read_kv(step_pool* pool, int layer, int kv_head, const int32_t* bloc
                     int seq_len, void* k_out, void* v_out, void* stream);
 /* Tuning knobs of decode_attention (0 keeps the current value): CTAs per launch, and whether
  * the tensor-core bf16 path may be used (1) or the scalar kernel is forced (-1).  The second also holds for
- * decode_attention_tree and decode_attention_weights, whose workspace sizes depend on it. */
+ * decode_attention_tree, decode_attention_weights and decode_attention_groups, whose workspace sizes depend on it. */
 int kv_pool_set_attention_config(step_pool* pool, int grid_ctas, int fast_path);
 /* How decode_attention's tensor-core launch spreads the KV pages over the SMs.  Of every (trace, KV head)
  * sequence the last dynamic_sixteenths / 16 of its pages (0 .. 12; default 4) are cut into chunks of at least
@@ -573,7 +576,8 @@ int kv_pool_set_attention_balance(step_pool* pool, int dynamic_sixteenths, int m
  * launches after it are unaffected: no state of the kernel outlives a launch).  Default 2,000,000,000 ns.
  * 0 = no waiting at all: a page that has not landed by the time it is first looked at counts as timed out - for testing this path, which no healthy device otherwise reaches.
  * The same limit holds for decode_attention_weights where that kernel serves it (out and weight_sum of such a call are
- * undefined) and for every wait of decode_attention_tree's tensor-core kernel, which winds down likewise. */
+ * undefined) and for every wait of decode_attention_tree's and decode_attention_groups' tensor-core kernels, which wind down
+ * likewise. */
 int kv_pool_set_wait_limit_ns(step_pool* pool, unsigned long long ns);
 /* Which first-layer kernel score_steps uses for bf16 scorers whose shape the tensor-core kernel covers
  * (D a multiple of 64, m a multiple of 64 and <= 1024, 16-byte aligned W1 and hidden): mode 0 (default)

@@ -245,6 +245,108 @@ def test_two_pools_at_once_on_streams_of_their_own():
         assert all(torch.equal(o, pairs[i][3]) for o in outs[i])
 
 
+@pytest.mark.parametrize("heads", [(3, 1, 128), (6, 1, 128), (14, 2, 128), (12, 1, 128), (8, 8, 128)])
+def test_other_numbers_of_heads_for_a_kv_head(heads):
+    """Tiles of query rows that the heads of a group do not fill."""
+    cfg = config(heads, "bf16", n=47, layers=1)
+    tw, rows, pages = build(cfg, [(333, np.random.default_rng(1).integers(0, 40, 44)), (90, [1, 20, 0])])
+    run(tw, rows, pages)
+
+
+def test_two_calls_on_one_pool_at_once():
+    """Layers of one pool, each call on a stream and with a workspace of its own."""
+    cfg = config((8, 2, 128), "bf16", n=24, layers=2)
+    tw, rows, pages = build(cfg, [(1500, np.random.default_rng(2).integers(0, 300, 20)), (64, [5, 6, 7, 200])])
+    want = [run(tw, rows, pages, layer=l, poison=False) for l in range(2)]
+    q, _ = draw(cfg, W.TID_Q, (24, 8, 128), 5)
+    v, r, p = tw.gpu.views(), dev(rows), dev(pages)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    spaces = [torch.empty(96 << 20, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(20):
+        for l in range(2):
+            outs[l].append(tw.gpu.decode_attention_groups(l, q, v["block_table"], v["seq_lens"], r, p, workspace=spaces[l], stream=streams[l]))
+    torch.cuda.synchronize()
+    for l in range(2):
+        assert all(torch.equal(o, want[l]) for o in outs[l])
+
+
+@pytest.mark.parametrize("heads,dtype", [((8, 2, 128), "bf16"), ((4, 1, 64), "fp32")])
+def test_a_length_beyond_the_table_is_cut_and_flagged(heads, dtype):
+    cfg = config(heads, dtype, n=3, layers=1)
+    tw, rows, pages = build(cfg, [(32, [100, 60, 12])], max_pages=9)
+    v = tw.gpu.views()
+    q, qx = draw(cfg, W.TID_Q, (3, cfg.num_q_heads, cfg.head_dim), 5)
+    lens = tw.ora.seq_lens.copy()
+    lens[2] = -5
+    over = lens.copy()
+    over[0] = 1 << 30
+    table = v["block_table"].clone()
+    table[0, 8:] = table[0, 8].clone()                                    # trace 0 has 132 positions; the table holds 144
+    out = tw.gpu.decode_attention_groups(0, q, table, dev(over), dev(rows), dev(pages))
+    assert tw.gpu.last_error() == (4, 1 << 4)
+    lens[0] = 144
+    plain = tw.gpu.decode_attention_groups(0, q, table, dev(lens), None, None)
+    assert tw.gpu.last_error() == (0, 0)
+    assert torch.isfinite(out).all() and (out[2] == 0).all() and (plain[2] == 0).all()
+    # the same positions, summed in pieces of another number: fp32 errors, one rounding each of probabilities and output
+    half = BF16_HALF_STEP if dtype == "bf16" else 2.0 ** -24
+    assert (out - plain).abs().max().item() <= 4 * half * 6 + 1e-4 * (dtype == "fp32")
+
+
+def test_a_table_too_wide_for_32_bit_positions():
+    Hkv, d, pages = 64, 128, 1 << 25
+    pool = B.KVPool(1, Hkv, Hkv, d, 16, num_blocks=12, max_traces=1, max_pages_per_trace=pages)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    k, v, q = (torch.randn(s, generator=gen, device="cuda").bfloat16() for s in ((1, 50, 1, Hkv, d), (1, 50, 1, Hkv, d), (1, Hkv, d)))
+    pool.fork_prefix(1, 0, None, None)
+    pool.append_kv(torch.zeros(1, dtype=torch.int32, device="cuda"), 50, k, v)
+    w = pool.views()
+    out = pool.decode_attention_groups(0, q, w["block_table"], w["seq_lens"], None, None).double()
+    p = (torch.einsum("nhd,nshd->nhs", q.double(), k[:, :, 0].double()) / d ** 0.5).softmax(-1)
+    # fp32 arithmetic, one rounding of the output; values below 6
+    assert (out - torch.einsum("nhs,nshd->nhd", p, v[:, :, 0].double())).abs().max().item() <= 2 * BF16_HALF_STEP * 6
+    assert pool.last_error() == (0, 0)
+
+
+def test_a_captured_decode_step_replayed_over_growing_traces():
+    """extend, store and attend of two layers in one graph: lengths, shares and pieces are another at every replay."""
+    outs = []
+    for graphed in (False, True):
+        cfg = config((8, 2, 128), "bf16", n=10, layers=2)
+        tw, rows, pages = build(cfg, [(200, [14, 15, 0, 30, 100]), (48, [0, 1, 2, 15, 31])], spare=64, max_pages=30)
+        g, v, r = tw.gpu, tw.gpu.views(), B.Rotary(128)
+        kd, _ = draw(cfg, W.TID_KNEW, (10, 1, 2, 2, 128), 9)
+        vd, _ = draw(cfg, W.TID_VNEW, (10, 1, 2, 2, 128), 9)
+        qd, _ = draw(cfg, W.TID_Q, (2, 10, 1, 8, 128), 9)
+        ids, start = torch.arange(10, dtype=torch.int32, device="cuda"), torch.empty(10, dtype=torch.int32, device="cuda")
+        qo, out, gr, gp = torch.empty_like(qd), torch.empty((2, 10, 8, 128), dtype=torch.bfloat16, device="cuda"), dev(rows), dev(pages)
+
+        def step():
+            g.extend(ids, 1, start_out=start)
+            for l in range(2):
+                g.store_kv_rotated(l, ids, start, kd[:, :, l:l + 1], vd[:, :, l:l + 1], r, q=qd[l:l + 1], q_out=qo[l:l + 1])
+                g.decode_attention_groups(l, qo[l, :, 0], v["block_table"], v["seq_lens"], gr, gp, out=out[l])
+
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        got = []
+        with torch.cuda.stream(s):
+            graph = torch.cuda.CUDAGraph()
+            if graphed:
+                with torch.cuda.graph(graph, stream=s):
+                    step()
+            for _ in range(20):
+                graph.replay() if graphed else step()
+                got.append(out.clone())
+        s.synchronize()
+        assert g.last_error() == (0, 0)
+        assert v["seq_lens"].tolist() == [int(x) + 20 for x in tw.ora.seq_lens]
+        outs.append(got)
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
 @pytest.mark.parametrize("heads", [(8, 2, 128), (16, 2, 128)])
 def test_a_wait_that_runs_out_is_flagged_and_leaves_nothing_behind(heads):
     """A limit of zero takes whatever has not landed at the first look for lost (healthy copies, which land a microsecond
