@@ -118,6 +118,8 @@ __device__ inline Shape shape_of(const GroupArgs& a, int4 g) {
 }
 
 // ---------------------------------------------------------------- own pages
+__device__ inline void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ inline void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ inline void ldsm4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
@@ -130,7 +132,7 @@ __device__ inline void mma16816(float (&c)[4], const uint32_t* a, uint32_t b0, u
 }
 
 constexpr size_t kRing = (size_t)kStreamWarps * kStages * kPageBytes;                      // rings of own pages
-constexpr size_t kStreamSmem = 1024 + kRing + (kMaxTracesFast + 2) * 4 + 2 * kMaxTracesFast * 4 + kStreamWarps * kStages * 8;
+constexpr size_t kStreamSmem = 1024 + kRing + (kMaxTracesFast + 2) * 4 + 2 * kMaxTracesFast * 4;
 
 // What every CTA works out first, in shared memory behind the rings of own pages.
 struct Rows {
@@ -140,7 +142,7 @@ struct Rows {
 };
 
 // This CTA's share of the own pages: `share` of them for each of its warps, this one the me-th of all.
-__device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, unsigned char* sm, uint32_t base, uint32_t bars, int me, int total, int W) {
+__device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, unsigned char* sm, uint32_t base, int me, int total, int W) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int begin = (int)min((long long)total, (long long)me * W), end = min(total - begin, W) + begin;
   if (begin >= end) return;
@@ -194,20 +196,22 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
   int page = first_of(s), plast = last_of(s), win = page, put = 0;
   int ids = load_ids(s.row, win), ids_next = load_ids(s.row, win + 32), ids_row = win == 0 ? ids : load_ids(s.row, 0);
   int behind = row_behind(s.row), ids_behind = load_ids(behind, 0);
-  int copies = 0, used = 0;                                      // begun; done with
   bool any = page < plast;                                             // pages are left to copy
   prefetch_q(next_seq(s));
   auto issue = [&]() {
-    if (!any) return;
+    if (!any) {
+      cp_async_commit();                                               // (an empty group: the wait counts groups)
+      return;
+    }
     if (page - win >= 32) { win += 32; ids = ids_next; ids_next = load_ids(ps.row, win + 32); }
     int b = __shfl_sync(0xffffffffu, ids, page - win);
     if (b < 0 || b >= a.num_blocks) { if (lane == 0) flag_error(a.counters, STEP_ERR_BAD_BLOCK); b = 0; }
-    if (lane == 0) {
-      mbar_expect_tx(bars + 8 * put, kPageBytes);
-      bulk_load(ring + put * kPageBytes, a.kv + (((size_t)a.layer * a.num_blocks + b) * a.Hkv + ps.h) * (2 * kP * kD), kPageBytes, bars + 8 * put);
-    }
+    const __nv_bfloat16* src = a.kv + (((size_t)a.layer * a.num_blocks + b) * a.Hkv + ps.h) * (2 * kP * kD) + lane * 8;
+    const uint32_t dst = ring + put * kPageBytes + lane * 16;
+#pragma unroll
+    for (int x = 0; x < kPageBytes / 512; ++x) cp_async16(dst + x * 512, src + x * 256);
+    cp_async_commit();
     if (++put == kStages) put = 0;
-    ++copies;
     if (++page < plast) return;
     const int row = ps.row;
     ps = next_seq(ps);
@@ -226,8 +230,6 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
   const int kk = (lane >> 4) * 8 + (lane & 7), kc = (lane >> 3) & 1, vk = ((lane >> 3) & 1) * 8 + (lane & 7), vc = lane >> 4;
   const bool upper = a.G > 8;                                          // (rows from 8 on are heads too)
   int get = 0;
-  uint32_t ph = 0;
-  bool ok = true;
   for (; s.row < a.n && s.at + kOwnSetup < end; s = next_seq(s)) {
     const int page0 = first_of(s), cnt = last_of(s) - page0;
     const int S = rw.len[s.row] - s.own * kP;                          // own positions
@@ -243,13 +245,13 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
     float o[16][4] = {};
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
     for (int p = page0; p < page0 + cnt; ++p) {
-      if (!__all_sync(0xffffffffu, mbar_wait_bounded(bars + 8 * get, ph, a.wait_ns))) { ok = false; break; }
+      cp_async_wait<kStages - 1>();                                    // this lane's part of the page has landed; everyone's:
+      __syncwarp();
       const uint32_t pg = ring + get * kPageBytes;
       const int rows = S - p * kP;                                     // positions in this page and behind
       if (rows < kP) {                                                 // what a page holds behind the last position takes no part
         unsigned char* v = sm + (pg - base) + kP * kD * 2;
         for (int x = rows * 16 + lane; x < kP * 16; x += 32) *reinterpret_cast<uint4*>(v + x * 16) = make_uint4(0, 0, 0, 0);
-        fence_async_smem();                                            // (the slot's next page is written by the copy engine)
         __syncwarp();
       }
       float sc[2][4] = {};
@@ -298,12 +300,10 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
         mma16816(o[2 * x], pf, b[0], b[1]);
         mma16816(o[2 * x + 1], pf, b[2], b[3]);
       }
-      if (++get == kStages) { get = 0; ph ^= 1; }
+      if (++get == kStages) get = 0;
       __syncwarp();                                                    // all lanes have read the page
-      ++used;
       issue();
     }
-    if (!ok) break;
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
       l[z] += __shfl_xor_sync(0xffffffffu, l[z], 1);
@@ -329,16 +329,6 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
       }
     }
     prefetch_q(next_seq(next_seq(s)));
-  }
-  if (!ok) {
-    // a wait has run out: the copies in flight still write this CTA's shared memory
-    flag_error(a.counters, STEP_ERR_TIMEOUT);
-    if (lane == 0)
-      for (; used < copies; ++used) {
-        mbar_wait_bounded(bars + 8 * get, ph, kDrainNs);
-        if (++get == kStages) { get = 0; ph ^= 1; }
-      }
-    __syncwarp();
   }
 }
 
@@ -528,15 +518,9 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
   if ((int)blockIdx.x >= n_prefix) {
     // ================================================ own pages
     const int n_own = a.ctas - n_prefix;
-    const uint32_t bars = smem_u32(rw.len + kMaxTracesFast) + warp * kStages * 8;
     if (warp < kStreamWarps) {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-      if (lane == 0) {
-        for (int s = 0; s < kStages; ++s) mbar_init(bars + 8 * s, 1);
-        mbar_init_fence();
-      }
-      __syncwarp();
-      own_pages(a, rw, sm, base, bars, ((int)blockIdx.x - n_prefix) * kStreamWarps + warp, hd.pages, own_share(hd, n_own));
+      own_pages(a, rw, sm, base, ((int)blockIdx.x - n_prefix) * kStreamWarps + warp, hd.pages, own_share(hd, n_own));
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
     }
