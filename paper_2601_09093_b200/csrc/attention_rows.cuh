@@ -76,6 +76,7 @@ struct RowsArgs {
   int splits;
   float* part;                          // splits > 1: [n, Hkv, rows, splits, d] values, then (max, sum) pairs
   int32_t* counters;
+  const int32_t* group_rows; const int32_t* group_pages; int n_groups;   // decode_attention_groups: looked over, not used
 };
 
 constexpr int kRows = 16, kKeys = 32, kRowsThreads = 128, kAhead = 8;
@@ -120,6 +121,11 @@ __global__ void __launch_bounds__(kRowsThreads) attn_rows_kernel(RowsArgs a) {
   const int cpr = d / cpe;
   const T* kv = (const T*)a.kv;
   dependents_may_launch();
+  if (!kTree && !kScores && a.n_groups > 0 && blockIdx.x + blockIdx.y + blockIdx.z == 0) {   // a description that is not in order
+    for (int x = tid; x < a.n_groups; x += kRowsThreads)
+      if (a.group_rows[x] < 0 || a.group_rows[x + 1] < a.group_rows[x] || a.group_rows[x + 1] > (int)gridDim.z || a.group_pages[x] < 0 ||
+          a.group_pages[x] > g.max_pages) flag_error(a.counters, STEP_ERR_INVALID_ARG);
+  }
 
   int nodes = 1;
   if constexpr (kTree) {

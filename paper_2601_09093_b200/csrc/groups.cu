@@ -9,18 +9,6 @@
 
 using namespace stepk;
 
-namespace {
-
-// Raises the flag of a description that is not in order (it changes nothing else here: nothing is shared).
-__global__ void groups_check_kernel(const int32_t* group_rows, const int32_t* group_pages, int n_groups, int n, int max_pages, int32_t* counters) {
-  bool bad = false;
-  for (int g = threadIdx.x; g < n_groups; g += blockDim.x)
-    bad |= group_rows[g] < 0 || group_rows[g + 1] < group_rows[g] || group_rows[g + 1] > n || group_pages[g] < 0 || group_pages[g] > max_pages;
-  if (bad) flag_error(counters, STEP_ERR_INVALID_ARG);
-}
-
-}  // namespace
-
 extern "C" {
 
 int decode_attention_groups_workspace_bytes(const step_pool* pool, int n, int n_groups, size_t* bytes) {
@@ -52,10 +40,7 @@ int decode_attention_groups(step_pool* pool, int layer, const void* q, const int
   a.q = q; a.T = 1;
   a.block_table = block_table; a.seq_lens = seq_lens; a.out = out;
   a.counters = pool->v.counters;
-  if (n_groups > 0) {
-    groups_check_kernel<<<1, 256, 0, s>>>(group_rows, group_pages, n_groups, n, a.g.max_pages, a.counters);
-    if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
-  }
+  a.group_rows = group_rows; a.group_pages = group_pages; a.n_groups = n_groups;
   if (pool->cfg.dtype == STEP_BF16) return launch_attn_rows<__nv_bfloat16, __nv_bfloat16, false, false>(pool, a, n, (float*)workspace, s);
   return launch_attn_rows<float, float, false, false>(pool, a, n, (float*)workspace, s);
 }
