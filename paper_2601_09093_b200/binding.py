@@ -204,7 +204,7 @@ _INT_MAX = 0x7fffffff       # (ctypes cuts larger numbers down to 32 bits withou
 def _expect(fn, device, *wanted):
     """Every (tensor, shape, dtype) of `wanted` is a contiguous tensor of that shape and type on `device`; None passes."""
     for t, shape, dtype in wanted:
-        if t is not None and (t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous()):
+        if t is not None and (t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous()):
             raise StepError(fn, 1)
 
 
@@ -490,7 +490,7 @@ class KVPool:
         _expect(fn, self._device(), (q, rows, dt), (out, rows, dt), (block_table, (n, self.max_pages_per_trace), torch.int32),
                 (seq_lens, (n,), torch.int32), (group_rows, (n_groups + 1,), torch.int32), (group_pages, (n_groups,), torch.int32))
         if out is None:
-            out = self._empty(rows, dt, stream)
+            out = torch.empty_like(q) if stream is None else self._empty(rows, dt, stream)
         self._call(fn, (layer, q.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), n, _at(group_rows), _at(group_pages), n_groups,
                         out.data_ptr()), ("decode_attention_groups_workspace_bytes", n, n_groups), workspace, stream)
         return out

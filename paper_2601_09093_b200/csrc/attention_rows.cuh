@@ -1,5 +1,6 @@
 // Attention of several query rows of one trace and KV head on the CUDA cores, for any element type, head size and page
-// size: what decode_attention_tree and decode_attention_weights run on where their tensor-core kernels do not apply.
+// size: what decode_attention_tree, decode_attention_weights and decode_attention_groups run on where their tensor-core kernels
+// do not apply.
 //
 //   out[r] = sum_j softmax_j(q[r] . k[j] * scale) v[j]     over the S cached positions and, for a tree of drafted tokens,
 //                                                          over the drafted tokens that row r may see
@@ -9,6 +10,9 @@
 // widened to fp32 in shared memory, a thread makes four scores, a row's eight threads keep its running (max, sum) in fp32,
 // and in the second product a thread owns four dims of two or four rows.  fp32 throughout: one rounding, of the output.
 // With more than one range the pieces are combined by rows_merge_kernel, a programmatic dependent, in ascending order.
+//
+// decode_attention_groups (kGroups): a row's own keys, and the keys its group shares for kRows / G of the group's traces at a time,
+// are CTAs of one launch and always pieces: a row has `splits` of each kind.  A CTA works out for itself what its row shares.
 #pragma once
 
 #include "step_internal.cuh"
@@ -76,7 +80,7 @@ struct RowsArgs {
   int splits;
   float* part;                          // splits > 1: [n, Hkv, rows, splits, d] values, then (max, sum) pairs
   int32_t* counters;
-  const int32_t* group_rows; const int32_t* group_pages; int n_groups;   // decode_attention_groups: looked over, not used
+  const int32_t* group_rows; const int32_t* group_pages; int n_groups, n;   // kGroups: the groups, the rows of the call
 };
 
 constexpr int kRows = 16, kKeys = 32, kRowsThreads = 128, kAhead = 8;
@@ -97,15 +101,29 @@ inline size_t attn_rows_workspace(const step_pool* pool, int n, int T) {
   return splits == 1 ? 0 : (size_t)n * pool->cfg.num_kv_heads * T * pool->G * splits * (pool->cfg.head_dim + 2) * sizeof(float);
 }
 
+// kGroups: of each kind of keys, as many as kRows / G traces at a time need.  48 traces of two prompts of 4000, 8 / 2 heads of 64 in
+// bf16: 83 us, 124 with as many ranges as each trace by itself wants, 147 with every trace reading its own table.
+inline int attn_groups_splits(const step_pool* pool, int n) {
+  const int together = kRows / pool->G, s = attn_rows_splits(pool, (n + together - 1) / together, 1);
+  return s > 32 ? 32 : s;
+}
+inline size_t attn_groups_workspace(const step_pool* pool, int n) {
+  return (size_t)n * pool->cfg.num_q_heads * 2 * attn_groups_splits(pool, n) * (pool->cfg.head_dim + 2) * sizeof(float);
+}
+
 inline size_t attn_rows_smem(int d) { return ((size_t)kRows * (d + 4) + (size_t)kKeys * (d + 4) + (size_t)kKeys * d) * sizeof(float); }
 
 // kRpt rows and kNi times four dims of the output per thread: kRpt 2 for d <= 64, else 4; kNi 4 for d > 128.
-template <typename T, typename OutT, bool kTree, bool kScores, int kRpt, int kNi>
+template <typename T, typename OutT, bool kTree, bool kScores, bool kGroups, int kRpt, int kNi>
 __global__ void __launch_bounds__(kRowsThreads) attn_rows_kernel(RowsArgs a) {
   extern __shared__ float4 smem4[];
   const Geo& g = a.g;
-  const int d = g.d, G = g.G, h = blockIdx.y, t = blockIdx.z;
-  const int n_rows = a.T * G, blocks = (n_rows + kRows - 1) / kRows;
+  const int d = g.d, G = g.G;
+  const bool prefix = kGroups && (int)blockIdx.y >= g.Hkv;   // keys that a group shares
+  const int h = blockIdx.y - (prefix ? g.Hkv : 0);
+  const int t = blockIdx.z;
+  int n_rows = a.T * G, table = t;                       // query rows; whose table is read
+  const int blocks = kGroups ? 1 : (n_rows + kRows - 1) / kRows;
   const int r0 = (int)(blockIdx.x % blocks) * kRows, split = blockIdx.x / blocks;
   const int ld = d + 4;
   float* s_q = reinterpret_cast<float*>(smem4);
@@ -121,13 +139,44 @@ __global__ void __launch_bounds__(kRowsThreads) attn_rows_kernel(RowsArgs a) {
   const int cpr = d / cpe;
   const T* kv = (const T*)a.kv;
   dependents_may_launch();
-  if (!kTree && !kScores && a.n_groups > 0 && blockIdx.x + blockIdx.y + blockIdx.z == 0) {   // a description that is not in order
-    for (int x = tid; x < a.n_groups; x += kRowsThreads)
-      if (a.group_rows[x] < 0 || a.group_rows[x + 1] < a.group_rows[x] || a.group_rows[x + 1] > (int)gridDim.z || a.group_pages[x] < 0 ||
-          a.group_pages[x] > g.max_pages) flag_error(a.counters, STEP_ERR_INVALID_ARG);
+  // kGroups: row t and those behind it, as far as they are in its group and fit the tile (prefix); positions shared, if it shares any
+  int shared_keys = 0;
+  if constexpr (kGroups) {
+    __shared__ int s_group, s_leader, s_members;
+    if (tid == 0) { s_group = -1; s_leader = 0x7fffffff; s_members = 0; }
+    __syncthreads();
+    bool bad = false;
+    for (int x = tid; x < a.n_groups; x += kRowsThreads) {
+      const int first = a.group_rows[x], last = a.group_rows[x + 1], pages = a.group_pages[x];
+      bad |= first < 0 || last < first || last > a.n || pages < 0 || pages > g.max_pages;
+      if (first <= t && t < last) s_group = x;
+    }
+    if (__syncthreads_or(bad)) {                         // a description that is not in order is not followed
+      if (tid == 0 && blockIdx.x + blockIdx.y + blockIdx.z == 0) flag_error(a.counters, STEP_ERR_INVALID_ARG);
+      if (prefix) return;
+    } else if (s_group >= 0) {
+      const int first = a.group_rows[s_group], last = a.group_rows[s_group + 1], together = kRows / G;
+      const long long keys = (long long)a.group_pages[s_group] * g.P;
+      for (int x = first + tid; keys > 0 && x < last; x += kRowsThreads)
+        if (min((long long)a.seq_lens[x], (long long)g.max_pages * g.P) >= keys) { atomicAdd(&s_members, 1); atomicMin(&s_leader, x); }
+      __syncthreads();
+      const bool shares = s_members >= 2 && min((long long)a.seq_lens[t], (long long)g.max_pages * g.P) >= keys;
+      if (prefix) {
+        if (s_members < 2 || (t - first) % together != 0) return;
+        n_rows = min(together, last - t) * G;
+        shared_keys = (int)keys;
+        table = s_leader;
+      } else if (shares) {
+        shared_keys = (int)keys;
+      }
+    } else if (prefix) {
+      return;
+    }
   }
+  const int key0 = kGroups && !prefix ? shared_keys : 0;  // the first key
+  const size_t q0 = (size_t)t * (kGroups ? 1 : a.T);     // the first query row's token
 
-  int nodes = 1;
+  int nodes = kGroups ? n_rows / G : 1;
   if constexpr (kTree) {
     nodes = tree_nodes(a.n_nodes, t, a.T, a.counters);
     tree_masks(a.parents + (size_t)t * a.T, nodes, s_mask, s_up, a.counters);
@@ -135,17 +184,18 @@ __global__ void __launch_bounds__(kRowsThreads) attn_rows_kernel(RowsArgs a) {
   int S = a.seq_lens[t];
   if (S < 0) S = 0;
   if ((long long)S > (long long)g.max_pages * g.P) { S = g.max_pages * g.P; if (tid == 0) flag_error(a.counters, STEP_ERR_CAPACITY); }
+  if (prefix) S = shared_keys;
   const int n_keys = S + (kTree ? nodes : 0);
-  const int tiles = (n_keys + kKeys - 1) / kKeys, per = (tiles + a.splits - 1) / a.splits;
+  const int tiles = (n_keys - key0 + kKeys - 1) / kKeys, per = (tiles + a.splits - 1) / a.splits;
   const int it0 = min(tiles, split * per), it1 = min(tiles, it0 + per);
 
   // where the rows of a tile's keys are (a thread per key)
   auto locate = [&](int it) {
     if (tid < kKeys && it < it1) {
-      const int j = it * kKeys + tid;
+      const int j = key0 + it * kKeys + tid;
       const T *k = nullptr, *v = nullptr;
       if (j < S) {
-        int b = a.block_table[(size_t)t * g.max_pages + j / g.P];
+        int b = a.block_table[(size_t)table * g.max_pages + j / g.P];
         if (b < 0 || b >= g.num_blocks) { flag_error(a.counters, STEP_ERR_BAD_BLOCK); b = 0; }
         k = kv + kv_page_base(g, a.layer, b, h, 0) + (size_t)(j % g.P) * d;
         v = k + (size_t)g.P * d;
@@ -164,7 +214,7 @@ __global__ void __launch_bounds__(kRowsThreads) attn_rows_kernel(RowsArgs a) {
     const int rr = i / cpr, c = i - rr * cpr, r = r0 + rr;
     uint4 raw = make_uint4(0, 0, 0, 0);
     if (r < nodes * G)
-      raw = *reinterpret_cast<const uint4*>((const T*)a.q + (((size_t)t * a.T + r / G) * g.Hq + (size_t)h * G + r % G) * d + c * cpe);
+      raw = *reinterpret_cast<const uint4*>((const T*)a.q + ((q0 + r / G) * g.Hq + (size_t)h * G + r % G) * d + c * cpe);
     const T* e = reinterpret_cast<const T*>(&raw);
 #pragma unroll
     for (int x = 0; x < cpe; ++x) s_q[rr * ld + c * cpe + x] = to_f32(e[x]);
@@ -177,9 +227,9 @@ __global__ void __launch_bounds__(kRowsThreads) attn_rows_kernel(RowsArgs a) {
   if constexpr (kTree) sees = real ? s_mask[my_u] : 0ull;
   float m_run = -INFINITY, l_run = 0.f;
   // second product: thread x of the (row group, dims) tiles owns rows kRpt * (x % groups) .. and dims 4 * (x / groups) ..
-  constexpr int kGroups = kRows / kRpt;                 // (divides the threads: a thread's rows are the same in all of its tiles)
-  static_assert(kRowsThreads % kGroups == 0, "rows of a thread");
-  const int tiles_o = kGroups * (d / 4);
+  constexpr int kRowGroups = kRows / kRpt;              // (divides the threads: a thread's rows are the same in all of its tiles)
+  static_assert(kRowsThreads % kRowGroups == 0, "rows of a thread");
+  const int tiles_o = kRowGroups * (d / 4);
   float acc[kNi][kRpt][4];
 #pragma unroll
   for (int i = 0; i < kNi; ++i)
@@ -188,13 +238,13 @@ __global__ void __launch_bounds__(kRowsThreads) attn_rows_kernel(RowsArgs a) {
   unsigned long long see[kRpt];                          // the drafted tokens that these rows see
 #pragma unroll
   for (int y = 0; y < kRpt; ++y) {
-    const int r = r0 + tid % kGroups * kRpt + y;
+    const int r = r0 + tid % kRowGroups * kRpt + y;
     see[y] = kTree && r < nodes * G ? s_mask[r / G] : 0ull;
   }
   __syncthreads();
 
   for (int it = it0; it < it1; ++it) {
-    const int j0 = it * kKeys;
+    const int j0 = key0 + it * kKeys;
     // (kAhead loads of a thread are under way before the first of them is used)
     for (int i0 = tid; i0 < 2 * kKeys * cpr; i0 += kAhead * kRowsThreads) {
       uint4 raw[kAhead];
@@ -270,7 +320,7 @@ __global__ void __launch_bounds__(kRowsThreads) attn_rows_kernel(RowsArgs a) {
     for (int i = 0; i < kNi; ++i) {
       const int x = tid + i * kRowsThreads;
       if (x < tiles_o) {
-        const int rg = x % kGroups * kRpt, k = x / kGroups * 4;
+        const int rg = x % kRowGroups * kRpt, k = x / kRowGroups * 4;
 #pragma unroll
         for (int y = 0; y < kRpt; ++y) {
           const float c = s_corr[rg + y];
@@ -312,6 +362,31 @@ __global__ void __launch_bounds__(kRowsThreads) attn_rows_kernel(RowsArgs a) {
   }
   if (sub == 0) { s_m[row] = m_run; s_l[row] = l_run; }
   __syncthreads();
+  if constexpr (kGroups) {
+    // pieces of row (trace, query head): `splits` of its own keys, then as many of the shared ones, which for a row that shares
+    // nothing hold nothing
+    const int all = 2 * a.splits;
+    float2* ml_out = reinterpret_cast<float2*>(a.part + (size_t)a.n * g.Hq * all * d);
+    auto piece = [&](int r, bool of_prefix) { return ((q0 + r / G) * g.Hq + (size_t)h * G + r % G) * all + (of_prefix ? a.splits : 0) + split; };
+    auto mine_to_write = [&](int r) {                    // (a row of the group that is too short to share)
+      return r < n_rows && (!prefix || min((long long)a.seq_lens[q0 + r / G], (long long)g.max_pages * g.P) >= shared_keys);
+    };
+#pragma unroll
+    for (int i = 0; i < kNi; ++i) {
+      const int x = tid + i * kRowsThreads;
+      if (x >= tiles_o) break;
+      const int rg = x % kRowGroups * kRpt, k = x / kRowGroups * 4;
+#pragma unroll
+      for (int y = 0; y < kRpt; ++y)
+        if (mine_to_write(rg + y))
+          *reinterpret_cast<float4*>(a.part + piece(rg + y, prefix) * d + k) = make_float4(acc[i][y][0], acc[i][y][1], acc[i][y][2], acc[i][y][3]);
+    }
+    if (tid < kRows && mine_to_write(tid)) {
+      ml_out[piece(tid, prefix)] = make_float2(s_m[tid], s_l[tid]);
+      if (!prefix && shared_keys == 0) ml_out[piece(tid, true)] = make_float2(-INFINITY, 0.f);
+    }
+    return;
+  }
   const size_t head_rows = ((size_t)t * g.Hkv + h) * n_rows;          // this head's first row among all rows
   const size_t all_rows = (size_t)gridDim.z * g.Hkv * n_rows;
   float2* part_ml = reinterpret_cast<float2*>(a.part + all_rows * a.splits * d);
@@ -319,7 +394,7 @@ __global__ void __launch_bounds__(kRowsThreads) attn_rows_kernel(RowsArgs a) {
   for (int i = 0; i < kNi; ++i) {
     const int x = tid + i * kRowsThreads;
     if (x >= tiles_o) break;
-    const int rg = x % kGroups * kRpt, k = x / kGroups * 4;
+    const int rg = x % kRowGroups * kRpt, k = x / kRowGroups * 4;
 #pragma unroll
     for (int y = 0; y < kRpt; ++y) {
       const int r = r0 + rg + y;
@@ -343,7 +418,7 @@ __global__ void __launch_bounds__(kRowsThreads) attn_rows_kernel(RowsArgs a) {
 }
 
 // Combines the ranges of every row, in ascending order: a warp per row, lanes over the dims.
-template <typename OutT, bool kScores>
+template <typename OutT, bool kScores, bool kGroups>
 __global__ void __launch_bounds__(kRowsThreads) rows_merge_kernel(RowsArgs a, int n) {
   const Geo& g = a.g;
   const int d = g.d, G = g.G, n_rows = a.T * G, lane = threadIdx.x & 31;
@@ -374,7 +449,7 @@ __global__ void __launch_bounds__(kRowsThreads) rows_merge_kernel(RowsArgs a, in
 #pragma unroll 4
       for (int s = 0; s < a.splits; ++s) {
         const float w = __shfl_sync(0xffffffffu, s < 32 ? w0 : w1, s & 31);
-        if (k < d) {
+        if (k < d && !(kGroups && w == 0.f)) {           // (kGroups: a piece that holds nothing was not written)
           const float4 v = __ldcg(reinterpret_cast<const float4*>(a.part + (i * a.splits + s) * d + k));
           sum.x = fmaf(w, v.x, sum.x); sum.y = fmaf(w, v.y, sum.y); sum.z = fmaf(w, v.z, sum.z); sum.w = fmaf(w, v.w, sum.w);
         }
@@ -391,22 +466,24 @@ __global__ void __launch_bounds__(kRowsThreads) rows_merge_kernel(RowsArgs a, in
 }
 
 // a.splits and a.part are set here; `part` has attn_rows_workspace bytes.
-template <typename T, typename OutT, bool kTree, bool kScores>
+template <typename T, typename OutT, bool kTree, bool kScores, bool kGroups = false>
 int launch_attn_rows(const step_pool* pool, RowsArgs a, int n, float* part, cudaStream_t s) {
-  a.splits = attn_rows_splits(pool, n, a.T);
+  a.splits = kGroups ? attn_groups_splits(pool, n) : attn_rows_splits(pool, n, a.T);
   a.part = part;
+  a.n = n;
   const int d = a.g.d;
   const size_t smem = attn_rows_smem(d);
-  auto kern = d <= 64 ? attn_rows_kernel<T, OutT, kTree, kScores, 2, 1>
-                      : (d <= 128 ? attn_rows_kernel<T, OutT, kTree, kScores, 4, 1> : attn_rows_kernel<T, OutT, kTree, kScores, 4, 4>);
+  auto kern = d <= 64 ? attn_rows_kernel<T, OutT, kTree, kScores, kGroups, 2, 1>
+                      : (d <= 128 ? attn_rows_kernel<T, OutT, kTree, kScores, kGroups, 4, 1> : attn_rows_kernel<T, OutT, kTree, kScores, kGroups, 4, 4>);
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return STEP_ERR_CUDA;
   const int blocks = (a.T * a.g.G + kRows - 1) / kRows;
-  kern<<<dim3(blocks * a.splits, a.g.Hkv, n), kRowsThreads, smem, s>>>(a);
+  kern<<<dim3(blocks * a.splits, a.g.Hkv * (kGroups ? 2 : 1), n), kRowsThreads, smem, s>>>(a);
   if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
+  if (kGroups) a.splits *= 2;
   if (a.splits > 1) {
     const long long rows = (long long)n * a.g.Hkv * a.T * a.g.G;
     const int grid = (int)((rows + 3) / 4 < 8ll * pool->num_sms ? (rows + 3) / 4 : 8ll * pool->num_sms);
-    if (launch_dependent(rows_merge_kernel<OutT, kScores>, dim3(grid), dim3(kRowsThreads), 0, s, a, n) != cudaSuccess) return STEP_ERR_CUDA;
+    if (launch_dependent(rows_merge_kernel<OutT, kScores, kGroups>, dim3(grid), dim3(kRowsThreads), 0, s, a, n) != cudaSuccess) return STEP_ERR_CUDA;
   }
   return launch_ok();
 }

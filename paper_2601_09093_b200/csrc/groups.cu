@@ -3,8 +3,8 @@
 //
 //   out[i][h] = sum_j softmax_j(q[i][h] . K_i[j] / sqrt(d)) V_i[j],  j in [0, seq_lens[i]),
 //
-// where the first pages of a group's rows are the same blocks.  bf16 pools of the usual shape run on groups_tc.cu; elsewhere
-// every row reads its own table (attention_rows.cuh).
+// where the first pages of a group's rows are the same blocks.  bf16 pools of the usual shape run on groups_tc.cu, others on
+// attention_rows.cuh, which reads shared pages once for 16 / G traces.
 #include "attention_rows.cuh"
 
 using namespace stepk;
@@ -13,7 +13,9 @@ extern "C" {
 
 int decode_attention_groups_workspace_bytes(const step_pool* pool, int n, int n_groups, size_t* bytes) {
   if (!pool || !bytes || n < 0 || n_groups < 0 || n > 65535 || n_groups > 65535) return STEP_ERR_INVALID_ARG;
-  *bytes = groups_tc_supported(pool, n) ? groups_tc_workspace(pool, n, n_groups) : attn_rows_workspace(pool, n, 1);
+  *bytes = groups_tc_supported(pool, n) ? groups_tc_workspace(pool, n, n_groups)
+           : n_groups > 0               ? attn_groups_workspace(pool, n)
+                                        : attn_rows_workspace(pool, n, 1);
   return STEP_OK;
 }
 
@@ -41,8 +43,13 @@ int decode_attention_groups(step_pool* pool, int layer, const void* q, const int
   a.block_table = block_table; a.seq_lens = seq_lens; a.out = out;
   a.counters = pool->v.counters;
   a.group_rows = group_rows; a.group_pages = group_pages; a.n_groups = n_groups;
-  if (pool->cfg.dtype == STEP_BF16) return launch_attn_rows<__nv_bfloat16, __nv_bfloat16, false, false>(pool, a, n, (float*)workspace, s);
-  return launch_attn_rows<float, float, false, false>(pool, a, n, (float*)workspace, s);
+  const bool bf16 = pool->cfg.dtype == STEP_BF16;
+  float* part = (float*)workspace;
+  if (n_groups > 0)
+    return bf16 ? launch_attn_rows<__nv_bfloat16, __nv_bfloat16, false, false, true>(pool, a, n, part, s)
+                : launch_attn_rows<float, float, false, false, true>(pool, a, n, part, s);
+  return bf16 ? launch_attn_rows<__nv_bfloat16, __nv_bfloat16, false, false>(pool, a, n, part, s)
+              : launch_attn_rows<float, float, false, false>(pool, a, n, part, s);
 }
 
 }  // extern "C"
