@@ -350,7 +350,8 @@ typedef struct {
  * rows 16-byte aligned.  Positions have to exist (kv_pool_extend): an entry that reaches beyond its trace's length is
  * skipped whole (STEP_ERR_INVALID_ARG in the status word), as is one whose trace is not live (STEP_ERR_BAD_TRACE); q_out rows
  * of entries that are skipped or passed over are left as they are.  No two entries of a call may name the same position.
- * A page that several traces share is written for all of them.  Wants the pool's device to be current. */
+ * A page that several traces share is written for all of them.  q_out may be q with the same strides, and overlaps nothing else.
+ * Wants the pool's device to be current. */
 int store_kv_rotated(step_pool* pool, const kv_store_args* a, const step_rotary* rotary, void* stream);
 
 /* decode_attention for traces that were forked from several prompts (kv_pool_fork_prefix, once per problem), each prompt's pages

@@ -160,6 +160,20 @@ def test_many_groups_of_few_rows():
     run(tw, rows, pages)
 
 
+def test_many_pieces_of_one_tile_one_after_another():
+    """Sequences of shared pages that are a tile long: of the two chains of such a piece one has nothing to do, and runs ahead of
+    the other or falls behind it by whole pieces."""
+    rng = np.random.default_rng(7)
+    cfg = config((24, 8, 128), "bf16", n=150, layers=1)
+    tw, rows, pages = build(cfg, [(int(rng.integers(16, 260)), rng.integers(0, 120, 2 + k % 2)) for k in range(60)])
+    want = run(tw, rows, pages, poison=False)
+    q, _ = draw(cfg, W.TID_Q, (150, 24, 128), 5)
+    v, r, p = tw.gpu.views(), dev(rows), dev(pages)
+    outs = [tw.gpu.decode_attention_groups(0, q, v["block_table"], v["seq_lens"], r, p) for _ in range(3000)]
+    assert tw.gpu.last_error() == (0, 0)
+    assert all(torch.equal(o, want) for o in outs)
+
+
 def test_long_prompts_and_long_own_texts_are_cut_in_many_pieces():
     rng = np.random.default_rng(4)
     cfg = config((8, 2, 128), "bf16", n=40, layers=1)
