@@ -1,4 +1,6 @@
 """decode_attention_groups against the oracle."""
+import os
+
 import numpy as np
 import pytest
 import torch
@@ -444,6 +446,48 @@ def test_a_decode_step_layer_by_layer():
             check(tw, l, exact_f32(out), exact_f32(qo[0, :, 0]))
     tw.assert_meta_equal()
     assert g.last_error() == (0, 0)
+
+
+FUZZ = int(os.environ.get("STEP_FUZZ_SEEDS", "40"))
+
+
+@pytest.mark.parametrize("first", range(0, FUZZ, 20))
+def test_random_groups_against_the_plain_call(first):
+    """Heads, prompts, own texts, ended traces and declared pages at random, blocks shuffled, NaN wherever nothing is stored: what
+    decode_attention makes of the same pool, twice the same bits."""
+    for seed in range(first, min(FUZZ, first + 20)):
+        rng = np.random.default_rng(9000 + seed)
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        Hkv = int(rng.choice([1, 2, 3, 8]))
+        Hq = Hkv * int(rng.choice([1, 2, 3, 4, 5, 7, 8, 12, 16]))
+        d, P, dt = (128, 16, "bf16") if rng.random() < 0.8 else [(64, 16, "bf16"), (64, 8, "fp32"), (128, 32, "bf16")][rng.integers(3)]
+        few = rng.random() < 0.8
+        problems = [(int(rng.integers(0, 6000 if rng.random() < 0.2 else 400)), rng.choice([0, 1, 15, 16, 17, 90, 700 if rng.random() < 0.1 else 33],
+                     int(rng.choice([1, 2, 4, 17, 33, 65]) if few else rng.integers(1, 4)))) for _ in range(int(rng.integers(1, 5)) if few else 60)]
+        n, tdt = sum(len(o) for _, o in problems), torch.bfloat16 if dt == "bf16" else torch.float32
+        blocks = sum(p // P + sum((p % P + int(x)) // P + 2 for x in o) for p, o in problems) + 8
+        pool = B.KVPool(1, Hq, Hkv, d, P, num_blocks=blocks, max_traces=n, max_pages_per_trace=max(p + int(max(o)) for p, o in problems) // P + 1,
+                        dtype=B.STEP_BF16 if dt == "bf16" else B.STEP_FP32)
+        v = pool.views()
+        v["free_list"].copy_(torch.from_numpy(rng.permutation(blocks).astype(np.int32)))
+        pool.kv_storage.fill_(255)
+        rand = lambda *shape: torch.randn(shape, generator=gen, device="cuda").to(tdt)          # noqa: E731
+        for p, o in problems:
+            pool.fork_prefix(len(o), p, rand(1, Hkv, p, d), rand(1, Hkv, p, d))
+        for sel, inc in H.ragged_append_plan(np.concatenate([o for _, o in problems])):
+            pool.append_kv(dev(sel), inc, rand(len(sel), inc, 1, Hkv, d), rand(len(sel), inc, 1, Hkv, d))
+        ended = np.nonzero(rng.random(n) < rng.choice([0, 0.1, 0.5]))[0]
+        if len(ended):
+            pool.release_traces(dev(ended))
+        pages = np.array([p // P if rng.random() < 0.8 else rng.integers(0, p // P + 1) for p, _ in problems])
+        rows = dev(np.cumsum([0] + [len(o) for _, o in problems]))
+        q = rand(n, Hq, d)
+        got = [pool.decode_attention_groups(0, q, v["block_table"], v["seq_lens"], rows, dev(pages)) for _ in range(2)]
+        plain = pool.decode_attention(0, q, v["block_table"], v["seq_lens"])
+        # each side rounds its probabilities (bf16 pools), this one its output; values below 6.  fp32: sums in another order
+        tol = 3 * BF16_HALF_STEP * 6 if dt == "bf16" else 2e-4
+        assert pool.last_error() == (0, 0) and torch.equal(*got), seed
+        assert (got[0].float() - plain).abs().max().item() <= tol, seed
 
 
 def test_refusals():
