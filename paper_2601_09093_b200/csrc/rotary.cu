@@ -292,7 +292,8 @@ constexpr int kMaxPairs = 256;                                           // head
 // A CTA takes one (entry, token) row and a range of layers: cosines and sines of its position once, into shared memory;
 // where the row goes (block and slot, the same for every layer and head) once; then its warps share the heads.
 // kChunks: whole units (D a multiple of two chunks); else pair by pair.  32 tokens for 64 traces, 36 layers of 32 / 8 heads of 128 in
-// bf16, with their queries: 290 us, 1.81 GB at 6.3 TB/s; one token, one layer: 4 us, the latency of four dependent reads.
+// bf16, with their queries: 290 us, 1.81 GB at 6.3 TB/s; one token, one layer: the latency of three dependent reads (an extension, the
+// store and attention to the row together 12.4 us, 13.1 with the page looked up after the trace's length, a fourth).
 template <typename T, bool kPairs, bool kChunks>
 __global__ void __launch_bounds__(256) store_kernel(const StoreDev a) {
   constexpr int kU = 16 / (int)sizeof(T);
@@ -308,13 +309,17 @@ __global__ void __launch_bounds__(256) store_kernel(const StoreDev a) {
   for (int x = threadIdx.x; x < half; x += 256) angle_of(p, a.table[x], a.scale, s_c[x], s_s[x]);
   const bool live = a.live[t];
   const int S = a.seq_lens[t];
+  // (the page is looked up along with the trace's length, before that has been compared: one round of reads less.
+  // slot stays signed: unsigned took 51 registers instead of 48, four CTAs per SM instead of five: 325 us instead of 308 for the 64
+  // traces above and attention to one layer)
+  const unsigned page = ((unsigned)st + tok) / (unsigned)g.P;
+  const int slot = (int)((unsigned)st + tok - page * g.P);
+  const int b = a.block_table[(size_t)t * g.max_pages + min(page, (unsigned)g.max_pages - 1u)];
   if (!live) { if (reporter) flag_error(a.counters, STEP_ERR_BAD_TRACE); return; }
   if ((long long)st + a.n_tokens > S || (long long)S > (long long)g.max_pages * g.P) {
     if (reporter) flag_error(a.counters, STEP_ERR_INVALID_ARG);
     return;
   }
-  const int pos = st + tok, page = pos / g.P, slot = pos - page * g.P;
-  const int b = a.block_table[(size_t)t * g.max_pages + page];
   if (b < 0 || b >= g.num_blocks) { if (threadIdx.x == 0 && blockIdx.y == 0) flag_error(a.counters, STEP_ERR_BAD_BLOCK); return; }
   __syncthreads();
   const int l0 = blockIdx.y * a.layers_per_cta, l1 = min(a.n_layers, l0 + a.layers_per_cta);
