@@ -366,8 +366,8 @@ int store_kv_rotated(step_pool* pool, const kv_store_args* a, const step_rotary*
  * q and out: [n, num_q_heads, head_dim] in POOL DTYPE, 16-byte aligned; out is rounded once and must not overlap the inputs.
  * n, n_groups <= 65535.  Scores, maxima, sums and accumulators are fp32.  Where the tensor-core kernels serve the call (bf16 pools,
  * head_dim 128, page_size 16, n <= 2048, n * num_kv_heads * (max_pages_per_trace + 3) < 2^31, kv_pool_set_attention_config not -1)
- * the probabilities are rounded to bf16 on their way into the second product, as decode_attention_tree's are (2.3e-3 off in the
- * 2-norm, where rounding the output alone makes 1.7e-3); elsewhere they stay fp32, and shared pages are read once for 16 / G traces.
+ * a probability enters the second product as two bf16 numbers, which are off by at most 3.5e-5 of it (the output's rounding: 3.9e-3);
+ * elsewhere it stays fp32, and shared pages are read once for 16 / G traces.
  * Wants the pool's device to be current and a workspace of decode_attention_groups_workspace_bytes (host-only) bytes, 256-byte
  * aligned, in use from the call until its work on the stream is done; can be captured into a CUDA graph.  It keeps nothing in the
  * pool's metadata: calls that only read one pool may overlap if each has a workspace of its own. */

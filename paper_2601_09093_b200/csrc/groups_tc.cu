@@ -15,14 +15,14 @@
 //   costs such a kernel four tiles' time, more than a trace's own text often has.
 //   Shared pages: the query rows of a group's traces - (trace, head of the KV head's group) - are taken 256 at a time against
 //   one read of the keys, as decode_attention_tree does with a trace's drafted tokens: scores by tcgen05 into tensor memory, a
-//   thread per row for the softmax, probabilities rounded to bf16 over the scores, from where they are the second product's A
-//   operand.  Two chains ("lanes") run side by side: 128 rows each of the same tile of 128 keys, or, where a row block has
+//   thread per row for the softmax, probabilities as two bf16 numbers each over the scores, from where they are the second
+//   product's A operand.  Two chains ("lanes") run side by side: 128 rows each of the same tile of 128 keys, or, where a row block has
 //   at most 128 rows, even and odd tiles of the same rows.  The tiles of all (group, KV head, row block) sequences form one
 //   stream, cut into one equal share per CTA.
 //
-// 64 traces of a prompt of 32,768 with own texts of up to 1,024, 32 / 8 heads: 68 to 74 us, 270 MB (41 us at the measured copy rate) and
-// 35 GFLOP; as two kernels in a row 104.  8 prompts of 1,000 to 16,000 with 12 traces each and own texts of up to 3,000, 64 / 8
-// heads: 127 to 148 us, 0.75 to 0.87 of the measured copy.
+// 64 traces of a prompt of 32,768 with own texts of up to 1,024, 32 / 8 heads: 72 us, 270 MB (41 us at the measured copy rate) and
+// 35 GFLOP; as two kernels in a row 104 (with one bf16 number for a probability, as one kernel 69.5).  8 prompts of 1,000 to 16,000 with
+// 12 traces each and own texts of up to 3,000, 64 / 8 heads: 131 us, 0.84 of the measured copy.
 //
 // The partition is a function of lengths and groups alone and pieces are combined in stream order, so a call gives the same
 // bits every time.  Every wait for a barrier is bounded (kv_pool_set_wait_limit_ns); a CTA whose wait runs out raises
@@ -49,8 +49,9 @@ constexpr int kStreamWarps = 8, kStages = 3, kPageBytes = 2 * kP * kD * 2;
 constexpr int kTableGroups = 48;                  // groups whose table fits beside the rings; a longer one lies in the workspace
 // What a CTA takes, in nanoseconds (measured, 32 / 8 and 64 / 8 heads): a tile of shared pages with more than 128 rows (its products
 // and exponentials) and with fewer (1.0 alone, the latency of its copies when all SMs read); a page of a warp's own; what comes
-// before and behind them.
-constexpr int kWideNs = 2150, kNarrowNs = 1600, kPageNs = 1050, kPrefixNs = 9000, kOwnNs = 5000;
+// before and behind them.  (Tiles at 2150 and 1600: 64 traces of 32,768 take 75 us instead of 72, a layer of 2 x 32 traces of 8192 in a
+// decode step 84 instead of 79, 8 x 12 traces 128 instead of 131.)
+constexpr int kWideNs = 2600, kNarrowNs = 2000, kPageNs = 1050, kPrefixNs = 9000, kOwnNs = 5000;
 constexpr int kOwnSetup = 2;                      // pages' worth of time that a sequence of own pages takes besides them
 
 // Tiles in the prefix stream, own pages (of all KV heads; setups counted in both), groups of a valid description (else 0), CTAs that
@@ -86,6 +87,20 @@ struct GroupArgs {
   float *own_ml, *own_o;            // [warp][2][G] of the own pages' pieces that are not whole sequences
   float *all_ml, *all_o;            // [n][Hq] of those that are, where there are shared pages besides
 };
+
+// A probability enters the second product, whose V is bf16, as two bf16 numbers: hi = p cut off behind the bits that bf16 holds, and
+// lo = p kScale - hi, rounded to nearest; sums of probabilities are multiplied by kScale in the end.  lo is at most (2^-7 + 2^-10) p, so
+// that hi + lo is off by at most 2^-8 of that, 3.5e-5 of p, where the output's own rounding is up to 3.9e-3; one rounded bf16 number
+// made the output's error 2.3e-3 instead of 1.7e-3 in the 2-norm.  kScale makes lo positive (where p is above 2^-116): an infinity
+// in V keeps its sign in both products and their sum.  64 traces of a prompt of 32,768: 68.5 us with one number, 74.5 with two; with hi
+// rounded to nearest 75.6, with packed arithmetic (fma.f32x2, whose operands have to be moved together) 79.5.
+constexpr float kScale = 1.f + 0x1p-10f;
+__device__ inline void split2(float p0, float p1, uint32_t& hi, uint32_t& lo) {
+  hi = __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
+  p0 = fmaf(p0, kScale, -__uint_as_float(__float_as_uint(p0) & 0xffff0000u));
+  p1 = fmaf(p1, kScale, -__uint_as_float(__float_as_uint(p1) & 0xffff0000u));
+  lo = pack2(p0, p1);
+}
 
 __device__ inline int div_up(int x, int by) { return (int)(((unsigned)x + (unsigned)by - 1) / (unsigned)by); }
 
@@ -277,11 +292,16 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
           if (rows < kP && y * 8 + tq * 2 + (z & 1) >= rows) sc[y][z] = -INFINITY;
           mx[z >> 1] = fmaxf(mx[z >> 1], sc[y][z]);
         }
-      uint32_t pf[4];
+      uint32_t pf[4], pl[4];                                           // hi and lo parts of the probabilities
       float corr[2];
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
-        if (z == 1 && !upper) { corr[1] = 1.f; pf[1] = pf[3] = 0u; break; }
+        if (z == 1 && !upper) {                                        // the rows that are no heads take the others' lo parts
+          corr[1] = corr[0];
+          pf[1] = pl[0];
+          pf[3] = pl[2];
+          break;
+        }
         mx[z] = fmaxf(mx[z], __shfl_xor_sync(0xffffffffu, mx[z], 1));
         mx[z] = fmaxf(mx[z], __shfl_xor_sync(0xffffffffu, mx[z], 2));
         const float mn = fmaxf(m[z], mx[z]), off = mn == -INFINITY ? 0.f : mn;
@@ -290,21 +310,28 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
         const float p0 = exp2f(sc[0][2 * z] - off), p1 = exp2f(sc[0][2 * z + 1] - off);
         const float p2 = exp2f(sc[1][2 * z] - off), p3 = exp2f(sc[1][2 * z + 1] - off);
         l[z] = l[z] * corr[z] + ((p0 + p1) + (p2 + p3));
-        pf[z] = pack2(p0, p1);                                         // (rounded for the second product, whose V is bf16; the sum is not)
-        pf[2 + z] = pack2(p2, p3);
+        split2(p0, p1, pf[z], pl[z]);                                  // (the sum is that of the probabilities as they are)
+        split2(p2, p3, pf[2 + z], pl[2 + z]);
       }
       if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
 #pragma unroll
         for (int x = 0; x < 16; ++x) { o[x][0] *= corr[0]; o[x][1] *= corr[0]; o[x][2] *= corr[1]; o[x][3] *= corr[1]; }
       }
+      auto values = [&](bool twice) {
 #pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        uint32_t b[4];
-        const int c = 2 * x + vc;
-        ldsm4_t(b, pg + kP * kD * 2 + vk * 256 + ((c & 8) | ((c ^ vk) & 7)) * 16);
-        mma16816(o[2 * x], pf, b[0], b[1]);
-        mma16816(o[2 * x + 1], pf, b[2], b[3]);
-      }
+        for (int x = 0; x < 8; ++x) {
+          uint32_t b[4];
+          const int c = 2 * x + vc;
+          ldsm4_t(b, pg + kP * kD * 2 + vk * 256 + ((c & 8) | ((c ^ vk) & 7)) * 16);
+          mma16816(o[2 * x], pf, b[0], b[1]);
+          mma16816(o[2 * x + 1], pf, b[2], b[3]);
+          if (twice) {
+            mma16816(o[2 * x], pl, b[0], b[1]);
+            mma16816(o[2 * x + 1], pl, b[2], b[3]);
+          }
+        }
+      };
+      if (upper) values(true); else values(false);                     // (a branch per step keeps the steps from overlapping)
       if (++get == kStages) get = 0;
       __syncwarp();                                                    // all lanes have read the page
       issue();
@@ -313,6 +340,11 @@ __device__ __forceinline__ void own_pages(const GroupArgs& a, const Rows& rw, un
     for (int z = 0; z < 2; ++z) {
       l[z] += __shfl_xor_sync(0xffffffffu, l[z], 1);
       l[z] += __shfl_xor_sync(0xffffffffu, l[z], 2);
+      l[z] *= kScale;
+    }
+    if (!upper) {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) { o[x][0] += o[x][2]; o[x][1] += o[x][3]; }
     }
     const bool whole = cnt == s.pages;
 #pragma unroll
@@ -645,22 +677,26 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
         }
         const float off = m_ref == -INFINITY ? 0.f : m_ref;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        // in halves: the second product of the first 64 keys runs while the others' probabilities are made
+        // In halves: the second product of the first 64 keys runs while the others' probabilities are made.  16 keys' hi parts, then
+        // their lo parts take the columns of these keys' scores.
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int c0 = 0; c0 < kTile; c0 += 32) {
+          uint32_t p[32];
 #pragma unroll
-          for (int c = half * 64; c < half * 64 + 64; c += 2) {
+          for (int c = 0; c < 32; c += 2) {
             float p0, p1;
-            fma2(p0, p1, __uint_as_float(s[c]), __uint_as_float(s[c + 1]), a.scale_log2, -off);
+            fma2(p0, p1, __uint_as_float(s[c0 + c]), __uint_as_float(s[c0 + c + 1]), a.scale_log2, -off);
             p0 = exp2f(p0);
             p1 = exp2f(p1);
             add2(sum[c & 2], sum[(c & 2) + 1], p0, p1);
-            s[c / 2] = pack2(p0, p1);
+            split2(p0, p1, p[(c & 16) + (c & 15) / 2], p[(c & 16) + 8 + (c & 15) / 2]);
           }
-          tc_st32(t_s + half * 32, s + half * 32);
-          tc_wait_st();
-          tc_fence_before();
-          arrive_warp(bar_p + 8 * (half == 0 ? 2 + ln : ln));
+          tc_st32(t_s + c0, p);
+          if (c0 == 32 || c0 == 96) {
+            tc_wait_st();
+            tc_fence_before();
+            arrive_warp(bar_p + 8 * (c0 == 32 ? 2 + ln : ln));
+          }
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
@@ -681,7 +717,7 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
       const bool whole = pc.cnt == pc.tiles;
       const size_t at = whole ? ((size_t)(pc.two ? 0 : ln) * a.n + pc.row0 + (mine ? t : 0)) * a.Hq + (size_t)pc.h * a.G + row % a.G
                               : (((size_t)blockIdx.x * 2 + pc.slot) * 2 + ln) * kHalfRows + row;
-      if (mine) reinterpret_cast<float2*>(whole ? a.row_ml : a.pre_ml)[at] = make_float2(m_ref, l);
+      if (mine) reinterpret_cast<float2*>(whole ? a.row_ml : a.pre_ml)[at] = make_float2(m_ref, l * kScale);
       float* o_out = (whole ? a.row_o : a.pre_o) + at * kD;
       if (some) {
 #pragma unroll
@@ -822,7 +858,10 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
         const uint32_t vb = sm_ring + s * kSlotBytes;
 #pragma unroll
         for (int x = 0; x < 8; ++x)
-          if (x >= from && x < steps) tc_mma_bf16_ta(tm + 256 + ln * 128, tm + ln * 128 + x * 8, umma_desc_v(vb + x * 4096), id_pv, !(first && x == 0));
+          if (x >= from && x < steps) {
+            tc_mma_bf16_ta(tm + 256 + ln * 128, tm + ln * 128 + x * 16, umma_desc_v(vb + x * 4096), id_pv, !(first && x == 0));
+            tc_mma_bf16_ta(tm + 256 + ln * 128, tm + ln * 128 + x * 16 + 8, umma_desc_v(vb + x * 4096), id_pv, 1);
+          }
       };
       while (ok) {
         ok = wait_warp(bar_q, ph_q);
