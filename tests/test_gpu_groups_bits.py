@@ -1,5 +1,6 @@
 """decode_attention_groups to the last bits of its output: against torch in 64 bits, element by element."""
 import math
+import os
 
 import numpy as np
 import pytest
@@ -56,10 +57,11 @@ class Forks:
     def attend(self, q, pages):
         return self.pool.decode_attention_groups(0, q, self.views["block_table"], self.views["seq_lens"], self.rows, dev(pages))
 
-    def check(self, got, q, ended=()):
+    def check(self, got, q, ended=(), without=slice(0, 0)):
         """A weight is off by the errors of its score (a product of d terms, each of whose additions may lose a step; three roundings of a
         value up to the largest score; the exponential, 2 steps) in numerator and denominator and by a step per key in the sums, as
-        draft_common.relative_bound has it; by SPLIT besides, in bf16 pools.  The output is rounded once."""
+        draft_common.relative_bound has it; by SPLIT besides, in bf16 pools.  The output is rounded once.  without: positions that the
+        oracle leaves out."""
         half = BF16_HALF_STEP if self.dtype == "bf16" else FP32_HALF_STEP
         worst = 0.0
         for i in range(self.n):
@@ -71,6 +73,9 @@ class Forks:
             if S == 0:
                 assert (got[i] == 0).all(), i
                 continue
+            keep = torch.ones(S, dtype=torch.bool, device="cuda")
+            keep[without] = False
+            K, V = K[keep], V[keep]
             x = q[i].double().view(Hkv, -1, d)
             K, V = K.transpose(0, 1), V.transpose(0, 1)
             p = (x @ K.transpose(1, 2) / math.sqrt(d)).softmax(-1)
@@ -144,3 +149,43 @@ def test_an_infinite_value_keeps_its_sign():
                 rest = [i for i in range(3) if i not in rows]
                 assert (got[rows] == sign).all() and torch.equal(got[rest], clean[rest]), (G, page, sign)
         assert torch.equal(f.attend(q, [4]), clean)
+
+
+def test_the_bound_would_show_a_page_that_is_left_out():
+    """The oracle without 16 of 6000 positions, of the prompt or of an own text: the right results are far outside the bound."""
+    rng = np.random.default_rng(1)
+    make = normal(1)
+    f = Forks((8, 2, 128), "bf16", 16, [(5500, [600, 0, 33])], make, rng)
+    q = make(3, 8, 128).bfloat16()
+    got = f.attend(q, [343])
+    f.check(got, q)
+    for first in (0, 2560, 5472, 5600):
+        with pytest.raises(AssertionError):
+            f.check(got, q, without=slice(first, first + 16))
+
+
+FUZZ = int(os.environ.get("STEP_FUZZ_SEEDS", "40"))
+
+
+@pytest.mark.parametrize("first", range(0, FUZZ, 10))
+def test_random_groups_element_by_element(first):
+    """Heads, prompts, own texts, ended traces and declared pages at random, blocks shuffled, NaN wherever nothing is stored."""
+    for seed in range(first, min(FUZZ, first + 10)):
+        rng = np.random.default_rng(41000 + seed)
+        Hkv = int(rng.choice([1, 2, 3, 8]))
+        Hq = Hkv * int(rng.choice([1, 2, 3, 4, 5, 7, 8, 12, 16]))
+        d, P, dt = (128, 16, "bf16") if rng.random() < 0.8 else [(64, 16, "bf16"), (64, 8, "fp32"), (128, 32, "bf16")][rng.integers(3)]
+        few = rng.random() < 0.8
+        problems = []
+        for _ in range(int(rng.integers(1, 5)) if few else 60):
+            prompt = int(rng.integers(0, 6000 if rng.random() < 0.3 else 400))
+            traces = int(rng.choice([1, 2, 4, 17, 33, 65]) if few else rng.integers(1, 4))
+            problems.append((prompt, rng.choice([0, 1, 15, 16, 17, 90, 700 if rng.random() < 0.2 else 33], traces)))
+        f = Forks((Hq, Hkv, d), dt, P, problems, normal(seed), rng)
+        ended = np.nonzero(rng.random(f.n) < rng.choice([0, 0.1, 0.5]))[0]
+        if len(ended):
+            f.pool.release_traces(dev(ended))
+        q = normal(5000 + seed)(f.n, Hq, d).to(TYPES[dt][1])
+        got = f.attend(q, [p // P if rng.random() < 0.8 else rng.integers(0, p // P + 1) for p, _ in problems])
+        f.check(got, q, ended=set(ended.tolist()))
+        assert f.pool.last_error() == (0, 0), seed
