@@ -280,7 +280,7 @@ int kv_pool_evict_positions(step_pool* pool, const int32_t* trace_ids, int n, co
  * Pair i of the first D = rotary_dim dims of a head - dims i and i + D/2, or 2i and 2i + 1 if interleaved - at position p:
  *   (y1, y2) = scale * ( x1 cos a - x2 sin a,  x2 cos a + x1 sin a ),   a = p * f_i
  * Dims behind D are left as they are.  The frequencies f_i enter as a table of turns per position in units of 2^-64, so that
- * the angle of any int32 position is exact to 1e-9 of a turn; the arithmetic is fp32 with one rounding of the result. */
+ * the angle of any int32 position is exact to 1e-9 of a turn; the arithmetic is fp32 with one rounding of the result, subnormal numbers included. */
 enum { STEP_ROTARY_PLAIN = 0, STEP_ROTARY_LINEAR = 1, STEP_ROTARY_BASE = 2, STEP_ROTARY_YARN = 3, STEP_ROTARY_BANDS = 4 };
 
 /* t_i = base^(-2i / D); how far f_i is stretched for contexts `factor` times longer than original_positions:

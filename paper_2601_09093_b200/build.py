@@ -6,6 +6,7 @@ import os
 import shutil
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -13,8 +14,14 @@ LIB = os.path.join(HERE, "libstep.so")
 STAMP = os.path.join(HERE, "_build", "libstep.stamp")
 SOURCES = ["pool.cu", "attention.cu", "scorer.cu", "scorer_tc.cu", "prune.cu", "algorithm1.cu", "train.cu", "probe.cu",
            "tree.cu", "tree_tc.cu", "weights.cu", "evict.cu", "rotary.cu", "groups.cu", "groups_tc.cu"]
-FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-         "--use_fast_math", "-Xcompiler", "-fPIC", "-shared", "-Xptxas", "-v"]
+ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
+FLAGS = ARCH + ["-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
+# Rotations keep subnormal numbers, which fast arithmetic flushes (same registers, same times); the others do without them.
+PRECISE = ("rotary.cu",)
+
+
+def _flags(source: str) -> list[str]:
+    return FLAGS if source in PRECISE else FLAGS + ["--use_fast_math"]
 
 
 def _nvcc() -> str:
@@ -25,7 +32,7 @@ def _nvcc() -> str:
 
 
 def _digest() -> str:
-    h = hashlib.sha256(" ".join(FLAGS).encode())
+    h = hashlib.sha256(" ".join(f for s in SOURCES for f in [s] + _flags(s)).encode())
     files = [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC))]
     files.append(os.path.join(os.path.dirname(HERE), "include", "step.h"))
     for f in files:
@@ -40,12 +47,21 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and os.path.exists(LIB) and os.path.exists(STAMP) and open(STAMP).read() == dig:
         return LIB
     os.makedirs(os.path.dirname(STAMP), exist_ok=True)
-    cmd = [_nvcc()] + FLAGS + [os.path.join(CSRC, s) for s in SOURCES] + ["-o", LIB]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    log = res.stdout + res.stderr
+    nvcc = _nvcc()
+
+    def run(cmd):
+        res = subprocess.run([nvcc] + cmd, capture_output=True, text=True)
+        return res.returncode, res.stdout + res.stderr
+
+    objects = [os.path.join(os.path.dirname(STAMP), s + ".o") for s in SOURCES]
+    with ThreadPoolExecutor(os.cpu_count()) as pool:
+        done = list(pool.map(run, [_flags(s) + ["-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objects)]))
+    if not any(rc for rc, _ in done):
+        done.append(run(ARCH + ["-shared", "-Xcompiler", "-fPIC"] + objects + ["-o", LIB]))
+    log = "".join(text for _, text in done)
     with open(os.path.join(os.path.dirname(STAMP), "nvcc.log"), "w") as f:
         f.write(log)
-    if res.returncode != 0:
+    if any(rc for rc, _ in done):
         sys.stderr.write(log)
         raise RuntimeError("nvcc failed building libstep.so")
     if verbose:

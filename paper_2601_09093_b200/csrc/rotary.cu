@@ -12,7 +12,8 @@
 //
 // Both kernels are bound by memory: every element is read once and written once.  A thread owns kU = 16 bytes worth of
 // pairs ("unit"): two 16-byte chunks of a head - one in each half, or two neighbours - so that it reads and writes whole
-// chunks and both members of its pairs, in place as well.  Values are turned in fp32 and rounded once.
+// chunks and both members of its pairs, in place as well.  Values are turned in fp32 and rounded once; subnormal ones are kept (this
+// file is compiled without fast arithmetic, to the same registers and times).
 #include "step_internal.cuh"
 
 #include <math.h>

@@ -1,0 +1,61 @@
+"""rotate_positions and store_kv_rotated where values, sizes or tensors are unusual."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import rotary as OR
+from paper_2601_09093_b200 import binding as B
+
+from draft_common import FP32_HALF_STEP
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"bf16": torch.bfloat16, "fp32": torch.float32}
+# half of the spacing of subnormal numbers
+SMALLEST = {"bf16": 2.0 ** -134, "fp32": 2.0 ** -150}
+
+
+def subnormals(shape, dtype, seed=1):
+    """Numbers around the smallest normal one, 2^-126, most of them below it."""
+    x = torch.randn(shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float64) * 2.0 ** -127
+    x = x.to(TYPES[dtype])
+    return torch.where(x == 0, torch.full_like(x, 2.0 ** -128), x).cuda()
+
+
+def off(y, x, positions, f, D, dtype):
+    """Steps of the bound: products and their sum are rounded to the spacing of subnormal numbers (three times), cosine and sine as
+    elsewhere; then the type's rounding, relative above 2^-126 and absolute below."""
+    x, y = x.double().cpu().numpy(), y.double().cpu().numpy()
+    want = OR.rotate(x, positions, f, False)
+    big = 2 * np.abs(x).max()
+    tol = 8 * FP32_HALF_STEP * big + 3 * SMALLEST["fp32"] + (2.0 ** -8 * big + SMALLEST["bf16"] if dtype == "bf16" else 0.0)
+    return float((np.abs(y - want) / tol).max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads,d,D", [(32, 128, 128), (2, 64, 32), (3, 22, 6)])
+def test_subnormal_values_are_kept(dtype, heads, d, D):
+    """Rows of many heads, of few, and pair by pair.  At position 0 nothing is turned: the bits are those that went in."""
+    r, f = B.Rotary(D), OR.frequencies(D, 10000.0)
+    x = subnormals((9, heads, d), dtype)
+    y = B.rotate_positions(x, r)
+    assert torch.equal(y[0], x[0])
+    assert off(y, x, np.arange(9), f, D, dtype) <= 1.0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 12])
+def test_subnormal_values_are_stored(dtype, D):
+    pool = B.KVPool(1, 4, 2, 64, 16, num_blocks=4, max_traces=1, max_pages_per_trace=2, dtype=B.STEP_BF16 if dtype == "bf16" else B.STEP_FP32)
+    pool.fork_prefix(1, 0, None, None)
+    ids = torch.zeros(1, dtype=torch.int32, device="cuda")
+    start = pool.extend(ids, 5)
+    k, v, q = subnormals((1, 5, 1, 2, 64), dtype), subnormals((1, 5, 1, 2, 64), dtype, 2), subnormals((1, 1, 5, 4, 64), dtype, 3)
+    r, f = B.Rotary(D), OR.frequencies(D, 10000.0)
+    qo = pool.store_kv_rotated(0, ids, start, k, v, r, q=q)
+    assert torch.equal(qo[0, 0, 0], q[0, 0, 0]) and off(qo[0, 0], q[0, 0], np.arange(5), f, D, dtype) <= 1.0
+    for h in range(2):
+        kr, vr = pool.read_kv(0, h, pool.views()["block_table"][0], 5)
+        assert torch.equal(kr[0], k[0, 0, 0, h]) and torch.equal(vr, v[0, :, 0, h])
+        assert off(kr[:, None], k[0, :, 0, h:h + 1], np.arange(5), f, D, dtype) <= 1.0
+    assert pool.last_error() == (0, 0)
