@@ -674,10 +674,13 @@ class Rotary:
 def rotate_positions(x, rotary, positions=None, out=None, transpose=False, stream=None):
     """x [batch, rows, heads, d] or [rows, heads, d], any strides but the last dim's, turned by positions ([rows] or
     [batch, rows] int32; None: the row's number) -> out (a new contiguous tensor; it may be x).  transpose: the transposed
-    rotation, which takes the gradient of the result to the gradient of x."""
+    rotation, which takes the gradient of the result to the gradient of x.  torch does not record the call: an x or out that wants a
+    gradient is refused while it records (detach it, or turn the gradient with transpose in an autograd function of your own)."""
     fn, dev, shape = "rotate_positions", x.device, x.shape
     code = _STEP_DTYPE.get(x.dtype)
     if code is None or len(shape) not in (3, 4) or dev.type != "cuda" or dev != rotary.device or rotary.rotary_dim > shape[-1]:
+        raise StepError(fn, 1)
+    if (x.requires_grad or (out is not None and out.requires_grad)) and torch.is_grad_enabled():
         raise StepError(fn, 1)
     if stream is not None and stream.device != dev:
         raise StepError(fn, 1)

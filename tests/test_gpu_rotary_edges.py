@@ -59,3 +59,35 @@ def test_subnormal_values_are_stored(dtype, D):
         assert torch.equal(kr[0], k[0, 0, 0, h]) and torch.equal(vr, v[0, :, 0, h])
         assert off(kr[:, None], k[0, :, 0, h:h + 1], np.arange(5), f, D, dtype) <= 1.0
     assert pool.last_error() == (0, 0)
+
+
+def test_a_tensor_that_wants_a_gradient_is_refused_while_torch_records():
+    """The result would be cut off from x without a word; turned in place, x would change behind torch's back."""
+    r = B.Rotary(64)
+    x = torch.randn((3, 2, 64), generator=torch.Generator().manual_seed(7)).cuda()
+    want = B.rotate_positions(x, r)
+    leaf = x.clone().requires_grad_()
+    for a, kw in ((leaf, {}), (leaf * 1.0, {}), (leaf, dict(out=torch.empty_like(x))), (x, dict(out=leaf)), (leaf, dict(out=leaf)),
+                  (leaf, dict(stream=torch.cuda.Stream()))):
+        with pytest.raises(B.StepError) as e:
+            B.rotate_positions(a, r, **kw)
+        assert e.value.code == 1
+    assert torch.equal(leaf, x)
+    assert torch.equal(B.rotate_positions(leaf.detach(), r), want)
+    with torch.no_grad():
+        assert torch.equal(B.rotate_positions(leaf, r), want)
+
+    class Rotate(torch.autograd.Function):                              # as a training loop has it
+        @staticmethod
+        def forward(ctx, a):
+            return B.rotate_positions(a, r)
+
+        @staticmethod
+        def backward(ctx, g):
+            return B.rotate_positions(g.contiguous(), r, transpose=True)
+
+    y = Rotate.apply(leaf)
+    assert torch.equal(y, want)
+    w = torch.randn((3, 2, 64), generator=torch.Generator().manual_seed(8)).cuda()
+    (y * w).sum().backward()
+    assert torch.equal(leaf.grad, B.rotate_positions(w, r, transpose=True))
