@@ -291,7 +291,8 @@ enum { STEP_ROTARY_PLAIN = 0, STEP_ROTARY_LINEAR = 1, STEP_ROTARY_BASE = 2, STEP
  *           first = max(floor(c(fast)), 0), last = min(ceil(c(slow)), D - 1), c(n) = D ln(original_positions / (2 pi n)) / (2 ln base)
  *   BANDS   the same with r = clamp((fast - n_i) / (fast - slow), 0, 1), n_i = original_positions t_i / (2 pi) turns
  * fast > slow > 0 are turns over original_positions (usually 32 and 1 for YARN, 4 and 1 for BANDS).  divisors (HOST, [D / 2], may
- * be NULL): f_i is divided by divisors[i] besides.  output_scale: the scale above; 0 = 1, for YARN 0.1 ln(factor) + 1. */
+ * be NULL): f_i is divided by divisors[i] besides.  output_scale: the scale above; 0 = 1, for YARN 0.1 ln(factor) + 1.  Refused: an f_i of
+ * 2^16 turns a position or more, a scale beyond the range of a float. */
 typedef struct {
   int rotary_dim;                     /* even */
   int interleaved;                    /* 0 or 1 */

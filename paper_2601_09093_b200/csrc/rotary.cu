@@ -494,14 +494,15 @@ int step_rotary_table(const step_rotary_config* cfg, uint64_t* table_out, step_r
     if (cfg->divisors) f /= cfg->divisors[i];
     // turns per position; whole turns do not matter at whole positions
     long double x = f / turn;
+    if (!(x < 0x1p16L)) return STEP_ERR_INVALID_ARG;     // (x is good to 2^-60 of itself: nothing would be left at far positions)
     x = (x - floorl(x)) * 0x1p64L;
-    if (!(x >= 0.0L)) return STEP_ERR_INVALID_ARG;       // (a frequency beyond what a long double resolves)
     uint64_t u = x < 0x1p64L ? (uint64_t)x : 0;
     if (x < 0x1p64L && x - (long double)u >= 0.5L) ++u;
     table_out[i] = u;
   }
   double scale = cfg->output_scale;
   if (scale == 0.0) scale = kind == STEP_ROTARY_YARN && cfg->factor > 1.0 ? 0.1 * log(cfg->factor) + 1.0 : 1.0;
+  if (!isfinite((float)scale)) return STEP_ERR_INVALID_ARG;
   rotary_out->table = nullptr;
   rotary_out->rotary_dim = D;
   rotary_out->interleaved = cfg->interleaved;
