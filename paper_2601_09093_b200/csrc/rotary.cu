@@ -47,7 +47,7 @@ template <> __device__ inline __nv_bfloat16 from_float<__nv_bfloat16>(float x) {
 template <typename T, bool kPairs>
 __device__ inline void turn_unit(uint4& a, uint4& b, const float* c, const float* s) {
   constexpr int kU = 16 / (int)sizeof(T);
-  T x[2 * kU];
+  alignas(16) T x[2 * kU];
   *reinterpret_cast<uint4*>(x) = a;
   *reinterpret_cast<uint4*>(x + kU) = b;
 #pragma unroll
@@ -107,7 +107,7 @@ constexpr int kRotateWarps = kRotateThreads / 32;
 template <typename T, bool kPairs>
 __global__ void __launch_bounds__(kRotateThreads) rotate_rows_kernel(const __grid_constant__ RotateDev a) {
   constexpr int kU = 16 / (int)sizeof(T);
-  __shared__ float2 s_angle[kRotateAngles];
+  __shared__ __align__(16) float2 s_angle[kRotateAngles];               // (read two at a time)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long task = (long long)blockIdx.x * kRotateWarps + warp;
   const long long row = task / a.tasks_per_row;
@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kRotateThreads) rotate_rows_kernel(const __gri
 template <typename T, bool kPairs>
 __global__ void __launch_bounds__(kRotateThreads) rotate_flat_kernel(const __grid_constant__ RotateDev a) {
   constexpr int kU = 16 / (int)sizeof(T);
-  __shared__ float2 s_angle[kRotateAngles];
+  __shared__ __align__(16) float2 s_angle[kRotateAngles];               // (read two at a time)
   const int row0 = blockIdx.x * a.rows_per_cta, n_rows = min(a.rows_per_cta, a.batch * a.rows - row0);
   const int heads = a.heads, half = a.D / 2, units = a.D / (2 * kU);
   for (int x = threadIdx.x; x < n_rows * half; x += kRotateThreads) {
