@@ -413,12 +413,14 @@ int launch_rotate(const RotateDev& a0, int pairs, cudaStream_t s) {
   constexpr int kU = 16 / (int)sizeof(T);
   RotateDev a = a0;
   const long long strides = a.x_batch | a.x_row | a.x_head | a.out_batch | a.out_row | a.out_head;
-  // whole 16-byte chunks wherever the shape allows it
+  const int tail = a.copy_tail ? (a.d - a.D) / kU : 0;
+  // whole 16-byte chunks wherever the shape allows it, and what a CTA or a warp of those kernels counts in 32 bits fits: a head's copied
+  // dims are at most 2^16 chunks (times 512 rows of fewer than 64 heads), a row's heads at most 2^30
   const bool chunks = a.D % (2 * kU) == 0 && a.D / 2 <= kRotateAngles / kRotateWarps && (!a.copy_tail || a.d % kU == 0) && strides % kU == 0 &&
-                      !(((uintptr_t)a.x | (uintptr_t)a.out) & 15);
+                      !(((uintptr_t)a.x | (uintptr_t)a.out) & 15) && tail <= 1 << 16 && a.heads <= 1 << 30;
   const long long rows = (long long)a.batch * a.rows;
   const int half = a.D / 2, units = a.D / (2 * kU);
-  a.by_tail = quotient(a.copy_tail && chunks ? (a.d - a.D) / kU : 1);
+  a.by_tail = quotient(tail && chunks ? tail : 1);
   // (the flat form numbers its rows, and what one CTA goes through, in 31 bits)
   if (chunks && (long long)a.heads * units < 32 * kRotateAhead && rows <= 0x3fffffffll) {
     // kRotateAhead units a thread, unless that leaves SMs without work
@@ -432,10 +434,10 @@ int launch_rotate(const RotateDev& a0, int pairs, cudaStream_t s) {
     if (pairs) rotate_flat_kernel<T, true><<<ctas, kRotateThreads, 0, s>>>(a);
     else rotate_flat_kernel<T, false><<<ctas, kRotateThreads, 0, s>>>(a);
   } else if (chunks) {
-    // a warp takes all heads of a row; where that leaves SMs without work, fewer
+    // a warp takes all heads of a row; where that leaves SMs without work, or is more than 32 bits count, fewer
     const int together = units < 32 ? 32 / units : 1;
     int per = a.heads;
-    while (per > together && rows * ((a.heads + per - 1) / per) < 148ll * 16) per = (per + 1) / 2;
+    while (per > together && (rows * ((a.heads + per - 1) / per) < 148ll * 16 || (long long)per * tail > 1 << 30)) per = (per + 1) / 2;
     per = (per + together - 1) / together * together;
     a.heads_per_task = per;
     a.tasks_per_row = (a.heads + per - 1) / per;

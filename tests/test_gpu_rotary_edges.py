@@ -91,3 +91,17 @@ def test_a_tensor_that_wants_a_gradient_is_refused_while_torch_records():
     w = torch.randn((3, 2, 64), generator=torch.Generator().manual_seed(8)).cuda()
     (y * w).sum().backward()
     assert torch.equal(leaf.grad, B.rotate_positions(w, r, transpose=True))
+
+
+@pytest.mark.parametrize("heads,d,D", [(63, 273_000_016, 16), (4, 1 << 20, 64), (64, 600_000, 32)])
+def test_dims_that_are_copied_by_the_billion(heads, d, D):
+    """63 heads of 34 million chunks of 16 bytes: more of them in one row than 31 bits count.  (One head of x serves as all.)"""
+    r = B.Rotary(D)
+    x = torch.empty((1, 1, 1, d), dtype=torch.bfloat16, device="cuda")
+    x.view(torch.int16).copy_((torch.arange(d, dtype=torch.int32, device="cuda") * 40503 >> 3).to(torch.int16) & 0x3fff)
+    out = torch.zeros((1, 1, heads, d), dtype=torch.bfloat16, device="cuda")
+    p = torch.full((1,), 77, dtype=torch.int32, device="cuda")
+    assert B.rotate_positions(x.expand(1, 1, heads, d), r, p, out=out) is out
+    turned = B.rotate_positions(x[..., :D].contiguous(), r, p)
+    for h in range(heads):
+        assert torch.equal(out[0, 0, h, D:], x[0, 0, 0, D:]) and torch.equal(out[0, 0, h, :D], turned[0, 0, 0]), h
