@@ -323,8 +323,8 @@ typedef struct {
   int transpose;                      /* 1: the transposed rotation (angles negated), which turns dL/dy into dL/dx */
 } rotate_args;
 
-/* Rotates queries or keys.  out may be x with the same strides (in place); otherwise they must not overlap, and no two
- * elements of out may share a place.  The members of `a` are read during the call.  Device pointers; the current device's. */
+/* Rotates queries or keys.  out may be x with the same strides (in place; other strides are refused); otherwise they must not
+ * overlap, and no two elements of out may share a place (strides of 0 are refused).  The members of `a` are read during the call.  Device pointers; the current device's. */
 int rotate_positions(const rotate_args* a, const step_rotary* rotary, void* stream);
 
 /* Makes room for n_tokens new positions of each of the n listed traces, as append_kv does (order, what is skipped and
@@ -351,7 +351,8 @@ typedef struct {
  * rows 16-byte aligned.  Positions have to exist (kv_pool_extend): an entry that reaches beyond its trace's length is
  * skipped whole (STEP_ERR_INVALID_ARG in the status word), as is one whose trace is not live (STEP_ERR_BAD_TRACE); q_out rows
  * of entries that are skipped or passed over are left as they are.  No two entries of a call may name the same position.
- * A page that several traces share is written for all of them.  q_out may be q with the same strides, and overlaps nothing else.
+ * A page that several traces share is written for all of them.  q_out may be q with the same strides (others are refused), and
+ * overlaps nothing else.
  * Wants the pool's device to be current. */
 int store_kv_rotated(step_pool* pool, const kv_store_args* a, const step_rotary* rotary, void* stream);
 

@@ -756,7 +756,7 @@ int kv_pool_extend(step_pool* pool, const int32_t* trace_ids, int n, int n_token
   if (!pool || n < 0 || n_tokens < 0) return STEP_ERR_INVALID_ARG;
   if (n == 0) return STEP_OK;
   // ids must be distinct; the list is served by one CTA from shared memory (12 bytes per entry)
-  if (!trace_ids || !start_out || n > pool->cfg.max_traces || n > kMaxTracesFast) return STEP_ERR_INVALID_ARG;
+  if (!trace_ids || !start_out || start_out == trace_ids || n > pool->cfg.max_traces || n > kMaxTracesFast) return STEP_ERR_INVALID_ARG;
   const int st = on_pool_device(pool);
   if (st != STEP_OK) return st;
   DevViews v = pool->v;

@@ -530,6 +530,9 @@ int rotate_positions(const rotate_args* a, const step_rotary* rotary, void* stre
   if (r.batch == 1) r.x_batch = r.out_batch = 0;         // (a stride that is not used may be anything)
   if (r.rows == 1) r.x_row = r.out_row = 0;
   if (r.heads == 1) r.x_head = r.out_head = 0;
+  // results that would share a place, or lie over x in another order, depend on which thread comes first
+  if ((r.batch > 1 && r.out_batch == 0) || (r.rows > 1 && r.out_row == 0) || (r.heads > 1 && r.out_head == 0)) return STEP_ERR_INVALID_ARG;
+  if (r.x == r.out && (r.x_batch != r.out_batch || r.x_row != r.out_row || r.x_head != r.out_head)) return STEP_ERR_INVALID_ARG;
   r.scale = rotary->scale; r.sign = a->transpose ? -1.f : 1.f;
   r.copy_tail = a->x != a->out && r.D < r.d;
   return a->dtype == STEP_BF16 ? launch_rotate<__nv_bfloat16>(r, rotary->interleaved, (cudaStream_t)stream)
@@ -550,6 +553,8 @@ int store_kv_rotated(step_pool* pool, const kv_store_args* a, const step_rotary*
   const long long q_row = rows > 1 ? a->q_row : 0, q_out_row = rows > 1 ? a->q_out_row : 0;
   const long long q_layer = a->n_layers > 1 ? a->q_layer : 0, q_out_layer = a->n_layers > 1 ? a->q_out_layer : 0;
   if (((uintptr_t)a->k | (uintptr_t)a->v | (uintptr_t)a->q | (uintptr_t)a->q_out) & 15) return STEP_ERR_INVALID_ARG;
+  if (a->q && ((rows > 1 && q_out_row == 0) || (a->n_layers > 1 && q_out_layer == 0))) return STEP_ERR_INVALID_ARG;   // (as above)
+  if (a->q && a->q == a->q_out && (q_row != q_out_row || q_layer != q_out_layer)) return STEP_ERR_INVALID_ARG;
   if ((k_row | v_row) % cpe != 0 || (a->q && (q_row | q_layer | q_out_row | q_out_layer) % cpe != 0)) return STEP_ERR_INVALID_ARG;
   const int st = on_pool_device(pool);
   if (st != STEP_OK) return st;

@@ -105,3 +105,36 @@ def test_dims_that_are_copied_by_the_billion(heads, d, D):
     turned = B.rotate_positions(x[..., :D].contiguous(), r, p)
     for h in range(heads):
         assert torch.equal(out[0, 0, h, D:], x[0, 0, 0, D:]) and torch.equal(out[0, 0, h, :D], turned[0, 0, 0]), h
+
+
+def test_results_that_share_a_place_are_refused():
+    r = B.Rotary(64)
+    x = torch.randn((2, 3, 4, 64), generator=torch.Generator().manual_seed(9)).cuda()
+    keep = x.clone()
+    flat = x.view(-1)
+    for a, out in ((x, torch.zeros((2, 3, 1, 64), device="cuda").expand_as(x)), (x, torch.zeros((3, 4, 64), device="cuda").expand_as(x)),
+                   (x, flat.as_strided((2, 3, 4, 64), (768, 64, 192, 1))), (x[:1].expand_as(x), x[:1].expand_as(x))):
+        with pytest.raises(B.StepError) as e:
+            B.rotate_positions(a, r, out=out)
+        assert e.value.code == 1
+    assert torch.equal(x, keep)
+    # dims of one: a stride that is not used may be anything
+    assert torch.equal(B.rotate_positions(x[:1, :1], r, out=x[:1, :1].clone().as_strided((1, 1, 4, 64), (0, 0, 64, 1))), x[:1, :1])
+
+    pool = B.KVPool(2, 4, 2, 64, 16, num_blocks=4, max_traces=2, max_pages_per_trace=1, dtype=B.STEP_FP32)
+    pool.fork_prefix(2, 0, None, None)
+    ids = torch.arange(2, dtype=torch.int32, device="cuda")
+    with pytest.raises(B.StepError):
+        pool.extend(ids, 3, start_out=ids)
+    start = pool.extend(ids, 3)
+    k = torch.randn((2, 3, 2, 2, 64), generator=torch.Generator().manual_seed(10)).cuda()
+    q = torch.randn((2, 2, 3, 4, 64), generator=torch.Generator().manual_seed(11)).cuda()
+    before = q.clone()
+    for out in (torch.zeros((1, 2, 3, 4, 64), device="cuda").expand_as(q), torch.zeros((2, 1, 1, 4, 64), device="cuda").expand_as(q),
+                q.view(-1).as_strided(q.shape, (256, 3 * 512, 512, 64, 1))):
+        with pytest.raises(B.StepError) as e:
+            pool.store_kv_rotated(0, ids, start, k, k, r, q=q, q_out=out)
+        assert e.value.code == 1
+    assert torch.equal(q, before) and ids.tolist() == [0, 1]
+    pool.store_kv_rotated(0, ids, start, k, k, r, q=q, q_out=q)
+    assert pool.last_error() == (0, 0)

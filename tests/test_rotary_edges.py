@@ -1,6 +1,9 @@
 """Rotary positions without a GPU: frequencies and scales at the ends of their ranges."""
+import ctypes as C
+
 import numpy as np
 import pytest
+import torch
 
 from oracle import rotary as OR
 from paper_2601_09093_b200 import binding as B
@@ -30,3 +33,14 @@ def test_fast_frequencies_are_as_good_as_said():
 
 def test_the_largest_scale_that_is_a_float():
     assert B.Rotary(4, output_scale=3e38, device="cpu").struct.scale == np.float32(3e38)
+
+
+def test_results_that_share_a_place_are_refused():
+    """Before the device is looked at: rows, heads or batch entries of out in one place, x turned in place by other strides."""
+    r = B.Rotary(8, device="cpu")
+    some, other = torch.zeros(4096), torch.zeros(4096)
+    base = dict(x=some.data_ptr(), out=other.data_ptr(), dtype=1, batch=2, rows=3, heads=4, head_dim=8,
+                x_batch=96, x_row=32, x_head=8, out_batch=96, out_row=32, out_head=8)
+    for change in (dict(out_batch=0), dict(out_row=0), dict(out_head=0),
+                   dict(out=some.data_ptr(), out_batch=128), dict(out=some.data_ptr(), out_row=40), dict(x=other.data_ptr(), x_head=0)):
+        assert B.lib().rotate_positions(C.byref(B.rotate_args(**{**base, **change})), C.byref(r.struct), None) == 1, change
