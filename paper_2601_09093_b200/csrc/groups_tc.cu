@@ -1102,13 +1102,11 @@ size_t groups_tc_workspace(const step_pool* pool, int n, int n_groups) { return 
 
 int groups_tc_launch(step_pool* pool, int layer, const void* q, const int32_t* block_table, const int32_t* seq_lens, int n,
                      const int32_t* group_rows, const int32_t* group_pages, int n_groups, void* out, void* workspace, cudaStream_t s) {
-  EncodeTiledFn enc = encode_tiled_fn();
-  if (!enc) return STEP_ERR_CUDA;
   const Geo g = geo_of(pool);
   if (!pool->groups_ready) {
     CUtensorMap fresh;
     static_assert(sizeof(fresh) <= sizeof(pool->tmap_kv_bytes), "tensor map");
-    if (!encode_pool_map(enc, pool, &fresh)) return STEP_ERR_CUDA;
+    if (!encode_pool_map(pool, &fresh)) return STEP_ERR_CUDA;
     memcpy(pool->tmap_kv_bytes, &fresh, sizeof(fresh));                // (the same for every kernel that uses it)
     // (warps that ask for more registers than the launch has would wait for good)
     cudaFuncAttributes fa;
@@ -1133,8 +1131,9 @@ int groups_tc_launch(step_pool* pool, int layer, const void* q, const int32_t* b
   const cuuint64_t q_dims[3] = {kD, (cuuint64_t)g.Hq, (cuuint64_t)n};
   const cuuint64_t q_strides[2] = {kD * 2, (cuuint64_t)g.Hq * kD * 2};
   const cuuint32_t q_box[3] = {64, (cuuint32_t)g.G, (cuuint32_t)a.box}, estr[3] = {1, 1, 1};
-  if (enc(&map_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), q_dims, q_strides, q_box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+  if (!encode_tiled(&map_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), q_dims, q_strides, q_box, estr,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE))
     return STEP_ERR_CUDA;
   groups_kernel<<<a.ctas, kThreads, kSmem, s>>>(map, map_q, a);
   if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;

@@ -322,16 +322,14 @@ bool score_tc_supported(const scorer_weights* w, const void* hidden) {
 int score_tc_launch(step_pool* pool, const void* hidden, int Mc, const scorer_weights* w, cudaStream_t s) {
   static_assert(sizeof(CUtensorMap) <= sizeof(pool->tmap_bytes), "tensor map cache too small");
   if (pool->tmap_w1 != w->W1 || pool->tmap_D != w->D || pool->tmap_m != w->m) {
-    EncodeTiledFn enc = encode_tiled_fn();
-    if (!enc) return STEP_ERR_CUDA;
     CUtensorMap fresh;
     const cuuint64_t dims[2] = {(cuuint64_t)w->D, (cuuint64_t)w->m};       // innermost first
     const cuuint64_t strides[1] = {(cuuint64_t)w->D * 2};
     const cuuint32_t box[2] = {(cuuint32_t)kBK, (cuuint32_t)kBoxRows};
     const cuuint32_t estr[2] = {1, 1};
-    if (enc(&fresh, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(w->W1), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    if (!encode_tiled(&fresh, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(w->W1), dims, strides, box, estr,
+                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE))
       return STEP_ERR_CUDA;
     memcpy(pool->tmap_bytes, &fresh, sizeof(fresh));
     pool->tmap_w1 = w->W1; pool->tmap_D = w->D; pool->tmap_m = w->m;
@@ -340,16 +338,14 @@ int score_tc_launch(step_pool* pool, const void* hidden, int Mc, const scorer_we
   memcpy(&map, pool->tmap_bytes, sizeof(map));
   // the candidate rows as a [Mc, D] array of 128-row tiles, for launches in which every row ends a step
   if (pool->tmap_h_ptr != hidden || pool->tmap_h_D != w->D || pool->tmap_h_M != Mc) {
-    EncodeTiledFn enc = encode_tiled_fn();
-    if (!enc) return STEP_ERR_CUDA;
     CUtensorMap fresh;
     const cuuint64_t dims[2] = {(cuuint64_t)w->D, (cuuint64_t)Mc};
     const cuuint64_t strides[1] = {(cuuint64_t)w->D * 2};
     const cuuint32_t box[2] = {(cuuint32_t)kBK, (cuuint32_t)kHalfRows};
     const cuuint32_t estr[2] = {1, 1};
-    if (enc(&fresh, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(hidden), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    if (!encode_tiled(&fresh, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(hidden), dims, strides, box, estr,
+                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE))
       return STEP_ERR_CUDA;
     memcpy(pool->tmap_h_bytes, &fresh, sizeof(fresh));
     pool->tmap_h_ptr = hidden; pool->tmap_h_D = w->D; pool->tmap_h_M = Mc;

@@ -85,5 +85,15 @@ inline EncodeTiledFn encode_tiled_fn() {
   }
   return fn;
 }
+// A tensor map by that function.  It wants a current context, which a host thread that has made no runtime call of the kind that
+// needs one does not have yet: it then gets the current device's and asks again.
+template <typename... A>
+inline bool encode_tiled(A... a) {
+  const EncodeTiledFn enc = encode_tiled_fn();
+  if (!enc) return false;
+  if (enc(a...) == CUDA_SUCCESS) return true;
+  int dev = 0;
+  return cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess && enc(a...) == CUDA_SUCCESS;
+}
 
 }  // namespace stepk

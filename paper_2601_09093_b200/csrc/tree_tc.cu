@@ -864,13 +864,11 @@ int tree_tc_launch(step_pool* pool, int layer, const void* q, const void* k_draf
                    const int32_t* n_nodes, int T, const int32_t* block_table, const int32_t* seq_lens, int n, void* out,
                    void* workspace, cudaStream_t s) {
   const Geo g = geo_of(pool);
-  EncodeTiledFn enc = encode_tiled_fn();
-  if (!enc) return STEP_ERR_CUDA;
   const cuuint32_t estr[4] = {1, 1, 1, 1};
   if (!pool->tree_ready) {
     CUtensorMap fresh;
     static_assert(sizeof(fresh) <= sizeof(pool->tmap_kv_bytes), "tensor map");
-    if (!encode_pool_map(enc, pool, &fresh)) return STEP_ERR_CUDA;
+    if (!encode_pool_map(pool, &fresh)) return STEP_ERR_CUDA;
     memcpy(pool->tmap_kv_bytes, &fresh, sizeof(fresh));
     if (cudaFuncSetAttribute(tree_tc_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(true)) != cudaSuccess ||
         cudaFuncSetAttribute(tree_tc_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(false)) != cudaSuccess)
@@ -901,8 +899,9 @@ int tree_tc_launch(step_pool* pool, int layer, const void* q, const void* k_draf
   const cuuint64_t q_dims[3] = {kD, (cuuint64_t)g.Hq, (cuuint64_t)n * T};
   const cuuint64_t q_strides[2] = {kD * 2, (cuuint64_t)g.Hq * kD * 2};
   const cuuint32_t q_box[3] = {64, (cuuint32_t)g.G, (cuuint32_t)(a.tokens < T ? a.tokens : T)};
-  if (enc(&map_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), q_dims, q_strides, q_box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+  if (!encode_tiled(&map_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), q_dims, q_strides, q_box, estr,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE))
     return STEP_ERR_CUDA;
   kern<<<a.shares, kThreads, smem, s>>>(map, map_q, a);
   if (launch_ok() != STEP_OK) return STEP_ERR_CUDA;
