@@ -372,7 +372,7 @@ int store_kv_rotated(step_pool* pool, const kv_store_args* a, const step_rotary*
  * elsewhere it stays fp32, and shared pages are read once for 16 / G traces.
  * Wants the pool's device to be current and a workspace of decode_attention_groups_workspace_bytes (host-only) bytes, 256-byte
  * aligned, in use from the call until its work on the stream is done; can be captured into a CUDA graph.  It keeps nothing in the
- * pool's metadata: calls that only read one pool may overlap if each has a workspace of its own. */
+ * pool's metadata: calls that only read one pool may overlap, from several host threads too, if each has a workspace of its own. */
 int decode_attention_groups_workspace_bytes(const step_pool* pool, int n, int n_groups, size_t* bytes);
 int decode_attention_groups(step_pool* pool, int layer, const void* q, const int32_t* block_table, const int32_t* seq_lens,
                             int n, const int32_t* group_rows, const int32_t* group_pages, int n_groups, void* out,

@@ -122,10 +122,13 @@ __device__ inline uint32_t pack2(float lo, float hi) {
 }
 
 // Shapes these kernels are written for, pools that one tensor map can describe.
-inline bool attention_tc_covers(const step_pool* pool, int n) {
+inline bool attention_tc_fits(const step_pool* pool) {
   const kv_pool_config& c = pool->cfg;
-  return c.dtype == STEP_BF16 && c.head_dim == kD && c.page_size == kP && pool->swizzle && n <= kMaxTracesFast && pool->fast_path > 0 &&
+  return c.dtype == STEP_BF16 && c.head_dim == kD && c.page_size == kP && pool->swizzle &&
          (long long)c.num_layers * c.num_blocks * c.num_kv_heads * 2 * kP < (1ll << 31) && encode_tiled_fn() != nullptr;
+}
+inline bool attention_tc_covers(const step_pool* pool, int n) {
+  return n <= kMaxTracesFast && pool->fast_path > 0 && attention_tc_fits(pool);
 }
 // The pool as groups of 8 rows of 128 dims, seen as [group][half of the dims][row][64 dims]; a box is the two groups of a
 // page's K or V.

@@ -1098,16 +1098,21 @@ bool groups_tc_supported(const step_pool* pool, int n) {
   return attention_tc_covers(pool, n) && pool->num_sms >= 2 && (long long)n * pool->cfg.num_kv_heads * ((long long)pool->cfg.max_pages_per_trace + 3) < (1ll << 31);
 }
 
+void make_pool_map(step_pool* pool) {
+  CUtensorMap map;
+  static_assert(sizeof(map) <= sizeof(pool->tmap_kv_bytes), "tensor map");
+  if (!attention_tc_fits(pool) || !encode_pool_map(pool, &map)) return;
+  memcpy(pool->tmap_kv_bytes, &map, sizeof(map));
+  pool->tmap_kv_set = true;
+}
+
 size_t groups_tc_workspace(const step_pool* pool, int n, int n_groups) { return lay_out(pool, n, n_groups, nullptr, nullptr); }
 
 int groups_tc_launch(step_pool* pool, int layer, const void* q, const int32_t* block_table, const int32_t* seq_lens, int n,
                      const int32_t* group_rows, const int32_t* group_pages, int n_groups, void* out, void* workspace, cudaStream_t s) {
   const Geo g = geo_of(pool);
-  if (!pool->groups_ready) {
-    CUtensorMap fresh;
-    static_assert(sizeof(fresh) <= sizeof(pool->tmap_kv_bytes), "tensor map");
-    if (!encode_pool_map(pool, &fresh)) return STEP_ERR_CUDA;
-    memcpy(pool->tmap_kv_bytes, &fresh, sizeof(fresh));                // (the same for every kernel that uses it)
+  if (!pool->tmap_kv_set) return STEP_ERR_CUDA;
+  if (!pool->groups_ready) {                                           // (threads that come here at once do the same)
     // (warps that ask for more registers than the launch has would wait for good)
     cudaFuncAttributes fa;
     if (cudaFuncSetAttribute(groups_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess ||

@@ -15,6 +15,8 @@
 #include <stdint.h>
 #include <stddef.h>
 
+#include <atomic>
+
 #include "../../include/step.h"
 
 namespace stepk {
@@ -88,9 +90,11 @@ struct step_pool {
   alignas(64) unsigned char tmap_h_bytes[128];
   const void* tmap_h_ptr; int tmap_h_D, tmap_h_M;
   bool tc_smem_set;   // the scorer kernel's dynamic shared memory limit has been raised on this pool's device
-  // the tensor map of the whole pool (tree and group attention), and whether their kernels' shared memory limits have been raised
+  // the tensor map of the whole pool (tree and group attention), made with the pool and only read from then on, if it has one; and
+  // whether their kernels' shared memory limits have been raised.  (Calls that only read a pool may come from several host threads.)
   alignas(64) unsigned char tmap_kv_bytes[128];
-  bool tree_ready, groups_ready;
+  bool tmap_kv_set;
+  std::atomic<bool> tree_ready, groups_ready;
   int device;
   stepk::MetaLayout lay;
   stepk::DevViews v;
@@ -206,6 +210,7 @@ int tree_tc_launch(step_pool* pool, int layer, const void* q, const void* k_draf
                    void* workspace, cudaStream_t s);
 
 // ---- tensor-core attention of groups of traces (groups_tc.cu)
+void make_pool_map(step_pool* pool);       // tmap_kv_bytes, for pools that the tensor-core kernels cover
 bool groups_tc_supported(const step_pool* pool, int n);
 size_t groups_tc_workspace(const step_pool* pool, int n, int n_groups);
 int groups_tc_launch(step_pool* pool, int layer, const void* q, const int32_t* block_table, const int32_t* seq_lens, int n,

@@ -865,11 +865,8 @@ int tree_tc_launch(step_pool* pool, int layer, const void* q, const void* k_draf
                    void* workspace, cudaStream_t s) {
   const Geo g = geo_of(pool);
   const cuuint32_t estr[4] = {1, 1, 1, 1};
+  if (!pool->tmap_kv_set) return STEP_ERR_CUDA;
   if (!pool->tree_ready) {
-    CUtensorMap fresh;
-    static_assert(sizeof(fresh) <= sizeof(pool->tmap_kv_bytes), "tensor map");
-    if (!encode_pool_map(pool, &fresh)) return STEP_ERR_CUDA;
-    memcpy(pool->tmap_kv_bytes, &fresh, sizeof(fresh));
     if (cudaFuncSetAttribute(tree_tc_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(true)) != cudaSuccess ||
         cudaFuncSetAttribute(tree_tc_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(false)) != cudaSuccess)
       return STEP_ERR_CUDA;

@@ -1,6 +1,7 @@
 """decode_attention_groups to the last bits of its output: against torch in 64 bits, element by element."""
 import math
 import os
+import threading
 
 import numpy as np
 import pytest
@@ -162,6 +163,46 @@ def test_the_bound_would_show_a_page_that_is_left_out():
     for first in (0, 2560, 5472, 5600):
         with pytest.raises(AssertionError):
             f.check(got, q, without=slice(first, first + 16))
+
+
+def test_first_calls_of_several_host_threads_at_once():
+    """Threads that meet in a new pool's first call, each with a stream, a workspace and an output of its own; every other one attends with
+    a tree of one drafted token first, whose kernel reads the pool through the same description."""
+    rng = np.random.default_rng(2)
+    make = normal(2)
+    n_threads, wrong = 8, []
+    for turn in range(12):
+        f = Forks((8, 2, 128), "bf16", 16, [(200, [5, 40]), (33, [3])], make, rng)
+        q = make(f.n, 8, 128).bfloat16()
+        kd = make(f.n, 1, 1, 2, 128).bfloat16()
+        parents = torch.full((f.n, 1), -1, dtype=torch.int32, device="cuda")
+        pages, spaces = dev([12, 2]), [torch.empty(96 << 20, dtype=torch.uint8, device="cuda") for _ in range(n_threads)]
+        outs = [torch.zeros_like(q) for _ in range(n_threads)]
+        streams = [torch.cuda.Stream() for _ in range(n_threads)]
+        meet = threading.Barrier(n_threads)
+        torch.cuda.synchronize()
+
+        def work(i):
+            try:
+                table, lens = f.views["block_table"], f.views["seq_lens"]
+                meet.wait(20)
+                if i % 2:
+                    f.pool.decode_attention_tree(0, q[:, None], kd, kd, parents, table, lens, workspace=spaces[i], stream=streams[i])
+                f.pool.decode_attention_groups(0, q, table, lens, f.rows, pages, out=outs[i], workspace=spaces[i], stream=streams[i])
+            except Exception as e:                                     # noqa: BLE001 (told by the test's own thread)
+                wrong.append(e)
+
+        threads = [threading.Thread(target=work, args=(i,)) for i in range(n_threads)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        torch.cuda.synchronize()
+        assert not wrong, wrong
+        want = f.attend(q, [12, 2])
+        f.check(want, q)
+        assert all(torch.equal(o, want) for o in outs), turn
+        assert f.pool.last_error() == (0, 0)
 
 
 FUZZ = int(os.environ.get("STEP_FUZZ_SEEDS", "40"))
