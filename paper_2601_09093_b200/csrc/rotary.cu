@@ -18,6 +18,8 @@
 
 #include <math.h>
 
+#include <atomic>
+
 using namespace stepk;
 
 namespace {
@@ -408,10 +410,24 @@ StoreForm store_form(bool pairs, bool chunks) {
   return pairs ? store_kernel<T, true, false> : store_kernel<T, false, false>;
 }
 
+// Multiprocessors of the current device, asked for once per device; 0: not to be told.
+int sms_here() {
+  constexpr int kDevices = 64;
+  static std::atomic<int> known[kDevices];
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  if (dev < kDevices && (n = known[dev]) > 0) return n;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+  if (dev < kDevices) known[dev] = n;
+  return n;
+}
+
 template <typename T>
 int launch_rotate(const RotateDev& a0, int pairs, cudaStream_t s) {
   constexpr int kU = 16 / (int)sizeof(T);
   RotateDev a = a0;
+  const int sms = sms_here();
+  if (sms == 0) return STEP_ERR_CUDA;
   const long long strides = a.x_batch | a.x_row | a.x_head | a.out_batch | a.out_row | a.out_head;
   const int tail = a.copy_tail ? (a.d - a.D) / kU : 0;
   // whole 16-byte chunks wherever the shape allows it, and what a CTA or a warp of those kernels counts in 32 bits fits: a head's copied
@@ -427,7 +443,7 @@ int launch_rotate(const RotateDev& a0, int pairs, cudaStream_t s) {
     const int most = kRotateAngles / half, row_units = a.heads * units;
     long long per = (kRotateAhead * kRotateThreads + row_units - 1) / row_units;
     if (per > most) per = most;
-    if (per > rows / (2 * 148)) per = rows / (2 * 148);
+    if (per > rows / (2 * sms)) per = rows / (2 * sms);
     a.rows_per_cta = per < 1 ? 1 : (int)per;
     a.by_rows = quotient(a.rows); a.by_half = quotient(half); a.by_units = quotient(units); a.by_heads = quotient(a.heads);
     const unsigned ctas = (unsigned)((rows + a.rows_per_cta - 1) / a.rows_per_cta);
@@ -437,7 +453,7 @@ int launch_rotate(const RotateDev& a0, int pairs, cudaStream_t s) {
     // a warp takes all heads of a row; where that leaves SMs without work, or is more than 32 bits count, fewer
     const int together = units < 32 ? 32 / units : 1;
     int per = a.heads;
-    while (per > together && (rows * ((a.heads + per - 1) / per) < 148ll * 16 || (long long)per * tail > 1 << 30)) per = (per + 1) / 2;
+    while (per > together && (rows * ((a.heads + per - 1) / per) < 16ll * sms || (long long)per * tail > 1 << 30)) per = (per + 1) / 2;
     per = (per + together - 1) / together * together;
     a.heads_per_task = per;
     a.tasks_per_row = (a.heads + per - 1) / per;
@@ -447,7 +463,7 @@ int launch_rotate(const RotateDev& a0, int pairs, cudaStream_t s) {
     else rotate_rows_kernel<T, false><<<(unsigned)ctas, kRotateThreads, 0, s>>>(a);
   } else {
     const long long items = rows * a.heads * (a.D / 2 + (a.copy_tail ? a.d - a.D : 0));
-    const long long ctas = (items + 255) / 256 < 148 * 16 ? (items + 255) / 256 : 148 * 16;
+    const long long ctas = (items + 255) / 256 < 16 * sms ? (items + 255) / 256 : 16 * sms;
     if (pairs) rotate_any_kernel<T, true><<<(unsigned)ctas, 256, 0, s>>>(a);
     else rotate_any_kernel<T, false><<<(unsigned)ctas, 256, 0, s>>>(a);
   }
