@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(kRowsThreads) rows_merge_kernel(RowsArgs a, in
   }
 }
 
-// a.splits and a.part are set here; `part` has attn_rows_workspace bytes.
+// a.splits and a.part are set here; `part` has attn_rows_workspace bytes (kGroups: attn_groups_workspace).
 template <typename T, typename OutT, bool kTree, bool kScores, bool kGroups = false>
 int launch_attn_rows(const step_pool* pool, RowsArgs a, int n, float* part, cudaStream_t s) {
   a.splits = kGroups ? attn_groups_splits(pool, n) : attn_rows_splits(pool, n, a.T);

@@ -54,9 +54,9 @@ constexpr int kTableGroups = 48;                  // groups whose table fits bes
 constexpr int kWideNs = 2600, kNarrowNs = 2000, kPageNs = 1050, kPrefixNs = 9000, kOwnNs = 5000;
 constexpr int kOwnSetup = 2;                      // pages' worth of time that a sequence of own pages takes besides them
 
-// Tiles in the prefix stream, own pages (of all KV heads; setups counted in both), groups of a valid description (else 0), CTAs that
-// take shared pages (the others take own pages).
-struct Header { int units, pages, groups, n_prefix; };
+// Tiles in the prefix stream, own pages (of all KV heads; setups counted in both), CTAs that take shared pages (the others take own
+// pages).
+struct Header { int units, pages, n_prefix; };
 
 // What a row's result is combined from.
 struct RowPlan {                     // (positions in both streams fit 32 bits: groups_tc_supported)
@@ -529,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, 1) groups_kernel(const __grid_consta
   }
   __syncthreads();
   Header hd;
-  hd.units = s_header.units; hd.pages = rw.at[a.n] * a.Hkv; hd.groups = tab.n;
+  hd.units = s_header.units; hd.pages = rw.at[a.n] * a.Hkv;
   hd.n_prefix = choose_prefix(a, hd.units, s_unit_ns, hd.pages, lane);
   const int n_prefix = hd.n_prefix;
   if (first) {
