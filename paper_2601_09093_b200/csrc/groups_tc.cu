@@ -20,9 +20,10 @@
 //   at most 128 rows, even and odd tiles of the same rows.  The tiles of all (group, KV head, row block) sequences form one
 //   stream, cut into one equal share per CTA.
 //
-// 64 traces of a prompt of 32,768 with own texts of up to 1,024, 32 / 8 heads: 72 us, 270 MB (41 us at the measured copy rate) and
-// 35 GFLOP; as two kernels in a row 104 (with one bf16 number for a probability, as one kernel 69.5).  8 prompts of 1,000 to 16,000 with
-// 12 traces each and own texts of up to 3,000, 64 / 8 heads: 131 us, 0.84 of the measured copy.
+// 64 traces of a prompt of 32,768 with own texts of up to 1,024, 32 / 8 heads: 73.5 us, 270 MB (41 us at the measured copy rate) and
+// 35 GFLOP; 81 to 84 after half a second of nothing else, at the card's power limit.  (With one bf16 number for a probability 70 and 73;
+// as two kernels in a row 104.)  8 prompts of 1,000 to 16,000 with 12 traces each and own texts of up to 3,000, 64 / 8 heads: 131 to
+// 142 us, 0.78 to 0.84 of the measured copy.
 //
 // The partition is a function of lengths and groups alone and pieces are combined in stream order, so a call gives the same
 // bits every time.  Every wait for a barrier is bounded (kv_pool_set_wait_limit_ns); a CTA whose wait runs out raises
@@ -49,9 +50,10 @@ constexpr int kStreamWarps = 8, kStages = 3, kPageBytes = 2 * kP * kD * 2;
 constexpr int kTableGroups = 48;                  // groups whose table fits beside the rings; a longer one lies in the workspace
 // What a CTA takes, in nanoseconds (measured, 32 / 8 and 64 / 8 heads): a tile of shared pages with more than 128 rows (its products
 // and exponentials) and with fewer (1.0 alone, the latency of its copies when all SMs read); a page of a warp's own; what comes
-// before and behind them.  (Tiles at 2150 and 1600: 64 traces of 32,768 take 75 us instead of 72, a layer of 2 x 32 traces of 8192 in a
-// decode step 84 instead of 79, 8 x 12 traces 128 instead of 131.)
-constexpr int kWideNs = 2600, kNarrowNs = 2000, kPageNs = 1050, kPrefixNs = 9000, kOwnNs = 5000;
+// before and behind them.  (A tile of both lanes alone takes 2.4 to 2.6 us, 2.8 at the card's power limit.  64 traces of 32,768 in turn with
+// others: 76.7 us at 2150, 74.8 at 2600, 73.4 at 2800; a decode step of 2 x 32 traces of 8192, four layers: 349 at 1600, 337 at 1800, 331
+// at 2000; 8 x 12 traces 133.5, 135 and 137.7.)
+constexpr int kWideNs = 2800, kNarrowNs = 2000, kPageNs = 1050, kPrefixNs = 9000, kOwnNs = 5000;
 constexpr int kOwnSetup = 2;                      // pages' worth of time that a sequence of own pages takes besides them
 
 // Tiles in the prefix stream, own pages (of all KV heads; setups counted in both), CTAs that take shared pages (the others take own
@@ -92,8 +94,8 @@ struct GroupArgs {
 // lo = p kScale - hi, rounded to nearest; sums of probabilities are multiplied by kScale in the end.  lo is at most (2^-7 + 2^-10) p, so
 // that hi + lo is off by at most 2^-8 of that, 3.5e-5 of p, where the output's own rounding is up to 3.9e-3; one rounded bf16 number
 // made the output's error 2.3e-3 instead of 1.7e-3 in the 2-norm.  kScale makes lo positive (where p is above 2^-116): an infinity
-// in V keeps its sign in both products and their sum.  64 traces of a prompt of 32,768: 68.5 us with one number, 74.5 with two; with hi
-// rounded to nearest 75.6, with packed arithmetic (fma.f32x2, whose operands have to be moved together) 79.5.
+// in V keeps its sign in both products and their sum.  64 traces of a prompt of 32,768, SMs shared out as for one number: 68.5 us with one
+// number, 74.5 with two; with hi rounded to nearest 75.6, with packed arithmetic (fma.f32x2, whose operands have to be moved together) 79.5.
 constexpr float kScale = 1.f + 0x1p-10f;
 __device__ inline void split2(float p0, float p1, uint32_t& hi, uint32_t& lo) {
   hi = __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
