@@ -279,8 +279,9 @@ int kv_pool_evict_positions(step_pool* pool, const int32_t* trace_ids, int n, co
  *
  * Pair i of the first D = rotary_dim dims of a head - dims i and i + D/2, or 2i and 2i + 1 if interleaved - at position p:
  *   (y1, y2) = scale * ( x1 cos a - x2 sin a,  x2 cos a + x1 sin a ),   a = p * f_i
- * Dims behind D are left as they are.  The frequencies f_i enter as a table of turns per position in units of 2^-64, so that
- * the angle of any int32 position is exact to 1e-9 of a turn; the arithmetic is fp32 with one rounding of the result, subnormal numbers included. */
+ * Dims behind D are left as they are.  The frequencies f_i enter as a table of turns per position in units of 2^-64: the angle is
+ * good to |p| * 2^-63 of a turn (2.4e-10 at any int32 position; for f_i above 1 in proportion more) until it is rounded to fp32, by at
+ * most 2^-28 of a turn (3.7e-9).  The arithmetic is fp32 with one rounding of the result, subnormal numbers included. */
 enum { STEP_ROTARY_PLAIN = 0, STEP_ROTARY_LINEAR = 1, STEP_ROTARY_BASE = 2, STEP_ROTARY_YARN = 3, STEP_ROTARY_BANDS = 4 };
 
 /* t_i = base^(-2i / D); how far f_i is stretched for contexts `factor` times longer than original_positions:
@@ -324,7 +325,8 @@ typedef struct {
 } rotate_args;
 
 /* Rotates queries or keys.  out may be x with the same strides (in place; other strides are refused); otherwise they must not
- * overlap, and no two elements of out may share a place (strides of 0 are refused).  The members of `a` are read during the call.  Device pointers; the current device's. */
+ * overlap, and no two elements of out may share a place (strides of 0 are refused).  The members of `a` are read during the
+ * call.  Device pointers; the current device's. */
 int rotate_positions(const rotate_args* a, const step_rotary* rotary, void* stream);
 
 /* Makes room for n_tokens new positions of each of the n listed traces, as append_kv does (order, what is skipped and

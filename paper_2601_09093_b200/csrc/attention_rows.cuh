@@ -101,8 +101,8 @@ inline size_t attn_rows_workspace(const step_pool* pool, int n, int T) {
   return splits == 1 ? 0 : (size_t)n * pool->cfg.num_kv_heads * T * pool->G * splits * (pool->cfg.head_dim + 2) * sizeof(float);
 }
 
-// kGroups: of each kind of keys, as many as kRows / G traces at a time need.  48 traces of two prompts of 4000, 8 / 2 heads of 64 in
-// bf16: 83 us, 124 with as many ranges as each trace by itself wants, 147 with every trace reading its own table.
+// kGroups: of each kind of keys, as many as kRows / G traces at a time need (one number for both: most ranges of own keys are then empty
+// where prompts are long).  48 traces of two prompts of 4000, 8 / 2 heads of 64 in bf16: 83 us, 124 with as many ranges as each trace by itself wants, 147 with every trace reading its own table.
 inline int attn_groups_splits(const step_pool* pool, int n) {
   const int together = kRows / pool->G, s = attn_rows_splits(pool, (n + together - 1) / together, 1);
   return s > 32 ? 32 : s;

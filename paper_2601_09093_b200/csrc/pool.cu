@@ -754,6 +754,8 @@ int append_kv(step_pool* pool, const int32_t* trace_ids, int n, int n_tokens, co
   return stepk::append_kv_impl(pool, trace_ids, n, n_tokens, k_new, v_new, nullptr, 0, (cudaStream_t)stream, nullptr, 0);
 }
 
+// One token for 1, 64, 2048 traces: 4, 10.4, 204 us on the GPU, for a few bytes per trace; what bounds it is one thread that goes
+// through the list in order, 0.1 us per entry, since an entry's blocks depend on those before it.
 int kv_pool_extend(step_pool* pool, const int32_t* trace_ids, int n, int n_tokens, int32_t* start_out, void* stream) {
   if (!pool || n < 0 || n_tokens < 0) return STEP_ERR_INVALID_ARG;
   if (n == 0) return STEP_OK;

@@ -5,9 +5,9 @@
 //   (y1, y2) = scale * ( x1 cos a - x2 sin a,  x2 cos a + x1 sin a ),  a = p * f_i;      transposed: a = -p * f_i
 //
 // Angles.  f_i enters as turns per position in units of 2^-64 (a 64-bit integer, made once on the host): p times that, modulo
-// 2^64, IS the angle modulo a turn, with an error of p * 2^-65 turns - 1e-13 at a position of a million, where a 32-bit
-// product p * f would be off by 0.03.  The two top bits are the quadrant (rounded to nearest), what is left - at most an
-// eighth of a turn - becomes a float and goes through sincospif.  One 64-bit multiplication per pair and position, shared
+// 2^64, IS the angle modulo a turn, with an error of p * 2^-65 turns from the table's rounding - 1.7e-13 radians at a position of
+// a million, where a 32-bit product p * f would be off by 0.03.  The two top bits are the quadrant (rounded to nearest), what is
+// left - at most an eighth of a turn - becomes a float, which rounds it by at most 2^-28 of a turn, and goes through sincospif.  One 64-bit multiplication per pair and position, shared
 // by all heads of the token.
 //
 // Both kernels are bound by memory: every element is read once and written once.  A thread owns kU = 16 bytes worth of
@@ -173,7 +173,9 @@ __global__ void __launch_bounds__(kRotateThreads) rotate_rows_kernel(const __gri
 
 // Rows of few heads: a CTA takes up to rows_per_cta rows.  Cosines and sines of all pairs of its rows once,
 // into shared memory; then its threads go through the units of all heads of all rows, kRotateAhead of them under way at once.
-// 33 x 1021 rows of 5 heads of 64, fp32, half of each turned: 16.5 us where a warp per row took 37 (most of its lanes idle).
+// 33 x 1021 rows of 5 heads of 64, fp32, half of each turned, 86 MB: 16.5 us on the same inputs again (they stay in the L2), where a warp
+// per row took 37 (most of its lanes idle); 20.5 on inputs in turn (floor 13.2).  What bounds it is rounds of memory latency in a row - the
+// angles, the first units, a second round of few units, then the copied dims - at 35 % of the issue slots.
 template <typename T, bool kPairs>
 __global__ void __launch_bounds__(kRotateThreads) rotate_flat_kernel(const __grid_constant__ RotateDev a) {
   constexpr int kU = 16 / (int)sizeof(T);
@@ -251,7 +253,8 @@ __global__ void __launch_bounds__(kRotateThreads) rotate_flat_kernel(const __gri
   }
 }
 
-// Any alignment, any even D: a thread takes one pair, or one dim behind D, at a time.
+// Any alignment, any even D: a thread takes one pair, or one dim behind D, at a time, with a handful of divisions to know which.  8191 rows of
+// 40 heads of 96 in bf16, 24 dims turned: 180 us, where 32 dims turned in whole chunks take 33 and the bytes 19.
 template <typename T, bool kPairs>
 __global__ void __launch_bounds__(256) rotate_any_kernel(const __grid_constant__ RotateDev a) {
   const int half = a.D / 2, items = half + (a.copy_tail ? a.d - a.D : 0);
@@ -295,8 +298,10 @@ constexpr int kMaxPairs = 256;                                           // head
 // A CTA takes one (entry, token) row and a range of layers: cosines and sines of its position once, into shared memory;
 // where the row goes (block and slot, the same for every layer and head) once; then its warps share the heads.
 // kChunks: whole units (D a multiple of two chunks); else pair by pair.  32 tokens for 64 traces, 36 layers of 32 / 8 heads of 128 in
-// bf16, with their queries: 290 us, 1.81 GB at 6.3 TB/s; one token, one layer: the latency of three dependent reads (an extension, the
-// store and attention to the row together 12.4 us, 13.1 with the page looked up after the trace's length, a fourth).
+// bf16, with their queries: 290 us, 1.81 GB at 6.3 TB/s; one token, one layer: the latency of three dependent reads (the store and
+// attention to the row together 12.4 us, 13.1 with the page looked up after the trace's length, a fourth).  Pair by pair (D no multiple of two
+// chunks) a lane moves 2 or 4 bytes at a time: 32 tokens for 64 traces, 8 layers of 32 / 8 heads of 96 in bf16, 24 dims turned: 199 us, where
+// 32 dims turned take 66 and the bytes 46.
 template <typename T, bool kPairs, bool kChunks>
 __global__ void __launch_bounds__(256) store_kernel(const StoreDev a) {
   constexpr int kU = 16 / (int)sizeof(T);
