@@ -7,8 +7,8 @@
 // Angles.  f_i enters as turns per position in units of 2^-64 (a 64-bit integer, made once on the host): p times that, modulo
 // 2^64, IS the angle modulo a turn, with an error of p * 2^-65 turns from the table's rounding - 1.7e-13 radians at a position of
 // a million, where a 32-bit product p * f would be off by 0.03.  The two top bits are the quadrant (rounded to nearest), what is
-// left - at most an eighth of a turn - becomes a float, which rounds it by at most 2^-28 of a turn, and goes through sincospif.  One 64-bit multiplication per pair and position, shared
-// by all heads of the token.
+// left - at most an eighth of a turn - becomes a float, which rounds it by at most 2^-28 of a turn, and goes through sincospif.
+// One 64-bit multiplication per pair and position, shared by all heads of the token.
 //
 // Both kernels are bound by memory: every element is read once and written once.  A thread owns kU = 16 bytes worth of
 // pairs ("unit"): two 16-byte chunks of a head - one in each half, or two neighbours - so that it reads and writes whole
